@@ -19,7 +19,8 @@ OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libesp.so")
 
 SOURCES = ["esp_api.cu", "esp_kernels.cu", "esp_packed.cu", "esp_place.cu", "esp_load.cu", "esp_resident.cu", "esp_plan.cpp",
-           "esp_host.cpp", "esp_noalloc.cu", "esp_iac.cu"]
+           "esp_host.cpp", "esp_noalloc.cu", "esp_iac.cu", "esp_moe.cu", "esp_moe_route.cu", "esp_moe_combine.cu",
+           "esp_fp8.cu", "esp_fp8_gemm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-O2,-ffp-contract=off", "-I", INCLUDE, "-I", CSRC,
               "--expt-relaxed-constexpr"]

@@ -1,0 +1,457 @@
+// C entry points of the price-routed expert layer (include/esp_moe.h): checks of the arguments, work
+// space, and the launches of each call.
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+#include "esp_debug.h"
+#include "esp_moe_impl.h"
+#include "esp_moe_load.cuh"
+
+using namespace esp_moe_impl;
+
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffff00;   // row counts fit int32 with a tile to spare
+
+esp_status fail(esp_moe *m)
+{
+    cudaGetLastError();
+    m->poisoned = true;
+    return ESP_ERR_CUDA;
+}
+
+#define MOE_CUDA(call)              \
+    do {                            \
+        if ((call) != cudaSuccess)  \
+            return fail(m);         \
+    } while (0)
+
+// Common head of every call: the handle, its device current, no launches yet.
+esp_status begin(esp_moe *m)
+{
+    if (!m)
+        return ESP_ERR_INVALID_ARG;
+    if (m->poisoned)
+        return ESP_ERR_STATE;
+    m->launches = 0;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || (dev != m->device && cudaSetDevice(m->device) != cudaSuccess))
+        return fail(m);
+    return ESP_OK;
+}
+
+// At least `bytes` of work space. A larger block replaces the old one after the device is done with it.
+esp_status reserve(esp_moe *m, size_t bytes)
+{
+    if (bytes <= m->ws_bytes)
+        return ESP_OK;
+    if (m->ws) {
+        MOE_CUDA(cudaStreamSynchronize(m->stream));
+        MOE_CUDA(cudaFree(m->ws));
+        m->ws = nullptr;
+        m->ws_bytes = 0;
+    }
+    void *p = nullptr;
+    if (cudaMalloc(&p, bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return ESP_ERR_OOM;
+    }
+    m->ws = static_cast<unsigned char *>(p);
+    m->ws_bytes = bytes;
+    return ESP_OK;
+}
+
+size_t element_size(int32_t dtype)
+{
+    return dtype == ESP_MOE_F32 ? 4 : 2;
+}
+
+bool good_dtype(int32_t dtype)
+{
+    return dtype == ESP_MOE_F32 || dtype == ESP_MOE_BF16 || dtype == ESP_MOE_F16;
+}
+
+bool aligned_to(const void *p, size_t bytes)
+{
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0;
+}
+
+bool good_gate(const esp_moe_gate *g)
+{
+    return g && (g->kind == ESP_MOE_SOFTMAX || g->kind == ESP_MOE_SIGMOID) && std::isfinite(g->scale);
+}
+
+Gate to_gate(const esp_moe_gate *g)
+{
+    return Gate{g->kind == ESP_MOE_SIGMOID ? 1 : 0, g->renorm ? 1 : 0, g->scale};
+}
+
+bool good_choice(int64_t T, int32_t E, int32_t k)
+{
+    return E >= 1 && E <= ESP_MOE_MAX_EXPERTS && k >= 1 && k <= std::min(E, ESP_MOE_MAX_CHOICES) && T >= 0 &&
+           T <= kMaxRows / k;
+}
+
+bool good_weight(const esp_moe_weight *w)
+{
+    return w && w->E >= 1 && w->E <= ESP_MOE_MAX_EXPERTS && w->N >= 1 && w->K >= 1 && w->N <= (1 << 22) &&
+           w->K <= (1 << 22) && (int64_t)w->E * w->N <= kMaxRows && (int64_t)w->E * w->K <= kMaxRows &&
+           w->q && w->scale && w->ld >= w->K && w->ld % 16 == 0 && aligned_to(w->q, 16) &&
+           (!w->qt || (w->ldt >= w->N && w->ldt % 16 == 0 && aligned_to(w->qt, 16)));
+}
+
+bool good_product(int64_t T, int64_t M, const int32_t *rows, const esp_moe_weight *w, const int32_t *offsets)
+{
+    return good_weight(w) && T >= 0 && M >= 0 && T <= kMaxRows && M <= kMaxRows && (rows || M == T) &&
+           (offsets || w->E == 1);
+}
+
+int64_t round_up(int64_t v, int64_t to)
+{
+    return ceil_div(v, to) * to;
+}
+
+}  // namespace
+
+extern "C" {
+
+esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream)
+{
+    if (!out)
+        return ESP_ERR_INVALID_ARG;
+    *out = nullptr;
+    int n = 0;
+    if (cudaGetDeviceCount(&n) != cudaSuccess || n == 0) {
+        cudaGetLastError();
+        return ESP_ERR_UNSUPPORTED;
+    }
+    if (device < 0 && cudaGetDevice(&device) != cudaSuccess)
+        return ESP_ERR_CUDA;
+    if (device >= n)
+        return ESP_ERR_INVALID_ARG;
+    int major = 0, minor = 0, sms = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+        return ESP_ERR_CUDA;
+    if (major != 10 || minor != 3)
+        return ESP_ERR_UNSUPPORTED;
+    if (cudaSetDevice(device) != cudaSuccess)
+        return ESP_ERR_CUDA;
+    esp_moe *m = new (std::nothrow) esp_moe();
+    if (!m)
+        return ESP_ERR_OOM;
+    m->device = device;
+    m->stream = static_cast<cudaStream_t>(cuda_stream);
+    m->sm_count = sms;
+    void *words = nullptr;
+    const size_t bytes = (1 + kTickets) * sizeof(unsigned int);
+    if (cudaMalloc(&words, bytes) != cudaSuccess || cudaMemset(words, 0, bytes) != cudaSuccess ||
+        cudaEventCreateWithFlags(&m->handoff, cudaEventDisableTiming) != cudaSuccess) {
+        cudaGetLastError();
+        if (words)
+            cudaFree(words);
+        delete m;
+        return ESP_ERR_CUDA;
+    }
+    m->d_err = static_cast<unsigned int *>(words);
+    m->d_ticket = m->d_err + 1;
+    *out = m;
+    return ESP_OK;
+}
+
+esp_status esp_moe_set_stream(esp_moe *m, void *cuda_stream)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    const cudaStream_t next = static_cast<cudaStream_t>(cuda_stream);
+    if (next != m->stream) {
+        MOE_CUDA(cudaEventRecord(m->handoff, m->stream));
+        MOE_CUDA(cudaStreamWaitEvent(next, m->handoff, 0));
+        m->stream = next;
+    }
+    return ESP_OK;
+}
+
+esp_status esp_moe_route(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, int64_t T, int32_t E, int32_t k,
+                         int64_t ld, const void *logits, const float *prices, const uint8_t *valid, int32_t *idx,
+                         float *weight, int64_t *counts, int32_t *rows, int32_t *pos, int32_t *offsets)
+{
+    esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_gate(gate) || !good_dtype(dtype) || !good_choice(T, E, k) || ld < E || !counts ||
+        (T > 0 && (!logits || !idx || !weight)))
+        return ESP_ERR_INVALID_ARG;
+    const bool plan = rows || pos || offsets;
+    if (plan && (!offsets || (T > 0 && (!rows || !pos))))
+        return ESP_ERR_INVALID_ARG;
+    if (!aligned_to(logits, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    RouteArgs a{to_gate(gate), T, ld, E, k, logits, prices, valid, idx, weight, counts, rows, pos, offsets, nullptr};
+    const size_t ints = route_hist_ints(T, E, k);
+    if ((st = reserve(m, ints * sizeof(int32_t))) != ESP_OK)
+        return st;
+    a.hist = reinterpret_cast<int32_t *>(m->ws);
+    MOE_CUDA(launch_route(m, dtype, a));
+    return ESP_OK;
+}
+
+esp_status esp_moe_balance(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, int64_t T, int32_t E, int32_t k,
+                           int64_t ld, const void *logits, const int32_t *idx, int32_t B, const int32_t *seq_offsets,
+                           float *loss, int64_t *counts, float *share, int64_t *tokens)
+{
+    esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_gate(gate) || !good_dtype(dtype) || !good_choice(T, E, k) || ld < E || B < 1 ||
+        B > ESP_MOE_MAX_SEQUENCES || (!seq_offsets && B != 1) || !loss || !counts || !share || !tokens ||
+        (T > 0 && (!logits || !idx)) || !aligned_to(logits, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    BalanceArgs a{};
+    a.gate = to_gate(gate);
+    a.T = T;
+    a.ld = ld;
+    a.E = E;
+    a.k = k;
+    a.B = B;
+    a.logits = logits;
+    a.idx = idx;
+    a.seq = seq_offsets;
+    a.loss = loss;
+    a.counts = counts;
+    a.share = share;
+    a.tokens = tokens;
+    a.ticket = m->d_ticket;
+    const size_t slots = (size_t)balance_slots(T, B);
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        a.part_share = c.take<float>(slots * E);
+        a.part_count = c.take<int32_t>(slots * E);
+        a.part_lse = c.take<float>(slots);
+        a.part_tokens = c.take<int32_t>(slots);
+        a.seq_loss = c.take<float>(2 * (size_t)B);
+        if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
+            return st;
+    }
+    MOE_CUDA(launch_balance(m, dtype, a));
+    return ESP_OK;
+}
+
+esp_status esp_moe_route_backward(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, int64_t T, int32_t E, int32_t k,
+                                  int64_t ld, const void *logits, const int32_t *idx, const float *dweight, int32_t B,
+                                  const int32_t *seq_offsets, const int64_t *counts, const int64_t *tokens,
+                                  const float *dloss, int64_t ld_out, void *dlogits)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_gate(gate) || !good_dtype(dtype) || !good_choice(T, E, k) || ld < E || ld_out < E ||
+        (T > 0 && (!logits || !idx || !dlogits)) || !aligned_to(logits, element_size(dtype)) ||
+        !aligned_to(dlogits, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    if (dloss && (B < 1 || B > ESP_MOE_MAX_SEQUENCES || (!seq_offsets && B != 1) || !counts || !tokens))
+        return ESP_ERR_INVALID_ARG;
+    RouteBackwardArgs a{to_gate(gate), T,       ld,          ld_out, E,      k,      dloss ? B : 0,
+                        logits,        idx,     dweight,     seq_offsets,              counts, tokens, dloss,
+                        dlogits};
+    MOE_CUDA(launch_route_backward(m, dtype, a));
+    return ESP_OK;
+}
+
+esp_status esp_moe_step_prices(esp_moe *m, int32_t E, const int64_t *counts, double eta, double slack, float *prices)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (E < 1 || E > ESP_MOE_MAX_EXPERTS || !counts || !prices || !(eta > 0.0) || !std::isfinite(eta) ||
+        !(slack > 0.0) || !std::isfinite(slack))
+        return ESP_ERR_INVALID_ARG;
+    MOE_CUDA(launch_step_prices(m, E, counts, eta, slack, prices));
+    return ESP_OK;
+}
+
+esp_status esp_moe_quantize_weight(esp_moe *m, int32_t dtype, const void *w, int64_t ldw, const esp_moe_weight *out)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_dtype(dtype) || !w || !good_weight(out) || ldw < out->K || !aligned_to(w, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    MOE_CUDA(launch_quant_weight(m, dtype, w, ldw, *out));
+    return ESP_OK;
+}
+
+esp_status esp_moe_linear(esp_moe *m, int32_t dtype, int64_t T, int64_t ldx, const void *x, int64_t M,
+                          const int32_t *rows, const esp_moe_weight *w, const int32_t *offsets, int64_t ldy, void *y)
+{
+    esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_dtype(dtype) || !good_product(T, M, rows, w, offsets) || ldx < w->K || ldy < w->N ||
+        (M > 0 && (!y || (T > 0 && !x))) || !aligned_to(x, element_size(dtype)) || !aligned_to(y, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    if (M == 0)
+        return ESP_OK;
+    const int64_t kb = ceil_div(w->K, kBlock), nb = ceil_div(w->N, kBlock);
+    QuantRowsArgs q{M, T, ldx, round_up(w->K, 16), round_up(kb, 4), w->K, x, rows, nullptr, nullptr};
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        q.q = c.take<uint8_t>((size_t)(M * q.ldq));
+        q.scale = c.take<float>((size_t)(M * q.lds));
+        if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
+            return st;
+    }
+    MOE_CUDA(launch_quant_rows(m, dtype, q));
+    const GemmRowsArgs g{M, q.ldq, q.lds, w->ld, ldy, w->E, w->N, w->K, q.q, w->q, q.scale, w->scale,
+                         nb * kb, kb, 1, offsets, y};
+    MOE_CUDA(launch_gemm_rows(m, dtype, g));
+    return ESP_OK;
+}
+
+esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t ldx, const void *x, int64_t M,
+                                   const int32_t *rows, const esp_moe_weight *w, const int32_t *offsets, int64_t lddy,
+                                   const void *dy, int64_t lddx, void *dx, int64_t lddw, float *dw)
+{
+    esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_dtype(dtype) || !good_product(T, M, rows, w, offsets) || lddy < w->N ||
+        (M > 0 && !dy) || !aligned_to(dy, element_size(dtype)) || (dx && (!w->qt || lddx < w->K)) ||
+        !aligned_to(dx, element_size(dtype)) || !aligned_to(dw, 4) || (dw && (lddw < w->K || ldx < w->K)) ||
+        (dw && M > 0 && T > 0 && !x) || !aligned_to(x, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    const int64_t kb = ceil_div(w->K, kBlock), nb = ceil_div(w->N, kBlock);
+    const int64_t positions = (M / kBlock + w->E) * kBlock;   // every expert's rows rounded up to a block
+    const bool want_dx = dx && M > 0;
+    QuantRowsArgs q{M, M, lddy, round_up(w->N, 16), round_up(nb, 4), w->N, dy, nullptr, nullptr, nullptr};
+    QuantColsArgs cy{M, M, lddy, positions, round_up(w->N, 4), w->N, w->E, dy, nullptr, offsets, nullptr, nullptr};
+    QuantColsArgs cx{M, T, ldx, positions, round_up(w->K, 4), w->K, w->E, x, rows, offsets, nullptr, nullptr};
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        if (want_dx) {
+            q.q = c.take<uint8_t>((size_t)(M * q.ldq));
+            q.scale = c.take<float>((size_t)(M * q.lds));
+        }
+        if (dw) {
+            cy.q = c.take<uint8_t>((size_t)(w->N * cy.ldq));
+            cy.scale = c.take<float>((size_t)(positions / kBlock * cy.lds));
+            cx.q = c.take<uint8_t>((size_t)(w->K * cx.ldq));
+            cx.scale = c.take<float>((size_t)(positions / kBlock * cx.lds));
+        }
+        if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
+            return st;
+    }
+    if (want_dx) {
+        MOE_CUDA(launch_quant_rows(m, dtype, q));
+        const GemmRowsArgs g{M, q.ldq, q.lds, w->ldt, lddx, w->E, w->K, w->N, q.q, w->qt, q.scale, w->scale,
+                             nb * kb, 1, kb, offsets, dx};
+        MOE_CUDA(launch_gemm_rows(m, dtype, g));
+    }
+    if (dw) {
+        MOE_CUDA(launch_quant_cols(m, dtype, cy));
+        MOE_CUDA(launch_quant_cols(m, dtype, cx));
+        const GemmColsArgs g{M, cy.ldq, cx.ldq, cy.lds, cx.lds, lddw, w->E, w->N, w->K, cy.q, cx.q, cy.scale, cx.scale,
+                             offsets, dw};
+        MOE_CUDA(launch_gemm_cols(m, g));
+    }
+    return ESP_OK;
+}
+
+esp_status esp_moe_combine(esp_moe *m, int32_t dtype, int64_t T, int32_t k, int32_t H, int64_t M, int64_t ldy,
+                           const void *y, const int32_t *pos, const float *weight, int64_t ldo, void *out)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_dtype(dtype) || k < 1 || k > ESP_MOE_MAX_CHOICES || T < 0 || T > kMaxRows / k || H < 1 || M < 0 ||
+        M > kMaxRows || ldy < H || ldo < H || (T > 0 && (!pos || !out || (M > 0 && !y))) ||
+        !aligned_to(y, element_size(dtype)) || !aligned_to(out, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    CombineArgs a{};
+    a.T = T;
+    a.M = M;
+    a.k = k;
+    a.H = H;
+    a.ldy = ldy;
+    a.ldo = ldo;
+    a.y = y;
+    a.pos = pos;
+    a.weight = weight;
+    a.out = out;
+    MOE_CUDA(launch_combine(m, dtype, a));
+    return ESP_OK;
+}
+
+esp_status esp_moe_combine_backward(esp_moe *m, int32_t dtype, int64_t T, int32_t k, int32_t H, int64_t M, int64_t lddo,
+                                    const void *dout, int64_t ldy, const void *y, const int32_t *pos,
+                                    const float *weight, int64_t lddy, void *dy, float *dweight)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    if (!good_dtype(dtype) || k < 1 || k > ESP_MOE_MAX_CHOICES || T < 0 || T > kMaxRows / k || H < 1 || M < 0 ||
+        M > kMaxRows || lddo < H || (T > 0 && (!pos || !dout)) || (dweight && (ldy < H || (T > 0 && M > 0 && !y))) ||
+        (dy && lddy < H) || !aligned_to(y, element_size(dtype)) || !aligned_to(dout, element_size(dtype)) ||
+        !aligned_to(dy, element_size(dtype)))
+        return ESP_ERR_INVALID_ARG;
+    CombineArgs a{};
+    a.T = T;
+    a.M = M;
+    a.k = k;
+    a.H = H;
+    a.ldy = ldy;
+    a.lddo = lddo;
+    a.lddy = lddy;
+    a.y = y;
+    a.pos = pos;
+    a.weight = weight;
+    a.dout = dout;
+    a.dy = dy;
+    a.dweight = dweight;
+    MOE_CUDA(launch_combine_backward(m, dtype, a));
+    return ESP_OK;
+}
+
+esp_status esp_moe_synchronize(esp_moe *m)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    MOE_CUDA(cudaStreamSynchronize(m->stream));
+    unsigned int err = 0;
+    MOE_CUDA(cudaMemcpy(&err, m->d_err, sizeof(err), cudaMemcpyDeviceToHost));
+    if (err) {
+        m->poisoned = true;
+        return ESP_ERR_TIMEOUT;
+    }
+    return ESP_OK;
+}
+
+esp_status esp_moe_last_launch_count(esp_moe *m, int64_t *out)
+{
+    if (!m || !out)
+        return ESP_ERR_INVALID_ARG;
+    *out = m->launches;
+    return ESP_OK;
+}
+
+void esp_moe_destroy(esp_moe *m)
+{
+    if (!m)
+        return;
+    cudaSetDevice(m->device);
+    if (m->ws)
+        cudaFree(m->ws);
+    if (m->d_err)
+        cudaFree(m->d_err);
+    if (m->handoff)
+        cudaEventDestroy(m->handoff);
+    cudaGetLastError();
+    delete m;
+}
+
+}  // extern "C"

@@ -1,0 +1,190 @@
+// The experts' rows back into their tokens (include/esp_moe.h: esp_moe_combine and its gradients): one
+// CTA per token, a thread owns V consecutive columns (16 bytes where the rows allow it) of all the
+// token's rows, KT of them in flight at once.
+
+#include <algorithm>
+
+#include "esp_moe_impl.h"
+#include "esp_moe_load.cuh"
+
+namespace esp_moe_impl {
+
+namespace {
+
+constexpr int kMaxThreads = 256;
+
+// A token's rows and weights in shared memory; rows outside [0, M) become -1.
+struct Picks {
+    int32_t pos[ESP_MOE_MAX_CHOICES];
+    float weight[ESP_MOE_MAX_CHOICES];
+};
+
+__device__ __forceinline__ void load_picks(const CombineArgs &a, int64_t t, Picks &s)
+{
+    if (threadIdx.x < ESP_MOE_MAX_CHOICES) {
+        int32_t p = -1;
+        float w = 0.0f;
+        if ((int)threadIdx.x < a.k) {
+            p = a.pos[t * a.k + threadIdx.x];
+            w = a.weight ? a.weight[t * a.k + threadIdx.x] : 1.0f;
+        }
+        s.pos[threadIdx.x] = p >= 0 && p < a.M ? p : -1;
+        s.weight[threadIdx.x] = w;
+    }
+    __syncthreads();
+}
+
+template <typename T, int V, int KT>
+__global__ void __launch_bounds__(kMaxThreads) k_combine(const CombineArgs a)
+{
+    __shared__ Picks s;
+    const int64_t t = blockIdx.x;
+    load_picks(a, t, s);
+    const T *y = static_cast<const T *>(a.y);
+    T *out = static_cast<T *>(a.out) + t * a.ldo;
+    for (int h = threadIdx.x * V; h < a.H; h += blockDim.x * V) {
+        float acc[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            acc[i] = 0.0f;
+        for (int j0 = 0; j0 < a.k; j0 += KT) {
+            float v[KT][V];
+#pragma unroll
+            for (int j = 0; j < KT; ++j) {
+                const int32_t p = s.pos[j0 + j];   // -1 past k
+                if (p >= 0)
+                    load_pack<T, V>(y + p * a.ldy + h, v[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < KT; ++j)
+                if (s.pos[j0 + j] >= 0)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        acc[i] = fmaf(s.weight[j0 + j], v[j][i], acc[i]);
+        }
+        store_pack<T, V>(out + h, acc);
+    }
+}
+
+template <typename T, int V, int KT>
+__global__ void __launch_bounds__(kMaxThreads) k_combine_backward(const CombineArgs a)
+{
+    __shared__ Picks s;
+    __shared__ float part[ESP_MOE_MAX_CHOICES][kMaxThreads / 32];
+    const int64_t t = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    load_picks(a, t, s);
+    const T *y = static_cast<const T *>(a.y), *dout = static_cast<const T *>(a.dout) + t * a.lddo;
+    T *dy = static_cast<T *>(a.dy);
+    for (int j0 = 0; j0 < a.k; j0 += KT) {
+        float dot[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j)
+            dot[j] = 0.0f;
+        for (int h = threadIdx.x * V; h < a.H; h += blockDim.x * V) {
+            float d[V], v[KT][V];
+            load_pack<T, V>(dout + h, d);
+            if (a.dweight) {
+#pragma unroll
+                for (int j = 0; j < KT; ++j) {
+                    const int32_t p = s.pos[j0 + j];
+                    if (p >= 0)
+                        load_pack<T, V>(y + p * a.ldy + h, v[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < KT; ++j)
+                    if (s.pos[j0 + j] >= 0)
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            dot[j] = fmaf(d[i], v[j][i], dot[j]);
+            }
+            if (dy) {
+#pragma unroll
+                for (int j = 0; j < KT; ++j) {
+                    const int32_t p = s.pos[j0 + j];
+                    if (p >= 0) {
+                        float g[V];
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            g[i] = s.weight[j0 + j] * d[i];
+                        store_pack<T, V>(dy + p * a.lddy + h, g);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < KT; ++j) {
+            float x = dot[j];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                x += __shfl_xor_sync(0xffffffffu, x, o);
+            if (lane == 0 && j0 + j < ESP_MOE_MAX_CHOICES)
+                part[j0 + j][warp] = x;
+        }
+    }
+    if (!a.dweight)
+        return;
+    __syncthreads();
+    if ((int)threadIdx.x < a.k) {
+        float x = 0.0f;
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w)
+            x += part[threadIdx.x][w];
+        a.dweight[t * a.k + threadIdx.x] = x;
+    }
+}
+
+// Threads of a CTA: enough for a row, whole warps, at least one.
+int threads_for(int64_t H, int V)
+{
+    return (int)std::min<int64_t>(kMaxThreads, std::max<int64_t>(32, ceil_div(ceil_div(H, V), 32) * 32));
+}
+
+// Calls f(V, KT) for the widest load that every row allows and the rows in flight (8, or 4, of them).
+template <typename T, typename F>
+cudaError_t with_shape(bool wide, int k, F &&f)
+{
+    constexpr int W = 16 / (int)sizeof(T);
+    if (wide)
+        return k > 4 ? f(std::integral_constant<int, W>(), std::integral_constant<int, 8>())
+                     : f(std::integral_constant<int, W>(), std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+}
+
+}  // namespace
+
+cudaError_t launch_combine(esp_moe *m, int32_t dtype, const CombineArgs &a)
+{
+    if (a.T == 0 || a.H == 0)
+        return cudaSuccess;
+    return with_dtype(dtype, [&](auto elem) {
+        using T = decltype(elem);
+        const bool wide = rows_aligned(a.y, a.ldy, sizeof(T), 16) && rows_aligned(a.out, a.ldo, sizeof(T), 16) &&
+                          a.H * sizeof(T) % 16 == 0;
+        return with_shape<T>(wide, a.k, [&](auto v, auto kt) -> cudaError_t {
+            constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
+            k_combine<T, V, KT><<<(unsigned)a.T, threads_for(a.H, V), 0, m->stream>>>(a);
+            m->launches += 1;
+            return cudaGetLastError();
+        });
+    });
+}
+
+cudaError_t launch_combine_backward(esp_moe *m, int32_t dtype, const CombineArgs &a)
+{
+    if (a.T == 0)
+        return cudaSuccess;
+    return with_dtype(dtype, [&](auto elem) {
+        using T = decltype(elem);
+        const bool wide = (!a.dweight || rows_aligned(a.y, a.ldy, sizeof(T), 16)) &&
+                          (!a.dy || rows_aligned(a.dy, a.lddy, sizeof(T), 16)) &&
+                          rows_aligned(a.dout, a.lddo, sizeof(T), 16) && a.H * sizeof(T) % 16 == 0;
+        return with_shape<T>(wide, a.k, [&](auto v, auto kt) -> cudaError_t {
+            constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
+            k_combine_backward<T, V, KT><<<(unsigned)a.T, threads_for(a.H, V), 0, m->stream>>>(a);
+            m->launches += 1;
+            return cudaGetLastError();
+        });
+    });
+}
+
+}  // namespace esp_moe_impl
