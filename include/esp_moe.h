@@ -166,6 +166,12 @@ esp_status esp_moe_synchronize(esp_moe *m);
 /* Kernel launches of the handle's last call. */
 esp_status esp_moe_last_launch_count(esp_moe *m, int64_t *out);
 
+/* Failure detection without a GPU fault (tests): the waits of later products give up after about
+ * limit_ms milliseconds (0: the default, about 4 s), and the next product launch leaves out one load, so
+ * that its waits run out and esp_moe_synchronize reports ESP_ERR_TIMEOUT. */
+esp_status esp_moe_debug_set_wait_limit(esp_moe *m, uint32_t limit_ms);
+esp_status esp_moe_debug_hold_load(esp_moe *m);
+
 void esp_moe_destroy(esp_moe *m);
 
 #ifdef __cplusplus

@@ -1,9 +1,27 @@
-// Products of 8-bit codes with a scale per block of 128 (include/esp_moe.h): each block's products are
-// summed in fp32, scaled and added to the result.
+// Products of 8-bit codes with a scale per block of 128 (include/esp_moe.h) on the tensor cores.
+//
+// out[m][n] = sum over blocks b of sa[m][b] sb[n][b] (sum over the 128 codes of block b of A[m] B[n]). The
+// scales change from block to block, so a block's products (four tcgen05.mma kind::f8f6f4 of K = 32)
+// go into an accumulator stage of tensor memory of their own; the epilogue warps read it, scale it and
+// add it to fp32 sums in registers, while the tensor core works on the next stage.
+//
+// A tile is 128 rows (CG = 1: one CTA) or 256 rows (CG = 2: two CTAs of a cluster that share the MMAs,
+// each holding 128 rows of A and half of B) times BN columns; one block of K per shared-memory stage
+// (128 codes = one 128-byte swizzled row). Warps 0-3 own the first half of the columns, warps 4-7 the
+// second, a thread one row (its TMEM lane) of its half; warp 8 loads tiles by TMA, warp 9 issues the
+// MMAs. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
+// run during a tile's stores.
+//
+// GROUPED ROWS (forward, row gradient): expert e's rows times its own B; a tile never spans two experts,
+// rows past the expert's end are computed and dropped. sb is one value per 128 columns.
+// GROUPED INNER AXIS (weight gradient): expert e's blocks of 128 positions; sb is a value per column.
+//
+// Every wait is bounded; one that runs out sets a flag that ends the CTA's other waits, the error word
+// reports it, and the CTA drains its copies and MMAs (bounded) before it frees its tensor memory.
 
 #include <algorithm>
 
-#include <cuda_fp8.h>
+#include <cuda.h>
 
 #include "esp_moe_impl.h"
 #include "esp_moe_load.cuh"
@@ -12,106 +30,652 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kTile = 64, kStep = 32, kGemmThreads = 256;
+constexpr int kThreads = 320;
+constexpr int kEpilogueWarps = 8;
+constexpr int kRowsA = 128;                  // rows of A that a CTA holds
+constexpr int kStageA = kRowsA * kBlock;     // bytes
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kWaitHintNs = 1000000;
+constexpr int kStageCols = 16;               // columns of a warp's staged store
+constexpr int kSmemLimit = 232448;
 
-__device__ __forceinline__ float code_value(uint8_t c)
+template <int CG, int BN>
+struct Shape {
+    static constexpr int kRowsB = BN / CG;   // rows of B that a CTA holds
+    static constexpr int kStage = kStageA + kRowsB * kBlock;
+    static constexpr int kAcc = (int)kTmemCols / BN;
+    static constexpr int kWGCols = BN / 2;   // columns of a warpgroup
+    // after the stages: tile table, store staging, column scales, barriers
+    static constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4;
+    static constexpr int kStaging = kEpilogueWarps * 32 * (kStageCols + 1) * 4;
+    static constexpr int kColScales = 2 * 2 * kWGCols * 4;
+    static constexpr int kBars = 256;
+    static constexpr int kFixed = kTable + kStaging + kColScales + kBars + 1024;
+    static constexpr int kStages = std::min(8, (kSmemLimit - kFixed) / kStage);
+    static constexpr int kSmem = kStages * kStage + kFixed;
+    static_assert((2 * kStages + 2 * kAcc + 1) * 8 + 16 <= kBars, "barriers");
+};
+
+struct GemmParams {
+    int64_t M, lda_scale;            // rows of A (FWD); leading dimension of A's scales
+    int32_t E, N, K;                 // out columns N (FWD) / K (COLS), see the launchers
+    int32_t rows_b;                  // rows of B per expert (FWD)
+    const float *scale_a, *scale_b;
+    int64_t sb_e, sb_n, sb_k;
+    const int32_t *offsets;
+    void *out;
+    int64_t ldo;
+    bool wide_store;
+    unsigned int *err;
+    uint32_t polls;
+    int32_t hold;                    // leave out the CTAs' third load (failure detection)
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p)
 {
-    const __half_raw h = __nv_cvt_fp8_to_halfraw(c, __NV_E4M3);
-    return __half2float(__half(h));
+    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
-// acc[4][4] += the block's products of A rows a0.. and B rows b0.. (columns k0 .. k0 + 127 below K).
-__device__ void block_product(const uint8_t *A, int64_t lda, int rows_a, const uint8_t *B, int64_t ldb, int rows_b,
-                              int klen, float (&sa)[kTile][kStep + 1], float (&sb)[kTile][kStep + 1],
-                              float (&acc)[4][4])
+// Address of the same shared-memory location in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank)
 {
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int ks = 0; ks < klen; ks += kStep) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kTile * kStep; i += kGemmThreads) {
-            const int r = i / kStep, k = ks + i % kStep;
-            sa[r][i % kStep] = r < rows_a && k < klen ? code_value(A[r * lda + k]) : 0.0f;
-            sb[r][i % kStep] = r < rows_b && k < klen ? code_value(B[r * ldb + k]) : 0.0f;
-        }
-        __syncthreads();
-        for (int k = 0; k < kStep; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = fmaf(sa[ty * 4 + i][k], sb[tx * 4 + j][k], acc[i][j]);
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// Arrival on a barrier of this CTA or, through its cluster address, of another.
+__device__ __forceinline__ void mbar_arrive(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(kWaitHintNs)
+        : "memory");
+    return done != 0;
+}
+
+// Bounded wait (each poll lasts at most about a millisecond); gives up early once another wait of the CTA
+// did. On running out it sets the CTA's flag and the error word.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
+{
+    if (mbar_try(bar, parity))
+        return true;
+    for (uint32_t i = 0; i < p.polls; ++i) {
+        if (mbar_try(bar, parity))
+            return true;
+        if (*dead)
+            return false;
     }
+    *dead = 1;
+    atomicOr(p.err, 1u);
+    return false;
 }
 
+template <int CG>
+__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], "
+            "[%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, "
+            "{%2, %3}], [%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+
+// Shared-memory operand of 128-byte rows in the 128-byte swizzle: groups of 8 rows 1024 bytes apart
+// (stride offset), descriptor version 1 (bits 46-47), swizzle mode 2 (bits 61-63).
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+
+template <int CG>
+__device__ __forceinline__ void mma_codes(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+
+// The barrier (of every CTA that shares the MMAs) completes when the MMAs issued so far have.
+template <int CG>
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                     : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                bar),
+            "h"((uint16_t)3)
+            : "memory");
+}
+
+__device__ __forceinline__ void fence_after()
+{
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+
+__device__ __forceinline__ void fence_before()
+{
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+
+// 32 consecutive fp32 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32])
+{
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        v[i] = __uint_as_float(r[i]);
+}
+
+// Barrier of a warpgroup that also ANDs a predicate over it.
+__device__ __forceinline__ bool wg_sync_and(int id, bool v)
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, %2, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)v), "r"(id)
+        : "memory");
+    return r != 0;
+}
+
+__device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t M)
+{
+    return max((int64_t)0, min(M, v));
+}
+
+// Expert e's rows [lo, hi).
+__device__ __forceinline__ void expert_rows(const GemmParams &p, int e, int64_t &lo, int64_t &hi)
+{
+    lo = p.offsets ? clamp_row(p.offsets[e], p.M) : 0;
+    hi = p.offsets ? max(lo, clamp_row(p.offsets[e + 1], p.M)) : p.M;
+}
+
+// One tile of the list: rows m0 .. m0 + rows - 1 of the output's group e (a CTA of a pair adds its share),
+// columns n0 .., blocks kb0 .. kb1 - 1.
+struct Tile {
+    int e, rows, n0, kb0, kb1;
+    int64_t m0;
+};
+
+// table[e]: row tiles (FWD) or blocks (COLS) of the experts before e.
+template <int CG, int BN, bool COLS>
+__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int64_t w, Tile &t)
+{
+    constexpr int BM = kRowsA * CG;
+    const int nt = (p.N + BN - 1) / BN;
+    if (!COLS) {
+        const int64_t total = (int64_t)table[p.E] * nt;
+        if (w >= total)
+            return false;
+        int lo = 0, hi = p.E;   // the expert whose tiles hold w
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((int64_t)table[mid] * nt <= w)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        t.e = lo;
+        const int mt = table[lo + 1] - table[lo];
+        const int64_t i = w - (int64_t)table[lo] * nt;
+        int64_t a, b;
+        expert_rows(p, lo, a, b);
+        const int64_t skip = (i % mt) * BM;
+        t.m0 = a + skip;
+        t.rows = (int)min((int64_t)BM, b - t.m0);
+        t.n0 = (int)(i / mt) * BN;
+        t.kb0 = 0;
+        t.kb1 = (p.K + kBlock - 1) / kBlock;
+        return true;
+    }
+    const int mt = (p.rows_b + BM - 1) / BM;   // rows_b: output rows per expert
+    const int64_t per = (int64_t)mt * nt;
+    if (w >= per * p.E)
+        return false;
+    t.e = (int)(w / per);
+    const int64_t i = w % per;
+    t.m0 = (i % mt) * BM;
+    t.rows = (int)min((int64_t)BM, (int64_t)p.rows_b - t.m0);
+    t.n0 = (int)(i / mt) * BN;
+    t.kb0 = table[t.e];
+    t.kb1 = table[t.e + 1];
+    return true;
+}
+
+// A thread's 32 columns of a row of the output, row-major with any alignment: 32-byte stores where they
+// fit, else through the warp's staging so that a store's lanes cover consecutive columns.
 template <typename T>
-__global__ void __launch_bounds__(kGemmThreads) k_gemm_rows(const GemmRowsArgs a)
+__device__ __forceinline__ void store_cols32(T *out, int64_t ldo, int row, int rows, int col, int N, bool wide,
+                                             const float *v, float *stage, int lane)
 {
-    __shared__ float sa[kTile][kStep + 1], sb[kTile][kStep + 1];
-    int64_t base = 0, m0 = 0;
-    int rows = 0, e = 0;
-    for (; e < a.E; ++e) {
-        const int64_t lo = a.offsets ? max((int64_t)0, min(a.M, (int64_t)a.offsets[e])) : 0;
-        const int64_t hi = a.offsets ? max(lo, min(a.M, (int64_t)a.offsets[e + 1])) : a.M;
-        const int64_t tiles = (hi - lo + kTile - 1) / kTile;
-        if (blockIdx.x < base + tiles) {
-            m0 = lo + (blockIdx.x - base) * kTile;
-            rows = (int)min((int64_t)kTile, hi - m0);
-            break;
+    if (wide && col + 32 <= N) {
+        if (row < rows) {
+            T *dst = out + row * ldo + col;
+            constexpr int V = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < 32; i += V)
+                store_pack<T, V>(dst + i, v + i);
         }
-        base += tiles;
-    }
-    if (e == a.E)
         return;
-    const int n0 = blockIdx.y * kTile, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float out[4][4] = {};
-    for (int kb = 0; kb * kBlock < a.K; ++kb) {
-        float acc[4][4] = {};
-        block_product(a.A + m0 * a.lda + kb * kBlock, a.lda, rows, a.B + ((int64_t)e * a.N + n0) * a.ldb + kb * kBlock,
-                      a.ldb, min(kTile, a.N - n0), min(kBlock, a.K - kb * kBlock), sa, sb, acc);
-        const float s_b = a.scale_b[e * a.sb_e + (n0 / kBlock) * a.sb_n + kb * a.sb_k];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float s = ty * 4 + i < rows ? a.scale_a[(m0 + ty * 4 + i) * a.lds + kb] * s_b : 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                out[i][j] = fmaf(acc[i][j], s, out[i][j]);
-        }
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j)
-            if (ty * 4 + i < rows && n0 + tx * 4 + j < a.N)
-                static_cast<T *>(a.out)[(m0 + ty * 4 + i) * a.ldo + n0 + tx * 4 + j] = from_f32<T>(out[i][j]);
+#pragma unroll
+    for (int h = 0; h < 32; h += kStageCols) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kStageCols; ++i)
+            stage[lane * (kStageCols + 1) + i] = v[h + i];
+        __syncwarp();
+        const int c = lane % kStageCols, row0 = row - lane;
+        if (col + h + c < N)
+            for (int r = lane / kStageCols; r < 32 && row0 + r < rows; r += 32 / kStageCols)
+                out[(row0 + r) * ldo + col + h + c] = from_f32<T>(stage[r * (kStageCols + 1) + c]);
+    }
 }
 
-__global__ void __launch_bounds__(kGemmThreads) k_gemm_cols(const GemmColsArgs a)
+template <int CG, int BN, bool COLS, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmParams p)
 {
-    __shared__ float sa[kTile][kStep + 1], sb[kTile][kStep + 1];
-    const int e = blockIdx.z, k0 = blockIdx.x * kTile, n0 = blockIdx.y * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    int64_t run0 = 0, run1 = 0;
-    for (int i = 0; i <= e; ++i) {
-        const int64_t lo = a.offsets ? max((int64_t)0, min(a.M, (int64_t)a.offsets[i])) : 0;
-        const int64_t hi = a.offsets ? max(lo, min(a.M, (int64_t)a.offsets[i + 1])) : a.M;
-        run0 = run1;
-        run1 += (hi - lo + kBlock - 1) / kBlock;
+    using S = Shape<CG, BN>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *sm = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                                          ~static_cast<uintptr_t>(1023));
+    int *table = reinterpret_cast<int *>(sm + S::kStages * S::kStage);
+    float *staging = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(table) + S::kTable);
+    float *colscale = staging + S::kStaging / 4;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(
+        (reinterpret_cast<uintptr_t>(colscale + S::kColScales / 4) + 15) & ~static_cast<uintptr_t>(15));
+    const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, tfull = empty + 8 * S::kStages,
+                   tempty = tfull + 8 * S::kAcc, drain = tempty + 8 * S::kAcc;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 2 * S::kStages + 2 * S::kAcc + 1);
+    volatile int *dead = reinterpret_cast<volatile int *>(slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+
+    if (threadIdx.x == 0) {
+        *dead = 0;
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < S::kAcc; ++i) {
+            mbar_init(tfull + 8 * i, 1);
+            mbar_init(tempty + 8 * i, CG * kEpilogueWarps);
+        }
+        mbar_init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    float out[4][4] = {};
-    for (int64_t r = run0; r < run1; ++r) {
-        float acc[4][4] = {};
-        block_product(a.A + n0 * a.lda + r * kBlock, a.lda, min(kTile, a.N - n0), a.B + k0 * a.ldb + r * kBlock, a.ldb,
-                      min(kTile, a.K - k0), kBlock, sa, sb, acc);
+    if (warp == 8) {
+        // the experts' row tiles (blocks) before each: one warp's scan
+        int carry = 0;
+        for (int e0 = 0; e0 < p.E; e0 += 32) {
+            int n = 0;
+            if (e0 + lane < p.E) {
+                int64_t lo, hi;
+                expert_rows(p, e0 + lane, lo, hi);
+                const int64_t per = COLS ? kBlock : kRowsA * CG;
+                n = (int)((hi - lo + per - 1) / per);
+            }
+            int s = n;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (n0 + ty * 4 + i < a.N && k0 + tx * 4 + j < a.K)
-                    out[i][j] = fmaf(acc[i][j] * a.scale_a[r * a.lds_a + n0 + ty * 4 + i],
-                                     a.scale_b[r * a.lds_b + k0 + tx * 4 + j], out[i][j]);
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o)
+                    s += y;
+            }
+            if (e0 + lane < p.E)
+                table[e0 + lane] = carry + s - n;
+            carry += __shfl_sync(0xffffffffu, s, 31);
+        }
+        if (lane == 0)
+            table[p.E] = carry;
     }
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j)
-            if (n0 + ty * 4 + i < a.N && k0 + tx * 4 + j < a.K)
-                a.out[((int64_t)e * a.N + n0 + ty * 4 + i) * a.ldo + k0 + tx * 4 + j] = out[i][j];
+    if (warp == 9) {
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (CG == 2)
+        cluster_sync();
+    fence_after();
+    const uint32_t tmem = *slot;
+    const int64_t w0 = blockIdx.x / CG, dw = gridDim.x / CG;
+    int64_t issued = 0;   // loads issued by this CTA's producer
+
+    if (warp == 8) {
+        if (lane == 0) {
+            const uint32_t full0 = CG == 1 ? full : map_rank(full, 0);
+            int s = 0;
+            uint32_t ph = 1;
+            bool ok = true;
+            Tile t;
+            for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
+                const int ya = (int)t.m0 + (int)rank * kRowsA;
+                const int yb = (COLS ? 0 : t.e * p.rows_b) + t.n0 + (int)rank * S::kRowsB;
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!(ok = mbar_wait(empty + 8 * s, ph, p, dead)))
+                        break;
+                    const uint32_t dst = smem_u32(sm + s * S::kStage);
+                    if (rank == 0)
+                        mbar_expect(full + 8 * s, CG * S::kStage);
+                    if (!(p.hold && issued == 2)) {
+                        tma_tile<CG>(dst, &map_a, kb * kBlock, ya, full0 + 8 * s);
+                        tma_tile<CG>(dst + kStageA, &map_b, kb * kBlock, yb, full0 + 8 * s);
+                    }
+                    ++issued;
+                    if (++s == S::kStages) {
+                        s = 0;
+                        ph ^= 1;
+                    }
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kRowsA * CG >> 4) << 24);
+            int s = 0, acc = 0;
+            uint32_t ph = 0, aph = 1;
+            bool ok = true;
+            Tile t;
+            for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw)
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!(ok = mbar_wait(tempty + 8 * acc, aph, p, dead)) ||
+                        !(ok = mbar_wait(full + 8 * s, ph, p, dead)))
+                        break;
+                    fence_after();
+                    const uint64_t a = operand_desc(smem_u32(sm + s * S::kStage));
+                    const uint64_t b = operand_desc(smem_u32(sm + s * S::kStage + kStageA));
+#pragma unroll
+                    for (int k = 0; k < kBlock / 32; ++k)   // 32 bytes = 2 units of the descriptor's address
+                        mma_codes<CG>(tmem + acc * BN, a + 2 * k, b + 2 * k, idesc, k > 0);
+                    mma_commit<CG>(empty + 8 * s);
+                    mma_commit<CG>(tfull + 8 * acc);
+                    if (++s == S::kStages) {
+                        s = 0;
+                        ph ^= 1;
+                    }
+                    if (++acc == S::kAcc) {
+                        acc = 0;
+                        aph ^= 1;
+                    }
+                }
+        }
+    } else {
+        const int wg = warp >> 2, quarter = warp & 3;
+        const uint32_t lane_cols = ((uint32_t)(32 * quarter) << 16) + (uint32_t)(wg * S::kWGCols);
+        const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
+        float *stage = staging + warp * 32 * (kStageCols + 1);
+        float *cs = colscale + wg * 2 * S::kWGCols;
+        int acc = 0;
+        uint32_t aph = 0;
+        bool ok = true;
+        Tile t;
+        for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
+            const int row = 32 * quarter + lane;                    // of this CTA's 128
+            const int rows = t.rows - (int)rank * kRowsA;           // that exist
+            const int64_t m = t.m0 + rank * kRowsA + row;
+            const bool some = 32 * quarter < rows;                  // a row of this warp exists
+            const int c0 = t.n0 + wg * S::kWGCols;
+            float sum[S::kWGCols];
+#pragma unroll
+            for (int i = 0; i < S::kWGCols; ++i)
+                sum[i] = 0.0f;
+            // this block's scale factor (FWD: row times column block; COLS: row, columns in shared memory),
+            // fetched a block ahead
+            const int nb = min(c0, p.N - 1) / kBlock;
+            auto scale_of = [&](int kb) -> float {
+                if (kb >= t.kb1 || row >= rows)
+                    return 0.0f;
+                if (COLS)
+                    return p.scale_a[(int64_t)kb * p.lda_scale + m];
+                return p.scale_a[m * p.lda_scale + kb] * p.scale_b[t.e * p.sb_e + nb * p.sb_n + kb * p.sb_k];
+            };
+            auto col_scale_of = [&](int kb) -> float {
+                const int c = c0 + row;   // thread i of the warpgroup brings column i's
+                return row < S::kWGCols && kb < t.kb1 && c < p.N ? p.scale_b[(int64_t)kb * p.sb_k + c] : 0.0f;
+            };
+            float next = scale_of(t.kb0), next_col = COLS ? col_scale_of(t.kb0) : 0.0f;
+            for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                const float scale = next;
+                float *csb = cs + (kb & 1) * S::kWGCols;
+                if (COLS && row < S::kWGCols)
+                    csb[row] = next_col;
+                next = scale_of(kb + 1);
+                if (COLS)
+                    next_col = col_scale_of(kb + 1);
+                ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, aph, p, dead));
+                if (COLS)
+                    ok = wg_sync_and(1 + wg, ok);
+                if (!ok)
+                    break;
+                fence_after();
+                if (some) {
+#pragma unroll
+                    for (int c = 0; c < S::kWGCols; c += 32) {
+                        float v[32];
+                        tmem_ld32(tmem + acc * BN + lane_cols + c, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            if (COLS)
+                                sum[c + i] = fmaf(v[i] * scale, csb[c + i], sum[c + i]);
+                            else
+                                sum[c + i] = fmaf(v[i], scale, sum[c + i]);
+                        }
+                    }
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(tempty0 + 8 * acc);
+                if (++acc == S::kAcc) {
+                    acc = 0;
+                    aph ^= 1;
+                }
+            }
+            if (!ok || !some)
+                continue;
+            T *out = static_cast<T *>(p.out) + (COLS ? (int64_t)t.e * p.rows_b * p.ldo : 0) +
+                     (t.m0 + rank * kRowsA) * p.ldo;
+#pragma unroll
+            for (int c = 0; c < S::kWGCols; c += 32)
+                if (c0 + c < p.N)
+                    store_cols32<T>(out, p.ldo, row, rows, c0 + c, p.N, p.wide_store, sum + c, stage, lane);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (*dead) {
+        // nothing may still land in this CTA's memory: copies first (the leader's barriers count both
+        // CTAs'), then the MMAs
+        if (warp == 8 && lane == 0 && rank == 0)
+            for (int64_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
+                for (int poll = 0; poll < 50; ++poll)
+                    if (mbar_try(full + 8 * (uint32_t)(i % S::kStages), (uint32_t)(i / S::kStages) & 1))
+                        break;
+        if (warp == 9 && lane == 0 && rank == 0) {
+            mma_commit<CG>(drain);
+            for (int poll = 0; poll < 1000 && !mbar_try(drain, 0); ++poll) {
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (CG == 2)
+        cluster_sync();
+    fence_after();
+    if (warp == 9) {
+        if (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+// ---- launches
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// cuTensorMapEncodeTiled of the driver in use (null if it has none).
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) !=
+                cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return fn;
+}
+
+// Tiles of box_rows x 128 codes of a rows x cols matrix of codes; what lies outside reads zero.
+cudaError_t code_map(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(p), dims, strides, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int CG, int BN, bool COLS, typename T>
+cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, GemmParams p, int64_t tiles)
+{
+    using S = Shape<CG, BN>;
+    auto kernel = k_gemm<CG, BN, COLS, T>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.stream = m->stream;
+    int groups = m->sm_count;
+    if (CG == 2) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = CG;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (m->max_pairs == 0) {
+            cfg.gridDim = dim3((unsigned)(m->sm_count / CG * CG));
+            e = cudaOccupancyMaxActiveClusters(&m->max_pairs, kernel, &cfg);
+            if (e != cudaSuccess)
+                return e;
+        }
+        groups = std::max(1, m->max_pairs);
+    }
+    cfg.gridDim = dim3((unsigned)(CG * std::max<int64_t>(1, std::min<int64_t>(groups, tiles))));
+    m->launches += 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, p);
+}
+
+template <int CG, int BN, bool COLS, typename T>
+cudaError_t encode_and_launch(esp_moe *m, const uint8_t *A, int64_t rows_a, int64_t inner, int64_t lda, const uint8_t *B,
+                              int64_t rows_b, int64_t ldb, const GemmParams &p, int64_t tiles)
+{
+    CUtensorMap a, b;
+    cudaError_t e = code_map(&a, A, rows_a, inner, lda, kRowsA);
+    if (e == cudaSuccess)
+        e = code_map(&b, B, rows_b, inner, ldb, Shape<CG, BN>::kRowsB);
+    return e != cudaSuccess ? e : launch<CG, BN, COLS, T>(m, a, b, p, tiles);
+}
+
+GemmParams common(esp_moe *m)
+{
+    GemmParams p{};
+    p.err = m->d_err;
+    p.polls = m->wait_polls;
+    p.hold = m->hold_load ? 1 : 0;
+    m->hold_load = false;   // the hook holds one launch only
+    return p;
 }
 
 }  // namespace
@@ -120,19 +684,49 @@ cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
 {
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        const dim3 grid((unsigned)(a.M / kTile + a.E), (unsigned)ceil_div(a.N, kTile));
-        k_gemm_rows<T><<<grid, kGemmThreads, 0, m->stream>>>(a);
-        m->launches += 1;
-        return cudaGetLastError();
+        GemmParams p = common(m);
+        p.M = a.M;
+        p.lda_scale = a.lds;
+        p.E = a.E;
+        p.N = p.rows_b = a.N;
+        p.K = a.K;
+        p.scale_a = a.scale_a;
+        p.scale_b = a.scale_b;
+        p.sb_e = a.sb_e;
+        p.sb_n = a.sb_n;
+        p.sb_k = a.sb_k;
+        p.offsets = a.offsets;
+        p.out = a.out;
+        p.ldo = a.ldo;
+        p.wide_store = rows_aligned(a.out, a.ldo, sizeof(T), 16);
+        const int64_t experts = std::min<int64_t>(a.E, a.M);
+        if (a.M / a.E > 128) {
+            const int64_t tiles = (a.M / 256 + experts) * ceil_div(a.N, 256);
+            return encode_and_launch<2, 256, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, tiles);
+        }
+        const int64_t tiles = (a.M / 128 + experts) * ceil_div(a.N, 128);
+        return encode_and_launch<1, 128, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, tiles);
     });
 }
 
 cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &a)
 {
-    const dim3 grid((unsigned)ceil_div(a.K, kTile), (unsigned)ceil_div(a.N, kTile), (unsigned)a.E);
-    k_gemm_cols<<<grid, kGemmThreads, 0, m->stream>>>(a);
-    m->launches += 1;
-    return cudaGetLastError();
+    GemmParams p = common(m);
+    p.M = a.M;
+    p.lda_scale = a.lds_a;
+    p.E = a.E;
+    p.N = a.K;
+    p.rows_b = a.N;
+    p.scale_a = a.scale_a;
+    p.scale_b = a.scale_b;
+    p.sb_k = a.lds_b;
+    p.offsets = a.offsets;
+    p.out = a.out;
+    p.ldo = a.ldo;
+    p.wide_store = rows_aligned(a.out, a.ldo, 4, 16);
+    const int64_t positions = (a.M / kBlock + a.E) * kBlock;
+    return encode_and_launch<2, 256, true, float>(m, a.A, a.N, positions, a.lda, a.B, a.K, a.ldb, p,
+                                                  (int64_t)a.E * ceil_div(a.N, 256) * ceil_div(a.K, 256));
 }
 
 }  // namespace esp_moe_impl

@@ -439,6 +439,24 @@ esp_status esp_moe_last_launch_count(esp_moe *m, int64_t *out)
     return ESP_OK;
 }
 
+esp_status esp_moe_debug_set_wait_limit(esp_moe *m, uint32_t limit_ms)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    m->wait_polls = limit_ms == 0 ? kMoeWaitPolls : limit_ms;
+    return ESP_OK;
+}
+
+esp_status esp_moe_debug_hold_load(esp_moe *m)
+{
+    const esp_status st = begin(m);
+    if (st != ESP_OK)
+        return st;
+    m->hold_load = true;
+    return ESP_OK;
+}
+
 void esp_moe_destroy(esp_moe *m)
 {
     if (!m)

@@ -8,6 +8,8 @@
 
 #include "esp_moe.h"
 
+constexpr uint32_t kMoeWaitPolls = 4096;   // about 4 s of waiting before a timeout is reported
+
 struct esp_moe {
     int device = 0;
     cudaStream_t stream = nullptr;
@@ -19,6 +21,11 @@ struct esp_moe {
     size_t ws_bytes = 0;
     unsigned int *d_err = nullptr;   // device error word (timeouts of the product kernels)
     unsigned int *d_ticket = nullptr;   // arrival counters, zero between launches
+    int max_pairs = 0;               // CTA pairs of the product kernel that run at once (0: not asked yet)
+    // failure-detection hooks (esp_moe.h): polls of a bounded wait (about 1 ms each), and the next
+    // product launch leaving out one load
+    uint32_t wait_polls = kMoeWaitPolls;
+    bool hold_load = false;
 };
 
 namespace esp_moe_impl {

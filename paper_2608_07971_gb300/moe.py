@@ -30,6 +30,7 @@ EXPORTED = [
     "esp_moe_create", "esp_moe_set_stream", "esp_moe_route", "esp_moe_balance", "esp_moe_route_backward",
     "esp_moe_step_prices", "esp_moe_quantize_weight", "esp_moe_linear", "esp_moe_linear_backward", "esp_moe_combine",
     "esp_moe_combine_backward", "esp_moe_synchronize", "esp_moe_last_launch_count", "esp_moe_destroy",
+    "esp_moe_debug_set_wait_limit", "esp_moe_debug_hold_load",
 ]
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
@@ -71,6 +72,8 @@ def load_library():
         "esp_moe_synchronize": ([vp], st),
         "esp_moe_last_launch_count": ([vp, ctypes.POINTER(i64)], st),
         "esp_moe_destroy": ([vp], None),
+        "esp_moe_debug_set_wait_limit": ([vp, ctypes.c_uint32], st),
+        "esp_moe_debug_hold_load": ([vp], st),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)

@@ -537,3 +537,26 @@ def test_refusals(mm):
         assert err.value.status == esp.ESP_ERR_INVALID_ARG
     mm.route(z, 2)   # a refusal leaves the handle usable
     mm.synchronize()
+
+
+@pytest.mark.parametrize("M", [40, 2000])
+def test_wait_that_runs_out_is_reported(mm, M):
+    """A product whose load never comes ends by its bounded waits; the handle then refuses work."""
+    from paper_2608_07971_gb300 import esp, moe
+    m = moe.Moe()
+    x, w = torch.randn(M, 1024, device="cuda"), torch.randn(300, 1024, device="cuda")
+    q = m.quantize_weight(w)
+    want = m.linear(x, q)
+    m.synchronize()
+    lib = moe.load_library()
+    esp._check(lib.esp_moe_debug_set_wait_limit(m.h, 20), "set_wait_limit")
+    esp._check(lib.esp_moe_debug_hold_load(m.h), "hold_load")
+    m.linear(x, q)
+    with pytest.raises(esp.EspError) as err:
+        m.synchronize()
+    assert err.value.status == esp.ESP_ERR_TIMEOUT
+    with pytest.raises(esp.EspError) as err:
+        m.linear(x, q)
+    assert err.value.status == esp.ESP_ERR_STATE
+    m.close()
+    assert torch.equal(mm.linear(x, q), want)   # another handle works on

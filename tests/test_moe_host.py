@@ -41,6 +41,8 @@ def test_null_handle_rejected(lib):
     assert lib.esp_moe_linear_backward(N, 0, 0, 1, N, 0, N, w, N, 1, N, 1, N, 1, N) == bad
     assert lib.esp_moe_combine(N, 0, 0, 1, 1, 0, 1, N, N, N, 1, N) == bad
     assert lib.esp_moe_combine_backward(N, 0, 0, 1, 1, 0, 1, N, 1, N, N, N, 1, N, N) == bad
+    assert lib.esp_moe_debug_set_wait_limit(N, 0) == bad
+    assert lib.esp_moe_debug_hold_load(N) == bad
     assert lib.esp_moe_synchronize(N) == bad
     assert lib.esp_moe_last_launch_count(N, ctypes.byref(n)) == bad
     lib.esp_moe_destroy(N)
