@@ -30,13 +30,15 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, two idle (whole warpgroups)
+// registers per thread of the epilogue and of the other warpgroup: 2 * 208 + 88 = 3 * 168, the launch's
+constexpr int kEpilogueRegs = 208, kOtherRegs = 88;
 constexpr int kEpilogueWarps = 8;
 constexpr int kRowsA = 128;                  // rows of A that a CTA holds
 constexpr int kStageA = kRowsA * kBlock;     // bytes
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kWaitHintNs = 1000000;
-constexpr int kStageCols = 16;               // columns of a warp's staged store
+constexpr int kStoreBytes = 128;             // of a row in a warp's staged store
+constexpr int kStageRow = kStoreBytes + 16;  // padded: no bank conflicts by rows or by columns
 constexpr int kSmemLimit = 232448;
 
 template <int CG, int BN>
@@ -46,8 +48,8 @@ struct Shape {
     static constexpr int kAcc = (int)kTmemCols / BN;
     static constexpr int kWGCols = BN / 2;   // columns of a warpgroup
     // after the stages: tile table, store staging, column scales, barriers
-    static constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4;
-    static constexpr int kStaging = kEpilogueWarps * 32 * (kStageCols + 1) * 4;
+    static constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4 + 12;   // a multiple of 16
+    static constexpr int kStaging = kEpilogueWarps * 32 * kStageRow;
     static constexpr int kColScales = 2 * 2 * kWGCols * 4;
     static constexpr int kBars = 256;
     static constexpr int kFixed = kTable + kStaging + kColScales + kBars + 1024;
@@ -67,7 +69,7 @@ struct GemmParams {
     int64_t ldo;
     bool wide_store;
     unsigned int *err;
-    uint32_t polls;
+    uint32_t wait_ms;
     int32_t hold;                    // leave out the CTAs' third load (failure detection)
 };
 
@@ -106,10 +108,11 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// Arrival on a barrier of this CTA or, through its cluster address, of another.
+// Arrival on a barrier of this CTA or, through its cluster address, of another. Relaxed: it orders the
+// tensor-memory loads before it, which have completed; a release would wait for unrelated stores.
 __device__ __forceinline__ void mbar_arrive(uint32_t cluster_addr)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
@@ -117,26 +120,40 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(kWaitHintNs)
+        : "r"(bar), "r"(parity)
         : "memory");
     return done != 0;
 }
 
-// Bounded wait (each poll lasts at most about a millisecond); gives up early once another wait of the CTA
-// did. On running out it sets the CTA's flag and the error word.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
+__device__ __forceinline__ uint64_t global_ns()
 {
-    if (mbar_try(bar, parity))
-        return true;
-    for (uint32_t i = 0; i < p.polls; ++i) {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Waits for a phase for at most `ms` milliseconds of the GPU's timer.
+__device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
+{
+    const uint64_t end = global_ns() + (uint64_t)ms * 1000000ull;
+    do {
         if (mbar_try(bar, parity))
             return true;
-        if (*dead)
+        if (dead && *dead)
             return false;
-    }
+    } while (global_ns() < end);
+    return false;
+}
+
+// Bounded wait of a role; gives up early once another wait of the CTA did. On running out it sets the CTA's
+// flag and the error word.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
+{
+    if (mbar_try(bar, parity) || mbar_wait_ms(bar, parity, p.wait_ms, dead))
+        return true;
     *dead = 1;
     atomicOr(p.err, 1u);
     return false;
@@ -209,23 +226,29 @@ __device__ __forceinline__ void fence_before()
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
 }
 
-// 32 consecutive fp32 columns of this thread's TMEM lane.
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&v)[32])
+// Starts the load of 16 consecutive 32-bit columns of this thread's TMEM lane. The registers hold them after
+// tmem_wait16, which names them so that no use of theirs moves before it.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
 {
-    uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15}, [%16];"
+        :
+          "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr)
         : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-        v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 :
+                   "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                   "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
+                   "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
 }
 
 // Barrier of a warpgroup that also ANDs a predicate over it.
@@ -307,34 +330,32 @@ __device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, i
     return true;
 }
 
-// A thread's 32 columns of a row of the output, row-major with any alignment: 32-byte stores where they
-// fit, else through the warp's staging so that a store's lanes cover consecutive columns.
+// A warp's 32 rows of 128 bytes of the output (a lane holds a row's values), through its staging buffer so
+// that the lanes of a store cover whole lines: stored straight from the registers, a store touches 32
+// lines and the warps spend a sixth to a fifth of the product's time there. Rows at or past `rows` and
+// columns at or past N are dropped.
 template <typename T>
-__device__ __forceinline__ void store_cols32(T *out, int64_t ldo, int row, int rows, int col, int N, bool wide,
-                                             const float *v, float *stage, int lane)
+__device__ __forceinline__ void store_chunk(T *out, int64_t ldo, int rows, int cols, bool wide, const float *v,
+                                            unsigned char *stage, int lane)
 {
-    if (wide && col + 32 <= N) {
-        if (row < rows) {
-            T *dst = out + row * ldo + col;
-            constexpr int V = 16 / (int)sizeof(T);
+    constexpr int C = kStoreBytes / (int)sizeof(T), V = 16 / (int)sizeof(T);
+    __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; i += V)
-                store_pack<T, V>(dst + i, v + i);
-        }
+    for (int i = 0; i < C; i += V)
+        store_pack<T, V>(reinterpret_cast<T *>(stage + lane * kStageRow) + i, v + i);
+    __syncwarp();
+    if (wide && cols >= C) {
+        const int r0 = lane >> 3, b = (lane & 7) * 16;
+#pragma unroll
+        for (int r = r0; r < 32; r += 4)
+            if (r < rows)
+                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(out + r * ldo) + b) =
+                    *reinterpret_cast<const uint4 *>(stage + r * kStageRow + b);
         return;
     }
-#pragma unroll
-    for (int h = 0; h < 32; h += kStageCols) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < kStageCols; ++i)
-            stage[lane * (kStageCols + 1) + i] = v[h + i];
-        __syncwarp();
-        const int c = lane % kStageCols, row0 = row - lane;
-        if (col + h + c < N)
-            for (int r = lane / kStageCols; r < 32 && row0 + r < rows; r += 32 / kStageCols)
-                out[(row0 + r) * ldo + col + h + c] = from_f32<T>(stage[r * (kStageCols + 1) + c]);
-    }
+    for (int r = 0; r < 32 && r < rows; ++r)
+        for (int c = lane; c < C && c < cols; c += 32)
+            out[r * ldo + c] = reinterpret_cast<const T *>(stage + r * kStageRow)[c];
 }
 
 template <int CG, int BN, bool COLS, typename T>
@@ -346,8 +367,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     unsigned char *sm = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                           ~static_cast<uintptr_t>(1023));
     int *table = reinterpret_cast<int *>(sm + S::kStages * S::kStage);
-    float *staging = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(table) + S::kTable);
-    float *colscale = staging + S::kStaging / 4;
+    unsigned char *staging = sm + S::kStages * S::kStage + S::kTable;
+    float *colscale = reinterpret_cast<float *>(staging + S::kStaging);
     uint64_t *bars = reinterpret_cast<uint64_t *>(
         (reinterpret_cast<uintptr_t>(colscale + S::kColScales / 4) + 15) & ~static_cast<uintptr_t>(15));
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, tfull = empty + 8 * S::kStages,
@@ -417,8 +438,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t w0 = blockIdx.x / CG, dw = gridDim.x / CG;
     int64_t issued = 0;   // loads issued by this CTA's producer
 
-    if (warp == 8) {
-        if (lane == 0) {
+    if (warp >= kEpilogueWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 8 && lane == 0) {
             const uint32_t full0 = CG == 1 ? full : map_rank(full, 0);
             int s = 0;
             uint32_t ph = 1;
@@ -445,8 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
-    } else if (warp == 9) {
-        if (lane == 0 && rank == 0) {
+        if (warp == 9 && lane == 0 && rank == 0) {
             constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kRowsA * CG >> 4) << 24);
             int s = 0, acc = 0;
             uint32_t ph = 0, aph = 1;
@@ -476,10 +497,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
         }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
         const int wg = warp >> 2, quarter = warp & 3;
         const uint32_t lane_cols = ((uint32_t)(32 * quarter) << 16) + (uint32_t)(wg * S::kWGCols);
         const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
-        float *stage = staging + warp * 32 * (kStageCols + 1);
+        unsigned char *stage = staging + warp * 32 * kStageRow;
         float *cs = colscale + wg * 2 * S::kWGCols;
         int acc = 0;
         uint32_t aph = 0;
@@ -498,26 +520,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             // this block's scale factor (FWD: row times column block; COLS: row, columns in shared memory),
             // fetched a block ahead
             const int nb = min(c0, p.N - 1) / kBlock;
-            auto scale_of = [&](int kb) -> float {
-                if (kb >= t.kb1 || row >= rows)
-                    return 0.0f;
-                if (COLS)
-                    return p.scale_a[(int64_t)kb * p.lda_scale + m];
-                return p.scale_a[m * p.lda_scale + kb] * p.scale_b[t.e * p.sb_e + nb * p.sb_n + kb * p.sb_k];
+            float next_a = 0.0f, next_b = 0.0f;
+            auto fetch = [&](int kb) {
+                if (kb >= t.kb1)
+                    return;
+                if (COLS) {
+                    // thread i of the warpgroup brings column i's
+                    next_a = row < rows ? p.scale_a[(int64_t)kb * p.lda_scale + m] : 0.0f;
+                    next_b = row < S::kWGCols && c0 + row < p.N ? p.scale_b[(int64_t)kb * p.sb_k + c0 + row] : 0.0f;
+                } else {
+                    next_a = row < rows ? p.scale_a[m * p.lda_scale + kb] : 0.0f;
+                    next_b = p.scale_b[t.e * p.sb_e + nb * p.sb_n + kb * p.sb_k];
+                }
             };
-            auto col_scale_of = [&](int kb) -> float {
-                const int c = c0 + row;   // thread i of the warpgroup brings column i's
-                return row < S::kWGCols && kb < t.kb1 && c < p.N ? p.scale_b[(int64_t)kb * p.sb_k + c] : 0.0f;
-            };
-            float next = scale_of(t.kb0), next_col = COLS ? col_scale_of(t.kb0) : 0.0f;
+            fetch(t.kb0);
             for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                const float scale = next;
+                const float scale = COLS ? next_a : next_a * next_b;
                 float *csb = cs + (kb & 1) * S::kWGCols;
                 if (COLS && row < S::kWGCols)
-                    csb[row] = next_col;
-                next = scale_of(kb + 1);
-                if (COLS)
-                    next_col = col_scale_of(kb + 1);
+                    csb[row] = next_b;
+                fetch(kb + 1);
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, aph, p, dead));
                 if (COLS)
                     ok = wg_sync_and(1 + wg, ok);
@@ -525,16 +547,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                     break;
                 fence_after();
                 if (some) {
+// 16 columns at a time, the next ones on their way meanwhile
+                    uint32_t v[2][16];
+                    tmem_ld16(tmem + acc * BN + lane_cols, v[0]);
 #pragma unroll
-                    for (int c = 0; c < S::kWGCols; c += 32) {
-                        float v[32];
-                        tmem_ld32(tmem + acc * BN + lane_cols + c, v);
+                    for (int c = 0; c < S::kWGCols; c += 16) {
+                        uint32_t(&now)[16] = v[(c >> 4) & 1];
+                        tmem_wait16(now);
+                        if (c + 16 < S::kWGCols)
+                            tmem_ld16(tmem + acc * BN + lane_cols + c + 16, v[((c >> 4) + 1) & 1]);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
+                        for (int i = 0; i < 16; ++i) {
                             if (COLS)
-                                sum[c + i] = fmaf(v[i] * scale, csb[c + i], sum[c + i]);
+                                sum[c + i] = fmaf(__uint_as_float(now[i]) * scale, csb[c + i], sum[c + i]);
                             else
-                                sum[c + i] = fmaf(v[i], scale, sum[c + i]);
+                                sum[c + i] = fmaf(__uint_as_float(now[i]), scale, sum[c + i]);
                         }
                     }
                 }
@@ -550,11 +577,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok || !some)
                 continue;
             T *out = static_cast<T *>(p.out) + (COLS ? (int64_t)t.e * p.rows_b * p.ldo : 0) +
-                     (t.m0 + rank * kRowsA) * p.ldo;
+                     (t.m0 + rank * kRowsA + 32 * quarter) * p.ldo + c0;
+            constexpr int C = kStoreBytes / (int)sizeof(T);
 #pragma unroll
-            for (int c = 0; c < S::kWGCols; c += 32)
+            for (int c = 0; c < S::kWGCols; c += C)
                 if (c0 + c < p.N)
-                    store_cols32<T>(out, p.ldo, row, rows, c0 + c, p.N, p.wide_store, sum + c, stage, lane);
+                    store_chunk<T>(out + c, p.ldo, rows - 32 * quarter, p.N - c0 - c, p.wide_store, sum + c, stage, lane);
         }
     }
     fence_before();
@@ -565,13 +593,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         // CTAs'), then the MMAs
         if (warp == 8 && lane == 0 && rank == 0)
             for (int64_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
-                for (int poll = 0; poll < 50; ++poll)
-                    if (mbar_try(full + 8 * (uint32_t)(i % S::kStages), (uint32_t)(i / S::kStages) & 1))
-                        break;
+                mbar_wait_ms(full + 8 * (uint32_t)(i % S::kStages), (uint32_t)(i / S::kStages) & 1, 20, nullptr);
         if (warp == 9 && lane == 0 && rank == 0) {
             mma_commit<CG>(drain);
-            for (int poll = 0; poll < 1000 && !mbar_try(drain, 0); ++poll) {
-            }
+            mbar_wait_ms(drain, 0, 1000, nullptr);
         }
     }
     fence_before();
@@ -672,7 +697,7 @@ GemmParams common(esp_moe *m)
 {
     GemmParams p{};
     p.err = m->d_err;
-    p.polls = m->wait_polls;
+    p.wait_ms = m->wait_ms;
     p.hold = m->hold_load ? 1 : 0;
     m->hold_load = false;   // the hook holds one launch only
     return p;

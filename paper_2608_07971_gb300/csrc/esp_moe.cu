@@ -444,7 +444,7 @@ esp_status esp_moe_debug_set_wait_limit(esp_moe *m, uint32_t limit_ms)
     const esp_status st = begin(m);
     if (st != ESP_OK)
         return st;
-    m->wait_polls = limit_ms == 0 ? kMoeWaitPolls : limit_ms;
+    m->wait_ms = limit_ms == 0 ? kMoeWaitMs : limit_ms;
     return ESP_OK;
 }
 

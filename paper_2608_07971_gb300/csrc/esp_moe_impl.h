@@ -8,7 +8,7 @@
 
 #include "esp_moe.h"
 
-constexpr uint32_t kMoeWaitPolls = 4096;   // about 4 s of waiting before a timeout is reported
+constexpr uint32_t kMoeWaitMs = 4000;   // a bounded wait's limit
 
 struct esp_moe {
     int device = 0;
@@ -22,9 +22,9 @@ struct esp_moe {
     unsigned int *d_err = nullptr;   // device error word (timeouts of the product kernels)
     unsigned int *d_ticket = nullptr;   // arrival counters, zero between launches
     int max_pairs = 0;               // CTA pairs of the product kernel that run at once (0: not asked yet)
-    // failure-detection hooks (esp_moe.h): polls of a bounded wait (about 1 ms each), and the next
+    // failure-detection hooks (esp_moe.h): limit of a bounded wait, and the next
     // product launch leaving out one load
-    uint32_t wait_polls = kMoeWaitPolls;
+    uint32_t wait_ms = kMoeWaitMs;
     bool hold_load = false;
 };
 
