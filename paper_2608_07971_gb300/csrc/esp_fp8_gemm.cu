@@ -31,8 +31,8 @@ namespace esp_moe_impl {
 namespace {
 
 constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, two idle (whole warpgroups)
-// registers per thread of the epilogue and of the other warpgroup: 2 * 208 + 88 = 3 * 168, the launch's
-constexpr int kEpilogueRegs = 208, kOtherRegs = 88;
+// registers per thread of the epilogue and of the other warpgroup: 2 * 216 + 72 = 3 * 168, the launch's
+constexpr int kEpilogueRegs = 216, kOtherRegs = 72;
 constexpr int kEpilogueWarps = 8;
 constexpr int kRowsA = 128;                  // rows of A that a CTA holds
 constexpr int kStageA = kRowsA * kBlock;     // bytes
@@ -59,8 +59,8 @@ struct Shape {
 };
 
 struct GemmParams {
-    int64_t M, lda_scale;            // rows of A (FWD); leading dimension of A's scales
-    int32_t E, N, K;                 // out columns N (FWD) / K (COLS), see the launchers
+    int32_t M, E, N, K;              // rows over all experts; N: the output's columns; K: of the inner axis (FWD)
+    int64_t sa_row, sa_k;            // steps of A's scales by row and block
     int32_t rows_b;                  // rows of B per expert (FWD)
     const float *scale_a, *scale_b;
     int64_t sb_e, sb_n, sb_k;
@@ -227,7 +227,7 @@ __device__ __forceinline__ void fence_before()
 }
 
 // Starts the load of 16 consecutive 32-bit columns of this thread's TMEM lane. The registers hold them after
-// tmem_wait16, which names them so that no use of theirs moves before it.
+// tmem_wait, which names them so that no use of theirs moves before it.
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
 {
     asm volatile(
@@ -240,15 +240,41 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
+__device__ __forceinline__ void pin16(uint32_t (&r)[16])
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
+    asm volatile(""
                  :
                    "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
                    "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
-                   "+r"(r[14]), "+r"(r[15])
-                 :
-                 : "memory");
+                   "+r"(r[14]), "+r"(r[15]));
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[N][16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int h = 0; h < N; ++h)
+        pin16(r[h]);
+}
+
+// (c, d) += (a, b) * (s, t) and (a, b) *= s, each one instruction on pairs of registers.
+__device__ __forceinline__ void fma_pair(float &c, float &d, float a, float b, float s, float t)
+{
+    asm("{\n\t.reg .b64 x, y, z;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%0, %1};\n\t"
+        "fma.rn.f32x2 z, x, y, z;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "+f"(c), "+f"(d)
+        : "f"(a), "f"(b), "f"(s), "f"(t));
+}
+
+__device__ __forceinline__ void mul_pair(float &a, float &b, float s)
+{
+    asm("{\n\t.reg .b64 x, y;\n\t"
+        "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\t"
+        "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(a), "+f"(b)
+        : "f"(s));
 }
 
 // Barrier of a warpgroup that also ANDs a predicate over it.
@@ -266,65 +292,57 @@ __device__ __forceinline__ bool wg_sync_and(int id, bool v)
     return r != 0;
 }
 
-__device__ __forceinline__ int64_t clamp_row(int64_t v, int64_t M)
-{
-    return max((int64_t)0, min(M, v));
-}
-
 // Expert e's rows [lo, hi).
-__device__ __forceinline__ void expert_rows(const GemmParams &p, int e, int64_t &lo, int64_t &hi)
+__device__ __forceinline__ void expert_rows(const GemmParams &p, int e, int &lo, int &hi)
 {
-    lo = p.offsets ? clamp_row(p.offsets[e], p.M) : 0;
-    hi = p.offsets ? max(lo, clamp_row(p.offsets[e + 1], p.M)) : p.M;
+    lo = p.offsets ? max(0, min(p.M, p.offsets[e])) : 0;
+    hi = p.offsets ? max(lo, min(p.M, p.offsets[e + 1])) : p.M;
 }
 
-// One tile of the list: rows m0 .. m0 + rows - 1 of the output's group e (a CTA of a pair adds its share),
-// columns n0 .., blocks kb0 .. kb1 - 1.
+// One tile of the list: rows m0 .. m0 + rows - 1 of expert e (COLS: of its output), columns n0 .., blocks
+// kb0 .. kb1 - 1.
 struct Tile {
-    int e, rows, n0, kb0, kb1;
-    int64_t m0;
+    int e, m0, rows, n0, kb0, kb1;
 };
 
-// table[e]: row tiles (FWD) or blocks (COLS) of the experts before e.
+// table[e]: row tiles (COLS: blocks) of the experts before e. Tiles run over an expert's rows first, so that
+// the tiles in flight share columns of B.
 template <int CG, int BN, bool COLS>
-__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int64_t w, Tile &t)
+__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int w, Tile &t)
 {
     constexpr int BM = kRowsA * CG;
     const int nt = (p.N + BN - 1) / BN;
     if (!COLS) {
-        const int64_t total = (int64_t)table[p.E] * nt;
-        if (w >= total)
+        if (w >= table[p.E] * nt)
             return false;
         int lo = 0, hi = p.E;   // the expert whose tiles hold w
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((int64_t)table[mid] * nt <= w)
+            if (table[mid] * nt <= w)
                 lo = mid;
             else
                 hi = mid;
         }
         t.e = lo;
-        const int mt = table[lo + 1] - table[lo];
-        const int64_t i = w - (int64_t)table[lo] * nt;
-        int64_t a, b;
+        const int mt = table[lo + 1] - table[lo], i = w - table[lo] * nt;
+        int a, b;
         expert_rows(p, lo, a, b);
-        const int64_t skip = (i % mt) * BM;
-        t.m0 = a + skip;
-        t.rows = (int)min((int64_t)BM, b - t.m0);
-        t.n0 = (int)(i / mt) * BN;
+        t.m0 = a + (i % mt) * BM;
+        t.rows = min(BM, b - t.m0);
+        t.n0 = (i / mt) * BN;
         t.kb0 = 0;
         t.kb1 = (p.K + kBlock - 1) / kBlock;
         return true;
     }
     const int mt = (p.rows_b + BM - 1) / BM;   // rows_b: output rows per expert
-    const int64_t per = (int64_t)mt * nt;
+    const int per = mt * nt;
     if (w >= per * p.E)
         return false;
-    t.e = (int)(w / per);
-    const int64_t i = w % per;
+    t.e = w / per;
+    const int i = w % per;
     t.m0 = (i % mt) * BM;
-    t.rows = (int)min((int64_t)BM, (int64_t)p.rows_b - t.m0);
-    t.n0 = (int)(i / mt) * BN;
+    t.rows = min(BM, p.rows_b - t.m0);
+    t.n0 = (i / mt) * BN;
     t.kb0 = table[t.e];
     t.kb1 = table[t.e + 1];
     return true;
@@ -397,10 +415,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int e0 = 0; e0 < p.E; e0 += 32) {
             int n = 0;
             if (e0 + lane < p.E) {
-                int64_t lo, hi;
+                int lo, hi;
                 expert_rows(p, e0 + lane, lo, hi);
-                const int64_t per = COLS ? kBlock : kRowsA * CG;
-                n = (int)((hi - lo + per - 1) / per);
+                constexpr int per = COLS ? kBlock : kRowsA * CG;
+                n = (hi - lo) / per + ((hi - lo) % per != 0);
             }
             int s = n;
 #pragma unroll
@@ -435,8 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         cluster_sync();
     fence_after();
     const uint32_t tmem = *slot;
-    const int64_t w0 = blockIdx.x / CG, dw = gridDim.x / CG;
-    int64_t issued = 0;   // loads issued by this CTA's producer
+    const int w0 = blockIdx.x / CG, dw = gridDim.x / CG;
+    uint32_t issued = 0;   // loads issued by this CTA's producer
 
     if (warp >= kEpilogueWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -446,8 +464,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t ph = 1;
             bool ok = true;
             Tile t;
-            for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
-                const int ya = (int)t.m0 + (int)rank * kRowsA;
+            for (int w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
+                const int ya = t.m0 + (int)rank * kRowsA;
                 const int yb = (COLS ? 0 : t.e * p.rows_b) + t.n0 + (int)rank * S::kRowsB;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!(ok = mbar_wait(empty + 8 * s, ph, p, dead)))
@@ -473,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint32_t ph = 0, aph = 1;
             bool ok = true;
             Tile t;
-            for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw)
+            for (int w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw)
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!(ok = mbar_wait(tempty + 8 * acc, aph, p, dead)) ||
                         !(ok = mbar_wait(full + 8 * s, ph, p, dead)))
@@ -503,72 +521,94 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
         unsigned char *stage = staging + warp * 32 * kStageRow;
         float *cs = colscale + wg * 2 * S::kWGCols;
-        int acc = 0;
+        int acc = 0, turn = 0;
         uint32_t aph = 0;
         bool ok = true;
         Tile t;
-        for (int64_t w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
+        for (int w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw) {
             const int row = 32 * quarter + lane;                    // of this CTA's 128
             const int rows = t.rows - (int)rank * kRowsA;           // that exist
-            const int64_t m = t.m0 + rank * kRowsA + row;
             const bool some = 32 * quarter < rows;                  // a row of this warp exists
             const int c0 = t.n0 + wg * S::kWGCols;
             float sum[S::kWGCols];
 #pragma unroll
             for (int i = 0; i < S::kWGCols; ++i)
                 sum[i] = 0.0f;
-            // this block's scale factor (FWD: row times column block; COLS: row, columns in shared memory),
-            // fetched a block ahead
-            const int nb = min(c0, p.N - 1) / kBlock;
+            // Scales: a row's (of the last row past the end) and the columns' of this warpgroup: one value, or
+            // (COLS) thread i brings column i's to shared memory. Fetched a block ahead.
+            const int ra = t.m0 + min((int)rank * kRowsA + row, t.rows - 1);
+            const float *pa = p.scale_a + ra * p.sa_row + t.kb0 * p.sa_k;
+            const float *pb = p.scale_b + (COLS ? (int64_t)min(c0 + row, p.N - 1)
+                                                : t.e * p.sb_e + min(c0, p.N - 1) / kBlock * p.sb_n) +
+                              t.kb0 * p.sb_k;
             float next_a = 0.0f, next_b = 0.0f;
-            auto fetch = [&](int kb) {
-                if (kb >= t.kb1)
-                    return;
-                if (COLS) {
-                    // thread i of the warpgroup brings column i's
-                    next_a = row < rows ? p.scale_a[(int64_t)kb * p.lda_scale + m] : 0.0f;
-                    next_b = row < S::kWGCols && c0 + row < p.N ? p.scale_b[(int64_t)kb * p.sb_k + c0 + row] : 0.0f;
-                } else {
-                    next_a = row < rows ? p.scale_a[m * p.lda_scale + kb] : 0.0f;
-                    next_b = p.scale_b[t.e * p.sb_e + nb * p.sb_n + kb * p.sb_k];
-                }
-            };
-            fetch(t.kb0);
-            for (int kb = t.kb0; kb < t.kb1; ++kb) {
+            if (t.kb0 < t.kb1) {
+                next_a = *pa;
+                next_b = *pb;
+            }
+            for (int left = t.kb1 - t.kb0; left > 0; --left) {
                 const float scale = COLS ? next_a : next_a * next_b;
-                float *csb = cs + (kb & 1) * S::kWGCols;
+                // the buffers alternate over all blocks of all tiles: a block's is written again only after the
+                // next block's barrier, which every thread passes when it is done with this one's
+                float *csb = cs + turn * S::kWGCols;
+                turn ^= 1;
                 if (COLS && row < S::kWGCols)
                     csb[row] = next_b;
-                fetch(kb + 1);
+                if (left > 1) {
+                    pa += p.sa_k;
+                    pb += p.sb_k;
+                    next_a = *pa;
+                    next_b = *pb;
+                }
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, aph, p, dead));
                 if (COLS)
                     ok = wg_sync_and(1 + wg, ok);
                 if (!ok)
                     break;
                 fence_after();
+                // The stage is given back as soon as its last columns are in registers: the MMAs of the block
+                // after next wait for it, and what the stage's turn takes beyond the other stage's MMAs
+                // is time that the tensor core stands still.
                 if (some) {
-// 16 columns at a time, the next ones on their way meanwhile
-                    uint32_t v[2][16];
-                    tmem_ld16(tmem + acc * BN + lane_cols, v[0]);
+                    const uint32_t src = tmem + acc * BN + lane_cols;
+                    constexpr int D = 3, chunks = S::kWGCols / 16;   // loads in flight, loads in all
+                    uint32_t v[D][16];
 #pragma unroll
-                    for (int c = 0; c < S::kWGCols; c += 16) {
-                        uint32_t(&now)[16] = v[(c >> 4) & 1];
-                        tmem_wait16(now);
-                        if (c + 16 < S::kWGCols)
-                            tmem_ld16(tmem + acc * BN + lane_cols + c + 16, v[((c >> 4) + 1) & 1]);
+                    for (int c = 0; c < D; ++c)
+                        tmem_ld16(src + 16 * c, v[c]);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (COLS)
-                                sum[c + i] = fmaf(__uint_as_float(now[i]) * scale, csb[c + i], sum[c + i]);
-                            else
-                                sum[c + i] = fmaf(__uint_as_float(now[i]), scale, sum[c + i]);
+                    for (int c0 = 0; c0 < chunks; c0 += D) {
+                        tmem_wait(v);
+                        if (c0 + D >= chunks) {
+                            fence_before();
+                            __syncwarp();
+                            if (lane == 0)
+                                mbar_arrive(tempty0 + 8 * acc);
+                        }
+#pragma unroll
+                        for (int j = 0; j < D; ++j) {
+                            const int c = c0 + j;
+                            if (c >= chunks)
+                                continue;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                float &lo = sum[16 * c + i], &hi = sum[16 * c + i + 1];
+                                float a = __uint_as_float(v[j][i]), b = __uint_as_float(v[j][i + 1]);
+                                if (COLS) {
+                                    const float2 s2 = *reinterpret_cast<const float2 *>(csb + 16 * c + i);
+                                    mul_pair(a, b, scale);
+                                    fma_pair(lo, hi, a, b, s2.x, s2.y);
+                                } else {
+                                    fma_pair(lo, hi, a, b, scale, scale);
+                                }
+                            }
+                            if (c + D < chunks)
+                                tmem_ld16(src + 16 * (c + D), v[j]);
                         }
                     }
-                }
-                fence_before();
-                __syncwarp();
-                if (lane == 0)
+                } else if (lane == 0) {
                     mbar_arrive(tempty0 + 8 * acc);
+                }
                 if (++acc == S::kAcc) {
                     acc = 0;
                     aph ^= 1;
@@ -576,8 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok || !some)
                 continue;
-            T *out = static_cast<T *>(p.out) + (COLS ? (int64_t)t.e * p.rows_b * p.ldo : 0) +
-                     (t.m0 + rank * kRowsA + 32 * quarter) * p.ldo + c0;
+            T *out = static_cast<T *>(p.out) + ((COLS ? (int64_t)t.e * p.rows_b : 0) + t.m0 + rank * kRowsA + 32 * quarter) * p.ldo + c0;
             constexpr int C = kStoreBytes / (int)sizeof(T);
 #pragma unroll
             for (int c = 0; c < S::kWGCols; c += C)
@@ -592,8 +631,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         // nothing may still land in this CTA's memory: copies first (the leader's barriers count both
         // CTAs'), then the MMAs
         if (warp == 8 && lane == 0 && rank == 0)
-            for (int64_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
-                mbar_wait_ms(full + 8 * (uint32_t)(i % S::kStages), (uint32_t)(i / S::kStages) & 1, 20, nullptr);
+            for (uint32_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
+                mbar_wait_ms(full + 8 * (i % S::kStages), (i / S::kStages) & 1, 20, nullptr);
         if (warp == 9 && lane == 0 && rank == 0) {
             mma_commit<CG>(drain);
             mbar_wait_ms(drain, 0, 1000, nullptr);
@@ -710,8 +749,9 @@ cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
         GemmParams p = common(m);
-        p.M = a.M;
-        p.lda_scale = a.lds;
+        p.M = (int32_t)a.M;
+        p.sa_row = a.lds;
+        p.sa_k = 1;
         p.E = a.E;
         p.N = p.rows_b = a.N;
         p.K = a.K;
@@ -737,8 +777,9 @@ cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
 cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &a)
 {
     GemmParams p = common(m);
-    p.M = a.M;
-    p.lda_scale = a.lds_a;
+    p.M = (int32_t)a.M;
+    p.sa_row = 1;
+    p.sa_k = a.lds_a;
     p.E = a.E;
     p.N = a.K;
     p.rows_b = a.N;

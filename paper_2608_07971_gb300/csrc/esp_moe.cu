@@ -14,6 +14,7 @@ using namespace esp_moe_impl;
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffff00;   // row counts fit int32 with a tile to spare
+constexpr int64_t kMaxTiles = 1 << 30;
 
 esp_status fail(esp_moe *m)
 {
@@ -104,8 +105,12 @@ bool good_weight(const esp_moe_weight *w)
 
 bool good_product(int64_t T, int64_t M, const int32_t *rows, const esp_moe_weight *w, const int32_t *offsets)
 {
-    return good_weight(w) && T >= 0 && M >= 0 && T <= kMaxRows && M <= kMaxRows && (rows || M == T) &&
-           (offsets || w->E == 1);
+    if (!good_weight(w) || T < 0 || M < 0 || T > kMaxRows || M > kMaxRows || (!rows && M != T) ||
+        (!offsets && w->E != 1))
+        return false;
+    // the kernels number their tiles in int32
+    const int64_t nb = ceil_div(w->N, kBlock), kb = ceil_div(w->K, kBlock);
+    return (M / kBlock + w->E) * std::max(nb, kb) <= kMaxTiles && w->E * nb * kb <= kMaxTiles;
 }
 
 int64_t round_up(int64_t v, int64_t to)
