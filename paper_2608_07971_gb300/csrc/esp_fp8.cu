@@ -7,6 +7,8 @@
 // finite makes inv 0 and the scale NaN, so that every result that reads the block shows it.
 
 #include <algorithm>
+#include <cstring>
+#include <type_traits>
 
 #include <cuda_fp8.h>
 
@@ -37,251 +39,356 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
     return lo | (hi << 16);
 }
 
-__device__ __forceinline__ bool is_finite(float v)
+// Magnitudes compare as integers: a value's bits without the sign, NaN above infinity above all others.
+template <typename T>
+__device__ __forceinline__ float magnitude_value(uint32_t bits);
+template <>
+__device__ __forceinline__ float magnitude_value<float>(uint32_t bits) { return __uint_as_float(bits); }
+template <>
+__device__ __forceinline__ float magnitude_value<__nv_bfloat16>(uint32_t bits) { return __uint_as_float(bits << 16); }
+template <>
+__device__ __forceinline__ float magnitude_value<__half>(uint32_t bits)
 {
-    return fabsf(v) <= 3.4028234663852886e38f;
+    return __half2float(__ushort_as_half((unsigned short)bits));
 }
 
-// ---- rows: 16 lanes per block of 128, 8 elements per lane
+// Eight consecutive elements of a row, as stored.
+template <typename T>
+struct Eight {
+    static constexpr int kWords = (int)sizeof(T) * 2;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            w[i] = 0;
+    }
+    // n of them exist (others become zero); aligned: p is a multiple of 16 bytes
+    __device__ __forceinline__ void load(const T *p, int n, bool aligned)
+    {
+        if (aligned && n >= 8) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint32_t *>(p) + i);
+                w[i] = v.x;
+                w[i + 1] = v.y;
+                w[i + 2] = v.z;
+                w[i + 3] = v.w;
+            }
+            return;
+        }
+        T v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = i < n ? p[i] : from_f32<T>(0.0f);
+        memcpy(w, v, sizeof(v));
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(w[i]);
+        else if constexpr (std::is_same<T, __half>::value)
+            return __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (16 * (i & 1)))));
+        else
+            return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+    // words of magnitudes: one per element, or two elements in the halves of a word
+    __device__ __forceinline__ uint32_t magnitudes(int i) const
+    {
+        return w[i] & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu);
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+    {
+        return sizeof(T) == 4 ? max(a, b) : __vmaxu2(a, b);
+    }
+    // the larger of a word's halves
+    static __device__ __forceinline__ uint32_t flat(uint32_t m)
+    {
+        return sizeof(T) == 4 ? m : max(m & 0xffffu, m >> 16);
+    }
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        uint32_t m = magnitudes(0);
+#pragma unroll
+        for (int i = 1; i < kWords; ++i)
+            m = larger(m, magnitudes(i));
+        return m;
+    }
+};
+
+// Scale and inverse of a block from the bits of its greatest magnitude.
+template <typename T>
+__device__ __forceinline__ void scale_of(uint32_t bits, float &scale, float &inv)
+{
+    const float amax = magnitude_value<T>(bits);
+    block_scale(amax, amax <= 3.4028234663852886e38f, scale, inv);
+}
+
+// With an inverse of 0 (a block that is not finite) every code is 0: infinities and NaN times 0 are NaN,
+// so they are replaced.
+template <typename T>
+__device__ __forceinline__ uint2 codes8(const Eight<T> &x, float inv)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = x.get(i);
+    if (inv == 0.0f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = 0.0f;
+    }
+    return make_uint2(codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv));
+}
+
+// ---- rows: 4 lanes per block of 128, four times 8 elements per lane. Bound by the bytes; a block's two
+// divisions are done by its 4 lanes only, and a lane's four loads are in flight at once.
 
 constexpr int kRowThreads = 256;
+constexpr int kRowBlocks = kRowThreads / 4;   // of a CTA
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const QuantRowsArgs a, int blocks_k, bool aligned)
 {
-    const int lane16 = threadIdx.x & 15;
-    const int64_t total = a.M * blocks_k;
-    const int64_t stride = (int64_t)gridDim.x * (kRowThreads / 16);
-    const int64_t rounds = (total + stride - 1) / stride;   // whole warps take every turn of the loop
-    int64_t i = (int64_t)blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4);
-    for (int64_t turn = 0; turn < rounds; ++turn, i += stride) {
-        const bool on = i < total;
-        const int64_t row = on ? i / blocks_k : 0;
-        const int kb = on ? (int)(i - row * blocks_k) : 0;
-        int64_t src = row;
-        if (on && a.rows)
-            src = a.rows[row];
-        const bool there = on && src >= 0 && src < a.T;
-        const int k0 = kb * kBlock + lane16 * 8;
-        float v[8];
+    const int lane4 = threadIdx.x & 3;
+    const int64_t total = a.M * blocks_k, i = (int64_t)blockIdx.x * kRowBlocks + (threadIdx.x >> 2);
+    const bool on = i < total;
+    const int64_t row = !on ? 0 : total <= 0x7fffffff ? (int64_t)((uint32_t)i / (uint32_t)blocks_k) : i / blocks_k;
+    const int kb = (int)(i - row * blocks_k);
+    int64_t src = row;
+    if (on && a.rows)
+        src = a.rows[row];
+    const bool there = on && src >= 0 && src < a.T;
+    const int k0 = kb * kBlock + lane4 * 8;
+    const T *p = static_cast<const T *>(a.x) + src * a.ldx + k0;
+    Eight<T> x[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = 0.0f;
-        if (there) {
-            const T *p = static_cast<const T *>(a.x) + src * a.ldx + k0;
-            constexpr int W = 16 / (int)sizeof(T) < 8 ? 16 / (int)sizeof(T) : 8;
-            if (aligned && k0 + 8 <= a.K) {
-#pragma unroll
-                for (int c = 0; c < 8 / W; ++c)
-                    load_pack<T, W>(p + c * W, v + c * W);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k0 + j < a.K)
-                        v[j] = to_f32(p[j]);
-            }
-        }
-        float amax = 0.0f;
-        bool finite = true;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            amax = fmaxf(amax, fabsf(v[j]));
-            finite = finite && is_finite(v[j]);
-        }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            finite = __shfl_xor_sync(0xffffffffu, (int)finite, o) && finite;
-        }
-        float scale, inv;
-        block_scale(amax, finite, scale, inv);
-        if (!on)
-            continue;
-        if (!finite) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                v[j] = 0.0f;
-        }
-        // codes past K (up to the padded row) are zero
-        uint2 q;
-        q.x = codes4(v[0], v[1], v[2], v[3], inv);
-        q.y = codes4(v[4], v[5], v[6], v[7], inv);
-        if (k0 < a.ldq)
-            *reinterpret_cast<uint2 *>(a.q + row * a.ldq + k0) = q;
-        if (lane16 == 0)
-            a.scale[row * a.lds + kb] = scale;
+    for (int c = 0; c < 4; ++c) {
+        x[c].zero();
+        if (there)
+            x[c].load(p + 32 * c, a.K - k0 - 32 * c, aligned);
     }
-}
-
-// ---- columns: a CTA takes 128 positions of an expert's run and 64 columns
-
-constexpr int kColTile = 64;
-constexpr int kColThreads = 256;
-
-// Expert and first source row of the run of 128 positions number `tile` (false past the last). The
-// offsets are read by every thread in turn: at most 1024 experts.
-__device__ bool find_run(const int32_t *offsets, int E, int64_t M, int64_t tile, int64_t &row0, int &n)
-{
-    int64_t base = 0;
-    for (int e = 0; e < E; ++e) {
-        const int64_t a = offsets ? max((int64_t)0, min(M, (int64_t)offsets[e])) : 0;
-        const int64_t b = offsets ? max(a, min(M, (int64_t)offsets[e + 1])) : M;
-        const int64_t runs = (b - a + kBlock - 1) / kBlock;
-        if (tile < base + runs) {
-            row0 = a + (tile - base) * kBlock;
-            n = (int)min((int64_t)kBlock, b - row0);
-            return true;
-        }
-        base += runs;
-    }
-    return false;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kColThreads) k_quant_cols(const QuantColsArgs a)
-{
-    __shared__ float tile[kBlock][kColTile + 1];
-    __shared__ int64_t s_row0;
-    __shared__ int s_n;
-    if (threadIdx.x == 0) {
-        int64_t row0 = 0;
-        int n = 0;
-        s_n = find_run(a.offsets, a.E, a.M, blockIdx.x, row0, n) ? n : 0;
-        s_row0 = row0;
-    }
-    __syncthreads();
-    const int n = s_n;
-    if (n == 0)
+    uint32_t m = x[0].largest();
+#pragma unroll
+    for (int c = 1; c < 4; ++c)
+        m = Eight<T>::larger(m, x[c].largest());
+    m = Eight<T>::flat(m);
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    if (!on)
         return;
-    const int c0 = blockIdx.y * kColTile;
-    for (int i = threadIdx.x; i < kBlock * kColTile; i += kColThreads) {
-        const int r = i / kColTile, c = i % kColTile;
-        float v = 0.0f;
-        if (r < n && c0 + c < a.K) {
-            const int64_t src = a.rows ? a.rows[s_row0 + r] : s_row0 + r;
-            if (src >= 0 && src < a.T)
-                v = to_f32(static_cast<const T *>(a.x)[src * a.ldx + c0 + c]);
-        }
-        tile[r][c] = v;
-    }
-    __syncthreads();
-    // four threads per column, 32 positions each
-    const int c = threadIdx.x >> 2, part = threadIdx.x & 3;
-    float amax = 0.0f;
-    bool finite = true;
-    for (int r = 0; r < 32; ++r) {
-        const float v = tile[part * 32 + r][c];
-        amax = fmaxf(amax, fabsf(v));
-        finite = finite && is_finite(v);
-    }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        finite = __shfl_xor_sync(0xffffffffu, (int)finite, o) && finite;
-    }
     float scale, inv;
-    block_scale(amax, finite, scale, inv);
-    if (c0 + c >= a.K)
-        return;
-    uint32_t q[8];
+    scale_of<T>(m, scale, inv);
+    uint8_t *q = a.q + row * a.ldq + k0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        float v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = finite ? tile[part * 32 + 4 * j + i][c] : 0.0f;
-        q[j] = codes4(v[0], v[1], v[2], v[3], inv);
-    }
-    uint4 *dst = reinterpret_cast<uint4 *>(a.q + (int64_t)(c0 + c) * a.ldq + (int64_t)blockIdx.x * kBlock + part * 32);
-    dst[0] = make_uint4(q[0], q[1], q[2], q[3]);
-    dst[1] = make_uint4(q[4], q[5], q[6], q[7]);
-    if (part == 0)
-        a.scale[(int64_t)blockIdx.x * a.lds + c0 + c] = scale;
+    for (int c = 0; c < 4; ++c)
+        if (k0 + 32 * c < a.ldq)   // codes past K, up to the padded row, are zero
+            *reinterpret_cast<uint2 *>(q + 32 * c) = codes8<T>(x[c], inv);
+    if (lane4 == 0)
+        a.scale[row * a.lds + kb] = scale;
 }
 
-// ---- weights: a CTA per block of 128 x 128
+// ---- tiles of 128 x 128: thread (r, c) of 16 x 16 holds 8 consecutive columns of every 16th row
 
-constexpr int kWThreads = 512;
+constexpr int kTileThreads = 256;
+constexpr int kPitch = kBlock / 4 + 1;   // words of a row of codes in shared memory
 
-template <typename T>
-__global__ void __launch_bounds__(kWThreads) k_quant_weight(const T *w, int64_t ldw, const esp_moe_weight o, bool aligned)
+struct TileSmem {
+    uint32_t codes[kBlock][kPitch];
+    uint32_t turned[kBlock][kPitch];
+    uint32_t high[16][kBlock];           // greatest magnitudes by thread row and column
+    float inv[kBlock];
+};
+
+// codes -> turned: bytes (row, column) exchanged, in 4 x 4 squares. Called by the whole CTA between barriers.
+__device__ __forceinline__ void turn_codes(TileSmem &s)
 {
-    __shared__ float red[kWThreads / 32];
-    __shared__ int bad;
-    __shared__ uint32_t codes[kBlock][kBlock / 4 + 1];
-    const int kb = blockIdx.x, nb = blockIdx.y, e = blockIdx.z;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x == 0)
-        bad = 0;
-    __syncthreads();
-    // thread: 4 columns (4 * lane) of the rows warp, warp + 16, ...
-    constexpr int kRows = kBlock / (kWThreads / 32);
-    float v[kRows][4];
-    const int k0 = kb * kBlock + 4 * lane;
-    float amax = 0.0f;
-    bool finite = true;
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        const int n = nb * kBlock + warp + r * (kWThreads / 32);
+    for (int i = threadIdx.x; i < 32 * 32; i += kTileThreads) {
+        // 8 x 4 squares per warp: its reads fall on 32 banks
+        const int a = (i & 7) | ((i >> 5) & 3) << 3, b = ((i >> 3) & 3) | (i >> 7) << 2;
+        uint32_t r[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            v[r][j] = 0.0f;
-        if (n < o.N) {
-            const T *p = w + ((int64_t)e * o.N + n) * ldw + k0;
-            if (aligned && k0 + 4 <= o.K) {
-                load_pack<T, 4>(p, v[r]);
-            } else {
+            r[j] = s.codes[4 * a + j][b];
+        const uint32_t lo01 = __byte_perm(r[0], r[1], 0x5140), lo23 = __byte_perm(r[2], r[3], 0x5140);
+        const uint32_t hi01 = __byte_perm(r[0], r[1], 0x7362), hi23 = __byte_perm(r[2], r[3], 0x7362);
+        s.turned[4 * b][a] = __byte_perm(lo01, lo23, 0x5410);
+        s.turned[4 * b + 1][a] = __byte_perm(lo01, lo23, 0x7632);
+        s.turned[4 * b + 2][a] = __byte_perm(hi01, hi23, 0x5410);
+        s.turned[4 * b + 3][a] = __byte_perm(hi01, hi23, 0x7632);
+    }
+}
+
+// Rows [0, rows) of the turned codes to dst, ld bytes apart, the first `bytes` (a multiple of 16) of each.
+__device__ __forceinline__ void store_turned(const TileSmem &s, uint8_t *dst, int64_t ld, int rows, int bytes)
+{
+    for (int i = threadIdx.x; i < kBlock * 8; i += kTileThreads) {
+        const int r = i >> 3, w = (i & 7) * 4;
+        if (r < rows && 4 * w < bytes)
+            *reinterpret_cast<uint4 *>(dst + r * ld + 4 * w) =
+                make_uint4(s.turned[r][w], s.turned[r][w + 1], s.turned[r][w + 2], s.turned[r][w + 3]);
+    }
+}
+
+// A block of 128 x 128 of the weights: one scale, codes and (qt) transposed codes from one read.
+template <typename T>
+__global__ void __launch_bounds__(kTileThreads) k_quant_weight(const T *w, int64_t ldw, const esp_moe_weight o,
+                                                               bool aligned)
+{
+    __shared__ TileSmem s;
+    __shared__ uint32_t high[kTileThreads / 32];
+    const int kb = blockIdx.x, nb = blockIdx.y, e = blockIdx.z;
+    const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    const int k0 = kb * kBlock + 8 * c, n0 = nb * kBlock;
+    Eight<T> x[8];
+    uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (k0 + j < o.K)
-                        v[r][j] = to_f32(p[j]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            amax = fmaxf(amax, fabsf(v[r][j]));
-            finite = finite && is_finite(v[r][j]);
-        }
+    for (int i = 0; i < 8; ++i) {
+        const int n = n0 + r0 + 16 * i;
+        x[i].zero();
+        if (n < o.N && k0 < o.K)
+            x[i].load(w + ((int64_t)e * o.N + n) * ldw + k0, o.K - k0, aligned);
     }
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1)
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, s));
-    if (lane == 0)
-        red[warp] = amax;
-    if (!finite)
-        bad = 1;
+    for (int i = 0; i < 8; ++i)
+        m = Eight<T>::larger(m, x[i].largest());
+    m = __reduce_max_sync(0xffffffffu, Eight<T>::flat(m));
+    if ((threadIdx.x & 31) == 0)
+        high[threadIdx.x >> 5] = m;
     __syncthreads();
-    finite = bad == 0;
-    amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kWThreads / 32; ++i)
-        amax = fmaxf(amax, red[i]);
+    for (int i = 0; i < kTileThreads / 32; ++i)
+        m = max(m, high[i]);
     float scale, inv;
-    block_scale(amax, finite, scale, inv);
+    scale_of<T>(m, scale, inv);
     if (threadIdx.x == 0)
         o.scale[((int64_t)e * gridDim.y + nb) * gridDim.x + kb] = scale;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        const int i = warp + r * (kWThreads / 32), n = nb * kBlock + i;
-        const uint32_t q = finite ? codes4(v[r][0], v[r][1], v[r][2], v[r][3], inv) : 0u;
-        codes[i][lane] = q;
-        if (n < o.N && k0 < o.ld)
-            *reinterpret_cast<uint32_t *>(o.q + ((int64_t)e * o.N + n) * o.ld + k0) = q;
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        const uint2 q = codes8<T>(x[i], inv);
+        s.codes[r][2 * c] = q.x;
+        s.codes[r][2 * c + 1] = q.y;
+        if (n0 + r < o.N && k0 < o.ld)
+            *reinterpret_cast<uint2 *>(o.q + ((int64_t)e * o.N + n0 + r) * o.ld + k0) = q;
     }
     if (!o.qt)
         return;
     __syncthreads();
-    // transposed: a word holds four consecutive n of one k
-    for (int i = threadIdx.x; i < kBlock * kBlock / 4; i += kWThreads) {
-        const int k = i / (kBlock / 4), n4 = 4 * (i % (kBlock / 4));
-        if (kb * kBlock + k >= o.K || nb * kBlock + n4 >= o.ldt)
-            continue;
-        uint32_t q = 0;
+    turn_codes(s);
+    __syncthreads();
+    store_turned(s, o.qt + ((int64_t)e * o.K + kb * kBlock) * o.ldt + n0, o.ldt, o.K - kb * kBlock,
+                 (int)min((int64_t)kBlock, o.ldt - n0));
+}
+
+// First source row and row count of the experts' run of 128 positions number `tile` (n = 0 past the last).
+// Called by the whole CTA (256 threads).
+__device__ void find_run(const int32_t *offsets, int E, int64_t M, int tile, int &row0, int &n)
+{
+    __shared__ int s_row0, s_n;
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int carry = 0;
+        if (lane == 0)
+            s_n = 0;
+        __syncwarp();
+        for (int e0 = 0; e0 < E; e0 += 32) {
+            int a = 0, b = 0;
+            if (e0 + lane < E) {
+                a = offsets ? max(0, min((int)M, offsets[e0 + lane])) : 0;
+                b = offsets ? max(a, min((int)M, offsets[e0 + lane + 1])) : (int)M;
+            }
+            const int runs = (b - a) / kBlock + ((b - a) % kBlock != 0);
+            int sum = runs;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            q |= ((codes[n4 + j][k >> 2] >> (8 * (k & 3))) & 0xffu) << (8 * j);
-        *reinterpret_cast<uint32_t *>(o.qt + ((int64_t)e * o.K + kb * kBlock + k) * o.ldt + nb * kBlock + n4) = q;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o)
+                    sum += y;
+            }
+            const int first = carry + sum - runs;
+            if (tile >= first && tile < first + runs) {
+                s_row0 = a + (tile - first) * kBlock;
+                s_n = min(kBlock, b - s_row0);
+            }
+            carry += __shfl_sync(0xffffffffu, sum, 31);
+            if (carry > tile)
+                break;
+        }
     }
+    __syncthreads();
+    row0 = s_row0;
+    n = s_n;
+}
+
+// A run of up to 128 rows of an expert and 128 columns: a scale per column, codes transposed.
+template <typename T>
+__global__ void __launch_bounds__(kTileThreads) k_quant_cols(const QuantColsArgs a, bool aligned)
+{
+    __shared__ TileSmem s;
+    const int tiles_k = (a.K + kBlock - 1) / kBlock, run = blockIdx.x / tiles_k;
+    int row0, n;
+    find_run(a.offsets, a.E, a.M, run, row0, n);
+    if (n == 0)
+        return;
+    const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    const int c0 = (blockIdx.x - run * tiles_k) * kBlock;
+    Eight<T> x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        x[i].zero();
+        if (r < n && c0 + 8 * c < a.K) {
+            const int64_t src = a.rows ? a.rows[row0 + r] : row0 + r;
+            if (src >= 0 && src < a.T)
+                x[i].load(static_cast<const T *>(a.x) + src * a.ldx + c0 + 8 * c, a.K - c0 - 8 * c, aligned);
+        }
+    }
+    // greatest magnitudes: over the thread's rows, then over the thread rows
+#pragma unroll
+    for (int w = 0; w < Eight<T>::kWords; ++w) {
+        uint32_t m = x[0].magnitudes(w);
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            m = Eight<T>::larger(m, x[i].magnitudes(w));
+        if (sizeof(T) == 4) {
+            s.high[r0][8 * c + w] = m;
+        } else {
+            s.high[r0][8 * c + 2 * w] = m & 0xffffu;
+            s.high[r0][8 * c + 2 * w + 1] = m >> 16;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < kBlock) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            m = max(m, s.high[r][threadIdx.x]);
+        float scale, inv;
+        scale_of<T>(m, scale, inv);
+        s.inv[threadIdx.x] = inv;
+        if (c0 + (int)threadIdx.x < a.K)
+            a.scale[(int64_t)run * a.lds + c0 + threadIdx.x] = scale;
+    }
+    __syncthreads();
+    float inv[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        inv[j] = s.inv[8 * c + j];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = inv[j] == 0.0f ? 0.0f : __fmul_rn(x[i].get(j), inv[j]);
+        s.codes[r0 + 16 * i][2 * c] = codes4(v[0], v[1], v[2], v[3], 1.0f);
+        s.codes[r0 + 16 * i][2 * c + 1] = codes4(v[4], v[5], v[6], v[7], 1.0f);
+    }
+    __syncthreads();
+    turn_codes(s);
+    __syncthreads();
+    store_turned(s, a.q + (int64_t)c0 * a.ldq + (int64_t)run * kBlock, a.ldq, a.K - c0, kBlock);
 }
 
 }  // namespace
@@ -294,8 +401,7 @@ cudaError_t launch_quant_rows(esp_moe *m, int32_t dtype, const QuantRowsArgs &a)
         return cudaSuccess;
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        const int64_t ctas = ceil_div(total, kRowThreads / 16);
-        k_quant_rows<T><<<(unsigned)std::min<int64_t>(ctas, (int64_t)m->sm_count * 32), kRowThreads, 0, m->stream>>>(
+        k_quant_rows<T><<<(unsigned)ceil_div(total, kRowBlocks), kRowThreads, 0, m->stream>>>(
             a, blocks_k, rows_aligned(a.x, a.ldx, sizeof(T), 16));
         m->launches += 1;
         return cudaGetLastError();
@@ -310,8 +416,7 @@ cudaError_t launch_quant_cols(esp_moe *m, int32_t dtype, const QuantColsArgs &a)
         using T = decltype(elem);
         // runs of 128 positions: at most this many, some past the last
         const int64_t runs = a.M / kBlock + a.E;
-        const dim3 grid((unsigned)runs, (unsigned)ceil_div(a.K, kColTile));
-        k_quant_cols<T><<<grid, kColThreads, 0, m->stream>>>(a);
+        k_quant_cols<T><<<(unsigned)(runs * ceil_div(a.K, kBlock)), kTileThreads, 0, m->stream>>>(a, rows_aligned(a.x, a.ldx, sizeof(T), 16));
         m->launches += 1;
         return cudaGetLastError();
     });
@@ -322,8 +427,8 @@ cudaError_t launch_quant_weight(esp_moe *m, int32_t dtype, const void *w, int64_
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
         const dim3 grid((unsigned)ceil_div(o.K, kBlock), (unsigned)ceil_div(o.N, kBlock), (unsigned)o.E);
-        k_quant_weight<T><<<grid, kWThreads, 0, m->stream>>>(static_cast<const T *>(w), ldw, o,
-                                                             rows_aligned(w, ldw, sizeof(T), 4 * sizeof(T)));
+        k_quant_weight<T><<<grid, kTileThreads, 0, m->stream>>>(static_cast<const T *>(w), ldw, o,
+                                                             rows_aligned(w, ldw, sizeof(T), 16));
         m->launches += 1;
         return cudaGetLastError();
     });

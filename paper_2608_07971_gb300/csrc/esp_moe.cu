@@ -14,7 +14,7 @@ using namespace esp_moe_impl;
 namespace {
 
 constexpr int64_t kMaxRows = 0x7fffff00;   // row counts fit int32 with a tile to spare
-constexpr int64_t kMaxTiles = 1 << 30;
+constexpr int64_t kMaxTiles = 1 << 29;
 
 esp_status fail(esp_moe *m)
 {
