@@ -158,8 +158,6 @@ __device__ __forceinline__ float gate_weight(const Gate &g, bool on, float zj, f
     return g.sigmoid ? sigmoid_f(zj) : expf(zj - m) / zsum;
 }
 
-// ---- plan: stable positions of a run of slots
-
 // Exclusive scan of v[0..E) in shared memory into out[0..E] by one warp.
 __device__ __forceinline__ void warp_scan(const int *v, int E, int *out, int lane)
 {
@@ -181,86 +179,131 @@ __device__ __forceinline__ void warp_scan(const int *v, int E, int *out, int lan
         out[E] = carry;
 }
 
-// Positions of the slots [s0, s1) (experts idx[s], negative: none): those of expert e follow base[e] in the
-// slots' order. wcount: warps x E ints of shared memory. Called by the whole CTA.
-__device__ void place_slots(const int32_t *idx, int64_t s0, int64_t s1, int k, int E, const int *base, int *wcount,
-                            int32_t *rows, int32_t *pos)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int64_t per = ((s1 - s0 + warps - 1) / warps + 31) & ~(int64_t)31;
-    const int64_t a = min(s1, s0 + warp * per), b = min(s1, a + per);
-    for (int i = threadIdx.x; i < warps * E; i += blockDim.x)
-        wcount[i] = 0;
-    __syncthreads();
-    int *mine = wcount + warp * E;
-    for (int64_t s = a; s < b; s += 32) {
-        const int e = s + lane < b ? idx[s + lane] : -1;
-        const uint32_t same = __match_any_sync(kFull, e);
-        if (e >= 0 && lane == __ffs(same) - 1)
-            mine[e] += __popc(same);
-        __syncwarp();
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < E; e += blockDim.x) {
-        int run = base[e];
-        for (int w = 0; w < warps; ++w) {
-            const int c = wcount[w * E + e];
-            wcount[w * E + e] = run;
-            run += c;
-        }
-    }
-    __syncthreads();
-    for (int64_t s = a; s < b; s += 32) {
-        const int e = s + lane < b ? idx[s + lane] : -1;
-        const uint32_t same = __match_any_sync(kFull, e);
-        const int rank = __popc(same & ((1u << lane) - 1u));
-        int p = -1;
-        if (e >= 0)
-            p = mine[e] + rank;
-        __syncwarp();
-        if (e >= 0 && rank == 0)
-            mine[e] += __popc(same);
-        __syncwarp();
-        if (s + lane < b) {
-            pos[s + lane] = p;
-            if (p >= 0)
-                rows[p] = (int32_t)((s + lane) / k);
-        }
-    }
-}
-
 // ---- route
 
-// Tokens [blockIdx.x * chunk, ...) of one CTA. FUSED (one CTA in all): counts, offsets and the plan too;
-// otherwise the CTA's demand per expert goes to hist[blockIdx.x] for k_plan.
-template <typename T, int VPT, bool FUSED>
-__global__ void __launch_bounds__(kThreads) k_route(const RouteArgs a, int64_t chunk, bool aligned)
+// Threads of k_route's CTAs: every SM holds one, and 32 warps hide the chain of a token's k rounds; rows of
+// more than 256 experts keep up to 32 values a lane, and the registers of 16 warps.
+template <int VPT>
+constexpr int kRouteThreads = VPT <= 8 ? 1024 : 512;
+
+// A lane's values in descending order of key, equal keys in ascending order of element (Batcher's odd-even
+// merge sort), so that a round of the choice looks at the lanes' first values only.
+template <int VPT>
+__device__ __forceinline__ void sort_lane(uint32_t (&key)[VPT], int (&el)[VPT])
+{
+#pragma unroll
+    for (int p = 1; p < VPT; p <<= 1)
+#pragma unroll
+        for (int k = p; k >= 1; k >>= 1)
+#pragma unroll
+            for (int j = k % p; j + k < VPT; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < VPT && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const int x = i + j, y = i + j + k;
+                        const bool swap = key[x] < key[y] || (key[x] == key[y] && el[x] > el[y]);
+                        const uint32_t kx = key[x];
+                        const int ex = el[x];
+                        key[x] = swap ? key[y] : kx;
+                        el[x] = swap ? el[y] : ex;
+                        key[y] = swap ? kx : key[y];
+                        el[y] = swap ? ex : el[y];
+                    }
+}
+
+// The k elements of greatest key of a row (0: cannot be chosen), ties to the lower element: lane j gets the
+// j-th, or -1.
+template <typename T, int VPT>
+__device__ __forceinline__ int choose(uint32_t (&key)[VPT], int k, int lane)
 {
     using S = RowShape<T, VPT>;
-    extern __shared__ int sm[];
-    int *hist = sm;                 // E
-    int *offs = sm + a.E;           // E + 1 (FUSED)
-    int *wcount = sm + 2 * a.E + 1; // warps x E (FUSED)
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int E = a.E, k = a.k;
-    for (int e = threadIdx.x; e < E; e += kThreads)
-        hist[e] = 0;
-    __syncthreads();
-    float price[VPT];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int e = S::element(i, lane);
-        price[i] = a.prices && e < E ? a.prices[e] : 0.0f;
-    }
-    const int64_t t0 = blockIdx.x * chunk, t1 = min(a.T, t0 + chunk);
-    for (int64_t t = t0 + warp; t < t1; t += kWarps) {
-        float z[VPT];
-        load_row<T, VPT>(static_cast<const T *>(a.logits) + t * a.ld, E, aligned, lane, z);
-        const bool open = !a.valid || a.valid[t] != 0;
-        uint32_t key[VPT];
+    int sel = -1;
+    if constexpr (VPT <= 8) {
+        int el[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
-            key[i] = open ? order_key(__fsub_rn(z[i], price[i])) : 0u;
+            el[i] = S::element(i, lane);
+        sort_lane<VPT>(key, el);
+        for (int j = 0; j < k; ++j) {
+            const uint32_t top = __reduce_max_sync(kFull, key[0]);
+            if (top == 0u)
+                break;
+            const int e = (int)__reduce_min_sync(kFull, key[0] == top ? (unsigned)el[0] : 0xffffffffu);
+            const bool mine = key[0] == top && el[0] == e;
+            if (lane == j)
+                sel = e;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                key[i] = !mine ? key[i] : i + 1 < VPT ? key[i + 1 < VPT ? i + 1 : i] : 0u;
+                el[i] = mine && i + 1 < VPT ? el[i + 1 < VPT ? i + 1 : i] : el[i];
+            }
+        }
+    } else {
+        for (int j = 0; j < k; ++j) {
+            uint32_t best = key[0];
+#pragma unroll
+            for (int i = 1; i < VPT; ++i)
+                best = max(best, key[i]);
+            const uint32_t top = __reduce_max_sync(kFull, best);
+            if (top == 0u)
+                break;
+            unsigned cand = 0xffffffffu;
+#pragma unroll
+            for (int i = VPT - 1; i >= 0; --i)
+                if (key[i] == top)
+                    cand = (unsigned)S::element(i, lane);
+            const int e = (int)__reduce_min_sync(kFull, cand);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                if (S::element(i, lane) == e)
+                    key[i] = 0u;
+            if (lane == j)
+                sel = e;
+        }
+    }
+    return sel;
+}
+
+// Tokens [blockIdx.x * chunk, ...) of one CTA, a run of consecutive ones per warp. A choice's rank among its
+// CTA's choices of the same expert (in the order of the tokens) is the expert's count in its warp so far,
+// plus the counts of the warps before. FUSED (one CTA in all): counts, offsets and the plan too; otherwise
+// the ranks go to pos and the CTA's demand per expert to hist[blockIdx.x], for k_plan.
+template <typename T, int VPT, bool FUSED>
+__global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a, int64_t chunk, bool aligned)
+{
+    using S = RowShape<T, VPT>;
+    constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
+    extern __shared__ int sm[];
+    int *wcount = sm;               // W x E
+    int *hist = sm + W * a.E;       // E
+    int *offs = hist + a.E;         // E + 1 (FUSED)
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int E = a.E, k = a.k;
+    const bool plan = a.offsets != nullptr;
+    const int64_t t0 = blockIdx.x * chunk, t1 = min(a.T, t0 + chunk);
+    const int64_t per = (t1 - t0 + W - 1) / W, ta = min(t1, t0 + warp * per), tb = min(t1, ta + per);
+    const T *logits = static_cast<const T *>(a.logits);
+    float next[VPT];
+    if (ta < tb)
+        load_row<T, VPT>(logits + ta * a.ld, E, aligned, lane, next);
+    int *mine = wcount + warp * E;
+    for (int e = lane; e < E; e += 32)
+        mine[e] = 0;
+    __syncwarp();
+    for (int64_t t = ta; t < tb; ++t) {
+        const T *row = logits + t * a.ld;
+        const bool open = !a.valid || a.valid[t] != 0;
+        float z[VPT];
+        uint32_t key[VPT];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            z[i] = next[i];
+            const int e = S::element(i, lane);
+            const float price = a.prices && e < E ? __ldg(a.prices + e) : 0.0f;
+            key[i] = open ? order_key(__fsub_rn(z[i], price)) : 0u;
+        }
+        if (t + 1 < tb)
+            load_row<T, VPT>(row + a.ld, E, aligned, lane, next);
         float m = -INFINITY, zsum = 0.0f;
         if (!a.gate.renorm && !a.gate.sigmoid) {
 #pragma unroll
@@ -274,78 +317,75 @@ __global__ void __launch_bounds__(kThreads) k_route(const RouteArgs a, int64_t c
                 zsum = warp_sum(zsum);
             }
         }
-        int sel = -1;
-        float zsel = 0.0f;
-        for (int j = 0; j < k; ++j) {
-            uint32_t best = key[0];
-#pragma unroll
-            for (int i = 1; i < VPT; ++i)
-                best = max(best, key[i]);
-            const uint32_t top = __reduce_max_sync(kFull, best);
-            if (top == 0u)
-                break;
-            int cand = 0x7fffffff;
-#pragma unroll
-            for (int i = VPT - 1; i >= 0; --i)
-                if (key[i] == top)
-                    cand = S::element(i, lane);
-            const int e = (int)__reduce_min_sync(kFull, (unsigned)cand);
-            float zv = 0.0f;
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-                if (S::element(i, lane) == e) {
-                    key[i] = 0u;
-                    zv = z[i];
-                }
-            zv = __shfl_sync(kFull, zv, (e / S::V) & 31);
-            if (lane == j) {
-                sel = e;
-                zsel = zv;
-            }
-        }
+        const int sel = choose<T, VPT>(key, k, lane);
+        const float zsel = sel >= 0 ? clean(to_f32(row[sel])) : 0.0f;
         const float w = gate_weight(a.gate, sel >= 0, zsel, m, zsum);
         if (lane < k) {
             a.idx[t * k + lane] = sel;
             a.weight[t * k + lane] = __fmul_rn(a.gate.scale, w);
+            int rank = -1;
             if (sel >= 0)
-                atomicAdd(hist + sel, 1);
+                rank = mine[sel]++;   // a token's choices differ: no two lanes meet
+            if (plan)
+                a.pos[t * k + lane] = rank;
         }
+        __syncwarp();
     }
     __syncthreads();
-    if (!FUSED) {
-        for (int e = threadIdx.x; e < E; e += kThreads)
-            a.hist[(int64_t)blockIdx.x * E + e] = hist[e];
-        return;
+    // counts of the warps before, and the CTA's
+    for (int e = threadIdx.x; e < E; e += kThr) {
+        int run = 0;
+#pragma unroll 8
+        for (int w = 0; w < W; ++w) {
+            const int c = wcount[w * E + e];
+            wcount[w * E + e] = run;
+            run += c;
+        }
+        if (!FUSED)
+            a.hist[(int64_t)blockIdx.x * E + e] = run;
+        else
+            a.counts[e] = hist[e] = run;
     }
-    if (warp == 0)
-        warp_scan(hist, E, offs, lane);
-    for (int e = threadIdx.x; e < E; e += kThreads)
-        a.counts[e] = hist[e];
-    __syncthreads();
-    if (!a.offsets)
+    if (!plan)
         return;
-    for (int e = threadIdx.x; e <= E; e += kThreads)
-        a.offsets[e] = offs[e];
-    for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += kThreads)
-        a.rows[p] = -1;
-    place_slots(a.idx, 0, a.T * k, k, E, offs, wcount, a.rows, a.pos);
+    __syncthreads();
+    if (FUSED) {
+        if (warp == 0)
+            warp_scan(hist, E, offs, lane);
+        __syncthreads();
+        for (int e = threadIdx.x; e <= E; e += kThr)
+            a.offsets[e] = offs[e];
+        for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += kThr)
+            a.rows[p] = -1;
+    }
+    for (int64_t i = ta * k + lane; i < tb * k; i += 32) {
+        const int e = a.idx[i];
+        if (e < 0)
+            continue;
+        const int p = a.pos[i] + mine[e] + (FUSED ? offs[e] : 0);
+        a.pos[i] = p;
+        if (FUSED)
+            a.rows[p] = (int32_t)(i / k);
+    }
 }
 
-// Counts, offsets and plan from the CTAs' demands hist[nb][E]: every CTA sums the columns (all, and those of
-// the chunks before its own) and places its chunk's slots.
-__global__ void __launch_bounds__(kThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
+// Counts and offsets from the CTAs' demands hist[nb][E]; the ranks in pos become rows: every CTA sums the
+// columns (all, and those of the chunks before its own).
+constexpr int kPlanThreads = 1024;
+
+__global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
 {
     extern __shared__ int sm[];
     const int E = a.E, k = a.k;
-    int *total = sm, *before = sm + E, *offs = sm + 2 * E, *wcount = sm + 3 * E + 1;
-    for (int e = threadIdx.x; e < E; e += kThreads)
+    int *total = sm, *before = sm + E, *offs = sm + 2 * E;
+    for (int e = threadIdx.x; e < E; e += kPlanThreads)
         total[e] = before[e] = 0;
     __syncthreads();
-    const int groups = max(1, kThreads / E);
-    for (int i = threadIdx.x; i < groups * E; i += kThreads) {
+    const int groups = max(1, kPlanThreads / E);
+    for (int i = threadIdx.x; i < groups * E; i += kPlanThreads) {
         const int e = i % E, g = i / E;
         int all = 0, bef = 0;
-#pragma unroll 8
+#pragma unroll 16
         for (int b = g; b < nb; b += groups) {
             const int h = a.hist[(int64_t)b * E + e];
             all += h;
@@ -359,22 +399,26 @@ __global__ void __launch_bounds__(kThreads) k_plan(const RouteArgs a, int64_t ch
         warp_scan(total, E, offs, threadIdx.x);
     __syncthreads();
     if (blockIdx.x == 0) {
-        for (int e = threadIdx.x; e < E; e += kThreads)
+        for (int e = threadIdx.x; e < E; e += kPlanThreads)
             a.counts[e] = total[e];
         if (a.offsets)
-            for (int e = threadIdx.x; e <= E; e += kThreads)
+            for (int e = threadIdx.x; e <= E; e += kPlanThreads)
                 a.offsets[e] = offs[e];
     }
     if (!a.offsets)
         return;
-    for (int64_t p = offs[E] + (int64_t)blockIdx.x * kThreads + threadIdx.x; p < a.T * k;
-         p += (int64_t)gridDim.x * kThreads)
+    for (int64_t p = offs[E] + (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; p < a.T * k;
+         p += (int64_t)gridDim.x * kPlanThreads)
         a.rows[p] = -1;
-    for (int e = threadIdx.x; e < E; e += kThreads)
-        before[e] += offs[e];
-    __syncthreads();
-    const int64_t s0 = blockIdx.x * chunk * k;
-    place_slots(a.idx, s0, min(a.T * k, s0 + chunk * k), k, E, before, wcount, a.rows, a.pos);
+    const int64_t s0 = blockIdx.x * chunk * k, s1 = min(a.T * k, s0 + chunk * k);
+    for (int64_t i = s0 + threadIdx.x; i < s1; i += kPlanThreads) {
+        const int e = a.idx[i];
+        if (e < 0)
+            continue;
+        const int p = a.pos[i] + offs[e] + before[e];
+        a.pos[i] = p;
+        a.rows[p] = (int32_t)(i / k);
+    }
 }
 
 // ---- balance
@@ -730,11 +774,10 @@ __global__ void __launch_bounds__(kThreads) k_step_prices(int32_t E, const int64
 
 // ---- launches
 
-// Tokens of a CTA: enough CTAs for every SM, whole rounds of its warps.
+// Tokens of a CTA: one CTA for every SM, a token for each of its warps at least.
 int64_t route_chunk(int64_t T)
 {
-    const int64_t per = ceil_div(T, 152);
-    return std::max<int64_t>(kWarps, ceil_div(per, kWarps) * kWarps);
+    return std::max<int64_t>(kWarps, ceil_div(T, 152));
 }
 
 bool fused(int64_t T, int32_t k)
@@ -782,23 +825,23 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &a)
             constexpr int VPT = decltype(vpt)::value;
             using S = RowShape<T, VPT>;
             const bool aligned = rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T));
+            constexpr int kThr = kRouteThreads<VPT>;
+            const size_t route_smem = (size_t)((kThr / 32 + 2) * a.E + 1) * sizeof(int);
             if (fused(a.T, a.k)) {
-                const size_t smem = (size_t)(2 * a.E + 1 + kWarps * a.E) * sizeof(int);
-                const cudaError_t e = allow_smem(k_route<T, VPT, true>, smem);
+                const cudaError_t e = allow_smem(k_route<T, VPT, true>, route_smem);
                 if (e != cudaSuccess)
                     return e;
-                k_route<T, VPT, true><<<1, kThreads, smem, m->stream>>>(a, a.T, aligned);
+                k_route<T, VPT, true><<<1, kThr, route_smem, m->stream>>>(a, a.T, aligned);
                 m->launches += 1;
                 return cudaGetLastError();
             }
             const int64_t chunk = route_chunk(a.T);
             const int nb = (int)ceil_div(a.T, chunk);
-            k_route<T, VPT, false><<<nb, kThreads, a.E * sizeof(int), m->stream>>>(a, chunk, aligned);
-            const size_t smem = (size_t)(3 * a.E + 1 + kWarps * a.E) * sizeof(int);
-            const cudaError_t e = allow_smem(k_plan, smem);
+            const cudaError_t e = allow_smem(k_route<T, VPT, false>, route_smem);
             if (e != cudaSuccess)
                 return e;
-            k_plan<<<a.offsets ? nb : 1, kThreads, smem, m->stream>>>(a, chunk, nb);
+            k_route<T, VPT, false><<<nb, kThr, route_smem, m->stream>>>(a, chunk, aligned);
+            k_plan<<<a.offsets ? nb : 1, kPlanThreads, (size_t)(3 * a.E + 1) * sizeof(int), m->stream>>>(a, chunk, nb);
             m->launches += 2;
             return cudaGetLastError();
         });

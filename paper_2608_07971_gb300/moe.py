@@ -144,19 +144,16 @@ class Weight:
         return self.q.view(torch.float8_e4m3fn)[:, :, :self.K]
 
 
+# the current stream's handle without a Stream object around it (0.1 instead of 2 us per call)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _pad16(n: int) -> int:
     return (n + 15) // 16 * 16
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
-
-
-def _ld(t, name: str) -> int:
-    """Elements between the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.numel() > 0 and t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: a matrix with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 class Moe:
@@ -171,6 +168,7 @@ class Moe:
         if device.type != "cuda":
             raise ValueError(f"a CUDA device expected, not {device}")
         self.device = torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
+        self._index = self.device.index
         self._follow = stream is None
         self._stream = torch.cuda.current_stream(self.device).cuda_stream if stream is None else int(stream)
         h = ctypes.c_void_p()
@@ -183,7 +181,7 @@ class Moe:
         if self.h is None:
             raise ValueError("the handle is closed")
         if self._follow:
-            s = torch.cuda.current_stream(self.device).cuda_stream
+            s = _raw_stream(self._index)
             if s != self._stream:
                 self.set_stream(s)
 
@@ -198,25 +196,33 @@ class Moe:
             if optional:
                 return
             raise ValueError(f"{name} is missing")
-        if t.device != self.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
-        if dtype is not None and t.dtype != dtype:
+        if dtype is not None and t.dtype is not dtype:
             raise ValueError(f"{name}: {dtype} expected, not {t.dtype}")
-        if shape is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name}: shape {tuple(shape)} expected, not {tuple(t.shape)}")
-        if shape is not None and not t.is_contiguous():
-            raise ValueError(f"{name} is not contiguous")
+        if shape is not None:
+            if t.shape != shape:
+                raise ValueError(f"{name}: shape {shape} expected, not {tuple(t.shape)}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} is not contiguous")
 
     def _matrix(self, t, name: str, rows=None, cols=None, dtype=None) -> Tuple[int, int]:
         """Checks a matrix of a floating-point type; returns its type code and leading dimension."""
-        self._need(t, name)
+        if t is None:
+            raise ValueError(f"{name} is missing")
+        if t.get_device() != self._index:
+            raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
         code = _DTYPES.get(t.dtype)
-        if code is None or (dtype is not None and t.dtype != dtype):
+        if code is None or (dtype is not None and t.dtype is not dtype):
             raise ValueError(f"{name}: type {t.dtype} not taken here")
-        ld = _ld(t, name)
-        if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-            raise ValueError(f"{name}: shape ({rows}, {cols}) expected, not {tuple(t.shape)}")
-        return code, ld
+        shape = t.shape
+        if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+            raise ValueError(f"{name}: shape ({rows}, {cols}) expected, not {tuple(shape)}")
+        n, m = shape
+        step, unit = t.stride()
+        if unit != 1 and m > 1 and n > 0:
+            raise ValueError(f"{name}: a matrix with contiguous rows expected")
+        return code, step if n > 1 else m
 
     def _new(self, shape, dtype):
         return torch.empty(shape, dtype=dtype, device=self.device)
