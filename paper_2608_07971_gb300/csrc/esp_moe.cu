@@ -196,7 +196,7 @@ esp_status esp_moe_route(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, in
         return ESP_ERR_INVALID_ARG;
     if (!aligned_to(logits, element_size(dtype)))
         return ESP_ERR_INVALID_ARG;
-    RouteArgs a{to_gate(gate), T, ld, E, k, logits, prices, valid, idx, weight, counts, rows, pos, offsets, nullptr};
+    RouteArgs a{to_gate(gate), T, ld, E, k, logits, prices, valid, idx, weight, counts, rows, pos, offsets, nullptr, false};
     const size_t ints = route_hist_ints(T, E, k);
     if ((st = reserve(m, ints * sizeof(int32_t))) != ESP_OK)
         return st;

@@ -74,6 +74,7 @@ struct RouteArgs {
     int64_t *counts;
     int32_t *rows, *pos, *offsets;
     int32_t *hist;        // work space: route_hist_ints
+    bool hist16;          // its numbers have 16 bits (set by the launcher)
 };
 size_t route_hist_ints(int64_t T, int32_t E, int32_t k);
 cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &a);

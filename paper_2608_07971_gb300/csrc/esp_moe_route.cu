@@ -32,7 +32,14 @@ struct RowShape {
 // A gate's reading of a logit: +inf as the largest finite value, NaN as -inf.
 __device__ __forceinline__ float clean(float z)
 {
-    return z > -INFINITY ? fminf(z, FLT_MAX) : -INFINITY;
+    return fminf(fmaxf(z, -INFINITY), FLT_MAX);   // fmaxf of a NaN and a number is the number
+}
+
+// What a price adds to a logit: its negative, with +0 for both zeros (then a sum of 0 is +0, whatever the
+// logit's sign) and NaN closing the expert. Clean logits plus it are never NaN.
+__device__ __forceinline__ float price_term(float price)
+{
+    return price == 0.0f ? 0.0f : fminf(fmaxf(-price, -INFINITY), FLT_MAX);
 }
 
 template <typename T, int VPT>
@@ -81,21 +88,21 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Order-preserving key of a float; 0 for NaN and -inf (below every other key), one key for both zeros.
+// Order-preserving key of a float that is neither NaN nor -0; kClosed is -inf's.
+constexpr uint32_t kClosed = 0x007fffffu;
+
 __device__ __forceinline__ uint32_t order_key(float v)
 {
-    if (!(v > -INFINITY))
-        return 0u;
-    const uint32_t u = __float_as_uint(v + 0.0f);
+    const uint32_t u = __float_as_uint(v);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ float key_value(uint32_t k)
 {
-    return k == 0u ? -INFINITY : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 
-// Largest value over the warp (values cleaned: no NaN).
+// Largest value over the warp (no NaN among them; -0 counts as less than +0).
 __device__ __forceinline__ float warp_max(float v)
 {
     return key_value(__reduce_max_sync(kFull, order_key(v)));
@@ -181,16 +188,31 @@ __device__ __forceinline__ void warp_scan(const int *v, int E, int *out, int lan
 
 // ---- route
 
+// The chunks' demands between k_route and k_plan, in 16 bits where a chunk's tokens fit: k_plan reads all of
+// them in every CTA.
+__device__ __forceinline__ void store_demand(const RouteArgs &a, int64_t i, int n)
+{
+    if (a.hist16)
+        reinterpret_cast<uint16_t *>(a.hist)[i] = (uint16_t)n;
+    else
+        a.hist[i] = n;
+}
+
 // Threads of k_route's CTAs: every SM holds one, and 32 warps hide the chain of a token's k rounds; rows of
 // more than 256 experts keep up to 32 values a lane, and the registers of 16 warps.
 template <int VPT>
 constexpr int kRouteThreads = VPT <= 8 ? 1024 : 512;
 
-// A lane's values in descending order of key, equal keys in ascending order of element (Batcher's odd-even
-// merge sort), so that a round of the choice looks at the lanes' first values only.
+// A lane's values in descending order of key, equal keys in their order (Batcher's odd-even merge sort), so
+// that a round of the choice looks at the lanes' first values only; packed: the sorted values' places
+// before, four bits each, the first in the lowest.
 template <int VPT>
-__device__ __forceinline__ void sort_lane(uint32_t (&key)[VPT], int (&el)[VPT])
+__device__ __forceinline__ uint32_t sort_lane(uint32_t (&key)[VPT])
 {
+    uint32_t at[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+        at[i] = i;
 #pragma unroll
     for (int p = 1; p < VPT; p <<= 1)
 #pragma unroll
@@ -201,41 +223,44 @@ __device__ __forceinline__ void sort_lane(uint32_t (&key)[VPT], int (&el)[VPT])
                 for (int i = 0; i < k; ++i)
                     if (i + j + k < VPT && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
                         const int x = i + j, y = i + j + k;
-                        const bool swap = key[x] < key[y] || (key[x] == key[y] && el[x] > el[y]);
-                        const uint32_t kx = key[x];
-                        const int ex = el[x];
+                        const bool swap = key[x] < key[y] || (key[x] == key[y] && at[x] > at[y]);
+                        const uint32_t kx = key[x], ax = at[x];
                         key[x] = swap ? key[y] : kx;
-                        el[x] = swap ? el[y] : ex;
+                        at[x] = swap ? at[y] : ax;
                         key[y] = swap ? kx : key[y];
-                        el[y] = swap ? ex : el[y];
+                        at[y] = swap ? ax : at[y];
                     }
+    uint32_t packed = 0;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+        packed |= at[i] << (4 * i);
+    return packed;
 }
 
-// The k elements of greatest key of a row (0: cannot be chosen), ties to the lower element: lane j gets the
-// j-th, or -1.
+// The k elements of greatest key of a row (kClosed or less: cannot be chosen), ties to the lower element:
+// lane j gets the j-th, or -1.
 template <typename T, int VPT>
 __device__ __forceinline__ int choose(uint32_t (&key)[VPT], int k, int lane)
 {
     using S = RowShape<T, VPT>;
     int sel = -1;
     if constexpr (VPT <= 8) {
-        int el[VPT];
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-            el[i] = S::element(i, lane);
-        sort_lane<VPT>(key, el);
+        uint32_t places = sort_lane<VPT>(key);
         for (int j = 0; j < k; ++j) {
             const uint32_t top = __reduce_max_sync(kFull, key[0]);
-            if (top == 0u)
+            if (top <= kClosed)
                 break;
-            const int e = (int)__reduce_min_sync(kFull, key[0] == top ? (unsigned)el[0] : 0xffffffffu);
-            const bool mine = key[0] == top && el[0] == e;
+            const int i = places & 15u;
+            const unsigned el = (unsigned)((i / S::V) * 32 * S::V + lane * S::V + i % S::V);
+            const bool tied = key[0] == top;
+            const unsigned e = __reduce_min_sync(kFull, tied ? el : 0xffffffffu);
             if (lane == j)
-                sel = e;
+                sel = (int)e;
+            if (tied && el == e) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                key[i] = !mine ? key[i] : i + 1 < VPT ? key[i + 1 < VPT ? i + 1 : i] : 0u;
-                el[i] = mine && i + 1 < VPT ? el[i + 1 < VPT ? i + 1 : i] : el[i];
+                for (int q = 0; q < VPT; ++q)
+                    key[q] = q + 1 < VPT ? key[q + 1 < VPT ? q + 1 : q] : 0u;
+                places >>= 4;
             }
         }
     } else {
@@ -245,7 +270,7 @@ __device__ __forceinline__ int choose(uint32_t (&key)[VPT], int k, int lane)
             for (int i = 1; i < VPT; ++i)
                 best = max(best, key[i]);
             const uint32_t top = __reduce_max_sync(kFull, best);
-            if (top == 0u)
+            if (top <= kClosed)
                 break;
             unsigned cand = 0xffffffffu;
 #pragma unroll
@@ -274,9 +299,11 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     using S = RowShape<T, VPT>;
     constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
     extern __shared__ int sm[];
-    int *wcount = sm;               // W x E
-    int *hist = sm + W * a.E;       // E
-    int *offs = hist + a.E;         // E + 1 (FUSED)
+    constexpr int kPadded = 32 * VPT;                  // E rounded up to the lanes' elements
+    float *price = reinterpret_cast<float *>(sm);      // kPadded price terms
+    int *wcount = sm + kPadded;                        // W x E
+    int *hist = wcount + W * a.E;                      // E
+    int *offs = hist + a.E;                            // E + 1 (FUSED)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int E = a.E, k = a.k;
     const bool plan = a.offsets != nullptr;
@@ -289,7 +316,9 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     int *mine = wcount + warp * E;
     for (int e = lane; e < E; e += 32)
         mine[e] = 0;
-    __syncwarp();
+    for (int e = threadIdx.x; e < kPadded; e += kThr)
+        price[e] = a.prices && e < E ? price_term(a.prices[e]) : 0.0f;
+    __syncthreads();
     for (int64_t t = ta; t < tb; ++t) {
         const T *row = logits + t * a.ld;
         const bool open = !a.valid || a.valid[t] != 0;
@@ -298,9 +327,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             z[i] = next[i];
-            const int e = S::element(i, lane);
-            const float price = a.prices && e < E ? __ldg(a.prices + e) : 0.0f;
-            key[i] = open ? order_key(__fsub_rn(z[i], price)) : 0u;
+            key[i] = order_key(__fadd_rn(z[i], price[S::element(i, lane)]));
         }
         if (t + 1 < tb)
             load_row<T, VPT>(row + a.ld, E, aligned, lane, next);
@@ -317,7 +344,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
                 zsum = warp_sum(zsum);
             }
         }
-        const int sel = choose<T, VPT>(key, k, lane);
+        const int sel = open ? choose<T, VPT>(key, k, lane) : -1;   // the same for every lane
         const float zsel = sel >= 0 ? clean(to_f32(row[sel])) : 0.0f;
         const float w = gate_weight(a.gate, sel >= 0, zsel, m, zsum);
         if (lane < k) {
@@ -342,7 +369,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
             run += c;
         }
         if (!FUSED)
-            a.hist[(int64_t)blockIdx.x * E + e] = run;
+            store_demand(a, (int64_t)blockIdx.x * E + e, run);
         else
             a.counts[e] = hist[e] = run;
     }
@@ -365,60 +392,76 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
         const int p = a.pos[i] + mine[e] + (FUSED ? offs[e] : 0);
         a.pos[i] = p;
         if (FUSED)
-            a.rows[p] = (int32_t)(i / k);
+            a.rows[p] = (int32_t)((uint32_t)i / (uint32_t)k);
     }
 }
 
-// Counts and offsets from the CTAs' demands hist[nb][E]; the ranks in pos become rows: every CTA sums the
-// columns (all, and those of the chunks before its own).
-constexpr int kPlanThreads = 1024;
+// Counts and offsets from the chunks' demands hist[nb][E]; the ranks in pos become rows. A CTA takes
+// kPlanChunks chunks and sums the columns over all chunks and over those before its own.
+constexpr int kPlanThreads = 1024, kPlanChunks = 2;
 
-__global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
+template <typename D>
+__device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0, int *total, int *before, int *second)
 {
-    extern __shared__ int sm[];
-    const int E = a.E, k = a.k;
-    int *total = sm, *before = sm + E, *offs = sm + 2 * E;
-    for (int e = threadIdx.x; e < E; e += kPlanThreads)
-        total[e] = before[e] = 0;
-    __syncthreads();
     const int groups = max(1, kPlanThreads / E);
     for (int i = threadIdx.x; i < groups * E; i += kPlanThreads) {
         const int e = i % E, g = i / E;
         int all = 0, bef = 0;
 #pragma unroll 16
         for (int b = g; b < nb; b += groups) {
-            const int h = a.hist[(int64_t)b * E + e];
+            const int h = hist[(int64_t)b * E + e];
             all += h;
-            bef += b < (int)blockIdx.x ? h : 0;
+            bef += b < c0 ? h : 0;
         }
         atomicAdd(total + e, all);
         atomicAdd(before + e, bef);
     }
+    for (int e = threadIdx.x; e < E; e += kPlanThreads)
+        second[e] = hist[(int64_t)c0 * E + e];
+}
+
+__global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
+{
+    extern __shared__ int sm[];
+    const int E = a.E, k = a.k, c0 = blockIdx.x * kPlanChunks;
+    int *total = sm, *before = sm + E, *second = sm + 2 * E, *offs = sm + 3 * E;
+    for (int e = threadIdx.x; e < E; e += kPlanThreads)
+        total[e] = before[e] = 0;
+    // the first slots' ranks are on their way while the columns are summed
+    const int64_t s0 = c0 * chunk * k, s1 = a.offsets ? min(a.T * k, s0 + kPlanChunks * chunk * k) : s0;
+    const int64_t mid = s0 + chunk * k;
+    int64_t i = s0 + threadIdx.x;
+    int e = i < s1 ? a.idx[i] : -1, rank = i < s1 ? a.pos[i] : 0;
+    __syncthreads();
+    if (a.hist16)
+        sum_columns(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
+    else
+        sum_columns(a.hist, E, nb, c0, total, before, second);
     __syncthreads();
     if (threadIdx.x < 32)
         warp_scan(total, E, offs, threadIdx.x);
     __syncthreads();
-    if (blockIdx.x == 0) {
-        for (int e = threadIdx.x; e < E; e += kPlanThreads)
-            a.counts[e] = total[e];
-        if (a.offsets)
-            for (int e = threadIdx.x; e <= E; e += kPlanThreads)
-                a.offsets[e] = offs[e];
-    }
+    if (blockIdx.x == 0)
+        for (int q = threadIdx.x; q < E; q += kPlanThreads)
+            a.counts[q] = total[q];
     if (!a.offsets)
         return;
+    if (blockIdx.x == 0)
+        for (int q = threadIdx.x; q <= E; q += kPlanThreads)
+            a.offsets[q] = offs[q];
+    for (; i < s1;) {
+        if (e >= 0) {
+            const int p = rank + offs[e] + before[e] + (i >= mid ? second[e] : 0);
+            a.pos[i] = p;
+            a.rows[p] = (int32_t)((uint32_t)i / (uint32_t)k);
+        }
+        i += kPlanThreads;
+        e = i < s1 ? a.idx[i] : -1;
+        rank = i < s1 ? a.pos[i] : 0;
+    }
     for (int64_t p = offs[E] + (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; p < a.T * k;
          p += (int64_t)gridDim.x * kPlanThreads)
         a.rows[p] = -1;
-    const int64_t s0 = blockIdx.x * chunk * k, s1 = min(a.T * k, s0 + chunk * k);
-    for (int64_t i = s0 + threadIdx.x; i < s1; i += kPlanThreads) {
-        const int e = a.idx[i];
-        if (e < 0)
-            continue;
-        const int p = a.pos[i] + offs[e] + before[e];
-        a.pos[i] = p;
-        a.rows[p] = (int32_t)(i / k);
-    }
 }
 
 // ---- balance
@@ -471,15 +514,28 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
             acc[i] = 0.0f;
         float lse2 = 0.0f;
         int tokens = 0;
+        // the next token's row and choices are on their way while a token is summed
+        float next[VPT];
+        int next_idx = -1;
+        auto fetch = [&](int64_t t) {
+            if (t < hi) {
+                next_idx = lane < k ? a.idx[t * k + lane] : -1;
+                load_row<T, VPT>(static_cast<const T *>(a.logits) + t * a.ld, E, aligned, lane, next);
+            }
+        };
+        fetch(lo + warp);
         for (int64_t t = lo + warp; t < hi; t += kWarps) {
-            const int mine = lane < k ? a.idx[t * k + lane] : -1;
+            const int mine = next_idx;
+            float z[VPT], p[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                z[i] = next[i];
+            fetch(t + kWarps);
             if (__shfl_sync(kFull, mine, 0) < 0)
                 continue;
             if (mine >= 0 && mine < E)
                 atomicAdd(hist + mine, 1);
             ++tokens;
-            float z[VPT], p[VPT];
-            load_row<T, VPT>(static_cast<const T *>(a.logits) + t * a.ld, E, aligned, lane, z);
             const float lse = row_softmax<VPT>(z, p);
             lse2 += lse * lse;
             if (a.gate.sigmoid) {
@@ -543,6 +599,7 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
 {
     extern __shared__ float smf[];
     __shared__ float buf[kWarps];
+    __shared__ int nbuf[kWarps];
     __shared__ bool last;
     const int E = a.E, s = blockIdx.x;
     const int groups = max(1, kThreads / E);
@@ -552,7 +609,7 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     const int64_t b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
     int n = 0;
     float lse = 0.0f;
-    for (int64_t b = b0; b < b1; ++b) {
+    for (int64_t b = b0 + threadIdx.x; b < b1; b += kThreads) {
         n += a.part_tokens[b + s];
         lse += a.part_lse[b + s];
     }
@@ -560,7 +617,7 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
         const int e = i % E, g = i / E;
         float v = 0.0f;
         int c = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t b = b0 + g; b < b1; b += groups) {
             v += a.part_share[(b + s) * E + e];
             c += a.part_count[(b + s) * E + e];
@@ -568,7 +625,13 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
         share[i] = v;
         count[i] = c;
     }
-    __syncthreads();
+    n = __reduce_add_sync(kFull, n);
+    if ((threadIdx.x & 31) == 0)
+        nbuf[threadIdx.x >> 5] = n;
+    lse = block_sum(lse, buf);   // its barriers publish the parts too
+    n = 0;
+    for (int w = 0; w < kWarps; ++w)
+        n += nbuf[w];
     float dot = 0.0f;
     for (int e = threadIdx.x; e < E; e += kThreads) {
         float v = 0.0f;
@@ -618,135 +681,141 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
 
 constexpr int kBwdThreads = 256;
 
-template <typename T, int VPT>
+// BALANCE: with the losses' gradient. A warp takes consecutive tokens; the next token's row, choices and
+// gradients are on their way while a token is worked on.
+template <typename T, int VPT, bool BALANCE>
 __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackwardArgs a, int64_t per_warp,
                                                                  bool aligned, bool aligned_out)
 {
     using S = RowShape<T, VPT>;
     extern __shared__ float smf[];
-    __shared__ float buf[kBwdThreads / 32];
     const int E = a.E, k = a.k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float *row = smf + warp * E;   // the chosen experts' part, zero elsewhere
-    for (int e = lane; e < E; e += 32)
-        row[e] = 0.0f;
+    float *row = smf + warp * 32 * VPT;   // the chosen experts' part, zero elsewhere
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+        row[32 * i + lane] = 0.0f;
+    const int64_t w = (int64_t)blockIdx.x * (kBwdThreads / 32) + warp;
+    const int64_t t0 = w * per_warp, t1 = min(a.T, t0 + per_warp);
+    const T *logits = static_cast<const T *>(a.logits);
+    float next[VPT], next_g = 0.0f;
+    int next_e = -1;
+    auto fetch = [&](int64_t t) {
+        if (t < t1) {
+            load_row<T, VPT>(logits + t * a.ld, E, aligned, lane, next);
+            next_e = lane < k ? a.idx[t * k + lane] : -1;
+            if (a.dweight)
+                next_g = lane < k ? a.dweight[t * k + lane] : 0.0f;
+        }
+    };
+    fetch(t0);
     float g0 = 0.0f, g1 = 0.0f;
-    if (a.dloss) {
+    if (BALANCE) {
         float used = 0.0f, tok = 0.0f;
-        for (int b = threadIdx.x; b < a.B; b += kBwdThreads) {
+        for (int b = lane; b < a.B; b += 32) {
             const int64_t n = a.tokens[b];
             used += n > 0 ? 1.0f : 0.0f;
             tok += (float)n;
         }
-        used = block_sum(used, buf);
-        tok = block_sum(tok, buf);
+        used = warp_sum(used);
+        tok = warp_sum(tok);
         g0 = used > 0.0f ? a.dloss[0] * (float)E / ((float)k * used) : 0.0f;
         g1 = tok > 0.0f ? 2.0f * a.dloss[1] / tok : 0.0f;
     }
-    __syncwarp();
     const bool dense_softmax = !a.gate.sigmoid && !a.gate.renorm;
-    float coef[VPT];   // gradient of a counted token's r, for the sequence `held`
+    float coef[BALANCE ? VPT : 1];   // gradient of a counted token's r, for the sequence `held`
     int held = -1;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-        coef[i] = 0.0f;
-    const int64_t w = (int64_t)blockIdx.x * (kBwdThreads / 32) + warp;
-    const int64_t t0 = w * per_warp, t1 = min(a.T, t0 + per_warp);
+    __syncwarp();
     for (int64_t t = t0; t < t1; ++t) {
-        const T *zrow = static_cast<const T *>(a.logits) + t * a.ld;
         T *drow = static_cast<T *>(a.dlogits) + t * a.ld_out;
-        int e = lane < k ? a.idx[t * k + lane] : -1;
-        float d[VPT];
+        const int e = next_e;
+        const float gw = next_g;
+        float z[VPT], p[VPT], d[VPT];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) {
+            z[i] = next[i];
             d[i] = 0.0f;
+        }
+        fetch(t + 1);
         if (__shfl_sync(kFull, e, 0) < 0) {
             store_row<T, VPT>(drow, E, aligned_out, lane, d);
             continue;
         }
         const bool on = e >= 0 && e < E;
-        float z[VPT], p[VPT];
-        load_row<T, VPT>(zrow, E, aligned, lane, z);
-        const float zj = on ? clean(to_f32(zrow[e])) : 0.0f;
         float lse = 0.0f;
-        if (dense_softmax || a.dloss)
+        if (dense_softmax || BALANCE)
             lse = row_softmax<VPT>(z, p);
         if (a.dweight) {
-            const float g = on ? a.gate.scale * a.dweight[t * k + lane] : 0.0f;
-            if (dense_softmax) {
-                if (on)
-                    row[e] = g;
-                __syncwarp();
-                float dot = 0.0f;
-#pragma unroll
-                for (int i = 0; i < VPT; ++i) {
-                    const int q = S::element(i, lane);
-                    d[i] = q < E ? row[q] : 0.0f;
-                    dot += p[i] * d[i];
-                }
-                dot = warp_sum(dot);
-#pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    d[i] = p[i] * (d[i] - dot);
-            } else {
-                float dj;
+            const float g = on ? a.gate.scale * gw : 0.0f;
+            float dj = g;
+            if (!dense_softmax) {
+                const float zj = on ? clean(to_f32(logits[t * a.ld + e])) : 0.0f;
                 if (a.gate.renorm) {
                     const float pj = gate_weight(a.gate, on, zj, 0.0f, 1.0f);
                     const float dot = warp_sum(g * pj);
                     dj = pj * (g - dot) * (a.gate.sigmoid ? sigmoid_f(-zj) : 1.0f);
                 } else {
-                    const float s = sigmoid_f(zj);
-                    dj = g * s * sigmoid_f(-zj);
-                }
-                if (on)
-                    row[e] = dj;
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < VPT; ++i) {
-                    const int q = S::element(i, lane);
-                    d[i] = q < E ? row[q] : 0.0f;
+                    dj = g * sigmoid_f(zj) * sigmoid_f(-zj);
                 }
             }
+            if (on)
+                row[e] = dj;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                d[i] = row[S::element(i, lane)];
             __syncwarp();
             if (on)
                 row[e] = 0.0f;
+            if (dense_softmax) {
+                float dot = 0.0f;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+                    dot += p[i] * d[i];
+                dot = warp_sum(dot);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+                    d[i] = p[i] * (d[i] - dot);
+            }
             __syncwarp();
         }
-        const int s = !a.dloss ? a.B : (a.seq ? seq_of(a.seq, a.B, t) : 0);
-        if (a.dloss && s < a.B && (!a.seq || t >= a.seq[s])) {
-            if (s != held) {
-                held = s;
-                const float n = (float)a.tokens[s];
-                const float c = n > 0.0f ? g0 / (n * n) : 0.0f;
+        if constexpr (BALANCE) {
+            const int s = a.seq ? seq_of(a.seq, a.B, t) : 0;
+            if (s < a.B && (!a.seq || t >= a.seq[s])) {
+                if (s != held) {
+                    held = s;
+                    const float n = (float)a.tokens[s];
+                    const float c = n > 0.0f ? g0 / (n * n) : 0.0f;
 #pragma unroll
-                for (int i = 0; i < VPT; ++i) {
-                    const int q = S::element(i, lane);
-                    coef[i] = q < E ? c * (float)a.counts[(int64_t)s * E + q] : 0.0f;
+                    for (int i = 0; i < VPT; ++i) {
+                        const int q = S::element(i, lane);
+                        coef[i] = q < E ? c * (float)(int32_t)a.counts[(int64_t)s * E + q] : 0.0f;   // below 2^31
+                    }
                 }
-            }
-            const float gz = g1 * lse;
-            if (!a.gate.sigmoid) {
-                float dot = 0.0f;
+                const float gz = g1 * lse;
+                if (!a.gate.sigmoid) {
+                    float dot = 0.0f;
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    dot += coef[i] * p[i];
-                dot = warp_sum(dot);
+                    for (int i = 0; i < VPT; ++i)
+                        dot += coef[i] * p[i];
+                    dot = warp_sum(dot);
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    d[i] += p[i] * (coef[i] - dot + gz);
-            } else {
-                float r[VPT], la[VPT];
+                    for (int i = 0; i < VPT; ++i)
+                        d[i] += p[i] * (coef[i] - dot + gz);
+                } else {
+                    float r[VPT], la[VPT];
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    la[i] = log_sigmoid(z[i]);
-                row_softmax<VPT>(la, r);
-                float dot = 0.0f;
+                    for (int i = 0; i < VPT; ++i)
+                        la[i] = log_sigmoid(z[i]);
+                    row_softmax<VPT>(la, r);
+                    float dot = 0.0f;
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    dot += coef[i] * r[i];
-                dot = warp_sum(dot);
+                    for (int i = 0; i < VPT; ++i)
+                        dot += coef[i] * r[i];
+                    dot = warp_sum(dot);
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    d[i] += r[i] * (coef[i] - dot) * sigmoid_f(-z[i]) + p[i] * gz;
+                    for (int i = 0; i < VPT; ++i)
+                        d[i] += r[i] * (coef[i] - dot) * sigmoid_f(-z[i]) + p[i] * gz;
+                }
             }
         }
         store_row<T, VPT>(drow, E, aligned_out, lane, d);
@@ -817,8 +886,10 @@ size_t route_hist_ints(int64_t T, int32_t E, int32_t k)
     return fused(T, k) ? 0 : (size_t)ceil_div(T, route_chunk(T)) * E;
 }
 
-cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &a)
+cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
 {
+    RouteArgs a = args;
+    a.hist16 = route_chunk(a.T) < 65536;
     return with_dtype(dtype, [&](auto elem) {
         using T = decltype(elem);
         return with_vpt(a.E, [&](auto vpt) -> cudaError_t {
@@ -826,7 +897,7 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &a)
             using S = RowShape<T, VPT>;
             const bool aligned = rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T));
             constexpr int kThr = kRouteThreads<VPT>;
-            const size_t route_smem = (size_t)((kThr / 32 + 2) * a.E + 1) * sizeof(int);
+            const size_t route_smem = (size_t)(32 * VPT + (kThr / 32 + 2) * a.E + 1) * sizeof(int);
             if (fused(a.T, a.k)) {
                 const cudaError_t e = allow_smem(k_route<T, VPT, true>, route_smem);
                 if (e != cudaSuccess)
@@ -841,7 +912,8 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &a)
             if (e != cudaSuccess)
                 return e;
             k_route<T, VPT, false><<<nb, kThr, route_smem, m->stream>>>(a, chunk, aligned);
-            k_plan<<<a.offsets ? nb : 1, kPlanThreads, (size_t)(3 * a.E + 1) * sizeof(int), m->stream>>>(a, chunk, nb);
+            k_plan<<<a.offsets ? (int)ceil_div(nb, kPlanChunks) : 1, kPlanThreads, (size_t)(4 * a.E + 1) * sizeof(int),
+                     m->stream>>>(a, chunk, nb);
             m->launches += 2;
             return cudaGetLastError();
         });
@@ -894,9 +966,13 @@ cudaError_t launch_route_backward(esp_moe *m, int32_t dtype, const RouteBackward
             const int64_t warps = std::min<int64_t>(a.T, (int64_t)m->sm_count * 6 * kW);
             const int64_t per = ceil_div(a.T, warps);
             const int grid = (int)ceil_div(ceil_div(a.T, per), kW);
-            k_route_backward<T, VPT><<<grid, kBwdThreads, (size_t)kW * a.E * sizeof(float), m->stream>>>(
-                a, per, rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T)),
-                rows_aligned(a.dlogits, a.ld_out, sizeof(T), S::V * sizeof(T)));
+            const size_t smem = (size_t)kW * 32 * VPT * sizeof(float);
+            const bool in = rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T));
+            const bool out = rows_aligned(a.dlogits, a.ld_out, sizeof(T), S::V * sizeof(T));
+            if (a.dloss)
+                k_route_backward<T, VPT, true><<<grid, kBwdThreads, smem, m->stream>>>(a, per, in, out);
+            else
+                k_route_backward<T, VPT, false><<<grid, kBwdThreads, smem, m->stream>>>(a, per, in, out);
             m->launches += 1;
             return cudaGetLastError();
         });
