@@ -238,7 +238,7 @@ esp_status esp_moe_balance(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, 
         a.part_count = c.take<int32_t>(slots * E);
         a.part_lse = c.take<float>(slots);
         a.part_tokens = c.take<int32_t>(slots);
-        a.seq_loss = c.take<float>(2 * (size_t)B);
+        a.seq_loss = c.take<float>(3 * (size_t)B);
         if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
             return st;
     }

@@ -3,6 +3,8 @@
 // token's rows, KT of them in flight at once.
 
 #include <algorithm>
+#include <cstring>
+#include <type_traits>
 
 #include "esp_moe_impl.h"
 #include "esp_moe_load.cuh"
@@ -34,6 +36,26 @@ __device__ __forceinline__ void load_picks(const CombineArgs &a, int64_t t, Pick
     __syncthreads();
 }
 
+// V elements as loaded, for a load that may be left out (a row that does not exist: zeros).
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_if(bool on, const T *p)
+{
+    Pack<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        r.v[i] = from_f32<T>(0.0f);
+    if (on) {
+        if constexpr (sizeof(r) == 16) {
+            // read once: evicted first
+            const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(p));
+            memcpy(&r, &w, 16);
+        } else {
+            r = *reinterpret_cast<const Pack<T, V> *>(p);
+        }
+    }
+    return r;
+}
+
 template <typename T, int V, int KT>
 __global__ void __launch_bounds__(kMaxThreads) k_combine(const CombineArgs a)
 {
@@ -48,19 +70,20 @@ __global__ void __launch_bounds__(kMaxThreads) k_combine(const CombineArgs a)
         for (int i = 0; i < V; ++i)
             acc[i] = 0.0f;
         for (int j0 = 0; j0 < a.k; j0 += KT) {
-            float v[KT][V];
+            Pack<T, V> v[KT];
 #pragma unroll
             for (int j = 0; j < KT; ++j) {
                 const int32_t p = s.pos[j0 + j];   // -1 past k
-                if (p >= 0)
-                    load_pack<T, V>(y + p * a.ldy + h, v[j]);
+                v[j] = load_if<T, V>(p >= 0, y + p * a.ldy + h);
             }
 #pragma unroll
-            for (int j = 0; j < KT; ++j)
+            for (int j = 0; j < KT; ++j) {
+                const float w = s.weight[j0 + j];
                 if (s.pos[j0 + j] >= 0)
 #pragma unroll
                     for (int i = 0; i < V; ++i)
-                        acc[i] = fmaf(s.weight[j0 + j], v[j][i], acc[i]);
+                        acc[i] = fmaf(w, to_f32(v[j].v[i]), acc[i]);
+            }
         }
         store_pack<T, V>(out + h, acc);
     }
@@ -82,33 +105,29 @@ __global__ void __launch_bounds__(kMaxThreads) k_combine_backward(const CombineA
         for (int j = 0; j < KT; ++j)
             dot[j] = 0.0f;
         for (int h = threadIdx.x * V; h < a.H; h += blockDim.x * V) {
-            float d[V], v[KT][V];
-            load_pack<T, V>(dout + h, d);
-            if (a.dweight) {
+            float d[V];
+            Pack<T, V> v[KT];
 #pragma unroll
-                for (int j = 0; j < KT; ++j) {
-                    const int32_t p = s.pos[j0 + j];
-                    if (p >= 0)
-                        load_pack<T, V>(y + p * a.ldy + h, v[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < KT; ++j)
-                    if (s.pos[j0 + j] >= 0)
-#pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            dot[j] = fmaf(d[i], v[j][i], dot[j]);
+            for (int j = 0; j < KT; ++j) {
+                const int32_t p = s.pos[j0 + j];
+                v[j] = load_if<T, V>(a.dweight && p >= 0, y + p * a.ldy + h);
             }
-            if (dy) {
+            load_pack<T, V>(dout + h, d);
 #pragma unroll
-                for (int j = 0; j < KT; ++j) {
-                    const int32_t p = s.pos[j0 + j];
-                    if (p >= 0) {
-                        float g[V];
+            for (int j = 0; j < KT; ++j) {
+                const int32_t p = s.pos[j0 + j];
+                if (p < 0)
+                    continue;
 #pragma unroll
-                        for (int i = 0; i < V; ++i)
-                            g[i] = s.weight[j0 + j] * d[i];
-                        store_pack<T, V>(dy + p * a.lddy + h, g);
-                    }
+                for (int i = 0; i < V; ++i)
+                    dot[j] = fmaf(d[i], to_f32(v[j].v[i]), dot[j]);
+                if (dy) {
+                    const float w = s.weight[j0 + j];
+                    float g[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        g[i] = w * d[i];
+                    store_pack<T, V>(dy + p * a.lddy + h, g);
                 }
             }
         }

@@ -95,7 +95,7 @@ struct BalanceArgs {
     int32_t *part_count;  // slots x E
     float *part_lse;      // slots
     int32_t *part_tokens; // slots
-    float *seq_loss;      // B x 2
+    float *seq_loss;      // B x 3: balance loss, sum of squares, tokens
     unsigned int *ticket;
 };
 int64_t balance_slots(int64_t T, int32_t B);

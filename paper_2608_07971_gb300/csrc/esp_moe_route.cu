@@ -165,12 +165,15 @@ __device__ __forceinline__ float gate_weight(const Gate &g, bool on, float zj, f
     return g.sigmoid ? sigmoid_f(zj) : expf(zj - m) / zsum;
 }
 
-// Exclusive scan of v[0..E) in shared memory into out[0..E] by one warp.
-__device__ __forceinline__ void warp_scan(const int *v, int E, int *out, int lane)
+// Exclusive scan of v[0..E) in shared memory into out[0..E] by the whole CTA (at least E threads, or E in
+// steps of its threads); sums: a word per warp. Barriers before and after are inside.
+__device__ __forceinline__ void block_scan(const int *v, int E, int *out, int *sums)
 {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     int carry = 0;
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int x = e0 + lane < E ? v[e0 + lane] : 0;
+    for (int e0 = 0; e0 < E; e0 += blockDim.x) {
+        __syncthreads();
+        const int e = e0 + threadIdx.x, x = e < E ? v[e] : 0;
         int s = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -178,12 +181,18 @@ __device__ __forceinline__ void warp_scan(const int *v, int E, int *out, int lan
             if (lane >= o)
                 s += y;
         }
-        if (e0 + lane < E)
-            out[e0 + lane] = carry + s - x;
-        carry += __shfl_sync(kFull, s, 31);
+        if (lane == 31)
+            sums[warp] = s;
+        __syncthreads();
+        const int part = lane < warps ? sums[lane] : 0;
+        const int before = __reduce_add_sync(kFull, lane < warp ? part : 0);
+        if (e < E)
+            out[e] = carry + before + s - x;
+        carry += __reduce_add_sync(kFull, part);
     }
-    if (lane == 0)
+    if (threadIdx.x == 0)
         out[E] = carry;
+    __syncthreads();
 }
 
 // ---- route
@@ -304,6 +313,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     int *wcount = sm + kPadded;                        // W x E
     int *hist = wcount + W * a.E;                      // E
     int *offs = hist + a.E;                            // E + 1 (FUSED)
+    __shared__ int sums[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int E = a.E, k = a.k;
     const bool plan = a.offsets != nullptr;
@@ -375,11 +385,10 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     }
     if (!plan)
         return;
-    __syncthreads();
-    if (FUSED) {
-        if (warp == 0)
-            warp_scan(hist, E, offs, lane);
+    if (!FUSED)
         __syncthreads();
+    if (FUSED) {
+        block_scan(hist, E, offs, sums);
         for (int e = threadIdx.x; e <= E; e += kThr)
             a.offsets[e] = offs[e];
         for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += kThr)
@@ -400,21 +409,31 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
 // kPlanChunks chunks and sums the columns over all chunks and over those before its own.
 constexpr int kPlanThreads = 1024, kPlanChunks = 2;
 
-template <typename D>
+// D: a demand; a thread adds V columns (one load) of every groups-th chunk.
+template <typename D, int V>
 __device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0, int *total, int *before, int *second)
 {
-    const int groups = max(1, kPlanThreads / E);
-    for (int i = threadIdx.x; i < groups * E; i += kPlanThreads) {
-        const int e = i % E, g = i / E;
-        int all = 0, bef = 0;
-#pragma unroll 16
+    struct alignas(sizeof(D) * V) Row {
+        D v[V];
+    };
+    const int cols = E / V, groups = max(1, kPlanThreads / cols);
+    for (int i = threadIdx.x; i < groups * cols; i += kPlanThreads) {
+        const int c = i % cols, g = i / cols;
+        int all[V] = {}, bef[V] = {};
+#pragma unroll 8
         for (int b = g; b < nb; b += groups) {
-            const int h = hist[(int64_t)b * E + e];
-            all += h;
-            bef += b < c0 ? h : 0;
+            const Row r = *reinterpret_cast<const Row *>(hist + (int64_t)b * E + c * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                all[j] += r.v[j];
+                bef[j] += b < c0 ? r.v[j] : 0;
+            }
         }
-        atomicAdd(total + e, all);
-        atomicAdd(before + e, bef);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            atomicAdd(total + c * V + j, all[j]);
+            atomicAdd(before + c * V + j, bef[j]);
+        }
     }
     for (int e = threadIdx.x; e < E; e += kPlanThreads)
         second[e] = hist[(int64_t)c0 * E + e];
@@ -423,6 +442,7 @@ __device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0
 __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
 {
     extern __shared__ int sm[];
+    __shared__ int sums[kPlanThreads / 32];
     const int E = a.E, k = a.k, c0 = blockIdx.x * kPlanChunks;
     int *total = sm, *before = sm + E, *second = sm + 2 * E, *offs = sm + 3 * E;
     for (int e = threadIdx.x; e < E; e += kPlanThreads)
@@ -433,14 +453,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_
     int64_t i = s0 + threadIdx.x;
     int e = i < s1 ? a.idx[i] : -1, rank = i < s1 ? a.pos[i] : 0;
     __syncthreads();
-    if (a.hist16)
-        sum_columns(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
+    if (!a.hist16)
+        sum_columns<int32_t, 1>(a.hist, E, nb, c0, total, before, second);
+    else if (E % 4 == 0)
+        sum_columns<uint16_t, 4>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
     else
-        sum_columns(a.hist, E, nb, c0, total, before, second);
-    __syncthreads();
-    if (threadIdx.x < 32)
-        warp_scan(total, E, offs, threadIdx.x);
-    __syncthreads();
+        sum_columns<uint16_t, 1>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
+    block_scan(total, E, offs, sums);
     if (blockIdx.x == 0)
         for (int q = threadIdx.x; q < E; q += kPlanThreads)
             a.counts[q] = total[q];
@@ -486,15 +505,16 @@ __device__ __forceinline__ int seq_of(const int32_t *seq, int B, int64_t t)
 }
 
 template <typename T, int VPT>
-__global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64_t chunk, bool aligned)
+__global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArgs a, int64_t chunk, bool aligned)
 {
     using S = RowShape<T, VPT>;
+    constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
     extern __shared__ float smf[];
     const int E = a.E, k = a.k;
     float *red = smf;                                      // warps x E
-    int *hist = reinterpret_cast<int *>(red + kWarps * E); // E
-    __shared__ float lse_w[kWarps];
-    __shared__ int tok_w[kWarps];
+    int *hist = reinterpret_cast<int *>(red + W * E); // E
+    __shared__ float lse_w[W];
+    __shared__ int tok_w[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c0 = blockIdx.x * chunk, c1 = min(a.T, c0 + chunk);
     for (int s = a.seq ? seq_of(a.seq, a.B, c0) : 0; s < a.B; ++s) {
@@ -505,7 +525,7 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
         if (lo >= hi)
             continue;
         __syncthreads();
-        for (int e = threadIdx.x; e < E; e += kThreads)
+        for (int e = threadIdx.x; e < E; e += kThr)
             hist[e] = 0;
         __syncthreads();
         float acc[VPT];
@@ -524,13 +544,13 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
             }
         };
         fetch(lo + warp);
-        for (int64_t t = lo + warp; t < hi; t += kWarps) {
+        for (int64_t t = lo + warp; t < hi; t += W) {
             const int mine = next_idx;
             float z[VPT], p[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
                 z[i] = next[i];
-            fetch(t + kWarps);
+            fetch(t + W);
             if (__shfl_sync(kFull, mine, 0) < 0)
                 continue;
             if (mine >= 0 && mine < E)
@@ -560,9 +580,9 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
         }
         __syncthreads();
         const int64_t slot = (int64_t)blockIdx.x + s;
-        for (int e = threadIdx.x; e < E; e += kThreads) {
+        for (int e = threadIdx.x; e < E; e += kThr) {
             float v = 0.0f;
-            for (int w = 0; w < kWarps; ++w)
+            for (int w = 0; w < W; ++w)
                 v += red[w * E + e];
             a.part_share[slot * E + e] = v;
             a.part_count[slot * E + e] = hist[e];
@@ -570,7 +590,7 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
         if (threadIdx.x == 0) {
             float l = 0.0f;
             int n = 0;
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < W; ++w) {
                 l += lse_w[w];
                 n += tok_w[w];
             }
@@ -580,25 +600,33 @@ __global__ void __launch_bounds__(kThreads) k_balance(const BalanceArgs a, int64
     }
 }
 
-// Sum over a CTA in a fixed order (warp trees, then the warps in turn); every thread gets it.
-__device__ float block_sum(float v, float *buf)
+// Sums over a CTA of kThreads in a fixed order (warp trees, then the warps in turn); every thread gets them.
+// buf: N words per warp, not read by the CTA since its last barrier.
+template <int N>
+__device__ __forceinline__ void block_sums(float (&v)[N], float (*buf)[N])
 {
-    v = warp_sum(v);
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] = warp_sum(v[i]);
     if ((threadIdx.x & 31) == 0)
-        buf[threadIdx.x >> 5] = v;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            buf[threadIdx.x >> 5][i] = v[i];
     __syncthreads();
-    float s = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w)
-        s += buf[w];
-    return s;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            v[i] += buf[w][i];
+    }
 }
 
 // One CTA per sequence: the chunks' parts in order; the last CTA to finish sums the sequences' losses.
 __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, int64_t chunk)
 {
     extern __shared__ float smf[];
-    __shared__ float buf[kWarps];
+    __shared__ float buf1[kWarps][1], buf2[kWarps][1], buf4[kWarps][4];
     __shared__ int nbuf[kWarps];
     __shared__ bool last;
     const int E = a.E, s = blockIdx.x;
@@ -608,10 +636,10 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     const int64_t lo = a.seq ? seq_bound(a.seq, s, a.T) : 0, hi = a.seq ? seq_bound(a.seq, s + 1, a.T) : a.T;
     const int64_t b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
     int n = 0;
-    float lse = 0.0f;
+    float lse[1] = {0.0f};
     for (int64_t b = b0 + threadIdx.x; b < b1; b += kThreads) {
         n += a.part_tokens[b + s];
-        lse += a.part_lse[b + s];
+        lse[0] += a.part_lse[b + s];
     }
     for (int i = threadIdx.x; i < groups * E; i += kThreads) {
         const int e = i % E, g = i / E;
@@ -628,11 +656,11 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     n = __reduce_add_sync(kFull, n);
     if ((threadIdx.x & 31) == 0)
         nbuf[threadIdx.x >> 5] = n;
-    lse = block_sum(lse, buf);   // its barriers publish the parts too
+    block_sums<1>(lse, buf1);   // its barrier publishes the parts too
     n = 0;
     for (int w = 0; w < kWarps; ++w)
         n += nbuf[w];
-    float dot = 0.0f;
+    float dot[1] = {0.0f};
     for (int e = threadIdx.x; e < E; e += kThreads) {
         float v = 0.0f;
         int c = 0;
@@ -643,13 +671,15 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
         const float mean = n > 0 ? v / (float)n : 0.0f;
         a.share[(int64_t)s * E + e] = mean;
         a.counts[(int64_t)s * E + e] = c;
-        dot += (float)c * mean;
+        dot[0] += (float)c * mean;
     }
-    dot = block_sum(dot, buf);
+    block_sums<1>(dot, buf2);
     if (threadIdx.x == 0) {
         a.tokens[s] = n;
-        a.seq_loss[2 * s] = n > 0 ? (float)E * dot / ((float)a.k * (float)n) : 0.0f;
-        a.seq_loss[2 * s + 1] = lse;
+        float *mine = a.seq_loss + 3 * s;
+        mine[0] = n > 0 ? (float)E * dot[0] / ((float)a.k * (float)n) : 0.0f;
+        mine[1] = lse[0];
+        mine[2] = (float)n;
         __threadfence();
         last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
     }
@@ -657,22 +687,19 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     if (!last)
         return;
     __threadfence();
-    float bal = 0.0f, zl = 0.0f, used = 0.0f;
-    double tok = 0.0;
+    // balance losses, squares, sequences in use, tokens
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int b = threadIdx.x; b < a.B; b += kThreads) {
-        bal += __ldcg(a.seq_loss + 2 * b);
-        zl += __ldcg(a.seq_loss + 2 * b + 1);
-        const long long nb = __ldcg(reinterpret_cast<const long long *>(a.tokens) + b);
-        used += nb > 0 ? 1.0f : 0.0f;
-        tok += (double)nb;
+        const float n_b = __ldcg(a.seq_loss + 3 * b + 2);
+        sum[0] += __ldcg(a.seq_loss + 3 * b);
+        sum[1] += __ldcg(a.seq_loss + 3 * b + 1);
+        sum[2] += n_b > 0.0f ? 1.0f : 0.0f;
+        sum[3] += n_b;
     }
-    bal = block_sum(bal, buf);
-    zl = block_sum(zl, buf);
-    used = block_sum(used, buf);
-    const float total = block_sum((float)tok, buf);
+    block_sums<4>(sum, buf4);
     if (threadIdx.x == 0) {
-        a.loss[0] = used > 0.0f ? bal / used : 0.0f;
-        a.loss[1] = total > 0.0f ? zl / total : 0.0f;
+        a.loss[0] = sum[2] > 0.0f ? sum[0] / sum[2] : 0.0f;
+        a.loss[1] = sum[3] > 0.0f ? sum[1] / sum[3] : 0.0f;
         *a.ticket = 0u;
     }
 }
@@ -724,6 +751,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
     const bool dense_softmax = !a.gate.sigmoid && !a.gate.renorm;
     float coef[BALANCE ? VPT : 1];   // gradient of a counted token's r, for the sequence `held`
     int held = -1;
+    int64_t held_end = 0;   // the first token past the stretch that `held` describes (-1: in no sequence)
     __syncwarp();
     for (int64_t t = t0; t < t1; ++t) {
         T *drow = static_cast<T *>(a.dlogits) + t * a.ld_out;
@@ -779,9 +807,13 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
             __syncwarp();
         }
         if constexpr (BALANCE) {
-            const int s = a.seq ? seq_of(a.seq, a.B, t) : 0;
-            if (s < a.B && (!a.seq || t >= a.seq[s])) {
-                if (s != held) {
+            if (t >= held_end) {   // the token's sequence, if it lies in one
+                const int s = a.seq ? seq_of(a.seq, a.B, t) : 0;
+                const bool in = s < a.B && (!a.seq || t >= a.seq[s]);
+                held_end = a.seq ? (in ? (int64_t)a.seq[s + 1] : s < a.B ? (int64_t)a.seq[s] : a.T) : a.T;
+                if (!in)
+                    held = -1;
+                if (in && s != held) {
                     held = s;
                     const float n = (float)a.tokens[s];
                     const float c = n > 0.0f ? g0 / (n * n) : 0.0f;
@@ -791,6 +823,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
                         coef[i] = q < E ? c * (float)(int32_t)a.counts[(int64_t)s * E + q] : 0.0f;   // below 2^31
                     }
                 }
+            }
+            if (held >= 0) {
                 const float gz = g1 * lse;
                 if (!a.gate.sigmoid) {
                     float dot = 0.0f;
@@ -934,11 +968,12 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
             return with_vpt(a.E, [&](auto vpt) -> cudaError_t {
                 constexpr int VPT = decltype(vpt)::value;
                 using S = RowShape<T, VPT>;
-                const size_t smem = (size_t)(kWarps + 1) * a.E * sizeof(float);
+                constexpr int kThr = kRouteThreads<VPT>;
+                const size_t smem = (size_t)(kThr / 32 + 1) * a.E * sizeof(float);
                 const cudaError_t e2 = allow_smem(k_balance<T, VPT>, smem);
                 if (e2 != cudaSuccess)
                     return e2;
-                k_balance<T, VPT><<<(int)ceil_div(a.T, chunk), kThreads, smem, m->stream>>>(
+                k_balance<T, VPT><<<(int)ceil_div(a.T, chunk), kThr, smem, m->stream>>>(
                     a, chunk, rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T)));
                 m->launches += 1;
                 return cudaGetLastError();
@@ -963,7 +998,8 @@ cudaError_t launch_route_backward(esp_moe *m, int32_t dtype, const RouteBackward
             constexpr int VPT = decltype(vpt)::value;
             using S = RowShape<T, VPT>;
             constexpr int kW = kBwdThreads / 32;
-            const int64_t warps = std::min<int64_t>(a.T, (int64_t)m->sm_count * 6 * kW);
+            // resident at once: with the losses a warp first reads its sequence's counts, so it takes more tokens
+            const int64_t warps = std::min<int64_t>(a.T, (int64_t)m->sm_count * (a.dloss ? 2 : 4) * kW);
             const int64_t per = ceil_div(a.T, warps);
             const int grid = (int)ceil_div(ceil_div(a.T, per), kW);
             const size_t smem = (size_t)kW * 32 * VPT * sizeof(float);
