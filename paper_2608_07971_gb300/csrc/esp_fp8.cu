@@ -13,6 +13,7 @@
 #include <cuda_fp8.h>
 
 #include "esp_moe_impl.h"
+#include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
 
 namespace esp_moe_impl {
@@ -151,6 +152,7 @@ constexpr int kRowBlocks = kRowThreads / 4;   // of a CTA
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const QuantRowsArgs a, int blocks_k, bool aligned)
 {
+    let_next_launch_start();
     const int lane4 = threadIdx.x & 3;
     const int64_t total = a.M * blocks_k, i = (int64_t)blockIdx.x * kRowBlocks + (threadIdx.x >> 2);
     const bool on = i < total;
@@ -327,6 +329,7 @@ template <typename T>
 __global__ void __launch_bounds__(kTileThreads) k_quant_cols(const QuantColsArgs a, bool aligned)
 {
     __shared__ TileSmem s;
+    let_next_launch_start();
     const int tiles_k = (a.K + kBlock - 1) / kBlock, run = blockIdx.x / tiles_k;
     int row0, n;
     find_run(a.offsets, a.E, a.M, run, row0, n);

@@ -24,6 +24,7 @@
 #include <cuda.h>
 
 #include "esp_moe_impl.h"
+#include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
 
 namespace esp_moe_impl {
@@ -70,6 +71,12 @@ struct GemmParams {
     bool wide_store;
     unsigned int *err;
     uint32_t wait_ms;
+    // parts of every tile's inner axis, each a work item of its own (CG = 1); their sums meet in
+    // partial[item][BN / 4][128][4] (lanes hold rows: consecutive rows, four columns each, lie together), and
+    // the last part of a tile to arrive adds them up in order
+    int32_t splits;
+    float *partial;
+    unsigned int *tickets;           // one per tile, zero between launches
     int32_t hold;                    // leave out the CTAs' third load (failure detection)
 };
 
@@ -277,17 +284,18 @@ __device__ __forceinline__ void mul_pair(float &a, float &b, float s)
         : "f"(s));
 }
 
-// Barrier of a warpgroup that also ANDs a predicate over it.
-__device__ __forceinline__ bool wg_sync_and(int id, bool v)
+// Barrier of N threads that also ANDs a predicate over them.
+template <int N>
+__device__ __forceinline__ bool sync_and(int id, bool v)
 {
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %1, 0;\n\t"
-        "bar.red.and.pred q, %2, 128, p;\n\t"
+        "bar.red.and.pred q, %2, %3, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}"
         : "=r"(r)
-        : "r"((uint32_t)v), "r"(id)
+        : "r"((uint32_t)v), "r"(id), "n"(N)
         : "memory");
     return r != 0;
 }
@@ -299,18 +307,34 @@ __device__ __forceinline__ void expert_rows(const GemmParams &p, int e, int &lo,
     hi = p.offsets ? max(lo, min(p.M, p.offsets[e + 1])) : p.M;
 }
 
-// One tile of the list: rows m0 .. m0 + rows - 1 of expert e (COLS: of its output), columns n0 .., blocks
-// kb0 .. kb1 - 1.
+// One item of the list: rows m0 .. m0 + rows - 1 of expert e (COLS: of its output), columns n0 .., blocks
+// kb0 .. kb1 - 1 (of a tile's, where its inner axis is split).
 struct Tile {
     int e, m0, rows, n0, kb0, kb1;
 };
 
+// Part number `part` of the tile's blocks.
+template <int CG>
+__device__ __forceinline__ void take_part(const GemmParams &p, int part, Tile &t)
+{
+    if (CG == 2 || p.splits == 1)
+        return;
+    const int first = t.kb0, n = t.kb1 - t.kb0;
+    t.kb0 = first + (int)((int64_t)n * part / p.splits);
+    t.kb1 = first + (int)((int64_t)n * (part + 1) / p.splits);
+}
+
 // table[e]: row tiles (COLS: blocks) of the experts before e. Tiles run over an expert's rows first, so that
 // the tiles in flight share columns of B.
 template <int CG, int BN, bool COLS>
-__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int w, Tile &t)
+__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int item, Tile &t)
 {
     constexpr int BM = kRowsA * CG;
+    int w = item, part = 0;
+    if (CG == 1 && p.splits > 1) {
+        w = item / p.splits;
+        part = item - w * p.splits;
+    }
     const int nt = (p.N + BN - 1) / BN;
     if (!COLS) {
         if (w >= table[p.E] * nt)
@@ -332,6 +356,7 @@ __device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, i
         t.n0 = (i / mt) * BN;
         t.kb0 = 0;
         t.kb1 = (p.K + kBlock - 1) / kBlock;
+        take_part<CG>(p, part, t);
         return true;
     }
     const int mt = (p.rows_b + BM - 1) / BM;   // rows_b: output rows per expert
@@ -345,6 +370,7 @@ __device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, i
     t.n0 = (i / mt) * BN;
     t.kb0 = table[t.e];
     t.kb1 = table[t.e + 1];
+    take_part<CG>(p, part, t);
     return true;
 }
 
@@ -376,6 +402,53 @@ __device__ __forceinline__ void store_chunk(T *out, int64_t ldo, int rows, int c
             out[r * ldo + c] = reinterpret_cast<const T *>(stage + r * kStageRow)[c];
 }
 
+// Joins the parts of a split tile: every part's sums go to memory, and the CTA whose part is the last to
+// arrive gets back true and the sums over all parts, in their order. Called by all epilogue threads, those
+// whose waits ran out (ok false) too: then ok is false for all.
+template <int BN, int C>
+__device__ __forceinline__ bool join_parts(const GemmParams &p, int item, int row, int rows, int col, float (&sum)[C],
+                                           volatile int *last, bool &ok)
+{
+    const int tile = item / p.splits;
+    constexpr int64_t kPart = (int64_t)kRowsA * BN;
+    float4 *mine = reinterpret_cast<float4 *>(p.partial + item * kPart) + (col / 4) * kRowsA + row;
+    if (row < rows)
+#pragma unroll
+        for (int i = 0; i < C / 4; ++i)
+            __stcg(mine + i * kRowsA, make_float4(sum[4 * i], sum[4 * i + 1], sum[4 * i + 2], sum[4 * i + 3]));
+    __threadfence();
+    ok = sync_and<32 * kEpilogueWarps>(7, ok);
+    if (!ok)
+        return false;
+    if (threadIdx.x == 0) {
+        const bool l = atomicAdd(p.tickets + tile, 1u) == (unsigned)p.splits - 1;
+        if (l)
+            p.tickets[tile] = 0u;
+        *last = l;
+        __threadfence();
+    }
+    asm volatile("bar.sync 7, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
+    if (!*last)
+        return false;
+    const float4 *all =
+        reinterpret_cast<const float4 *>(p.partial + tile * (int64_t)p.splits * kPart) + (col / 4) * kRowsA + row;
+    if (row < rows) {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            sum[i] = 0.0f;
+        for (int q = 0; q < p.splits; ++q)
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i) {
+                const float4 v = __ldcg(all + q * (kPart / 4) + i * kRowsA);
+                sum[4 * i] += v.x;
+                sum[4 * i + 1] += v.y;
+                sum[4 * i + 2] += v.z;
+                sum[4 * i + 3] += v.w;
+            }
+    }
+    return true;
+}
+
 template <int CG, int BN, bool COLS, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmParams p)
@@ -392,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, tfull = empty + 8 * S::kStages,
                    tempty = tfull + 8 * S::kAcc, drain = tempty + 8 * S::kAcc;
     uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 2 * S::kStages + 2 * S::kAcc + 1);
-    volatile int *dead = reinterpret_cast<volatile int *>(slot + 1);
+    volatile int *dead = reinterpret_cast<volatile int *>(slot + 1), *last = dead + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
 
@@ -409,6 +482,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 9) {
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    // what follows reads what the launch before wrote (the codes) or is ordered after it
+    wait_for_launch_before();
     if (warp == 8) {
         // the experts' row tiles (blocks) before each: one warp's scan
         int carry = 0;
@@ -433,19 +521,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (lane == 0)
             table[p.E] = carry;
-    }
-    if (warp == 9) {
-        if (CG == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
-                         "r"(kTmemCols)
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
-                         "r"(kTmemCols)
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        }
     }
     fence_before();
     __syncthreads();
@@ -562,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, aph, p, dead));
                 if (COLS)
-                    ok = wg_sync_and(1 + wg, ok);
+                    ok = sync_and<128>(1 + wg, ok);
                 if (!ok)
                     break;
                 fence_after();
@@ -613,6 +688,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     acc = 0;
                     aph ^= 1;
                 }
+            }
+            if (CG == 1 && p.splits > 1) {
+                if (!join_parts<BN, S::kWGCols>(p, w, row, rows, wg * S::kWGCols, sum, last, ok))
+                    continue;
             }
             if (!ok || !some)
                 continue;
@@ -693,21 +772,23 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, GemmP
 {
     using S = Shape<CG, BN>;
     auto kernel = k_gemm<CG, BN, COLS, T>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    cudaError_t e = allow_smem<k_gemm<CG, BN, COLS, T>>(S::kSmem, m->device);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
+    attr[0] = after_launch_before();
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = m->stream;
     int groups = m->sm_count;
     if (CG == 2) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = CG;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = CG;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
         if (m->max_pairs == 0) {
             cfg.gridDim = dim3((unsigned)(m->sm_count / CG * CG));
             e = cudaOccupancyMaxActiveClusters(&m->max_pairs, kernel, &cfg);
@@ -739,10 +820,47 @@ GemmParams common(esp_moe *m)
     p.wait_ms = m->wait_ms;
     p.hold = m->hold_load ? 1 : 0;
     m->hold_load = false;   // the hook holds one launch only
+    p.splits = 1;
+    p.tickets = m->d_ticket + 1;
     return p;
 }
 
+// Which tiles a product takes: pairs of CTAs with 256 x 256, or single CTAs with 128 x 128 whose inner axis
+// may be split into parts. Times in units of a single CTA's block (about 0.4 us): rounds of tiles over the
+// SMs times the blocks of each. A pair's block takes 1.35 units (4096 x 4096 x 4096 as pairs 73 us, as
+// single CTAs 91; 1000 x 2000 x 2050: 15.9 and 14.3); joining parts takes 8 and 1 to
+// 1.5 for each part (128 x 4096 x 4096 in 4 parts 14.9 us, whole 16.6; 256 x 2048 x 2048 12.1 and 10.6).
+struct Choice {
+    bool pair;
+    int splits;
+};
+
+Choice choose_tiles(const esp_moe *m, int64_t tiles_pair, int64_t tiles_one, int64_t blocks, int64_t rows)
+{
+    const double t_pair = 1.35 * (double)(ceil_div(tiles_pair, std::max(1, m->sm_count / 2)) * blocks);
+    Choice best{true, 1};
+    double t_best = t_pair;
+    for (int splits = 1; splits <= 16; ++splits) {
+        // parts fill at most one round and keep four blocks each
+        if (splits > 1 && (tiles_one * splits > m->sm_count || blocks < 4 * splits))
+            break;
+        double t = (double)(ceil_div(tiles_one * splits, m->sm_count) * ceil_div(blocks, splits));
+        if (splits > 1)
+            t += 8.0 + splits * std::max(1.0, 1.5 * (double)std::min<int64_t>(rows, kRowsA) / kRowsA);
+        if (t < t_best) {
+            t_best = t;
+            best = Choice{false, splits};
+        }
+    }
+    return best;
+}
+
 }  // namespace
+
+size_t gemm_partial_floats(const esp_moe *m)
+{
+    return (size_t)m->sm_count * kRowsA * 128;   // parts fill at most one round
+}
 
 cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
 {
@@ -764,13 +882,17 @@ cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
         p.out = a.out;
         p.ldo = a.ldo;
         p.wide_store = rows_aligned(a.out, a.ldo, sizeof(T), 16);
+        p.partial = a.partial;
+        // at most this many tiles: every expert with rows has one that is not full
         const int64_t experts = std::min<int64_t>(a.E, a.M);
-        if (a.M / a.E > 128) {
-            const int64_t tiles = (a.M / 256 + experts) * ceil_div(a.N, 256);
-            return encode_and_launch<2, 256, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, tiles);
-        }
-        const int64_t tiles = (a.M / 128 + experts) * ceil_div(a.N, 128);
-        return encode_and_launch<1, 128, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, tiles);
+        const int64_t pair = (a.E == 1 ? ceil_div(a.M, 256) : a.M / 256 + experts) * ceil_div(a.N, 256);
+        const int64_t one = (a.E == 1 ? ceil_div(a.M, 128) : a.M / 128 + experts) * ceil_div(a.N, 128);
+        const Choice c = choose_tiles(m, pair, one, ceil_div(a.K, kBlock), a.M / a.E);
+        if (c.pair)
+            return encode_and_launch<2, 256, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, pair);
+        p.splits = c.splits;
+        return encode_and_launch<1, 128, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p,
+                                                   one * c.splits);
     });
 }
 
@@ -790,9 +912,15 @@ cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &a)
     p.out = a.out;
     p.ldo = a.ldo;
     p.wide_store = rows_aligned(a.out, a.ldo, 4, 16);
+    p.partial = a.partial;
     const int64_t positions = (a.M / kBlock + a.E) * kBlock;
-    return encode_and_launch<2, 256, true, float>(m, a.A, a.N, positions, a.lda, a.B, a.K, a.ldb, p,
-                                                  (int64_t)a.E * ceil_div(a.N, 256) * ceil_div(a.K, 256));
+    const int64_t pair = (int64_t)a.E * ceil_div(a.N, 256) * ceil_div(a.K, 256);
+    const int64_t one = (int64_t)a.E * ceil_div(a.N, 128) * ceil_div(a.K, 128);
+    const Choice c = choose_tiles(m, pair, one, ceil_div(a.M, kBlock * a.E), a.N);   // blocks: the experts' mean
+    if (c.pair)
+        return encode_and_launch<2, 256, true, float>(m, a.A, a.N, positions, a.lda, a.B, a.K, a.ldb, p, pair);
+    p.splits = c.splits;
+    return encode_and_launch<1, 128, true, float>(m, a.A, a.N, positions, a.lda, a.B, a.K, a.ldb, p, one * c.splits);
 }
 
 }  // namespace esp_moe_impl

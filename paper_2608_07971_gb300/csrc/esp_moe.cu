@@ -303,16 +303,18 @@ esp_status esp_moe_linear(esp_moe *m, int32_t dtype, int64_t T, int64_t ldx, con
         return ESP_OK;
     const int64_t kb = ceil_div(w->K, kBlock), nb = ceil_div(w->N, kBlock);
     QuantRowsArgs q{M, T, ldx, round_up(w->K, 16), round_up(kb, 4), w->K, x, rows, nullptr, nullptr};
+    float *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
         q.q = c.take<uint8_t>((size_t)(M * q.ldq));
         q.scale = c.take<float>((size_t)(M * q.lds));
+        partial = c.take<float>(gemm_partial_floats(m));
         if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
             return st;
     }
     MOE_CUDA(launch_quant_rows(m, dtype, q));
     const GemmRowsArgs g{M, q.ldq, q.lds, w->ld, ldy, w->E, w->N, w->K, q.q, w->q, q.scale, w->scale,
-                         nb * kb, kb, 1, offsets, y};
+                         nb * kb, kb, 1, offsets, y, partial};
     MOE_CUDA(launch_gemm_rows(m, dtype, g));
     return ESP_OK;
 }
@@ -335,8 +337,10 @@ esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t
     QuantRowsArgs q{M, M, lddy, round_up(w->N, 16), round_up(nb, 4), w->N, dy, nullptr, nullptr, nullptr};
     QuantColsArgs cy{M, M, lddy, positions, round_up(w->N, 4), w->N, w->E, dy, nullptr, offsets, nullptr, nullptr};
     QuantColsArgs cx{M, T, ldx, positions, round_up(w->K, 4), w->K, w->E, x, rows, offsets, nullptr, nullptr};
+    float *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
+        partial = c.take<float>(gemm_partial_floats(m));
         if (want_dx) {
             q.q = c.take<uint8_t>((size_t)(M * q.ldq));
             q.scale = c.take<float>((size_t)(M * q.lds));
@@ -353,14 +357,14 @@ esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t
     if (want_dx) {
         MOE_CUDA(launch_quant_rows(m, dtype, q));
         const GemmRowsArgs g{M, q.ldq, q.lds, w->ldt, lddx, w->E, w->K, w->N, q.q, w->qt, q.scale, w->scale,
-                             nb * kb, 1, kb, offsets, dx};
+                             nb * kb, 1, kb, offsets, dx, partial};
         MOE_CUDA(launch_gemm_rows(m, dtype, g));
     }
     if (dw) {
         MOE_CUDA(launch_quant_cols(m, dtype, cy));
         MOE_CUDA(launch_quant_cols(m, dtype, cx));
         const GemmColsArgs g{M, cy.ldq, cx.ldq, cy.lds, cx.lds, lddw, w->E, w->N, w->K, cy.q, cx.q, cy.scale, cx.scale,
-                             offsets, dw};
+                             offsets, dw, partial};
         MOE_CUDA(launch_gemm_cols(m, g));
     }
     return ESP_OK;

@@ -31,7 +31,7 @@ struct esp_moe {
 namespace esp_moe_impl {
 
 constexpr int kBlock = ESP_MOE_BLOCK;
-constexpr int kTickets = 1;
+constexpr int kTickets = 1 + 256;   // the losses', and one per tile of a split product (fewer tiles than SMs)
 
 // Carves the handle's work space into 256-byte aligned parts.
 class Carver {
@@ -171,6 +171,7 @@ struct GemmRowsArgs {
     int64_t sb_e, sb_n, sb_k;
     const int32_t *offsets;
     void *out;
+    float *partial;   // work space: gemm_partial_floats
 };
 cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a);
 
@@ -183,7 +184,10 @@ struct GemmColsArgs {
     const float *scale_a, *scale_b;
     const int32_t *offsets;
     float *out;
+    float *partial;
 };
+// Work space of a product whose tiles' inner axes are split over CTAs.
+size_t gemm_partial_floats(const esp_moe *m);
 cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &a);
 
 }  // namespace esp_moe_impl

@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "esp_moe_impl.h"
+#include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
 
 namespace esp_moe_impl {
@@ -308,6 +309,8 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     using S = RowShape<T, VPT>;
     constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
     extern __shared__ int sm[];
+    if (!FUSED)
+        let_next_launch_start();
     constexpr int kPadded = 32 * VPT;                  // E rounded up to the lanes' elements
     float *price = reinterpret_cast<float *>(sm);      // kPadded price terms
     int *wcount = sm + kPadded;                        // W x E
@@ -447,6 +450,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_
     int *total = sm, *before = sm + E, *second = sm + 2 * E, *offs = sm + 3 * E;
     for (int e = threadIdx.x; e < E; e += kPlanThreads)
         total[e] = before[e] = 0;
+    wait_for_launch_before();
     // the first slots' ranks are on their way while the columns are summed
     const int64_t s0 = c0 * chunk * k, s1 = a.offsets ? min(a.T * k, s0 + kPlanChunks * chunk * k) : s0;
     const int64_t mid = s0 + chunk * k;
@@ -513,6 +517,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
     const int E = a.E, k = a.k;
     float *red = smf;                                      // warps x E
     int *hist = reinterpret_cast<int *>(red + W * E); // E
+    let_next_launch_start();
     __shared__ float lse_w[W];
     __shared__ int tok_w[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -633,6 +638,7 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     const int groups = max(1, kThreads / E);
     float *share = smf;                                          // groups x E
     int *count = reinterpret_cast<int *>(smf + groups * E);      // groups x E
+    wait_for_launch_before();
     const int64_t lo = a.seq ? seq_bound(a.seq, s, a.T) : 0, hi = a.seq ? seq_bound(a.seq, s + 1, a.T) : a.T;
     const int64_t b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
     int n = 0;
@@ -905,14 +911,6 @@ cudaError_t with_vpt(int32_t E, F &&f)
     return f(std::integral_constant<int, 32>());
 }
 
-template <typename K>
-cudaError_t allow_smem(K kernel, size_t bytes)
-{
-    return bytes > 48 * 1024
-               ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)
-               : cudaSuccess;
-}
-
 }  // namespace
 
 size_t route_hist_ints(int64_t T, int32_t E, int32_t k)
@@ -933,7 +931,7 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
             constexpr int kThr = kRouteThreads<VPT>;
             const size_t route_smem = (size_t)(32 * VPT + (kThr / 32 + 2) * a.E + 1) * sizeof(int);
             if (fused(a.T, a.k)) {
-                const cudaError_t e = allow_smem(k_route<T, VPT, true>, route_smem);
+                const cudaError_t e = allow_smem<k_route<T, VPT, true>>(route_smem, m->device);
                 if (e != cudaSuccess)
                     return e;
                 k_route<T, VPT, true><<<1, kThr, route_smem, m->stream>>>(a, a.T, aligned);
@@ -942,14 +940,13 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
             }
             const int64_t chunk = route_chunk(a.T);
             const int nb = (int)ceil_div(a.T, chunk);
-            const cudaError_t e = allow_smem(k_route<T, VPT, false>, route_smem);
+            const cudaError_t e = allow_smem<k_route<T, VPT, false>>(route_smem, m->device);
             if (e != cudaSuccess)
                 return e;
             k_route<T, VPT, false><<<nb, kThr, route_smem, m->stream>>>(a, chunk, aligned);
-            k_plan<<<a.offsets ? (int)ceil_div(nb, kPlanChunks) : 1, kPlanThreads, (size_t)(4 * a.E + 1) * sizeof(int),
-                     m->stream>>>(a, chunk, nb);
             m->launches += 2;
-            return cudaGetLastError();
+            return launch_after(k_plan, dim3(a.offsets ? (unsigned)ceil_div(nb, kPlanChunks) : 1u), kPlanThreads,
+                                (size_t)(4 * a.E + 1) * sizeof(int), m->stream, a, chunk, nb);
         });
     });
 }
@@ -970,7 +967,7 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
                 using S = RowShape<T, VPT>;
                 constexpr int kThr = kRouteThreads<VPT>;
                 const size_t smem = (size_t)(kThr / 32 + 1) * a.E * sizeof(float);
-                const cudaError_t e2 = allow_smem(k_balance<T, VPT>, smem);
+                const cudaError_t e2 = allow_smem<k_balance<T, VPT>>(smem, m->device);
                 if (e2 != cudaSuccess)
                     return e2;
                 k_balance<T, VPT><<<(int)ceil_div(a.T, chunk), kThr, smem, m->stream>>>(
@@ -983,9 +980,8 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
             return e;
     }
     const size_t smem = (size_t)std::max(1, kThreads / a.E) * a.E * (sizeof(float) + sizeof(int));
-    k_balance_sum<<<a.B, kThreads, smem, m->stream>>>(a, chunk);
     m->launches += 1;
-    return cudaGetLastError();
+    return launch_after(k_balance_sum, dim3((unsigned)a.B), kThreads, smem, m->stream, a, chunk);
 }
 
 cudaError_t launch_route_backward(esp_moe *m, int32_t dtype, const RouteBackwardArgs &a)
