@@ -38,8 +38,8 @@ constexpr int kEpilogueWarps = 8;
 constexpr int kRowsA = 128;                  // rows of A that a CTA holds
 constexpr int kStageA = kRowsA * kBlock;     // bytes
 constexpr uint32_t kTmemCols = 512;
-constexpr int kStoreBytes = 128;             // of a row in a warp's staged store
-constexpr int kStageRow = kStoreBytes + 16;  // padded: no bank conflicts by rows or by columns
+constexpr int kBoxBytes = 128, kBox = 32 * kBoxBytes;   // a warp's staged store: 128 bytes of 32 rows
+constexpr int kStageBoxes = 2;               // of a warp
 constexpr int kSmemLimit = 232448;
 
 template <int CG, int BN>
@@ -48,9 +48,9 @@ struct Shape {
     static constexpr int kStage = kStageA + kRowsB * kBlock;
     static constexpr int kAcc = (int)kTmemCols / BN;
     static constexpr int kWGCols = BN / 2;   // columns of a warpgroup
-    // after the stages: tile table, store staging, column scales, barriers
+    // after the stages: store staging, tile table, column scales, barriers
     static constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4 + 12;   // a multiple of 16
-    static constexpr int kStaging = kEpilogueWarps * 32 * kStageRow;
+    static constexpr int kStaging = kEpilogueWarps * kStageBoxes * kBox;
     static constexpr int kColScales = 2 * 2 * kWGCols * 4;
     static constexpr int kBars = 256;
     static constexpr int kFixed = kTable + kStaging + kColScales + kBars + 1024;
@@ -374,32 +374,41 @@ __device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, i
     return true;
 }
 
-// A warp's 32 rows of 128 bytes of the output (a lane holds a row's values), through its staging buffer so
-// that the lanes of a store cover whole lines: stored straight from the registers, a store touches 32
-// lines and the warps spend a sixth to a fifth of the product's time there. Rows at or past `rows` and
-// columns at or past N are dropped.
+// A warp's 32 rows of one box of the output: 128 bytes of every row (a lane holds a row's values), staged in
+// the 128-byte swizzle (16-byte chunk j of row r at place j ^ (r & 7): no bank conflicts). Whole boxes leave
+// by one TMA store, so that the warp goes on while they are written; with a bulk copy for every row instead,
+// 65536 x 4096 x 2048 takes 596 us, and 514 without the copies. Boxes that reach past the expert's last row,
+// and outputs that are not 16-byte aligned, are stored by the lanes: rows at or past `rows` and columns at
+// or past `cols` are dropped.
 template <typename T>
-__device__ __forceinline__ void store_chunk(T *out, int64_t ldo, int rows, int cols, bool wide, const float *v,
-                                            unsigned char *stage, int lane)
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int x, int y, T *out, int64_t ldo, int rows, int cols,
+                                          bool wide, const float *v, unsigned char *box, int lane)
 {
-    constexpr int C = kStoreBytes / (int)sizeof(T), V = 16 / (int)sizeof(T);
-    __syncwarp();
+    constexpr int V = 16 / (int)sizeof(T), C = kBoxBytes / (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < C; i += V)
-        store_pack<T, V>(reinterpret_cast<T *>(stage + lane * kStageRow) + i, v + i);
-    __syncwarp();
-    if (wide && cols >= C) {
-        const int r0 = lane >> 3, b = (lane & 7) * 16;
-#pragma unroll
-        for (int r = r0; r < 32; r += 4)
-            if (r < rows)
-                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(out + r * ldo) + b) =
-                    *reinterpret_cast<const uint4 *>(stage + r * kStageRow + b);
+        store_pack<T, V>(reinterpret_cast<T *>(box + lane * kBoxBytes + (((i / V) ^ (lane & 7)) * 16)), v + i);
+    if (wide && rows >= 32) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0)
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map),
+                         "r"(x), "r"(y), "r"(smem_u32(box))
+                         : "memory");
         return;
     }
-    for (int r = 0; r < 32 && r < rows; ++r)
-        for (int c = lane; c < C && c < cols; c += 32)
-            out[r * ldo + c] = reinterpret_cast<const T *>(stage + r * kStageRow)[c];
+    __syncwarp();
+    if (wide && cols >= C) {
+        const int j = lane & 7;
+        for (int r = lane >> 3; r < 32 && r < rows; r += 4)
+            *reinterpret_cast<uint4 *>(out + r * ldo + j * V) =
+                *reinterpret_cast<const uint4 *>(box + r * kBoxBytes + ((j ^ (r & 7)) * 16));
+    } else {
+        for (int r = 0; r < 32 && r < rows; ++r)
+            for (int c = lane; c < C && c < cols; c += 32)
+                out[r * ldo + c] =
+                    reinterpret_cast<const T *>(box + r * kBoxBytes + (((c / V) ^ (r & 7)) * 16))[c % V];
+    }
 }
 
 // Joins the parts of a split tile: every part's sums go to memory, and the CTA whose part is the last to
@@ -451,15 +460,16 @@ __device__ __forceinline__ bool join_parts(const GemmParams &p, int item, int ro
 
 template <int CG, int BN, bool COLS, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmParams p)
+    k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+           const __grid_constant__ CUtensorMap map_out, const GemmParams p)
 {
     using S = Shape<CG, BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *sm = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                           ~static_cast<uintptr_t>(1023));
-    int *table = reinterpret_cast<int *>(sm + S::kStages * S::kStage);
-    unsigned char *staging = sm + S::kStages * S::kStage + S::kTable;
-    float *colscale = reinterpret_cast<float *>(staging + S::kStaging);
+    unsigned char *staging = sm + S::kStages * S::kStage;   // its boxes are 1024-byte aligned
+    int *table = reinterpret_cast<int *>(staging + S::kStaging);
+    float *colscale = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(table) + S::kTable);
     uint64_t *bars = reinterpret_cast<uint64_t *>(
         (reinterpret_cast<uintptr_t>(colscale + S::kColScales / 4) + 15) & ~static_cast<uintptr_t>(15));
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, tfull = empty + 8 * S::kStages,
@@ -594,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int wg = warp >> 2, quarter = warp & 3;
         const uint32_t lane_cols = ((uint32_t)(32 * quarter) << 16) + (uint32_t)(wg * S::kWGCols);
         const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
-        unsigned char *stage = staging + warp * 32 * kStageRow;
+        unsigned char *stage = staging + warp * kStageBoxes * kBox;
         float *cs = colscale + wg * 2 * S::kWGCols;
         int acc = 0, turn = 0;
         uint32_t aph = 0;
@@ -695,13 +705,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!ok || !some)
                 continue;
-            T *out = static_cast<T *>(p.out) + ((COLS ? (int64_t)t.e * p.rows_b : 0) + t.m0 + rank * kRowsA + 32 * quarter) * p.ldo + c0;
-            constexpr int C = kStoreBytes / (int)sizeof(T);
+            const int y = (COLS ? t.e * p.rows_b : 0) + t.m0 + (int)rank * kRowsA + 32 * quarter;
+            T *out = static_cast<T *>(p.out) + y * p.ldo + c0;
+            constexpr int C = kBoxBytes / (int)sizeof(T);
 #pragma unroll
-            for (int c = 0; c < S::kWGCols; c += C)
+            for (int c = 0; c < S::kWGCols; c += C) {
+                if (c / C % kStageBoxes == 0) {   // the boxes before have been read
+                    asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                }
                 if (c0 + c < p.N)
-                    store_chunk<T>(out + c, p.ldo, rows - 32 * quarter, p.N - c0 - c, p.wide_store, sum + c, stage, lane);
+                    store_box<T>(&map_out, c0 + c, y, out + c, p.ldo, rows - 32 * quarter, p.N - c0 - c, p.wide_store,
+                                 sum + c, stage + c / C % kStageBoxes * kBox, lane);
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // the last boxes are read from this CTA's memory
     }
     fence_before();
     __syncthreads();
@@ -753,22 +772,27 @@ EncodeTiled encode_tiled()
     return fn;
 }
 
-// Tiles of box_rows x 128 codes of a rows x cols matrix of codes; what lies outside reads zero.
-cudaError_t code_map(CUtensorMap *map, const uint8_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows)
+// Boxes of box_rows rows and 128 bytes of a matrix of elements of 1, 2 or 4 bytes; what a load finds outside
+// is zero, what a store has outside is dropped.
+cudaError_t box_map(CUtensorMap *map, const void *p, int size, int64_t rows, int64_t cols, int64_t ld, int box_rows)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode)
         return cudaErrorNotSupported;
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {(cuuint32_t)kBlock, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(p), dims, strides, box, step,
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * size};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / size), (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUtensorMapDataType type = size == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                     : size == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16
+                                                 : CU_TENSOR_MAP_DATA_TYPE_UINT32;
+    const CUresult r = encode(map, type, 2, const_cast<void *>(p), dims, strides, box, step,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 template <int CG, int BN, bool COLS, typename T>
-cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, GemmParams p, int64_t tiles)
+cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const GemmParams &p,
+                   int64_t tiles)
 {
     using S = Shape<CG, BN>;
     auto kernel = k_gemm<CG, BN, COLS, T>;
@@ -799,18 +823,21 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, GemmP
     }
     cfg.gridDim = dim3((unsigned)(CG * std::max<int64_t>(1, std::min<int64_t>(groups, tiles))));
     m->launches += 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, p);
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, o, p);
 }
 
 template <int CG, int BN, bool COLS, typename T>
 cudaError_t encode_and_launch(esp_moe *m, const uint8_t *A, int64_t rows_a, int64_t inner, int64_t lda, const uint8_t *B,
                               int64_t rows_b, int64_t ldb, const GemmParams &p, int64_t tiles)
 {
-    CUtensorMap a, b;
-    cudaError_t e = code_map(&a, A, rows_a, inner, lda, kRowsA);
+    CUtensorMap a, b, o;
+    cudaError_t e = box_map(&a, A, 1, rows_a, inner, lda, kRowsA);
     if (e == cudaSuccess)
-        e = code_map(&b, B, rows_b, inner, ldb, Shape<CG, BN>::kRowsB);
-    return e != cudaSuccess ? e : launch<CG, BN, COLS, T>(m, a, b, p, tiles);
+        e = box_map(&b, B, 1, rows_b, inner, ldb, Shape<CG, BN>::kRowsB);
+    o = a;   // not used where the output is not aligned
+    if (e == cudaSuccess && p.wide_store)
+        e = box_map(&o, p.out, sizeof(T), COLS ? (int64_t)p.E * p.rows_b : p.M, p.N, p.ldo, 32);
+    return e != cudaSuccess ? e : launch<CG, BN, COLS, T>(m, a, b, o, p, tiles);
 }
 
 GemmParams common(esp_moe *m)
