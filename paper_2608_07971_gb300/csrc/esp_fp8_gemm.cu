@@ -9,7 +9,7 @@
 // each holding 128 rows of A and half of B) times BN columns; one block of K per shared-memory stage
 // (128 codes = one 128-byte swizzled row). Warps 0-3 own the first half of the columns, warps 4-7 the
 // second, a thread one row (its TMEM lane) of its half; warp 8 loads tiles by TMA, warp 9 issues the
-// MMAs. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
+// MMAs, warp 10 brings the column scales of the weight gradient to shared memory. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
 // run during a tile's stores.
 //
 // GROUPED ROWS (forward, row gradient): expert e's rows times its own B; a tile never spans two experts,
@@ -31,7 +31,7 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, two idle (whole warpgroups)
+constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, scales (COLS), one idle
 // registers per thread of the epilogue and of the other warpgroup: 2 * 216 + 72 = 3 * 168, the launch's
 constexpr int kEpilogueRegs = 216, kOtherRegs = 72;
 constexpr int kEpilogueWarps = 8;
@@ -48,15 +48,16 @@ struct Shape {
     static constexpr int kStage = kStageA + kRowsB * kBlock;
     static constexpr int kAcc = (int)kTmemCols / BN;
     static constexpr int kWGCols = BN / 2;   // columns of a warpgroup
-    // after the stages: store staging, tile table, column scales, barriers
+    // after the stages: store staging, tile table, scales, barriers
     static constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4 + 12;   // a multiple of 16
     static constexpr int kStaging = kEpilogueWarps * kStageBoxes * kBox;
-    static constexpr int kColScales = 2 * 2 * kWGCols * 4;
+    static constexpr int kScaleFloats = kRowsA + BN;   // of a stage: row and column scales (COLS)
+    static constexpr int kScales = kAcc * kScaleFloats * 4;
     static constexpr int kBars = 256;
-    static constexpr int kFixed = kTable + kStaging + kColScales + kBars + 1024;
+    static constexpr int kFixed = kTable + kStaging + kScales + kBars + 1024;
     static constexpr int kStages = std::min(8, (kSmemLimit - kFixed) / kStage);
     static constexpr int kSmem = kStages * kStage + kFixed;
-    static_assert((2 * kStages + 2 * kAcc + 1) * 8 + 16 <= kBars, "barriers");
+    static_assert((2 * kStages + 3 * kAcc + 1) * 8 + 16 <= kBars, "barriers");
 };
 
 struct GemmParams {
@@ -120,6 +121,11 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
 __device__ __forceinline__ void mbar_arrive(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive_cta(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
@@ -469,12 +475,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                                                           ~static_cast<uintptr_t>(1023));
     unsigned char *staging = sm + S::kStages * S::kStage;   // its boxes are 1024-byte aligned
     int *table = reinterpret_cast<int *>(staging + S::kStaging);
-    float *colscale = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(table) + S::kTable);
+    float *scales = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(table) + S::kTable);
     uint64_t *bars = reinterpret_cast<uint64_t *>(
-        (reinterpret_cast<uintptr_t>(colscale + S::kColScales / 4) + 15) & ~static_cast<uintptr_t>(15));
+        (reinterpret_cast<uintptr_t>(scales + S::kScales / 4) + 15) & ~static_cast<uintptr_t>(15));
     const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, tfull = empty + 8 * S::kStages,
-                   tempty = tfull + 8 * S::kAcc, drain = tempty + 8 * S::kAcc;
-    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 2 * S::kStages + 2 * S::kAcc + 1);
+                   tempty = tfull + 8 * S::kAcc, sempty = tempty + 8 * S::kAcc, drain = sempty + 8 * S::kAcc;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 2 * S::kStages + 3 * S::kAcc + 1);
     volatile int *dead = reinterpret_cast<volatile int *>(slot + 1), *last = dead + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
@@ -486,8 +492,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(empty + 8 * i, 1);
         }
         for (int i = 0; i < S::kAcc; ++i) {
-            mbar_init(tfull + 8 * i, 1);
+            mbar_init(tfull + 8 * i, COLS ? 2 : 1);   // the stage's MMAs, and (COLS) its scales
             mbar_init(tempty + 8 * i, CG * kEpilogueWarps);
+            mbar_init(sempty + 8 * i, kEpilogueWarps);
         }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -599,14 +606,72 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
         }
+        if (COLS && warp == 10) {
+            // a lane brings the scales of rows 4 l .. 4 l + 3 and of columns BN / 32 * l ..; the next block's,
+            // of the next tile too, are on their way while a stage is waited for
+            constexpr int R = kRowsA / 32, C = BN / 32;
+            int acc = 0, w = w0, left = 0;
+            uint32_t aph = 1;
+            Tile t;
+            const float *pa[R], *pb[C];
+            float a[R], b[C];
+            auto next = [&]() -> bool {   // moves to the next block, if there is one
+                if (left > 0) {
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+                        pa[i] += p.sa_k;
+#pragma unroll
+                    for (int i = 0; i < C; ++i)
+                        pb[i] += p.sb_k;
+                }
+                for (; left == 0; w += dw) {   // tiles may have no blocks
+                    if (!tile_at<CG, BN, COLS>(p, table, w, t))
+                        return false;
+                    left = t.kb1 - t.kb0;
+#pragma unroll
+                    for (int i = 0; i < R; ++i)   // rows past the end take the last one's
+                        pa[i] = p.scale_a + (t.m0 + min((int)rank * kRowsA + R * lane + i, t.rows - 1)) * p.sa_row +
+                                t.kb0 * p.sa_k;
+#pragma unroll
+                    for (int i = 0; i < C; ++i)
+                        pb[i] = p.scale_b + t.kb0 * p.sb_k + min(t.n0 + C * lane + i, p.N - 1);
+                }
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+                    a[i] = *pa[i];
+#pragma unroll
+                for (int i = 0; i < C; ++i)
+                    b[i] = *pb[i];
+                return true;
+            };
+            for (bool more = next(); more;) {
+                if (!__all_sync(0xffffffffu, mbar_wait(sempty + 8 * acc, aph, p, dead)))
+                    break;
+                float *to = scales + acc * S::kScaleFloats;
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+                    to[R * lane + i] = a[i];
+#pragma unroll
+                for (int i = 0; i < C; ++i)
+                    to[kRowsA + C * lane + i] = b[i];
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive_cta(tfull + 8 * acc);
+                --left;
+                more = next();
+                if (++acc == S::kAcc) {
+                    acc = 0;
+                    aph ^= 1;
+                }
+            }
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
         const int wg = warp >> 2, quarter = warp & 3;
         const uint32_t lane_cols = ((uint32_t)(32 * quarter) << 16) + (uint32_t)(wg * S::kWGCols);
         const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
         unsigned char *stage = staging + warp * kStageBoxes * kBox;
-        float *cs = colscale + wg * 2 * S::kWGCols;
-        int acc = 0, turn = 0;
+        int acc = 0;
         uint32_t aph = 0;
         bool ok = true;
         Tile t;
@@ -619,35 +684,26 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < S::kWGCols; ++i)
                 sum[i] = 0.0f;
-            // Scales: a row's (of the last row past the end) and the columns' of this warpgroup: one value, or
-            // (COLS) thread i brings column i's to shared memory. Fetched a block ahead.
+            // FWD: a row's scale (of the last row past the end) and the one of this warpgroup's columns, fetched a
+            // block ahead
             const int ra = t.m0 + min((int)rank * kRowsA + row, t.rows - 1);
-            const float *pa = p.scale_a + ra * p.sa_row + t.kb0 * p.sa_k;
-            const float *pb = p.scale_b + (COLS ? (int64_t)min(c0 + row, p.N - 1)
-                                                : t.e * p.sb_e + min(c0, p.N - 1) / kBlock * p.sb_n) +
-                              t.kb0 * p.sb_k;
+            const float *pa = p.scale_a + ra * p.sa_row;
+            const float *pb = p.scale_b + t.e * p.sb_e + min(c0, p.N - 1) / kBlock * p.sb_n + t.kb0 * p.sb_k;
             float next_a = 0.0f, next_b = 0.0f;
-            if (t.kb0 < t.kb1) {
+            if (!COLS) {
+                pa += t.kb0 * p.sa_k;
                 next_a = *pa;
                 next_b = *pb;
             }
             for (int left = t.kb1 - t.kb0; left > 0; --left) {
-                const float scale = COLS ? next_a : next_a * next_b;
-                // the buffers alternate over all blocks of all tiles: a block's is written again only after the
-                // next block's barrier, which every thread passes when it is done with this one's
-                float *csb = cs + turn * S::kWGCols;
-                turn ^= 1;
-                if (COLS && row < S::kWGCols)
-                    csb[row] = next_b;
-                if (left > 1) {
+                float scale = next_a * next_b;
+                if (!COLS && left > 1) {
                     pa += p.sa_k;
                     pb += p.sb_k;
                     next_a = *pa;
                     next_b = *pb;
                 }
                 ok = __all_sync(0xffffffffu, mbar_wait(tfull + 8 * acc, aph, p, dead));
-                if (COLS)
-                    ok = sync_and<128>(1 + wg, ok);
                 if (!ok)
                     break;
                 fence_after();
@@ -656,7 +712,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // is time that the tensor core stands still.
                 if (some) {
                     const uint32_t src = tmem + acc * BN + lane_cols;
-                    constexpr int D = 3, chunks = S::kWGCols / 16;   // loads in flight, loads in all
+                    const float *csb = scales + acc * S::kScaleFloats + kRowsA + wg * S::kWGCols;
+                    if (COLS)
+                        scale = scales[acc * S::kScaleFloats + row];
+                    constexpr int D = COLS ? 4 : 3, chunks = S::kWGCols / 16;   // loads in flight, loads in all
                     uint32_t v[D][16];
 #pragma unroll
                     for (int c = 0; c < D; ++c)
@@ -676,15 +735,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (c >= chunks)
                                 continue;
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
-                                float &lo = sum[16 * c + i], &hi = sum[16 * c + i + 1];
+                            for (int i = 0; i < 16; i += 4) {
+                                float *to = sum + 16 * c + i;
                                 float a = __uint_as_float(v[j][i]), b = __uint_as_float(v[j][i + 1]);
+                                float d = __uint_as_float(v[j][i + 2]), f = __uint_as_float(v[j][i + 3]);
                                 if (COLS) {
-                                    const float2 s2 = *reinterpret_cast<const float2 *>(csb + 16 * c + i);
+                                    const float4 s4 = *reinterpret_cast<const float4 *>(csb + 16 * c + i);
                                     mul_pair(a, b, scale);
-                                    fma_pair(lo, hi, a, b, s2.x, s2.y);
+                                    mul_pair(d, f, scale);
+                                    fma_pair(to[0], to[1], a, b, s4.x, s4.y);
+                                    fma_pair(to[2], to[3], d, f, s4.z, s4.w);
                                 } else {
-                                    fma_pair(lo, hi, a, b, scale, scale);
+                                    fma_pair(to[0], to[1], a, b, scale, scale);
+                                    fma_pair(to[2], to[3], d, f, scale, scale);
                                 }
                             }
                             if (c + D < chunks)
@@ -693,6 +756,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 } else if (lane == 0) {
                     mbar_arrive(tempty0 + 8 * acc);
+                }
+                if (COLS) {
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive_cta(sempty + 8 * acc);
                 }
                 if (++acc == S::kAcc) {
                     acc = 0;
