@@ -153,6 +153,7 @@ template <typename T>
 __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const QuantRowsArgs a, int blocks_k, bool aligned)
 {
     let_next_launch_start();
+    wait_for_launch_before();
     const int lane4 = threadIdx.x & 3;
     const int64_t total = a.M * blocks_k, i = (int64_t)blockIdx.x * kRowBlocks + (threadIdx.x >> 2);
     const bool on = i < total;
@@ -240,6 +241,8 @@ __global__ void __launch_bounds__(kTileThreads) k_quant_weight(const T *w, int64
 {
     __shared__ TileSmem s;
     __shared__ uint32_t high[kTileThreads / 32];
+    let_next_launch_start();
+    wait_for_launch_before();
     const int kb = blockIdx.x, nb = blockIdx.y, e = blockIdx.z;
     const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
     const int k0 = kb * kBlock + 8 * c, n0 = nb * kBlock;
@@ -324,74 +327,97 @@ __device__ void find_run(const int32_t *offsets, int E, int64_t M, int tile, int
     n = s_n;
 }
 
-// A run of up to 128 rows of an expert and 128 columns: a scale per column, codes transposed.
+// A run of up to 128 rows of an expert and `tiles` tiles of 128 columns: a scale per column, codes
+// transposed. The next tile's rows are on their way while a tile is rounded and turned.
 template <typename T>
-__global__ void __launch_bounds__(kTileThreads) k_quant_cols(const QuantColsArgs a, bool aligned)
+__global__ void __launch_bounds__(kTileThreads) k_quant_cols(const QuantColsArgs a, int tiles, bool aligned)
 {
     __shared__ TileSmem s;
+    __shared__ int64_t source[kBlock];   // element offset of each row (negative: zeros)
     let_next_launch_start();
-    const int tiles_k = (a.K + kBlock - 1) / kBlock, run = blockIdx.x / tiles_k;
+    wait_for_launch_before();
+    const int tiles_k = (a.K + kBlock - 1) / kBlock, groups = (tiles_k + tiles - 1) / tiles;
+    const int run = blockIdx.x / groups, first = (blockIdx.x - run * groups) * tiles;
     int row0, n;
     find_run(a.offsets, a.E, a.M, run, row0, n);
     if (n == 0)
         return;
-    const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-    const int c0 = (blockIdx.x - run * tiles_k) * kBlock;
-    Eight<T> x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = r0 + 16 * i;
-        x[i].zero();
-        if (r < n && c0 + 8 * c < a.K) {
-            const int64_t src = a.rows ? a.rows[row0 + r] : row0 + r;
-            if (src >= 0 && src < a.T)
-                x[i].load(static_cast<const T *>(a.x) + src * a.ldx + c0 + 8 * c, a.K - c0 - 8 * c, aligned);
-        }
-    }
-    // greatest magnitudes: over the thread's rows, then over the thread rows
-#pragma unroll
-    for (int w = 0; w < Eight<T>::kWords; ++w) {
-        uint32_t m = x[0].magnitudes(w);
-#pragma unroll
-        for (int i = 1; i < 8; ++i)
-            m = Eight<T>::larger(m, x[i].magnitudes(w));
-        if (sizeof(T) == 4) {
-            s.high[r0][8 * c + w] = m;
-        } else {
-            s.high[r0][8 * c + 2 * w] = m & 0xffffu;
-            s.high[r0][8 * c + 2 * w + 1] = m >> 16;
-        }
-    }
-    __syncthreads();
     if (threadIdx.x < kBlock) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            m = max(m, s.high[r][threadIdx.x]);
-        float scale, inv;
-        scale_of<T>(m, scale, inv);
-        s.inv[threadIdx.x] = inv;
-        if (c0 + (int)threadIdx.x < a.K)
-            a.scale[(int64_t)run * a.lds + c0 + threadIdx.x] = scale;
+        int64_t src = -1;
+        if ((int)threadIdx.x < n) {
+            src = a.rows ? a.rows[row0 + threadIdx.x] : row0 + (int)threadIdx.x;
+            src = src >= 0 && src < a.T ? src * a.ldx : -1;
+        }
+        source[threadIdx.x] = src;
     }
     __syncthreads();
-    float inv[8];
+    const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    const T *in = static_cast<const T *>(a.x);
+    Eight<T> next[8];
+    auto fetch = [&](int tile) {
+        const int k0 = tile * kBlock + 8 * c;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        inv[j] = s.inv[8 * c + j];
+        for (int i = 0; i < 8; ++i) {
+            const int64_t src = source[r0 + 16 * i];
+            next[i].zero();
+            if (src >= 0 && k0 < a.K)
+                next[i].load(in + src + k0, a.K - k0, aligned);
+        }
+    };
+    fetch(first);
+    for (int tile = first; tile < min(first + tiles, tiles_k); ++tile) {
+        const int c0 = tile * kBlock;
+        Eight<T> x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float v[8];
+        for (int i = 0; i < 8; ++i)
+            x[i] = next[i];
+        if (tile + 1 < min(first + tiles, tiles_k))
+            fetch(tile + 1);
+        // greatest magnitudes: over the thread's rows, then over the thread rows
+#pragma unroll
+        for (int w = 0; w < Eight<T>::kWords; ++w) {
+            uint32_t m = x[0].magnitudes(w);
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                m = Eight<T>::larger(m, x[i].magnitudes(w));
+            if (sizeof(T) == 4) {
+                s.high[r0][8 * c + w] = m;
+            } else {
+                s.high[r0][8 * c + 2 * w] = m & 0xffffu;
+                s.high[r0][8 * c + 2 * w + 1] = m >> 16;
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x < kBlock) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                m = max(m, s.high[r][threadIdx.x]);
+            float scale, inv;
+            scale_of<T>(m, scale, inv);
+            s.inv[threadIdx.x] = inv;
+            if (c0 + (int)threadIdx.x < a.K)
+                a.scale[(int64_t)run * a.lds + c0 + threadIdx.x] = scale;
+        }
+        __syncthreads();
+        float inv[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            v[j] = inv[j] == 0.0f ? 0.0f : __fmul_rn(x[i].get(j), inv[j]);
-        s.codes[r0 + 16 * i][2 * c] = codes4(v[0], v[1], v[2], v[3], 1.0f);
-        s.codes[r0 + 16 * i][2 * c + 1] = codes4(v[4], v[5], v[6], v[7], 1.0f);
+            inv[j] = s.inv[8 * c + j];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = inv[j] == 0.0f ? 0.0f : __fmul_rn(x[i].get(j), inv[j]);
+            s.codes[r0 + 16 * i][2 * c] = codes4(v[0], v[1], v[2], v[3], 1.0f);
+            s.codes[r0 + 16 * i][2 * c + 1] = codes4(v[4], v[5], v[6], v[7], 1.0f);
+        }
+        __syncthreads();
+        turn_codes(s);
+        __syncthreads();
+        store_turned(s, a.q + (int64_t)c0 * a.ldq + (int64_t)run * kBlock, a.ldq, a.K - c0, kBlock);
     }
-    __syncthreads();
-    turn_codes(s);
-    __syncthreads();
-    store_turned(s, a.q + (int64_t)c0 * a.ldq + (int64_t)run * kBlock, a.ldq, a.K - c0, kBlock);
 }
 
 }  // namespace
@@ -404,10 +430,9 @@ cudaError_t launch_quant_rows(esp_moe *m, int32_t dtype, const QuantRowsArgs &a)
         return cudaSuccess;
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        k_quant_rows<T><<<(unsigned)ceil_div(total, kRowBlocks), kRowThreads, 0, m->stream>>>(
-            a, blocks_k, rows_aligned(a.x, a.ldx, sizeof(T), 16));
         m->launches += 1;
-        return cudaGetLastError();
+        return launch_after(k_quant_rows<T>, dim3((unsigned)ceil_div(total, kRowBlocks)), kRowThreads, 0, m->stream, a,
+                            blocks_k, rows_aligned(a.x, a.ldx, sizeof(T), 16));
     });
 }
 
@@ -419,9 +444,12 @@ cudaError_t launch_quant_cols(esp_moe *m, int32_t dtype, const QuantColsArgs &a)
         using T = decltype(elem);
         // runs of 128 positions: at most this many, some past the last
         const int64_t runs = a.M / kBlock + a.E;
-        k_quant_cols<T><<<(unsigned)(runs * ceil_div(a.K, kBlock)), kTileThreads, 0, m->stream>>>(a, rows_aligned(a.x, a.ldx, sizeof(T), 16));
+        // several tiles per CTA once there are enough CTAs for every SM's four
+        const int64_t tiles_k = ceil_div(a.K, kBlock);
+        const int tiles = (int)std::max<int64_t>(1, std::min<int64_t>(8, runs * tiles_k / (4 * m->sm_count)));
         m->launches += 1;
-        return cudaGetLastError();
+        return launch_after(k_quant_cols<T>, dim3((unsigned)(runs * ceil_div(tiles_k, tiles))), kTileThreads, 0, m->stream, a,
+                            tiles, rows_aligned(a.x, a.ldx, sizeof(T), 16));
     });
 }
 
@@ -430,10 +458,9 @@ cudaError_t launch_quant_weight(esp_moe *m, int32_t dtype, const void *w, int64_
     return with_dtype(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
         const dim3 grid((unsigned)ceil_div(o.K, kBlock), (unsigned)ceil_div(o.N, kBlock), (unsigned)o.E);
-        k_quant_weight<T><<<grid, kTileThreads, 0, m->stream>>>(static_cast<const T *>(w), ldw, o,
-                                                             rows_aligned(w, ldw, sizeof(T), 16));
         m->launches += 1;
-        return cudaGetLastError();
+        return launch_after(k_quant_weight<T>, grid, kTileThreads, 0, m->stream, static_cast<const T *>(w), ldw, o,
+                            rows_aligned(w, ldw, sizeof(T), 16));
     });
 }
 

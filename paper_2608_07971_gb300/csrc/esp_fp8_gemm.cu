@@ -512,7 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
         }
     }
-    // what follows reads what the launch before wrote (the codes) or is ordered after it
+    // What follows reads what the launch before wrote (the codes) or is ordered after it. The launch after is
+    // not let start early: its waiting CTAs slow this kernel's tail (1001 x 1999 x 2050: 24.1 us, 19.3 without).
     wait_for_launch_before();
     if (warp == 8) {
         // the experts' row tiles (blocks) before each: one warp's scan

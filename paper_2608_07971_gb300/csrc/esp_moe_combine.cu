@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "esp_moe_impl.h"
+#include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
 
 namespace esp_moe_impl {
@@ -23,6 +24,8 @@ struct Picks {
 
 __device__ __forceinline__ void load_picks(const CombineArgs &a, int64_t t, Picks &s)
 {
+    let_next_launch_start();
+    wait_for_launch_before();
     if (threadIdx.x < ESP_MOE_MAX_CHOICES) {
         int32_t p = -1;
         float w = 0.0f;
@@ -181,9 +184,8 @@ cudaError_t launch_combine(esp_moe *m, int32_t dtype, const CombineArgs &a)
                           a.H * sizeof(T) % 16 == 0;
         return with_shape<T>(wide, a.k, [&](auto v, auto kt) -> cudaError_t {
             constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
-            k_combine<T, V, KT><<<(unsigned)a.T, threads_for(a.H, V), 0, m->stream>>>(a);
             m->launches += 1;
-            return cudaGetLastError();
+            return launch_after(k_combine<T, V, KT>, dim3((unsigned)a.T), threads_for(a.H, V), 0, m->stream, a);
         });
     });
 }
@@ -199,9 +201,8 @@ cudaError_t launch_combine_backward(esp_moe *m, int32_t dtype, const CombineArgs
                           rows_aligned(a.dout, a.lddo, sizeof(T), 16) && a.H * sizeof(T) % 16 == 0;
         return with_shape<T>(wide, a.k, [&](auto v, auto kt) -> cudaError_t {
             constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
-            k_combine_backward<T, V, KT><<<(unsigned)a.T, threads_for(a.H, V), 0, m->stream>>>(a);
             m->launches += 1;
-            return cudaGetLastError();
+            return launch_after(k_combine_backward<T, V, KT>, dim3((unsigned)a.T), threads_for(a.H, V), 0, m->stream, a);
         });
     });
 }

@@ -1,6 +1,7 @@
-// Launches of the expert layer's kernels: dependent launches (the second kernel of a call is launched while
-// the first still runs, does what needs none of its results, and then waits for it), and the shared-memory
-// limit of a kernel, raised once.
+// Launches of the expert layer's kernels. Every one is a dependent launch: it starts while the kernel before
+// it on the stream still runs (once all of that one's CTAs have started, where it says so), sets up what
+// needs no global memory, and then waits for it to finish. That hides a microsecond or so of launch latency
+// behind each kernel. And the shared-memory limit of a kernel, raised once.
 #pragma once
 
 #include <atomic>
@@ -13,13 +14,13 @@ namespace esp_moe_impl {
 namespace {
 
 // In a kernel launched with after_launch_before(): waits until the launch before it has finished and its
-// writes are visible. Nothing that it wrote may be read, and nothing that it reads written, before.
+// writes are visible. No global memory is touched before.
 __device__ __forceinline__ void wait_for_launch_before()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// In the first kernel: the dependent launch may start once every CTA has called this or ended.
+// The launch after may start once every CTA has called this or ended.
 __device__ __forceinline__ void let_next_launch_start()
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

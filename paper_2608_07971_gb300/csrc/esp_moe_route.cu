@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     using S = RowShape<T, VPT>;
     constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
     extern __shared__ int sm[];
-    if (!FUSED)
-        let_next_launch_start();
+    let_next_launch_start();
+    wait_for_launch_before();
     constexpr int kPadded = 32 * VPT;                  // E rounded up to the lanes' elements
     float *price = reinterpret_cast<float *>(sm);      // kPadded price terms
     int *wcount = sm + kPadded;                        // W x E
@@ -450,6 +450,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_
     int *total = sm, *before = sm + E, *second = sm + 2 * E, *offs = sm + 3 * E;
     for (int e = threadIdx.x; e < E; e += kPlanThreads)
         total[e] = before[e] = 0;
+    let_next_launch_start();
     wait_for_launch_before();
     // the first slots' ranks are on their way while the columns are summed
     const int64_t s0 = c0 * chunk * k, s1 = a.offsets ? min(a.T * k, s0 + kPlanChunks * chunk * k) : s0;
@@ -518,6 +519,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
     float *red = smf;                                      // warps x E
     int *hist = reinterpret_cast<int *>(red + W * E); // E
     let_next_launch_start();
+    wait_for_launch_before();
     __shared__ float lse_w[W];
     __shared__ int tok_w[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -638,6 +640,7 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     const int groups = max(1, kThreads / E);
     float *share = smf;                                          // groups x E
     int *count = reinterpret_cast<int *>(smf + groups * E);      // groups x E
+    let_next_launch_start();
     wait_for_launch_before();
     const int64_t lo = a.seq ? seq_bound(a.seq, s, a.T) : 0, hi = a.seq ? seq_bound(a.seq, s + 1, a.T) : a.T;
     const int64_t b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
@@ -727,6 +730,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
         row[32 * i + lane] = 0.0f;
+    let_next_launch_start();
+    wait_for_launch_before();
     const int64_t w = (int64_t)blockIdx.x * (kBwdThreads / 32) + warp;
     const int64_t t0 = w * per_warp, t1 = min(a.T, t0 + per_warp);
     const T *logits = static_cast<const T *>(a.logits);
@@ -866,6 +871,8 @@ __global__ void __launch_bounds__(kThreads) k_step_prices(int32_t E, const int64
                                                           float *prices)
 {
     __shared__ unsigned long long total;
+    let_next_launch_start();
+    wait_for_launch_before();
     if (threadIdx.x == 0)
         total = 0;
     __syncthreads();
@@ -934,16 +941,16 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
                 const cudaError_t e = allow_smem<k_route<T, VPT, true>>(route_smem, m->device);
                 if (e != cudaSuccess)
                     return e;
-                k_route<T, VPT, true><<<1, kThr, route_smem, m->stream>>>(a, a.T, aligned);
                 m->launches += 1;
-                return cudaGetLastError();
+                return launch_after(k_route<T, VPT, true>, dim3(1), kThr, route_smem, m->stream, a, a.T, aligned);
             }
             const int64_t chunk = route_chunk(a.T);
             const int nb = (int)ceil_div(a.T, chunk);
-            const cudaError_t e = allow_smem<k_route<T, VPT, false>>(route_smem, m->device);
+            cudaError_t e = allow_smem<k_route<T, VPT, false>>(route_smem, m->device);
+            if (e == cudaSuccess)
+                e = launch_after(k_route<T, VPT, false>, dim3((unsigned)nb), kThr, route_smem, m->stream, a, chunk, aligned);
             if (e != cudaSuccess)
                 return e;
-            k_route<T, VPT, false><<<nb, kThr, route_smem, m->stream>>>(a, chunk, aligned);
             m->launches += 2;
             return launch_after(k_plan, dim3(a.offsets ? (unsigned)ceil_div(nb, kPlanChunks) : 1u), kPlanThreads,
                                 (size_t)(4 * a.E + 1) * sizeof(int), m->stream, a, chunk, nb);
@@ -970,10 +977,9 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
                 const cudaError_t e2 = allow_smem<k_balance<T, VPT>>(smem, m->device);
                 if (e2 != cudaSuccess)
                     return e2;
-                k_balance<T, VPT><<<(int)ceil_div(a.T, chunk), kThr, smem, m->stream>>>(
-                    a, chunk, rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T)));
                 m->launches += 1;
-                return cudaGetLastError();
+                return launch_after(k_balance<T, VPT>, dim3((unsigned)ceil_div(a.T, chunk)), kThr, smem, m->stream, a, chunk,
+                                    rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T)));
             });
         });
         if (e != cudaSuccess)
@@ -1001,21 +1007,17 @@ cudaError_t launch_route_backward(esp_moe *m, int32_t dtype, const RouteBackward
             const size_t smem = (size_t)kW * 32 * VPT * sizeof(float);
             const bool in = rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T));
             const bool out = rows_aligned(a.dlogits, a.ld_out, sizeof(T), S::V * sizeof(T));
-            if (a.dloss)
-                k_route_backward<T, VPT, true><<<grid, kBwdThreads, smem, m->stream>>>(a, per, in, out);
-            else
-                k_route_backward<T, VPT, false><<<grid, kBwdThreads, smem, m->stream>>>(a, per, in, out);
             m->launches += 1;
-            return cudaGetLastError();
+            return launch_after(a.dloss ? k_route_backward<T, VPT, true> : k_route_backward<T, VPT, false>,
+                                dim3((unsigned)grid), kBwdThreads, smem, m->stream, a, per, in, out);
         });
     });
 }
 
 cudaError_t launch_step_prices(esp_moe *m, int32_t E, const int64_t *counts, double eta, double slack, float *prices)
 {
-    k_step_prices<<<1, kThreads, 0, m->stream>>>(E, counts, eta, slack, prices);
     m->launches += 1;
-    return cudaGetLastError();
+    return launch_after(k_step_prices, dim3(1), kThreads, 0, m->stream, E, counts, eta, slack, prices);
 }
 
 }  // namespace esp_moe_impl
