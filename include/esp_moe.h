@@ -77,7 +77,8 @@ typedef struct {
 esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream);
 
 /* Later calls run on `cuda_stream`, after what the handle queued on the stream it leaves (which must
- * still exist). */
+ * still exist). While either stream is being captured into a graph no such order is added: the program
+ * orders the graph's launches after the handle's other work, as they share its work space. */
 esp_status esp_moe_set_stream(esp_moe *m, void *cuda_stream);
 
 /* Routes T tokens over E experts (logits T x E). An expert can be chosen if profit = logit - price

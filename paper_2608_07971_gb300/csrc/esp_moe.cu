@@ -64,6 +64,16 @@ esp_status reserve(esp_moe *m, size_t bytes)
     return ESP_OK;
 }
 
+bool capturing(cudaStream_t s)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &status) != cudaSuccess) {
+        cudaGetLastError();
+        return true;   // the legacy stream while another stream is being captured
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
+
 size_t element_size(int32_t dtype)
 {
     return dtype == ESP_MOE_F32 ? 4 : 2;
@@ -174,8 +184,11 @@ esp_status esp_moe_set_stream(esp_moe *m, void *cuda_stream)
         return st;
     const cudaStream_t next = static_cast<cudaStream_t>(cuda_stream);
     if (next != m->stream) {
-        MOE_CUDA(cudaEventRecord(m->handoff, m->stream));
-        MOE_CUDA(cudaStreamWaitEvent(next, m->handoff, 0));
+        // an event cannot order a stream that is being captured after one that is not
+        if (!capturing(next) && !capturing(m->stream)) {
+            MOE_CUDA(cudaEventRecord(m->handoff, m->stream));
+            MOE_CUDA(cudaStreamWaitEvent(next, m->handoff, 0));
+        }
         m->stream = next;
     }
     return ESP_OK;
@@ -333,6 +346,8 @@ esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t
         return ESP_ERR_INVALID_ARG;
     const int64_t kb = ceil_div(w->K, kBlock), nb = ceil_div(w->N, kBlock);
     const int64_t positions = (M / kBlock + w->E) * kBlock;   // every expert's rows rounded up to a block
+    if (dw && positions > kMaxRows)
+        return ESP_ERR_INVALID_ARG;
     const bool want_dx = dx && M > 0;
     QuantRowsArgs q{M, M, lddy, round_up(w->N, 16), round_up(nb, 4), w->N, dy, nullptr, nullptr, nullptr};
     QuantColsArgs cy{M, M, lddy, positions, round_up(w->N, 4), w->N, w->E, dy, nullptr, offsets, nullptr, nullptr};

@@ -134,7 +134,15 @@ class Weight:
     qt: Optional[torch.Tensor] = None
 
     def __post_init__(self):
-        qt = self.qt
+        E, N, K, q, qt, scale = self.E, self.N, self.K, self.q, self.qt, self.scale
+
+        def codes(t, rows, cols):
+            return t.dtype is torch.uint8 and t.dim() == 3 and t.shape[:2] == (E, rows) and t.shape[2] >= cols and \
+                t.is_contiguous() and t.device == scale.device
+
+        if not codes(q, N, K) or (qt is not None and not codes(qt, K, N)) or scale.dtype is not torch.float32 or \
+                scale.shape != (E, -(-N // BLOCK), -(-K // BLOCK)) or not scale.is_contiguous():
+            raise ValueError("8-bit weights: contiguous uint8 codes (E, N, >= K), fp32 scales (E, N / 128, K / 128)")
         self._c = _CWeight(self.E, self.N, self.K, self.q.shape[2], qt.shape[2] if qt is not None else 0,
                            self.q.data_ptr(), qt.data_ptr() if qt is not None else None, self.scale.data_ptr())
         self._ref = ctypes.byref(self._c)
@@ -340,14 +348,15 @@ class Moe:
     def quantize_weight(self, w, transposed: bool = False, out: Optional[Weight] = None) -> Weight:
         """8-bit weights of w, (E, N, K) or (N, K) (esp_moe_quantize_weight)."""
         w3 = w if w.dim() == 3 else w[None]
+        if w3.dim() != 3 or not w3.is_contiguous():
+            raise ValueError("w: a contiguous (E, N, K) or (N, K) tensor expected")
         E, N, K = w3.shape
-        code, ld = self._matrix(w3.view(E * N, K) if w3.is_contiguous() else w3.reshape(E * N, K), "w")
+        code, ld = self._matrix(w3.view(E * N, K), "w")
         if out is None:
             out = self.empty_weight(E, N, K, transposed)
         elif (out.E, out.N, out.K) != (E, N, K):
             raise ValueError(f"out: weights of {(E, N, K)} expected")
-        if not w3.is_contiguous():
-            raise ValueError("w is not contiguous")
+        self._need(out.scale, "out")
         self._on_stream()
         esp._check(self._lib.esp_moe_quantize_weight(self.h, code, w3.data_ptr(), ld, out._ref),
                    "esp_moe_quantize_weight")
@@ -371,6 +380,7 @@ class Moe:
         return Weight(E, N, K, q, scale, qt)
 
     def _rows(self, x, weight: Weight, offsets, rows):
+        self._need(weight.scale, "weight")
         if offsets is not None:
             self._need(offsets, "offsets", torch.int32, (weight.E + 1,))
         elif weight.E != 1:

@@ -560,3 +560,55 @@ def test_wait_that_runs_out_is_reported(mm, M):
     assert err.value.status == esp.ESP_ERR_STATE
     m.close()
     assert torch.equal(mm.linear(x, q), want)   # another handle works on
+
+
+def test_wait_that_runs_out_in_the_weight_gradient(mm):
+    from paper_2608_07971_gb300 import esp, moe
+    for M, N, K in ((900, 300, 500), (300, 2100, 2000)):
+        m = moe.Moe()
+        x, dy = torch.randn(M, K, device="cuda"), torch.randn(M, N, device="cuda")
+        q = m.quantize_weight(torch.randn(N, K, device="cuda"))
+        want = m.linear_backward(dy, x, q, need=(False, True))[1]
+        m.synchronize()
+        lib = moe.load_library()
+        esp._check(lib.esp_moe_debug_set_wait_limit(m.h, 20), "set_wait_limit")
+        esp._check(lib.esp_moe_debug_hold_load(m.h), "hold_load")
+        m.linear_backward(dy, x, q, need=(False, True))
+        with pytest.raises(esp.EspError) as err:
+            m.synchronize()
+        assert err.value.status == esp.ESP_ERR_TIMEOUT
+        m.close()
+        assert torch.equal(mm.linear_backward(dy, x, q, need=(False, True))[1], want)
+
+
+def test_capture_on_another_stream(mm):
+    """Calls captured on a stream that the handle has not used, then replayed and called directly."""
+    z = make_logits(700, 32, "f32", 8)
+    want = mm.route(z, 3)
+    r = mm.routing(700, 32, 3)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=torch.cuda.Stream()):
+        mm.route(z, 3, out=r)
+    r.rows.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(r.rows, want.rows) and torch.equal(r.weight, want.weight)
+    assert torch.equal(mm.route(z, 3).rows, want.rows)
+
+
+def test_weight_refusals(mm):
+    from paper_2608_07971_gb300 import moe
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    f32 = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    moe.Weight(2, 10, 8, u8(2, 10, 16), f32(2, 1, 1))
+    for q, scale, qt in ((u8(2, 10, 7), f32(2, 1, 1), None), (u8(2, 9, 16), f32(2, 1, 1), None),
+                         (u8(2, 10, 16).float(), f32(2, 1, 1), None), (u8(2, 10, 16), f32(2, 1), None),
+                         (u8(2, 10, 16), f32(2, 1, 1), u8(2, 7, 16)), (u8(2, 10, 32)[:, :, ::2], f32(2, 1, 1), None)):
+        with pytest.raises(ValueError):
+            moe.Weight(2, 10, 8, q, scale, qt)
+    from paper_2608_07971_gb300 import esp
+    with pytest.raises(esp.EspError):   # rows of codes not a multiple of 16 bytes apart
+        mm.linear(f32(3, 8), moe.Weight(1, 10, 8, u8(1, 10, 8), f32(1, 1, 1)))
+    with pytest.raises(ValueError):
+        mm.quantize_weight(torch.randn(8, 10, device="cuda").t())
