@@ -320,12 +320,15 @@ __device__ void find_run(const int32_t *offsets, int E, int64_t M, int tile, int
 
 // A run of up to 128 rows of an expert and 128 columns: a scale per column, codes transposed. The four CTAs
 // of an SM overlap their loads, rounding and turning: 16384 gathered rows of 4096 bf16 (200 MB) take 45 us,
-// with several tiles per CTA, or the next tile's rows fetched ahead, 50 to 59.
-template <typename T>
+// with several tiles per CTA, or the next tile's rows fetched ahead, 50 to 59. ROWS: the rows' own codes and
+// scales (a tile is one block of each row) from the same read.
+template <typename T, bool ROWS>
 __global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : 4) k_quant_cols(const QuantColsArgs a, bool aligned)
 {
     __shared__ TileSmem s;
     __shared__ int64_t source[kBlock];   // element offset of each row (negative: zeros)
+    __shared__ uint32_t row_high[ROWS ? kBlock : 1];
+    __shared__ float row_inv[ROWS ? kBlock : 1];
     let_next_launch_start();
     wait_for_launch_before();
     const int tiles_k = (a.K + kBlock - 1) / kBlock, run = blockIdx.x / tiles_k;
@@ -371,19 +374,44 @@ __global__ void __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 2 : 4) k_quant_
     uint4 *hp = reinterpret_cast<uint4 *>(&s.high[r0][8 * c]);
     hp[0] = make_uint4(high[0], high[1], high[2], high[3]);
     hp[1] = make_uint4(high[4], high[5], high[6], high[7]);
+    if (ROWS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t m = Eight<T>::flat(x[i].largest());
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1)
+                m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if (c == 0)
+                row_high[r0 + 16 * i] = m;
+        }
+    }
     __syncthreads();
+    float scale, inv_of;
     if (threadIdx.x < kBlock) {
         uint32_t m = 0;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
             m = max(m, s.high[r][threadIdx.x]);
-        float scale, inv;
-        scale_of<T>(m, scale, inv);
-        s.inv[threadIdx.x] = inv;
+        scale_of<T>(m, scale, inv_of);
+        s.inv[threadIdx.x] = inv_of;
         if (c0 + (int)threadIdx.x < a.K)
             a.scale[(int64_t)run * a.lds + c0 + threadIdx.x] = scale;
+    } else if (ROWS) {
+        const int r = threadIdx.x - kBlock;
+        scale_of<T>(row_high[r], scale, inv_of);
+        row_inv[r] = inv_of;
+        if (r < n)
+            a.row_scale[(int64_t)(row0 + r) * a.row_lds + c0 / kBlock] = scale;
     }
     __syncthreads();
+    if (ROWS) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + 16 * i;
+            if (r < n && k0 < a.row_ldq)
+                *reinterpret_cast<uint2 *>(a.row_q + (int64_t)(row0 + r) * a.row_ldq + k0) = codes8<T>(x[i], row_inv[r]);
+        }
+    }
     const float4 i0 = *reinterpret_cast<const float4 *>(&s.inv[8 * c]);
     const float4 i1 = *reinterpret_cast<const float4 *>(&s.inv[8 * c + 4]);
     const float inv[8] = {i0.x, i0.y, i0.z, i0.w, i1.x, i1.y, i1.z, i1.w};
@@ -427,7 +455,8 @@ cudaError_t launch_quant_cols(esp_moe *m, int32_t dtype, const QuantColsArgs &a)
         // runs of 128 positions: at most this many, some past the last
         const int64_t runs = a.M / kBlock + a.E;
         m->launches += 1;
-        return launch_after(k_quant_cols<T>, dim3((unsigned)(runs * ceil_div(a.K, kBlock))), kTileThreads, 0, m->stream, a,
+        return launch_after(a.row_q ? k_quant_cols<T, true> : k_quant_cols<T, false>,
+                            dim3((unsigned)(runs * ceil_div(a.K, kBlock))), kTileThreads, 0, m->stream, a,
                             rows_aligned(a.x, a.ldx, sizeof(T), 16));
     });
 }

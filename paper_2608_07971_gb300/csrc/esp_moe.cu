@@ -350,8 +350,10 @@ esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t
         return ESP_ERR_INVALID_ARG;
     const bool want_dx = dx && M > 0;
     QuantRowsArgs q{M, M, lddy, round_up(w->N, 16), round_up(nb, 4), w->N, dy, nullptr, nullptr, nullptr};
-    QuantColsArgs cy{M, M, lddy, positions, round_up(w->N, 4), w->N, w->E, dy, nullptr, offsets, nullptr, nullptr};
-    QuantColsArgs cx{M, T, ldx, positions, round_up(w->K, 4), w->K, w->E, x, rows, offsets, nullptr, nullptr};
+    QuantColsArgs cy{M, M, lddy, positions, round_up(w->N, 4), w->N, w->E, dy, nullptr, offsets, nullptr, nullptr,
+                     nullptr, nullptr, 0, 0};
+    QuantColsArgs cx{M, T, ldx, positions, round_up(w->K, 4), w->K, w->E, x, rows, offsets, nullptr, nullptr,
+                     nullptr, nullptr, 0, 0};
     float *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
@@ -369,14 +371,22 @@ esp_status esp_moe_linear_backward(esp_moe *m, int32_t dtype, int64_t T, int64_t
         if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
             return st;
     }
+    if (want_dx && dw) {   // both roundings of dy from one read
+        cy.row_q = q.q;
+        cy.row_scale = q.scale;
+        cy.row_ldq = q.ldq;
+        cy.row_lds = q.lds;
+    }
+    if (dw)
+        MOE_CUDA(launch_quant_cols(m, dtype, cy));
     if (want_dx) {
-        MOE_CUDA(launch_quant_rows(m, dtype, q));
+        if (!dw)
+            MOE_CUDA(launch_quant_rows(m, dtype, q));
         const GemmRowsArgs g{M, q.ldq, q.lds, w->ldt, lddx, w->E, w->K, w->N, q.q, w->qt, q.scale, w->scale,
                              nb * kb, 1, kb, offsets, dx, partial};
         MOE_CUDA(launch_gemm_rows(m, dtype, g));
     }
     if (dw) {
-        MOE_CUDA(launch_quant_cols(m, dtype, cy));
         MOE_CUDA(launch_quant_cols(m, dtype, cx));
         const GemmColsArgs g{M, cy.ldq, cx.ldq, cy.lds, cx.lds, lddw, w->E, w->N, w->K, cy.q, cx.q, cy.scale, cx.scale,
                              offsets, dw, partial};

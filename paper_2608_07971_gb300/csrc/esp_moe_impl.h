@@ -155,6 +155,9 @@ struct QuantColsArgs {
     const int32_t *offsets;
     uint8_t *q;
     float *scale;
+    uint8_t *row_q;
+    float *row_scale;
+    int64_t row_ldq, row_lds;
 };
 cudaError_t launch_quant_cols(esp_moe *m, int32_t dtype, const QuantColsArgs &a);
 cudaError_t launch_quant_weight(esp_moe *m, int32_t dtype, const void *w, int64_t ldw, const esp_moe_weight &o);
