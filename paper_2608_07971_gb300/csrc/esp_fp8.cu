@@ -184,6 +184,35 @@ __global__ void __launch_bounds__(kRowThreads) k_quant_rows(const QuantRowsArgs 
         a.scale[row * a.lds + kb] = scale;
 }
 
+// A warp copies a row: 512 bytes of codes at a time, then the scales.
+__global__ void __launch_bounds__(kRowThreads) k_pick_rows(const PickRowsArgs a)
+{
+    let_next_launch_start();
+    wait_for_launch_before();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+    if (row >= a.M)
+        return;
+    int64_t src = a.rows[row];
+    src = src >= 0 && src < a.T ? src : a.T;
+    const uint4 *from = reinterpret_cast<const uint4 *>(a.from_q + src * a.ldq);
+    uint4 *to = reinterpret_cast<uint4 *>(a.q + row * a.ldq);
+    const int n = (int)(a.ldq / 16);
+    for (int i = lane; i < n; i += 128) {
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + 32 * j < n)
+                v[j] = from[i + 32 * j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + 32 * j < n)
+                to[i + 32 * j] = v[j];
+    }
+    for (int i = lane; i < a.lds; i += 32)
+        a.scale[row * a.lds + i] = a.from_scale[src * a.lds + i];
+}
+
 // ---- tiles of 128 x 128: thread (r, c) of 16 x 16 holds 8 consecutive columns of every 16th row
 
 constexpr int kTileThreads = 256;
@@ -444,6 +473,12 @@ cudaError_t launch_quant_rows(esp_moe *m, int32_t dtype, const QuantRowsArgs &a)
         return launch_after(k_quant_rows<T>, dim3((unsigned)ceil_div(total, kRowBlocks)), kRowThreads, 0, m->stream, a,
                             blocks_k, rows_aligned(a.x, a.ldx, sizeof(T), 16));
     });
+}
+
+cudaError_t launch_pick_rows(esp_moe *m, const PickRowsArgs &a)
+{
+    m->launches += 1;
+    return launch_after(k_pick_rows, dim3((unsigned)ceil_div(a.M, kRowThreads / 32)), kRowThreads, 0, m->stream, a);
 }
 
 cudaError_t launch_quant_cols(esp_moe *m, int32_t dtype, const QuantColsArgs &a)

@@ -315,18 +315,29 @@ esp_status esp_moe_linear(esp_moe *m, int32_t dtype, int64_t T, int64_t ldx, con
     if (M == 0)
         return ESP_OK;
     const int64_t kb = ceil_div(w->K, kBlock), nb = ceil_div(w->N, kBlock);
-    QuantRowsArgs q{M, T, ldx, round_up(w->K, 16), round_up(kb, 4), w->K, x, rows, nullptr, nullptr};
+    const bool pick = rows && pick_after_rounding(M, T, w->K);
+    // picked after rounding: the T rows once, and one more that is zero
+    QuantRowsArgs q{pick ? T + 1 : M, T, ldx, round_up(w->K, 16), round_up(kb, 4), w->K, x, pick ? nullptr : rows,
+                    nullptr, nullptr};
+    PickRowsArgs r{M, T, q.ldq, q.lds, rows, nullptr, nullptr, nullptr, nullptr};
     float *partial = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
-        q.q = c.take<uint8_t>((size_t)(M * q.ldq));
-        q.scale = c.take<float>((size_t)(M * q.lds));
+        q.q = c.take<uint8_t>((size_t)(q.M * q.ldq));
+        q.scale = c.take<float>((size_t)(q.M * q.lds));
+        r.q = pick ? c.take<uint8_t>((size_t)(M * q.ldq)) : q.q;
+        r.scale = pick ? c.take<float>((size_t)(M * q.lds)) : q.scale;
         partial = c.take<float>(gemm_partial_floats(m));
         if (pass == 0 && (st = reserve(m, c.used())) != ESP_OK)
             return st;
     }
     MOE_CUDA(launch_quant_rows(m, dtype, q));
-    const GemmRowsArgs g{M, q.ldq, q.lds, w->ld, ldy, w->E, w->N, w->K, q.q, w->q, q.scale, w->scale,
+    if (pick) {
+        r.from_q = q.q;
+        r.from_scale = q.scale;
+        MOE_CUDA(launch_pick_rows(m, r));
+    }
+    const GemmRowsArgs g{M, q.ldq, q.lds, w->ld, ldy, w->E, w->N, w->K, r.q, w->q, r.scale, w->scale,
                          nb * kb, kb, 1, offsets, y, partial};
     MOE_CUDA(launch_gemm_rows(m, dtype, g));
     return ESP_OK;

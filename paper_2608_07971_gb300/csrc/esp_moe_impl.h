@@ -143,6 +143,24 @@ struct QuantRowsArgs {
     float *scale;
 };
 cudaError_t launch_quant_rows(esp_moe *m, int32_t dtype, const QuantRowsArgs &a);
+// Rows of codes and scales picked from T + 1 (the last one zero): row i from rows[i], or from row T for an
+// index outside [0, T).
+struct PickRowsArgs {
+    int64_t M, T, ldq, lds;
+    const int32_t *rows;
+    const uint8_t *from_q;
+    const float *from_scale;
+    uint8_t *q;
+    float *scale;
+};
+cudaError_t launch_pick_rows(esp_moe *m, const PickRowsArgs &a);
+// Whether M gathered rows of T with K elements are rounded once and then copied, instead of rounding each row:
+// from two rows of each and 2^24 elements on (65536 rows of 2048 from 8192, the whole product: 580 us, 593
+// with every row rounded; smaller ones would pay a third launch for less).
+inline bool pick_after_rounding(int64_t M, int64_t T, int64_t K)
+{
+    return M >= 2 * T && M * K >= (int64_t)1 << 24;
+}
 
 // Columns as codes: expert e's rows i (source row rows[offsets[e] + i]) become positions base(e) + i of
 // column c's run q[c * ldq + ...], base(e) = the sum of the earlier experts' row counts, each rounded up

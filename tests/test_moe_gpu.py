@@ -612,3 +612,27 @@ def test_weight_refusals(mm):
         mm.linear(f32(3, 8), moe.Weight(1, 10, 8, u8(1, 10, 8), f32(1, 1, 1)))
     with pytest.raises(ValueError):
         mm.quantize_weight(torch.randn(8, 10, device="cuda").t())
+
+
+@pytest.mark.parametrize("T,E,k,N,K,dt", [(3000, 5, 4, 1040, 1408, "bf16"), (2100, 1, 8, 300, 2050, "f16"),
+                                          (9000, 40, 3, 1000, 640, "f32")])
+def test_rows_picked_after_rounding(mm, T, E, k, N, K, dt):
+    """Many rows for each token: they are rounded once and copied, with the results of rows picked before."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, K, generator=g, device="cuda").to(DT[dt])
+    q = mm.quantize_weight(torch.randn(E, N, K, generator=g, device="cuda") / math.sqrt(K))
+    M = T * k
+    rows = torch.randint(0, T, (M,), generator=g, device="cuda").int()
+    cut = torch.sort(torch.randint(0, M + 1, (E - 1,), generator=g, device="cuda"))[0].int()
+    offsets = torch.cat([cut.new_zeros(1), cut, cut.new_full((1,), M - 7)]).int().sort()[0]
+    rows[5], rows[M // 2] = -1, T          # read zeros
+    out = torch.full((M, N), 3.0, dtype=DT[dt], device="cuda")
+    mm.linear(x, q, offsets=offsets, rows=rows, out=out)
+    assert mm.last_launch_count() == 3
+    zero = torch.cat([x, torch.zeros(1, K, dtype=x.dtype, device="cuda")])
+    picked = zero[torch.where((rows < 0) | (rows >= T), torch.full_like(rows, T), rows).long()]
+    want = torch.full((M, N), 3.0, dtype=DT[dt], device="cuda")
+    mm.linear(picked, q, offsets=offsets, out=want)
+    assert mm.last_launch_count() == 2
+    assert torch.equal(out, want) and bool((out[M - 7:] == 3).all())
+    mm.synchronize()
