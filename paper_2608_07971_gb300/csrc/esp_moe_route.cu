@@ -307,7 +307,7 @@ template <typename T, int VPT, bool FUSED>
 __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a, int64_t chunk, bool aligned)
 {
     using S = RowShape<T, VPT>;
-    constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
+    const int threads = blockDim.x, W = blockDim.x >> 5;   // FUSED: as many warps as tokens, at least four
     extern __shared__ int sm[];
     let_next_launch_start();
     wait_for_launch_before();
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     int *wcount = sm + kPadded;                        // W x E
     int *hist = wcount + W * a.E;                      // E
     int *offs = hist + a.E;                            // E + 1 (FUSED)
-    __shared__ int sums[W];
+    __shared__ int sums[kRouteThreads<VPT> / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int E = a.E, k = a.k;
     const bool plan = a.offsets != nullptr;
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     int *mine = wcount + warp * E;
     for (int e = lane; e < E; e += 32)
         mine[e] = 0;
-    for (int e = threadIdx.x; e < kPadded; e += kThr)
+    for (int e = threadIdx.x; e < kPadded; e += threads)
         price[e] = a.prices && e < E ? price_term(a.prices[e]) : 0.0f;
     __syncthreads();
     for (int64_t t = ta; t < tb; ++t) {
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     }
     __syncthreads();
     // counts of the warps before, and the CTA's
-    for (int e = threadIdx.x; e < E; e += kThr) {
+    for (int e = threadIdx.x; e < E; e += threads) {
         int run = 0;
 #pragma unroll 8
         for (int w = 0; w < W; ++w) {
@@ -392,9 +392,9 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
         __syncthreads();
     if (FUSED) {
         block_scan(hist, E, offs, sums);
-        for (int e = threadIdx.x; e <= E; e += kThr)
+        for (int e = threadIdx.x; e <= E; e += threads)
             a.offsets[e] = offs[e];
-        for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += kThr)
+        for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += threads)
             a.rows[p] = -1;
     }
     for (int64_t i = ta * k + lane; i < tb * k; i += 32) {
@@ -941,8 +941,9 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
                 const cudaError_t e = allow_smem<k_route<T, VPT, true>>(route_smem, m->device);
                 if (e != cudaSuccess)
                     return e;
+                const int warps = std::min(kThr / 32, std::max(4, (int)a.T));
                 m->launches += 1;
-                return launch_after(k_route<T, VPT, true>, dim3(1), kThr, route_smem, m->stream, a, a.T, aligned);
+                return launch_after(k_route<T, VPT, true>, dim3(1), 32 * warps, route_smem, m->stream, a, a.T, aligned);
             }
             const int64_t chunk = route_chunk(a.T);
             const int nb = (int)ceil_div(a.T, chunk);

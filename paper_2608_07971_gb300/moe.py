@@ -98,10 +98,10 @@ class Gate:
         object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class Routing:
     """Results of ``Moe.route``: idx, weight (T, k); counts (E,); rows (T * k,), pos (T, k), offsets (E + 1,)
-    or None without a plan."""
+    or None without a plan. `checked` holds (device index, T, E, k) where ``Moe.routing`` made the tensors."""
 
     idx: torch.Tensor
     weight: torch.Tensor
@@ -109,16 +109,19 @@ class Routing:
     rows: Optional[torch.Tensor] = None
     pos: Optional[torch.Tensor] = None
     offsets: Optional[torch.Tensor] = None
+    checked: Optional[tuple] = None
 
 
-@dataclasses.dataclass
+@dataclasses.dataclass(frozen=True)
 class Balance:
-    """Results of ``Moe.balance``: loss (2,) = balance, logit; counts (B, E), share (B, E), tokens (B,)."""
+    """Results of ``Moe.balance``: loss (2,) = balance, logit; counts (B, E), share (B, E), tokens (B,). `checked`
+    holds (device index, B, E) where ``Moe.balancing`` made the tensors."""
 
     loss: torch.Tensor
     counts: torch.Tensor
     share: torch.Tensor
     tokens: torch.Tensor
+    checked: Optional[tuple] = None
 
 
 @dataclasses.dataclass
@@ -204,6 +207,8 @@ class Moe:
             if optional:
                 return
             raise ValueError(f"{name} is missing")
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self._index and t.is_contiguous():
+            return
         if t.get_device() != self._index:
             raise ValueError(f"{name} is on {t.device}, the handle on {self.device}")
         if dtype is not None and t.dtype is not dtype:
@@ -227,6 +232,8 @@ class Moe:
         if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
             raise ValueError(f"{name}: shape ({rows}, {cols}) expected, not {tuple(shape)}")
         n, m = shape
+        if t.is_contiguous():
+            return code, m
         step, unit = t.stride()
         if unit != 1 and m > 1 and n > 0:
             raise ValueError(f"{name}: a matrix with contiguous rows expected")
@@ -239,11 +246,11 @@ class Moe:
 
     def routing(self, T: int, E: int, k: int, plan: bool = True) -> Routing:
         """Empty results of ``route``, to pass as its ``out``."""
-        i32 = torch.int32
-        r = Routing(self._new((T, k), i32), self._new((T, k), torch.float32), self._new((E,), torch.int64))
+        i32, plan_of = torch.int32, (None, None, None)
         if plan:
-            r.rows, r.pos, r.offsets = self._new((T * k,), i32), self._new((T, k), i32), self._new((E + 1,), i32)
-        return r
+            plan_of = (self._new((T * k,), i32), self._new((T, k), i32), self._new((E + 1,), i32))
+        return Routing(self._new((T, k), i32), self._new((T, k), torch.float32), self._new((E,), torch.int64), *plan_of,
+                       checked=(self._index, T, E, k))
 
     def route(self, logits, k: int, gate: Gate = Gate(), prices=None, valid=None, plan: bool = True,
               out: Optional[Routing] = None) -> Routing:
@@ -255,7 +262,7 @@ class Moe:
         self._need(valid, "valid", torch.bool, (T,), optional=True)
         if out is None:
             out = self.routing(T, E, k, plan)
-        else:
+        elif out.checked != (self._index, T, E, k):
             self._need(out.idx, "out.idx", torch.int32, (T, k))
             self._need(out.weight, "out.weight", torch.float32, (T, k))
             self._need(out.counts, "out.counts", torch.int64, (E,))
@@ -273,7 +280,7 @@ class Moe:
     def balancing(self, B: int, E: int) -> Balance:
         """Empty results of ``balance``, to pass as its ``out``."""
         return Balance(self._new((2,), torch.float32), self._new((B, E), torch.int64), self._new((B, E), torch.float32),
-                       self._new((B,), torch.int64))
+                       self._new((B,), torch.int64), checked=(self._index, B, E))
 
     def balance(self, logits, idx, gate: Gate = Gate(), seq_offsets=None, out: Optional[Balance] = None) -> Balance:
         """Balance and logit losses of the choices idx, over the sequences that seq_offsets (B + 1,) int32 bounds
@@ -285,7 +292,7 @@ class Moe:
         self._need(seq_offsets, "seq_offsets", torch.int32, (B + 1,), optional=True)
         if out is None:
             out = self.balancing(B, E)
-        else:
+        elif out.checked != (self._index, B, E):
             self._need(out.loss, "out.loss", torch.float32, (2,))
             self._need(out.counts, "out.counts", torch.int64, (B, E))
             self._need(out.share, "out.share", torch.float32, (B, E))
@@ -314,8 +321,9 @@ class Moe:
             self._need(dloss, "dloss", torch.float32, (2,))
             self._need(seq_offsets, "seq_offsets", torch.int32, (B + 1,), optional=True)
             counts, tokens = balance.counts, balance.tokens
-            self._need(counts, "balance.counts", torch.int64, (B, E))
-            self._need(tokens, "balance.tokens", torch.int64, (B,))
+            if balance.checked != (self._index, B, E):
+                self._need(counts, "balance.counts", torch.int64, (B, E))
+                self._need(tokens, "balance.tokens", torch.int64, (B,))
         if out is None:
             out = self._new((T, E), logits.dtype)
         _, ldo = self._matrix(out, "out", T, E, logits.dtype)
