@@ -326,6 +326,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     float next[VPT];
     if (ta < tb)
         load_row<T, VPT>(logits + ta * a.ld, E, aligned, lane, next);
+    int last_e = -1, last_rank = -1;   // this lane's choice and rank for the warp's last token
     int *mine = wcount + warp * E;
     for (int e = lane; e < E; e += 32)
         mine[e] = 0;
@@ -366,8 +367,10 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
             int rank = -1;
             if (sel >= 0)
                 rank = mine[sel]++;   // a token's choices differ: no two lanes meet
-            if (plan)
+            if (plan && t + 1 < tb)
                 a.pos[t * k + lane] = rank;
+            last_e = sel;
+            last_rank = rank;
         }
         __syncwarp();
     }
@@ -397,15 +400,20 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
         for (int64_t p = offs[E] + threadIdx.x; p < a.T * k; p += threads)
             a.rows[p] = -1;
     }
-    for (int64_t i = ta * k + lane; i < tb * k; i += 32) {
-        const int e = a.idx[i];
-        if (e < 0)
-            continue;
-        const int p = a.pos[i] + mine[e] + (FUSED ? offs[e] : 0);
+    // the warps before count too: the last token's choices are still at hand
+    auto place = [&](int64_t i, int e, int rank) {
+        int p = -1;
+        if (e >= 0) {
+            p = rank + mine[e] + (FUSED ? offs[e] : 0);
+            if (FUSED)
+                a.rows[p] = (int32_t)((uint32_t)i / (uint32_t)k);
+        }
         a.pos[i] = p;
-        if (FUSED)
-            a.rows[p] = (int32_t)((uint32_t)i / (uint32_t)k);
-    }
+    };
+    for (int64_t i = ta * k + lane; i < (tb - 1) * k; i += 32)
+        place(i, a.idx[i], a.pos[i]);
+    if (ta < tb && lane < k)
+        place((tb - 1) * k + lane, last_e, last_rank);
 }
 
 // Counts and offsets from the chunks' demands hist[nb][E]; the ranks in pos become rows. A CTA takes
