@@ -503,16 +503,21 @@ __device__ __forceinline__ int seq_bound(const int32_t *seq, int b, int64_t T)
     return (int)max((int64_t)0, min(T, (int64_t)seq[b]));
 }
 
-// First sequence whose end lies beyond token t (B if none).
-__device__ __forceinline__ int seq_of(const int32_t *seq, int B, int64_t t)
+// First sequence whose end lies beyond token t (B if none). A whole warp looks: 32 ends at a time, so that up
+// to 32 sequences take one trip to memory and 65536 take four.
+__device__ __forceinline__ int seq_of(const int32_t *seq, int B, int64_t t, int lane)
 {
     int lo = 0, hi = B;
     while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)seq[mid + 1] > t)
-            hi = mid;
-        else
-            lo = mid + 1;
+        const int step = (hi - lo + 31) / 32, probe = min(lo + (lane + 1) * step, hi) - 1;
+        const uint32_t beyond = __ballot_sync(kFull, (int64_t)seq[probe + 1] > t);
+        if (beyond == 0)
+            return hi;
+        const int first = __ffs(beyond) - 1;
+        if (step == 1)
+            return min(lo + first, hi - 1);
+        lo += first * step;
+        hi = min(hi, lo + step);
     }
     return lo;
 }
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
     __shared__ int tok_w[W];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c0 = blockIdx.x * chunk, c1 = min(a.T, c0 + chunk);
-    for (int s = a.seq ? seq_of(a.seq, a.B, c0) : 0; s < a.B; ++s) {
+    for (int s = a.seq ? seq_of(a.seq, a.B, c0, lane) : 0; s < a.B; ++s) {
         const int64_t lo = a.seq ? max(c0, (int64_t)seq_bound(a.seq, s, a.T)) : c0;
         const int64_t hi = a.seq ? min(c1, (int64_t)seq_bound(a.seq, s + 1, a.T)) : c1;
         if (lo >= c1)
@@ -827,7 +832,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
         }
         if constexpr (BALANCE) {
             if (t >= held_end) {   // the token's sequence, if it lies in one
-                const int s = a.seq ? seq_of(a.seq, a.B, t) : 0;
+                const int s = a.seq ? seq_of(a.seq, a.B, t, lane) : 0;
                 const bool in = s < a.B && (!a.seq || t >= a.seq[s]);
                 held_end = a.seq ? (in ? (int64_t)a.seq[s + 1] : s < a.B ? (int64_t)a.seq[s] : a.T) : a.T;
                 if (!in)

@@ -636,3 +636,26 @@ def test_rows_picked_after_rounding(mm, T, E, k, N, K, dt):
     assert mm.last_launch_count() == 2
     assert torch.equal(out, want) and bool((out[M - 7:] == 3).all())
     mm.synchronize()
+
+
+@pytest.mark.parametrize("B,T", [(1, 5), (31, 100), (33, 400), (1100, 3000), (2500, 2500)])
+def test_balance_over_many_sequences(mm, B, T):
+    """Sequences found by searches of different depth, empty ones among them, tokens before and after all."""
+    rng = np.random.default_rng(B)
+    z = make_logits(T, 6, "f32", B)
+    idx = mo.choose(host(z), 2)
+    seq = np.sort(rng.integers(1, T - 1, B + 1)).astype(np.int32)
+    di, ds = dev(idx.astype(np.int32)), dev(seq)
+    b = mm.balance(z, di, seq_offsets=ds)
+    loss, counts, share, tokens = mo.balance(host(z), idx, "softmax", seq)
+    assert np.array_equal(host(b.counts), counts) and np.array_equal(host(b.tokens), tokens)
+    c = const(z) + T * U
+    close(b.share, share, c * share)
+    close(b.loss, loss, 4 * c * (loss + 1.0))
+    d = np.array([1.0, 0.5], np.float32)
+    got = mm.route_backward(z, di, balance=b, seq_offsets=ds, dloss=dev(d))
+    want = mo.balance_grad(host(z), idx, "softmax", d, seq)
+    n, used = max(tokens.sum(), 1), max((tokens > 0).sum(), 1)
+    least = tokens[tokens > 0].min() if used and tokens.any() else 1
+    size = 6.0 / (least * used) + 2 * 0.5 * (np.abs(host(z)).max() + 2) / n
+    close(got, want, c * size)
