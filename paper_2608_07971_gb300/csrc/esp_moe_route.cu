@@ -3,7 +3,9 @@
 //
 // A warp holds one token's row in registers, lane l the elements c * 32 V + l V .. + V - 1 of chunk c (V
 // elements = one load of up to 16 bytes), so a row is read once, coalesced, and the statistics are
-// warp reductions.
+// warp reductions. The bytes are few (16384 x 256 bf16: 8.4 MB, 1.3 us); what bounds the choice is
+// instruction issue (about 790 per token at k = 8: 17 us), the losses (12 us) and the gradients (8 and
+// 13 us) the chain of a warp's three or four tokens, each fetched while the one before is worked on.
 
 #include <algorithm>
 #include <cfloat>
