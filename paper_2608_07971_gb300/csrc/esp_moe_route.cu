@@ -30,6 +30,9 @@ struct RowShape {
     static constexpr int kMaxV = 16 / (int)sizeof(T);
     static constexpr int V = VPT < kMaxV ? VPT : kMaxV;
     static __device__ __forceinline__ int element(int i, int lane) { return (i / V) * 32 * V + lane * V + i % V; }
+    // Place of an element in a row of shared memory that lanes read value by value: 32 i + lane, no bank
+    // conflicts (in the elements' own order the lanes would be V words apart).
+    static __device__ __forceinline__ int place(int e) { return ((e / (32 * V)) * V + e % V) * 32 + e / V % 32; }
 };
 
 // A gate's reading of a logit: +inf as the largest finite value, NaN as -inf.
@@ -333,7 +336,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
     for (int e = lane; e < E; e += 32)
         mine[e] = 0;
     for (int e = threadIdx.x; e < kPadded; e += threads)
-        price[e] = a.prices && e < E ? price_term(a.prices[e]) : 0.0f;
+        price[S::place(e)] = a.prices && e < E ? price_term(a.prices[e]) : 0.0f;
     __syncthreads();
     for (int64_t t = ta; t < tb; ++t) {
         const T *row = logits + t * a.ld;
@@ -343,7 +346,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             z[i] = next[i];
-            key[i] = order_key(__fadd_rn(z[i], price[S::element(i, lane)]));
+            key[i] = order_key(__fadd_rn(z[i], price[32 * i + lane]));
         }
         if (t + 1 < tb)
             load_row<T, VPT>(row + a.ld, E, aligned, lane, next);
@@ -531,8 +534,9 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
     constexpr int kThr = kRouteThreads<VPT>, W = kThr / 32;
     extern __shared__ float smf[];
     const int E = a.E, k = a.k;
-    float *red = smf;                                      // warps x E
-    int *hist = reinterpret_cast<int *>(red + W * E); // E
+    constexpr int kRow = 32 * VPT;
+    float *red = smf;                                       // W rows of kRow, by place
+    int *hist = reinterpret_cast<int *>(red + W * kRow);    // E
     let_next_launch_start();
     wait_for_launch_before();
     __shared__ float lse_w[W];
@@ -591,33 +595,32 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
                 acc[i] += p[i];
         }
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int e = S::element(i, lane);
-            if (e < E)
-                red[warp * E + e] = acc[i];
-        }
+        for (int i = 0; i < VPT; ++i)
+            red[warp * kRow + 32 * i + lane] = acc[i];
         if (lane == 0) {
             lse_w[warp] = lse2;
             tok_w[warp] = tokens;
         }
         __syncthreads();
         const int64_t slot = (int64_t)blockIdx.x + s;
-        for (int e = threadIdx.x; e < E; e += kThr) {
+        for (int q = threadIdx.x; q < kRow; q += kThr) {
+            const int e = S::element(q / 32, q % 32);
+            if (e >= E)
+                continue;
             float v = 0.0f;
+#pragma unroll
             for (int w = 0; w < W; ++w)
-                v += red[w * E + e];
+                v += red[w * kRow + q];
             a.part_share[slot * E + e] = v;
             a.part_count[slot * E + e] = hist[e];
         }
-        if (threadIdx.x == 0) {
-            float l = 0.0f;
-            int n = 0;
-            for (int w = 0; w < W; ++w) {
-                l += lse_w[w];
-                n += tok_w[w];
+        if (warp == W - 1) {
+            const float l = warp_sum(lane < W ? lse_w[lane] : 0.0f);
+            const int n = __reduce_add_sync(kFull, lane < W ? tok_w[lane] : 0);
+            if (lane == 0) {
+                a.part_lse[slot] = l;
+                a.part_tokens[slot] = n;
             }
-            a.part_lse[slot] = l;
-            a.part_tokens[slot] = n;
         }
     }
 }
@@ -741,7 +744,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
     using S = RowShape<T, VPT>;
     extern __shared__ float smf[];
     const int E = a.E, k = a.k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float *row = smf + warp * 32 * VPT;   // the chosen experts' part, zero elsewhere
+    float *row = smf + warp * 32 * VPT;   // the chosen experts' part by place, zero elsewhere
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
         row[32 * i + lane] = 0.0f;
@@ -811,15 +814,16 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
                     dj = g * sigmoid_f(zj) * sigmoid_f(-zj);
                 }
             }
+            const int at = on ? S::place(e) : 0;
             if (on)
-                row[e] = dj;
+                row[at] = dj;
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                d[i] = row[S::element(i, lane)];
+                d[i] = row[32 * i + lane];
             __syncwarp();
             if (on)
-                row[e] = 0.0f;
+                row[at] = 0.0f;
             if (dense_softmax) {
                 float dot = 0.0f;
 #pragma unroll
@@ -989,7 +993,7 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
                 constexpr int VPT = decltype(vpt)::value;
                 using S = RowShape<T, VPT>;
                 constexpr int kThr = kRouteThreads<VPT>;
-                const size_t smem = (size_t)(kThr / 32 + 1) * a.E * sizeof(float);
+                const size_t smem = ((size_t)kThr * VPT + a.E) * sizeof(float);
                 const cudaError_t e2 = allow_smem<k_balance<T, VPT>>(smem, m->device);
                 if (e2 != cudaSuccess)
                     return e2;
