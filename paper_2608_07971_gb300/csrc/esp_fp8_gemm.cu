@@ -8,19 +8,19 @@
 // A tile is 128 rows (CG = 1: one CTA) or 256 rows (CG = 2: two CTAs of a cluster that share the MMAs,
 // each holding 128 rows of A and half of B) times BN columns; one block of K per shared-memory stage
 // (128 codes = one 128-byte swizzled row). Warps 0-3 own the first half of the columns, warps 4-7 the
-// second, a thread one row (its TMEM lane) of its half; warp 8 loads tiles by TMA, warp 9 issues the
-// MMAs, warp 10 brings the column scales of the weight gradient to shared memory. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
+// second, a thread one row (its TMEM lane) of its half; warp 8 loads tiles by TMA, warps 9 and 11 issue
+// the MMAs in turn, warp 10 brings the column scales of the weight gradient to shared memory. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
 // run during a tile's stores.
 //
 // GROUPED ROWS (forward, row gradient): expert e's rows times its own B; a tile never spans two experts,
 // rows past the expert's end are computed and dropped. sb is one value per 128 columns.
 // GROUPED INNER AXIS (weight gradient): expert e's blocks of 128 positions; sb is a value per column.
 //
-// Bound by a block's turn: MMAs, epilogue and the hand-back of the stage take longer than the two stages of 256
-// columns hide. 8192 x 8192 x 4096 takes 230 us (2.39 PFLOP/s), 183 with the loads and MMAs alone; 65536 rows over
-// 64 experts x 4096 x 2048 548 us; the weight gradient of 16384 rows x 2048 x 4096 over 16 experts 258 us. Tiles of
-// 128 columns with four stages are 1.35 times slower (an MMA of 128 columns takes as long as one of 256), 16
-// epilogue warps 1.3 times (two barriers and half the columns each), a single CTA with 256 columns equal.
+// Bound by a block's turn: issue, MMAs, epilogue and the hand-back of the stage take longer than the two stages of
+// 256 columns hide. 8192 x 8192 x 4096 takes 224 us (2.45 PFLOP/s), 166 with the loads and MMAs alone; 65536 rows
+// over 64 experts x 4096 x 2048 525 us; the weight gradient of 16384 rows x 2048 x 4096 over 16 experts 257 us.
+// Tiles of 128 columns with four stages are 1.13 to 1.25 times slower (they load and read more of A for each
+// column), single CTAs with 256 columns 1.04 times, 16 epilogue warps 1.1 to 1.2 times.
 //
 // Every wait is bounded; one that runs out sets a flag that ends the CTA's other waits, the error word
 // reports it, and the CTA drains its copies and MMAs (bounded) before it frees its tensor memory.
@@ -37,7 +37,7 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, scales (COLS), one idle
+constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, scales (COLS), MMAs
 // registers per thread of the epilogue and of the other warpgroup: 2 * 216 + 72 = 3 * 168, the launch's
 constexpr int kEpilogueRegs = 216, kOtherRegs = 72;
 constexpr int kEpilogueWarps = 8;
@@ -154,17 +154,22 @@ __device__ __forceinline__ uint64_t global_ns()
     return t;
 }
 
-// Waits for a phase for at most `ms` milliseconds of the GPU's timer.
+// Waits for a phase for at most `ms` milliseconds of the GPU's timer, which is read once in 256 polls.
 __device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
 {
-    const uint64_t end = global_ns() + (uint64_t)ms * 1000000ull;
-    do {
-        if (mbar_try(bar, parity))
-            return true;
+    uint64_t end = 0;
+    for (;;) {
+        for (int i = 0; i < 256; ++i)
+            if (mbar_try(bar, parity))
+                return true;
         if (dead && *dead)
             return false;
-    } while (global_ns() < end);
-    return false;
+        const uint64_t now = global_ns();
+        if (end == 0)
+            end = now + (uint64_t)ms * 1000000ull;
+        else if (now >= end)
+            return false;
+    }
 }
 
 // Bounded wait of a role; gives up early once another wait of the CTA did. On running out it sets the CTA's
@@ -502,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(tempty + 8 * i, CG * kEpilogueWarps);
             mbar_init(sempty + 8 * i, kEpilogueWarps);
         }
-        mbar_init(drain, 1);
+        mbar_init(drain, 2);   // both issuing threads
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -584,7 +589,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
-        if (warp == 9 && lane == 0 && rank == 0) {
+        if ((warp == 9 || warp == 11) && lane == 0 && rank == 0) {
+            // Two threads issue in turn, a block each: one alone takes about 490 cycles for a block's waits and
+            // commits and 60 for each MMA, more than the MMAs themselves (128 each); 8192 x 8192 x 4096 took 230 us.
+            const bool odd = warp == 11;
             constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kRowsA * CG >> 4) << 24);
             int s = 0, acc = 0;
             uint32_t ph = 0, aph = 1;
@@ -592,17 +600,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             Tile t;
             for (int w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw)
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!(ok = mbar_wait(tempty + 8 * acc, aph, p, dead)) ||
-                        !(ok = mbar_wait(full + 8 * s, ph, p, dead)))
-                        break;
-                    fence_after();
-                    const uint64_t a = operand_desc(smem_u32(sm + s * S::kStage));
-                    const uint64_t b = operand_desc(smem_u32(sm + s * S::kStage + kStageA));
+                    if ((bool)(acc & 1) == odd) {
+                        if (!(ok = mbar_wait(full + 8 * s, ph, p, dead)) ||
+                            !(ok = mbar_wait(tempty + 8 * acc, aph, p, dead)))
+                            break;
+                        fence_after();
+                        const uint64_t a = operand_desc(smem_u32(sm + s * S::kStage));
+                        const uint64_t b = operand_desc(smem_u32(sm + s * S::kStage + kStageA));
 #pragma unroll
-                    for (int k = 0; k < kBlock / 32; ++k)   // 32 bytes = 2 units of the descriptor's address
-                        mma_codes<CG>(tmem + acc * BN, a + 2 * k, b + 2 * k, idesc, k > 0);
-                    mma_commit<CG>(empty + 8 * s);
-                    mma_commit<CG>(tfull + 8 * acc);
+                        for (int k = 0; k < kBlock / 32; ++k)   // 32 bytes = 2 units of the descriptor's address
+                            mma_codes<CG>(tmem + acc * BN, a + 2 * k, b + 2 * k, idesc, k > 0);
+                        mma_commit<CG>(tfull + 8 * acc);
+                        mma_commit<CG>(empty + 8 * s);
+                    }
                     if (++s == S::kStages) {
                         s = 0;
                         ph ^= 1;
@@ -806,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp == 8 && lane == 0 && rank == 0)
             for (uint32_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
                 mbar_wait_ms(full + 8 * (i % S::kStages), (i / S::kStages) & 1, 20, nullptr);
-        if (warp == 9 && lane == 0 && rank == 0) {
+        if ((warp == 9 || warp == 11) && lane == 0 && rank == 0) {
             mma_commit<CG>(drain);
             mbar_wait_ms(drain, 0, 1000, nullptr);
         }

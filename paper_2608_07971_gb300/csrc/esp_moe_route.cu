@@ -4,8 +4,9 @@
 // A warp holds one token's row in registers, lane l the elements c * 32 V + l V .. + V - 1 of chunk c (V
 // elements = one load of up to 16 bytes), so a row is read once, coalesced, and the statistics are
 // warp reductions. The bytes are few (16384 x 256 bf16: 8.4 MB, 1.3 us); what bounds the choice is
-// instruction issue (about 790 per token at k = 8: 17 us), the losses (12 us) and the gradients (8 and
-// 13 us) the chain of a warp's three or four tokens, each fetched while the one before is worked on.
+// instruction issue (about 790 per token at k = 8: 15 us, and 5 of plan), the losses (10 us and 6 to join
+// the parts) and the gradients (8 us from the weights, 12 from the losses) the chain of a warp's tokens, each
+// fetched while the one before is worked on.
 
 #include <algorithm>
 #include <cfloat>
@@ -20,8 +21,9 @@ namespace esp_moe_impl {
 namespace {
 
 constexpr uint32_t kFull = 0xffffffffu;
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;           // k_balance_sum, k_step_prices
 constexpr int kWarps = kThreads / 32;
+constexpr int kLeastChunk = 16;          // tokens of a CTA
 // T * k up to which one CTA routes and plans in a single launch
 constexpr int kFusedSlots = 512;
 
@@ -421,13 +423,13 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
         place((tb - 1) * k + lane, last_e, last_rank);
 }
 
-// Counts and offsets from the chunks' demands hist[nb][E]; the ranks in pos become rows. A CTA takes
-// kPlanChunks chunks and sums the columns over all chunks and over those before its own.
-constexpr int kPlanThreads = 1024, kPlanChunks = 2;
+// Counts and offsets from the chunks' demands hist[nb][E]; the ranks in pos become rows. A CTA takes one chunk
+// and sums the columns over all chunks and over those before its own.
+constexpr int kPlanThreads = 1024;
 
 // D: a demand; a thread adds V columns (one load) of every groups-th chunk.
 template <typename D, int V>
-__device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0, int *total, int *before, int *second)
+__device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0, int *total, int *before)
 {
     struct alignas(sizeof(D) * V) Row {
         D v[V];
@@ -451,32 +453,29 @@ __device__ __forceinline__ void sum_columns(const D *hist, int E, int nb, int c0
             atomicAdd(before + c * V + j, bef[j]);
         }
     }
-    for (int e = threadIdx.x; e < E; e += kPlanThreads)
-        second[e] = hist[(int64_t)c0 * E + e];
 }
 
 __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_t chunk, int nb)
 {
     extern __shared__ int sm[];
     __shared__ int sums[kPlanThreads / 32];
-    const int E = a.E, k = a.k, c0 = blockIdx.x * kPlanChunks;
-    int *total = sm, *before = sm + E, *second = sm + 2 * E, *offs = sm + 3 * E;
+    const int E = a.E, k = a.k, c0 = blockIdx.x;
+    int *total = sm, *before = sm + E, *offs = sm + 2 * E;
     for (int e = threadIdx.x; e < E; e += kPlanThreads)
         total[e] = before[e] = 0;
     let_next_launch_start();
     wait_for_launch_before();
     // the first slots' ranks are on their way while the columns are summed
-    const int64_t s0 = c0 * chunk * k, s1 = a.offsets ? min(a.T * k, s0 + kPlanChunks * chunk * k) : s0;
-    const int64_t mid = s0 + chunk * k;
+    const int64_t s0 = c0 * chunk * k, s1 = a.offsets ? min(a.T * k, s0 + chunk * k) : s0;
     int64_t i = s0 + threadIdx.x;
     int e = i < s1 ? a.idx[i] : -1, rank = i < s1 ? a.pos[i] : 0;
     __syncthreads();
     if (!a.hist16)
-        sum_columns<int32_t, 1>(a.hist, E, nb, c0, total, before, second);
+        sum_columns<int32_t, 1>(a.hist, E, nb, c0, total, before);
     else if (E % 4 == 0)
-        sum_columns<uint16_t, 4>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
+        sum_columns<uint16_t, 4>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before);
     else
-        sum_columns<uint16_t, 1>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before, second);
+        sum_columns<uint16_t, 1>(reinterpret_cast<const uint16_t *>(a.hist), E, nb, c0, total, before);
     block_scan(total, E, offs, sums);
     if (blockIdx.x == 0)
         for (int q = threadIdx.x; q < E; q += kPlanThreads)
@@ -488,7 +487,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_plan(const RouteArgs a, int64_
             a.offsets[q] = offs[q];
     for (; i < s1;) {
         if (e >= 0) {
-            const int p = rank + offs[e] + before[e] + (i >= mid ? second[e] : 0);
+            const int p = rank + offs[e] + before[e];
             a.pos[i] = p;
             a.rows[p] = (int32_t)((uint32_t)i / (uint32_t)k);
         }
@@ -648,7 +647,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*buf)[N])
 }
 
 // One CTA per sequence: the chunks' parts in order; the last CTA to finish sums the sequences' losses.
-__global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, int64_t chunk)
+__global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, int chunk)
 {
     extern __shared__ float smf[];
     __shared__ float buf1[kWarps][1], buf2[kWarps][1], buf4[kWarps][4];
@@ -660,11 +659,11 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
     int *count = reinterpret_cast<int *>(smf + groups * E);      // groups x E
     let_next_launch_start();
     wait_for_launch_before();
-    const int64_t lo = a.seq ? seq_bound(a.seq, s, a.T) : 0, hi = a.seq ? seq_bound(a.seq, s + 1, a.T) : a.T;
-    const int64_t b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
+    const int lo = a.seq ? seq_bound(a.seq, s, a.T) : 0, hi = a.seq ? seq_bound(a.seq, s + 1, a.T) : (int)a.T;
+    const int b0 = lo / chunk, b1 = lo < hi ? (hi - 1) / chunk + 1 : b0;
     int n = 0;
     float lse[1] = {0.0f};
-    for (int64_t b = b0 + threadIdx.x; b < b1; b += kThreads) {
+    for (int b = b0 + threadIdx.x; b < b1; b += kThreads) {
         n += a.part_tokens[b + s];
         lse[0] += a.part_lse[b + s];
     }
@@ -672,10 +671,13 @@ __global__ void __launch_bounds__(kThreads) k_balance_sum(const BalanceArgs a, i
         const int e = i % E, g = i / E;
         float v = 0.0f;
         int c = 0;
+        const int64_t step = (int64_t)groups * E;
+        const float *ps = a.part_share + (int64_t)(b0 + g + s) * E + e;
+        const int32_t *pc = a.part_count + (int64_t)(b0 + g + s) * E + e;
 #pragma unroll 8
-        for (int64_t b = b0 + g; b < b1; b += groups) {
-            v += a.part_share[(b + s) * E + e];
-            c += a.part_count[(b + s) * E + e];
+        for (int b = b0 + g; b < b1; b += groups, ps += step, pc += step) {
+            v += *ps;
+            c += *pc;
         }
         share[i] = v;
         count[i] = c;
@@ -909,10 +911,10 @@ __global__ void __launch_bounds__(kThreads) k_step_prices(int32_t E, const int64
 
 // ---- launches
 
-// Tokens of a CTA: one CTA for every SM, a token for each of its warps at least.
+// Tokens of a CTA: one CTA for every SM, kLeastChunk at least.
 int64_t route_chunk(int64_t T)
 {
-    return std::max<int64_t>(kWarps, ceil_div(T, 152));
+    return std::max<int64_t>(kLeastChunk, ceil_div(T, 152));
 }
 
 bool fused(int64_t T, int32_t k)
@@ -972,8 +974,8 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
             if (e != cudaSuccess)
                 return e;
             m->launches += 2;
-            return launch_after(k_plan, dim3(a.offsets ? (unsigned)ceil_div(nb, kPlanChunks) : 1u), kPlanThreads,
-                                (size_t)(4 * a.E + 1) * sizeof(int), m->stream, a, chunk, nb);
+            return launch_after(k_plan, dim3(a.offsets ? (unsigned)nb : 1u), kPlanThreads,
+                                (size_t)(3 * a.E + 1) * sizeof(int), m->stream, a, chunk, nb);
         });
     });
 }
@@ -1007,7 +1009,7 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
     }
     const size_t smem = (size_t)std::max(1, kThreads / a.E) * a.E * (sizeof(float) + sizeof(int));
     m->launches += 1;
-    return launch_after(k_balance_sum, dim3((unsigned)a.B), kThreads, smem, m->stream, a, chunk);
+    return launch_after(k_balance_sum, dim3((unsigned)a.B), kThreads, smem, m->stream, a, (int)chunk);
 }
 
 cudaError_t launch_route_backward(esp_moe *m, int32_t dtype, const RouteBackwardArgs &a)
