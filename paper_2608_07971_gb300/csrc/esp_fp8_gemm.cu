@@ -9,8 +9,8 @@
 // each holding 128 rows of A and half of B) times BN columns; one block of K per shared-memory stage
 // (128 codes = one 128-byte swizzled row). Warps 0-3 own the first half of the columns, warps 4-7 the
 // second, a thread one row (its TMEM lane) of its half; warp 8 loads tiles by TMA, warps 9 and 11 issue
-// the MMAs in turn, warp 10 brings the column scales of the weight gradient to shared memory. CTAs are persistent: every role walks the same list of tiles, so loads and MMAs of the next tile
-// run during a tile's stores.
+// the MMAs in turn, warp 10 brings the scales of the weight gradient to shared memory. CTAs are persistent:
+// every role walks the same list of tiles, so loads and MMAs of the next tile run during a tile's stores.
 //
 // GROUPED ROWS (forward, row gradient): expert e's rows times its own B; a tile never spans two experts,
 // rows past the expert's end are computed and dropped. sb is one value per 128 columns.
@@ -170,6 +170,15 @@ __device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint
         else if (now >= end)
             return false;
     }
+}
+
+// One thread of a whole warp, the same at every call. What the warp computes stays in uniform registers, which
+// the MMA and TMA instructions read; a branch on a lane number moves every operand there first.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 
 // Bounded wait of a role; gives up early once another wait of the CTA did. On running out it sets the CTA's
@@ -562,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (warp >= kEpilogueWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == 8 && lane == 0) {
+        if (warp == 8) {
             const uint32_t full0 = CG == 1 ? full : map_rank(full, 0);
             int s = 0;
             uint32_t ph = 1;
@@ -572,15 +581,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int ya = t.m0 + (int)rank * kRowsA;
                 const int yb = (COLS ? 0 : t.e * p.rows_b) + t.n0 + (int)rank * S::kRowsB;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!(ok = mbar_wait(empty + 8 * s, ph, p, dead)))
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(empty + 8 * s, ph, p, dead))))
                         break;
                     const uint32_t dst = smem_u32(sm + s * S::kStage);
-                    if (rank == 0)
-                        mbar_expect(full + 8 * s, CG * S::kStage);
-                    if (!(p.hold && issued == 2)) {
-                        tma_tile<CG>(dst, &map_a, kb * kBlock, ya, full0 + 8 * s);
-                        tma_tile<CG>(dst + kStageA, &map_b, kb * kBlock, yb, full0 + 8 * s);
+                    if (elect_one()) {
+                        if (rank == 0)
+                            mbar_expect(full + 8 * s, CG * S::kStage);
+                        if (!(p.hold && issued == 2)) {
+                            tma_tile<CG>(dst, &map_a, kb * kBlock, ya, full0 + 8 * s);
+                            tma_tile<CG>(dst + kStageA, &map_b, kb * kBlock, yb, full0 + 8 * s);
+                        }
                     }
+                    __syncwarp();
                     ++issued;
                     if (++s == S::kStages) {
                         s = 0;
@@ -589,8 +601,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
-        if ((warp == 9 || warp == 11) && lane == 0 && rank == 0) {
-            // Two threads issue in turn, a block each: one alone takes about 490 cycles for a block's waits and
+        if ((warp == 9 || warp == 11) && rank == 0) {
+            // Two warps issue in turn, a block each: a single thread took about 490 cycles for a block's waits and
             // commits and 60 for each MMA, more than the MMAs themselves (128 each); 8192 x 8192 x 4096 took 230 us.
             const bool odd = warp == 11;
             constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kRowsA * CG >> 4) << 24);
@@ -601,17 +613,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int w = w0; ok && tile_at<CG, BN, COLS>(p, table, w, t); w += dw)
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if ((bool)(acc & 1) == odd) {
-                        if (!(ok = mbar_wait(full + 8 * s, ph, p, dead)) ||
-                            !(ok = mbar_wait(tempty + 8 * acc, aph, p, dead)))
+                        ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * s, ph, p, dead) &&
+                                                         mbar_wait(tempty + 8 * acc, aph, p, dead));
+                        if (!ok)
                             break;
                         fence_after();
                         const uint64_t a = operand_desc(smem_u32(sm + s * S::kStage));
                         const uint64_t b = operand_desc(smem_u32(sm + s * S::kStage + kStageA));
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kBlock / 32; ++k)   // 32 bytes = 2 units of the descriptor's address
-                            mma_codes<CG>(tmem + acc * BN, a + 2 * k, b + 2 * k, idesc, k > 0);
-                        mma_commit<CG>(tfull + 8 * acc);
-                        mma_commit<CG>(empty + 8 * s);
+                            for (int k = 0; k < kBlock / 32; ++k)   // 32 bytes = 2 units of the descriptor's address
+                                mma_codes<CG>(tmem + acc * BN, a + 2 * k, b + 2 * k, idesc, k > 0);
+                            mma_commit<CG>(tfull + 8 * acc);
+                            mma_commit<CG>(empty + 8 * s);
+                        }
+                        __syncwarp();
                     }
                     if (++s == S::kStages) {
                         s = 0;
@@ -737,40 +753,43 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                     for (int c = 0; c < D; ++c)
                         tmem_ld16(src + 16 * c, v[c]);
+// chunk c is held in v[c % D] until it is added
+                    auto add = [&](int c) {
+                        const uint32_t(&x)[16] = v[c % D];
 #pragma unroll
-                    for (int c0 = 0; c0 < chunks; c0 += D) {
-                        tmem_wait(v);
-                        if (c0 + D >= chunks) {
-                            fence_before();
-                            __syncwarp();
-                            if (lane == 0)
-                                mbar_arrive(tempty0 + 8 * acc);
-                        }
-#pragma unroll
-                        for (int j = 0; j < D; ++j) {
-                            const int c = c0 + j;
-                            if (c >= chunks)
-                                continue;
-#pragma unroll
-                            for (int i = 0; i < 16; i += 4) {
-                                float *to = sum + 16 * c + i;
-                                float a = __uint_as_float(v[j][i]), b = __uint_as_float(v[j][i + 1]);
-                                float d = __uint_as_float(v[j][i + 2]), f = __uint_as_float(v[j][i + 3]);
-                                if (COLS) {
-                                    const float4 s4 = *reinterpret_cast<const float4 *>(csb + 16 * c + i);
-                                    mul_pair(a, b, scale);
-                                    mul_pair(d, f, scale);
-                                    fma_pair(to[0], to[1], a, b, s4.x, s4.y);
-                                    fma_pair(to[2], to[3], d, f, s4.z, s4.w);
-                                } else {
-                                    fma_pair(to[0], to[1], a, b, scale, scale);
-                                    fma_pair(to[2], to[3], d, f, scale, scale);
-                                }
+                        for (int i = 0; i < 16; i += 4) {
+                            float *to = sum + 16 * c + i;
+                            float a = __uint_as_float(x[i]), b = __uint_as_float(x[i + 1]);
+                            float d = __uint_as_float(x[i + 2]), f = __uint_as_float(x[i + 3]);
+                            if (COLS) {
+                                const float4 s4 = *reinterpret_cast<const float4 *>(csb + 16 * c + i);
+                                mul_pair(a, b, scale);
+                                mul_pair(d, f, scale);
+                                fma_pair(to[0], to[1], a, b, s4.x, s4.y);
+                                fma_pair(to[2], to[3], d, f, s4.z, s4.w);
+                            } else {
+                                fma_pair(to[0], to[1], a, b, scale, scale);
+                                fma_pair(to[2], to[3], d, f, scale, scale);
                             }
-                            if (c + D < chunks)
-                                tmem_ld16(src + 16 * (c + D), v[j]);
+                        }
+                    };
+#pragma unroll
+                    for (int c0 = 0; c0 + D < chunks; c0 += D) {
+                        tmem_wait(v);
+#pragma unroll
+                        for (int c = c0; c < c0 + D && c + D < chunks; ++c) {
+                            add(c);
+                            tmem_ld16(src + 16 * (c + D), v[c % D]);
                         }
                     }
+                    tmem_wait(v);
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        mbar_arrive(tempty0 + 8 * acc);
+#pragma unroll
+                    for (int c = chunks - D; c < chunks; ++c)
+                        add(c);
                 } else if (lane == 0) {
                     mbar_arrive(tempty0 + 8 * acc);
                 }
@@ -816,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp == 8 && lane == 0 && rank == 0)
             for (uint32_t i = issued < S::kStages ? 0 : issued - S::kStages; i < issued; ++i)
                 mbar_wait_ms(full + 8 * (i % S::kStages), (i / S::kStages) & 1, 20, nullptr);
-        if ((warp == 9 || warp == 11) && lane == 0 && rank == 0) {
+        if ((warp == 9 || warp == 11) && rank == 0 && elect_one()) {   // the threads that issued
             mma_commit<CG>(drain);
             mbar_wait_ms(drain, 0, 1000, nullptr);
         }

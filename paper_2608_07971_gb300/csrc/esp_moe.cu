@@ -5,7 +5,6 @@
 #include <cmath>
 #include <new>
 
-#include "esp_debug.h"
 #include "esp_moe_impl.h"
 #include "esp_moe_load.cuh"
 
