@@ -17,10 +17,10 @@
 // GROUPED INNER AXIS (weight gradient): expert e's blocks of 128 positions; sb is a value per column.
 //
 // Bound by a block's turn: issue, MMAs, epilogue and the hand-back of the stage take longer than the two stages of
-// 256 columns hide. 8192 x 8192 x 4096 takes 224 us (2.45 PFLOP/s), 166 with the loads and MMAs alone; 65536 rows
-// over 64 experts x 4096 x 2048 525 us; the weight gradient of 16384 rows x 2048 x 4096 over 16 experts 257 us.
-// Tiles of 128 columns with four stages are 1.13 to 1.25 times slower (they load and read more of A for each
-// column), single CTAs with 256 columns 1.04 times, 16 epilogue warps 1.1 to 1.2 times.
+// 256 columns hide. 8192 x 8192 x 4096 takes 222 us (2.48 PFLOP/s), 166 with the loads and MMAs alone; 65536 rows
+// over 64 experts x 4096 x 2048 515 us; the weight gradient of 16384 rows x 2048 x 4096 over 16 experts 257 us.
+// Tiles of 128 columns with four stages are 1.1 to 1.25 times slower (they load and read more of A for each
+// column), single CTAs with 256 columns 1.01 to 1.03 times, 16 epilogue warps 1.1 to 1.2 times.
 //
 // Every wait is bounded; one that runs out sets a flag that ends the CTA's other waits, the error word
 // reports it, and the CTA drains its copies and MMAs (bounded) before it frees its tensor memory.
@@ -958,9 +958,9 @@ GemmParams common(esp_moe *m)
 
 // Which tiles a product takes: pairs of CTAs with 256 x 256, or single CTAs with 128 x 128 whose inner axis
 // may be split into parts. Times in units of a single CTA's block (about 0.4 us): rounds of tiles over the
-// SMs times the blocks of each. A pair's block takes 1.35 units (4096 x 4096 x 4096 as pairs 73 us, as
-// single CTAs 91; 1000 x 2000 x 2050: 15.9 and 14.3); joining parts takes 8 and 1 to
-// 1.5 for each part (128 x 4096 x 4096 in 4 parts 14.9 us, whole 16.6; 256 x 2048 x 2048 12.1 and 10.6).
+// SMs times the blocks of each. A pair's block takes 1.35 units (4096 x 4096 x 4096 as pairs 67 us, as
+// single CTAs 74; 1000 x 2000 x 2050: 14.9 and 13.3); joining parts takes 8 and 1 to 1.5 for each part
+// (16 x 2048 x 4096 in parts 12.6 us, whole 16.3; 128 x 4096 x 4096 16.6 and 17.4).
 struct Choice {
     bool pair;
     int splits;
