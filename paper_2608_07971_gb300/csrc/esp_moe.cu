@@ -28,6 +28,16 @@ esp_status fail(esp_moe *m)
             return fail(m);         \
     } while (0)
 
+bool capturing(cudaStream_t s)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &status) != cudaSuccess) {
+        cudaGetLastError();
+        return true;   // the legacy stream while another stream is being captured
+    }
+    return status != cudaStreamCaptureStatusNone;
+}
+
 // Common head of every call: the handle, its device current, no launches yet.
 esp_status begin(esp_moe *m)
 {
@@ -39,17 +49,28 @@ esp_status begin(esp_moe *m)
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || (dev != m->device && cudaSetDevice(m->device) != cudaSuccess))
         return fail(m);
+    m->in_capture = capturing(m->stream);
     return ESP_OK;
 }
 
-// At least `bytes` of work space. A larger block replaces the old one after the device is done with it.
+// At least `bytes` of work space. A larger block replaces the old one, which is freed once the queued work is done
+// with it, or kept as long as the handle where a captured graph names it.
 esp_status reserve(esp_moe *m, size_t bytes)
 {
-    if (bytes <= m->ws_bytes)
+    if (bytes <= m->ws_bytes) {
+        m->ws_captured = m->ws_captured || m->in_capture;
         return ESP_OK;
+    }
     if (m->ws) {
-        MOE_CUDA(cudaStreamSynchronize(m->stream));
-        MOE_CUDA(cudaFree(m->ws));
+        if (m->ws_captured) {
+            esp_moe::Kept *k = new (std::nothrow) esp_moe::Kept{m->ws, m->kept};
+            if (!k)
+                return ESP_ERR_OOM;
+            m->kept = k;
+        } else {
+            MOE_CUDA(cudaStreamSynchronize(m->stream));
+            MOE_CUDA(cudaFree(m->ws));
+        }
         m->ws = nullptr;
         m->ws_bytes = 0;
     }
@@ -60,17 +81,8 @@ esp_status reserve(esp_moe *m, size_t bytes)
     }
     m->ws = static_cast<unsigned char *>(p);
     m->ws_bytes = bytes;
+    m->ws_captured = m->in_capture;
     return ESP_OK;
-}
-
-bool capturing(cudaStream_t s)
-{
-    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(s, &status) != cudaSuccess) {
-        cudaGetLastError();
-        return true;   // the legacy stream while another stream is being captured
-    }
-    return status != cudaStreamCaptureStatusNone;
 }
 
 size_t element_size(int32_t dtype)
@@ -508,6 +520,12 @@ void esp_moe_destroy(esp_moe *m)
     cudaSetDevice(m->device);
     if (m->ws)
         cudaFree(m->ws);
+    while (m->kept) {
+        esp_moe::Kept *k = m->kept;
+        m->kept = k->next;
+        cudaFree(k->p);
+        delete k;
+    }
     if (m->d_err)
         cudaFree(m->d_err);
     if (m->handoff)

@@ -19,6 +19,12 @@ struct esp_moe {
     int64_t launches = 0;
     unsigned char *ws = nullptr;     // work space of the call in flight (later calls run after it)
     size_t ws_bytes = 0;
+    bool ws_captured = false;        // a captured call uses it: its graph names the block as long as it lives
+    bool in_capture = false;         // the call in flight is being captured
+    struct Kept {                    // outgrown blocks that graphs name, freed with the handle
+        void *p;
+        Kept *next;
+    } *kept = nullptr;
     unsigned int *d_err = nullptr;   // device error word (timeouts of the product kernels)
     unsigned int *d_ticket = nullptr;   // arrival counters, zero between launches
     int max_pairs = 0;               // CTA pairs of the product kernel that run at once (0: not asked yet)

@@ -3,7 +3,8 @@
 Argument marshalling only: every step runs in the library's CUDA kernels (there is no CPU fallback). ``Moe``
 holds one handle. Its calls are queued on the stream given at creation, or without one on the caller's
 current torch stream at every call; they return without waiting. Every call takes ``out`` to reuse the
-tensors of an earlier one (a serving loop, a CUDA graph), else allocates its results.
+tensors of an earlier one (a serving loop, a CUDA graph), else allocates its results. A graph that captured calls
+uses the handle's work space, so the handle is kept as long as the graph is replayed.
 
     m = Moe()
     r = m.route(logits, k, gate=Gate("softmax"), prices=prices)      # choice, weights, demand, plan

@@ -1,0 +1,286 @@
+// Host checks of the expert layer's handle (csrc/esp_moe.cu) without a GPU: the CUDA runtime is a fake that follows
+// which work is ordered after which, which streams are being captured, and which memory a captured graph names. The
+// kernels' launchers are stubs that record a piece of work.
+//
+//   moe_handle_driver NAME     runs the check NAME; exit code 0 and "ok", or a line for each fault
+
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <set>
+#include <string>
+#include <vector>
+
+#include "esp_moe_impl.h"
+
+namespace {
+
+struct Stream {
+    bool capturing = false;
+    bool broken = false;      // its capture was ended by a call that cannot be captured
+    std::set<int> before;     // eager work that what comes next on the stream runs after
+};
+
+struct Event {
+    std::set<int> before;
+};
+
+struct Work {
+    bool captured;
+    const void *ws;
+};
+
+Stream legacy;
+std::vector<Work> works;
+std::set<int> finished;                  // work that the host has waited for
+std::map<const void *, size_t> memory;   // live blocks
+std::set<const void *> in_graph;         // blocks that captured work names
+std::vector<std::string> faults;
+int syncs_while_capturing = 0, allocations_while_capturing = 0;
+
+void fault(const std::string &what)
+{
+    faults.push_back(what);
+}
+
+Stream &of(cudaStream_t s)
+{
+    return s ? *reinterpret_cast<Stream *>(s) : legacy;
+}
+
+std::vector<Stream *> streams;
+
+cudaStream_t new_stream()
+{
+    streams.push_back(new Stream());
+    return reinterpret_cast<cudaStream_t>(streams.back());
+}
+
+bool any_capturing()
+{
+    for (Stream *s : streams)
+        if (s->capturing)
+            return true;
+    return false;
+}
+
+// A kernel queued on the handle's stream that uses its work space and counters.
+cudaError_t work(esp_moe *m)
+{
+    Stream &s = of(m->stream);
+    const int id = (int)works.size();
+    works.push_back(Work{s.capturing, m->ws});
+    if (m->ws && !memory.count(m->ws))
+        fault("work " + std::to_string(id) + " uses freed memory");
+    if (s.capturing) {
+        in_graph.insert(m->ws);
+        return cudaSuccess;
+    }
+    for (int i = 0; i < id; ++i)
+        if (!works[i].captured && !s.before.count(i) && !finished.count(i))
+            fault("work " + std::to_string(id) + " shares the work space with " + std::to_string(i) + " without order");
+    s.before.insert(id);
+    return cudaSuccess;
+}
+
+}  // namespace
+
+// ---- the CUDA runtime that csrc/esp_moe.cu calls
+
+extern "C" {
+
+cudaError_t cudaGetLastError() { return cudaSuccess; }
+cudaError_t cudaGetDevice(int *d)
+{
+    *d = 0;
+    return cudaSuccess;
+}
+cudaError_t cudaSetDevice(int) { return cudaSuccess; }
+cudaError_t cudaGetDeviceCount(int *n)
+{
+    *n = 1;
+    return cudaSuccess;
+}
+cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr a, int)
+{
+    *v = a == cudaDevAttrComputeCapabilityMajor ? 10 : a == cudaDevAttrComputeCapabilityMinor ? 3 : 152;
+    return cudaSuccess;
+}
+cudaError_t cudaMalloc(void **p, size_t n)
+{
+    if (any_capturing()) {
+        ++allocations_while_capturing;
+        for (Stream *s : streams)
+            s->broken = s->broken || s->capturing;
+        return cudaErrorStreamCaptureUnsupported;
+    }
+    *p = calloc(1, n < 4096 ? n : 4096);
+    memory[*p] = n;
+    return cudaSuccess;
+}
+cudaError_t cudaFree(void *p)
+{
+    if (in_graph.count(p))
+        fault("memory that a captured graph names is freed");
+    if (!memory.erase(p))
+        fault("memory is freed twice");
+    for (size_t i = 0; i < works.size(); ++i)
+        finished.insert((int)i);
+    free(p);
+    return cudaSuccess;
+}
+cudaError_t cudaMemset(void *p, int v, size_t n)
+{
+    memset(p, v, n);
+    return cudaSuccess;
+}
+cudaError_t cudaMemcpy(void *d, const void *s, size_t n, cudaMemcpyKind)
+{
+    memcpy(d, s, n);
+    return cudaSuccess;
+}
+cudaError_t cudaStreamSynchronize(cudaStream_t s)
+{
+    if (of(s).capturing) {
+        ++syncs_while_capturing;
+        of(s).broken = true;
+        return cudaErrorStreamCaptureUnsupported;
+    }
+    finished.insert(of(s).before.begin(), of(s).before.end());
+    return cudaSuccess;
+}
+cudaError_t cudaStreamIsCapturing(cudaStream_t s, cudaStreamCaptureStatus *st)
+{
+    *st = of(s).capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+    return cudaSuccess;
+}
+cudaError_t cudaEventCreateWithFlags(cudaEvent_t *e, unsigned int)
+{
+    *e = reinterpret_cast<cudaEvent_t>(new Event());
+    return cudaSuccess;
+}
+cudaError_t cudaEventDestroy(cudaEvent_t e)
+{
+    delete reinterpret_cast<Event *>(e);
+    return cudaSuccess;
+}
+cudaError_t cudaEventRecord(cudaEvent_t e, cudaStream_t s)
+{
+    if (of(s).capturing) {
+        of(s).broken = true;
+        return cudaErrorStreamCaptureUnsupported;
+    }
+    reinterpret_cast<Event *>(e)->before = of(s).before;
+    return cudaSuccess;
+}
+cudaError_t cudaStreamWaitEvent(cudaStream_t s, cudaEvent_t e, unsigned int)
+{
+    if (of(s).capturing) {
+        of(s).broken = true;
+        return cudaErrorStreamCaptureIsolation;
+    }
+    const Event *ev = reinterpret_cast<Event *>(e);
+    of(s).before.insert(ev->before.begin(), ev->before.end());
+    return cudaSuccess;
+}
+
+}  // extern "C"
+
+// ---- the launchers
+
+namespace esp_moe_impl {
+
+size_t route_hist_ints(int64_t T, int32_t E, int32_t) { return (size_t)(T * E); }
+cudaError_t launch_route(esp_moe *m, int32_t, const RouteArgs &) { return work(m); }
+int64_t balance_slots(int64_t T, int32_t B) { return T + B; }
+cudaError_t launch_balance(esp_moe *m, int32_t, const BalanceArgs &) { return work(m); }
+cudaError_t launch_route_backward(esp_moe *, int32_t, const RouteBackwardArgs &) { return cudaSuccess; }
+cudaError_t launch_step_prices(esp_moe *, int32_t, const int64_t *, double, double, float *) { return cudaSuccess; }
+cudaError_t launch_combine(esp_moe *, int32_t, const CombineArgs &) { return cudaSuccess; }
+cudaError_t launch_combine_backward(esp_moe *, int32_t, const CombineArgs &) { return cudaSuccess; }
+cudaError_t launch_quant_rows(esp_moe *m, int32_t, const QuantRowsArgs &) { return work(m); }
+cudaError_t launch_pick_rows(esp_moe *m, const PickRowsArgs &) { return work(m); }
+cudaError_t launch_quant_cols(esp_moe *m, int32_t, const QuantColsArgs &) { return work(m); }
+cudaError_t launch_quant_weight(esp_moe *, int32_t, const void *, int64_t, const esp_moe_weight &) { return cudaSuccess; }
+size_t gemm_partial_floats(const esp_moe *) { return 1024; }
+cudaError_t launch_gemm_rows(esp_moe *m, int32_t, const GemmRowsArgs &) { return work(m); }
+cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &) { return work(m); }
+
+}  // namespace esp_moe_impl
+
+// ---- checks
+
+namespace {
+
+esp_moe *open(cudaStream_t s)
+{
+    esp_moe *m = nullptr;
+    if (esp_moe_create(&m, 0, s) != ESP_OK)
+        fault("create");
+    return m;
+}
+
+// Work space grows with T.
+esp_status route(esp_moe *m, int64_t T)
+{
+    static int32_t idx[1];
+    static float weight[1], logits[1];
+    static int64_t counts[1];
+    const esp_moe_gate gate = {ESP_MOE_SOFTMAX, 1, 1.0f};
+    return esp_moe_route(m, &gate, ESP_MOE_F32, T, 8, 1, 8, logits, nullptr, nullptr, idx, weight, counts, nullptr,
+                         nullptr, nullptr);
+}
+
+void want(esp_status got, esp_status expected, const char *what)
+{
+    if (got != expected)
+        fault(std::string(what) + ": status " + std::to_string((int)got));
+}
+
+// A graph is captured, then a larger call makes the work space grow: the graph's block stays.
+void graph_keeps_its_block()
+{
+    cudaStream_t s = new_stream();
+    esp_moe *m = open(s);
+    want(route(m, 10), ESP_OK, "small call");
+    of(s).capturing = true;
+    want(route(m, 10), ESP_OK, "captured call");
+    of(s).capturing = false;
+    want(route(m, 1000), ESP_OK, "larger call");
+    of(s).capturing = true;
+    want(route(m, 1000), ESP_OK, "captured larger call");
+    of(s).capturing = false;
+    want(route(m, 5000), ESP_OK, "largest call");
+    want(route(m, 9000), ESP_OK, "larger still");   // a block that no graph names goes at once
+    if (memory.size() != 4)                         // the error word and counters, two kept, the present one
+        fault("blocks alive: " + std::to_string(memory.size()));
+    in_graph.clear();                               // the graphs end before the handle
+    esp_moe_destroy(m);
+    if (!memory.empty())
+        fault("memory left after the handle's end");
+}
+
+const std::map<std::string, void (*)()> checks = {
+    {"graph_keeps_its_block", graph_keeps_its_block},
+};
+
+}  // namespace
+
+int main(int argc, char **argv)
+{
+    const auto it = argc == 2 ? checks.find(argv[1]) : checks.end();
+    if (it == checks.end()) {
+        for (const auto &c : checks)
+            printf("%s\n", c.first.c_str());
+        return 2;
+    }
+    it->second();
+    for (const std::string &f : faults)
+        printf("%s\n", f.c_str());
+    for (Stream *s : streams)
+        delete s;
+    if (faults.empty())
+        printf("ok\n");
+    return faults.empty() ? 0 : 1;
+}

@@ -1,0 +1,37 @@
+"""The expert layer's handle against a fake CUDA runtime (no GPU): work space under captured graphs, the order of work
+across streams, refusals that leave the handle usable (tests/moe_handle_driver.cpp)."""
+
+import os
+import subprocess
+
+import pytest
+
+from paper_2608_07971_gb300 import build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+CHECKS = [
+    "graph_keeps_its_block",
+]
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("moe_handle") / "driver")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(build.nvcc()))), "include")
+    subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-I", build.INCLUDE, "-I", build.CSRC, "-I", cuda, "-x", "c++",
+                    os.path.join(build.CSRC, "esp_moe.cu"), os.path.join(HERE, "moe_handle_driver.cpp"), "-o", out],
+                   check=True, capture_output=True, text=True)
+    return out
+
+
+def test_every_check_is_listed(driver):
+    res = subprocess.run([driver], capture_output=True, text=True)
+    assert res.returncode == 2 and res.stdout.split() == sorted(CHECKS)
+
+
+@pytest.mark.parametrize("name", CHECKS)
+def test_handle(driver, name):
+    res = subprocess.run([driver, name], capture_output=True, text=True)
+    assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr

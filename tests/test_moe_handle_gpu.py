@@ -1,0 +1,50 @@
+"""Handles of the expert layer on the GPU: captured graphs beside direct calls, streams, work space."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def moe():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2608_07971_gb300 import build, moe
+    build.build()
+    return moe
+
+
+def test_graph_outlives_growing_work_space(moe):
+    """A step captured for a few tokens replays with the same results after calls that need far more work space."""
+    m = moe.Moe()
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, z = torch.randn(150, 2048, generator=g, device="cuda").bfloat16(), torch.randn(150, 16, generator=g, device="cuda")
+    q = m.quantize_weight(torch.randn(16, 256, 2048, generator=g, device="cuda"))
+    r, y = m.routing(150, 16, 4), torch.empty(600, 256, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        m.route(z, 4, out=r)
+        m.linear(x, q, offsets=r.offsets, rows=r.rows, out=y)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    want = (y.clone(), r.pos.clone())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for T in (3000, 20000):
+        big = m.route(torch.randn(T, 16, generator=g, device="cuda"), 4)
+        m.linear(torch.randn(T, 2048, generator=g, device="cuda"), q, offsets=big.offsets, rows=big.rows)
+        fill = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")   # memory that was freed is used again
+        y.zero_()
+        r.pos.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(r.pos, want[1]) and bool((fill == 255).all())
+    m.synchronize()
+    del graph
+    m.close()
