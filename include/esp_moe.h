@@ -19,15 +19,14 @@
  * boundary; every data pointer here is a CUDA device pointer on the handle's device, owned by the
  * caller; a handle is used by one host thread at a time and all its work runs on its stream, queued
  * without waiting. Work space belongs to the handle and grows when a call needs more than any
- * earlier one (ESP_ERR_OOM if there is none; growing waits for the handle's stream, so a program
- * that captures its calls in a CUDA graph makes each once before). Work space that a captured call
- * uses lives as long as the handle, also where later calls outgrow it: a graph may be replayed
- * until the handle is destroyed. Logits, rows and weights are fp32, bf16 or fp16 (esp_moe_dtype)
- * with any alignment of their elements' size; a leading dimension ("ld") counts elements between
- * rows and is at least the row's length. Sums, softmax statistics and products accumulate in fp32;
- * results in a 16-bit type are rounded once. Zero tokens or rows do nothing beyond writing empty
- * counts, offsets, losses and gradients. Results are the same from run to run (no floating-point
- * atomics).
+ * earlier one (ESP_ERR_OOM if there is none; growing waits for the handle's stream, except in a
+ * call that is being captured into a CUDA graph). Work space that captured calls use lives as long
+ * as the handle, also where later calls outgrow it: a graph may be replayed until the handle is
+ * destroyed. Logits, rows and weights are fp32, bf16 or fp16 (esp_moe_dtype) with any alignment of
+ * their elements' size; a leading dimension ("ld") counts elements between rows and is at least the
+ * row's length. Sums, softmax statistics and products accumulate in fp32; results in a 16-bit type
+ * are rounded once. Zero tokens or rows do nothing beyond writing empty counts, offsets, losses and
+ * gradients. Results are the same from run to run (no floating-point atomics).
  */
 #ifndef ESP_MOE_H
 #define ESP_MOE_H

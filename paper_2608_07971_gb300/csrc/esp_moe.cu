@@ -53,16 +53,30 @@ esp_status begin(esp_moe *m)
     return ESP_OK;
 }
 
+// While one lives, its thread's allocations are neither forbidden by a capture, of this stream or another, nor end it.
+class BesideCaptures {
+public:
+    BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+    ~BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode_); }
+    BesideCaptures(const BesideCaptures &) = delete;
+    BesideCaptures &operator=(const BesideCaptures &) = delete;
+
+private:
+    cudaStreamCaptureMode mode_ = cudaStreamCaptureModeRelaxed;
+};
+
 // At least `bytes` of work space. A larger block replaces the old one, which is freed once the queued work is done
-// with it, or kept as long as the handle where a captured graph names it.
+// with it, or kept as long as the handle: where a captured graph names it, or where the stream is being captured
+// and cannot be waited for.
 esp_status reserve(esp_moe *m, size_t bytes)
 {
     if (bytes <= m->ws_bytes) {
         m->ws_captured = m->ws_captured || m->in_capture;
         return ESP_OK;
     }
+    const BesideCaptures beside;
     if (m->ws) {
-        if (m->ws_captured) {
+        if (m->ws_captured || m->in_capture) {
             esp_moe::Kept *k = new (std::nothrow) esp_moe::Kept{m->ws, m->kept};
             if (!k)
                 return ESP_ERR_OOM;

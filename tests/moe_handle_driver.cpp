@@ -37,7 +37,7 @@ std::set<int> finished;                  // work that the host has waited for
 std::map<const void *, size_t> memory;   // live blocks
 std::set<const void *> in_graph;         // blocks that captured work names
 std::vector<std::string> faults;
-int syncs_while_capturing = 0, allocations_while_capturing = 0;
+cudaStreamCaptureMode mode = cudaStreamCaptureModeGlobal;   // of the calling thread
 
 void fault(const std::string &what)
 {
@@ -109,8 +109,7 @@ cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr a, int)
 }
 cudaError_t cudaMalloc(void **p, size_t n)
 {
-    if (any_capturing()) {
-        ++allocations_while_capturing;
+    if (any_capturing() && mode != cudaStreamCaptureModeRelaxed) {
         for (Stream *s : streams)
             s->broken = s->broken || s->capturing;
         return cudaErrorStreamCaptureUnsupported;
@@ -121,6 +120,11 @@ cudaError_t cudaMalloc(void **p, size_t n)
 }
 cudaError_t cudaFree(void *p)
 {
+    if (any_capturing() && mode != cudaStreamCaptureModeRelaxed) {
+        for (Stream *s : streams)
+            s->broken = s->broken || s->capturing;
+        return cudaErrorStreamCaptureUnsupported;
+    }
     if (in_graph.count(p))
         fault("memory that a captured graph names is freed");
     if (!memory.erase(p))
@@ -143,7 +147,6 @@ cudaError_t cudaMemcpy(void *d, const void *s, size_t n, cudaMemcpyKind)
 cudaError_t cudaStreamSynchronize(cudaStream_t s)
 {
     if (of(s).capturing) {
-        ++syncs_while_capturing;
         of(s).broken = true;
         return cudaErrorStreamCaptureUnsupported;
     }
@@ -153,6 +156,11 @@ cudaError_t cudaStreamSynchronize(cudaStream_t s)
 cudaError_t cudaStreamIsCapturing(cudaStream_t s, cudaStreamCaptureStatus *st)
 {
     *st = of(s).capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+    return cudaSuccess;
+}
+cudaError_t cudaThreadExchangeStreamCaptureMode(cudaStreamCaptureMode *m)
+{
+    std::swap(mode, *m);
     return cudaSuccess;
 }
 cudaError_t cudaEventCreateWithFlags(cudaEvent_t *e, unsigned int)
@@ -261,7 +269,36 @@ void graph_keeps_its_block()
         fault("memory left after the handle's end");
 }
 
+// A captured call that needs more work space gets it without touching the capture or the block in use.
+void growing_while_captured()
+{
+    for (int64_t before : {0, 10}) {
+        cudaStream_t s = new_stream();
+        esp_moe *m = open(s);
+        if (before)
+            want(route(m, before), ESP_OK, "call before");
+        of(s).capturing = true;
+        want(route(m, 1000), ESP_OK, "captured call that grows");
+        want(route(m, 3000), ESP_OK, "captured call that grows again");
+        if (of(s).broken)
+            fault("the capture is broken");
+        of(s).capturing = false;
+        want(route(m, 9000), ESP_OK, "call after");
+        cudaStream_t other = new_stream();   // a capture that is not the handle's
+        of(other).capturing = true;
+        want(route(m, 20000), ESP_OK, "call beside a capture");
+        if (of(other).broken)
+            fault("the other capture is broken");
+        of(other).capturing = false;
+        if (mode != cudaStreamCaptureModeGlobal)
+            fault("the thread's capture mode is left changed");
+        in_graph.clear();
+        esp_moe_destroy(m);
+    }
+}
+
 const std::map<std::string, void (*)()> checks = {
+    {"growing_while_captured", growing_while_captured},
     {"graph_keeps_its_block", graph_keeps_its_block},
 };
 

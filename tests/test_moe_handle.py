@@ -1,5 +1,5 @@
 """The expert layer's handle against a fake CUDA runtime (no GPU): work space under captured graphs, the order of work
-across streams, refusals that leave the handle usable (tests/moe_handle_driver.cpp)."""
+across streams (tests/moe_handle_driver.cpp)."""
 
 import os
 import subprocess
@@ -11,6 +11,7 @@ from paper_2608_07971_gb300 import build
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 CHECKS = [
+    "growing_while_captured",
     "graph_keeps_its_block",
 ]
 

@@ -48,3 +48,32 @@ def test_graph_outlives_growing_work_space(moe):
     m.synchronize()
     del graph
     m.close()
+
+
+def test_captured_call_that_needs_more_work_space(moe):
+    """It gets it; the capture, its graph and the handle go on."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z, big = torch.randn(700, 32, generator=g, device="cuda"), torch.randn(30000, 32, generator=g, device="cuda")
+    other = moe.Moe()
+    want, want_big = other.route(z, 3), other.route(big, 3)
+    for first in (False, True):
+        m = moe.Moe()
+        r, rb = m.routing(700, 32, 3), m.routing(30000, 32, 3)
+        if first:
+            m.route(z, 3, out=r)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            m.route(z, 3, out=r)
+            m.route(big, 3, out=rb)
+        m.route(torch.randn(90000, 32, device="cuda"), 3)
+        r.rows.zero_()
+        rb.rows.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(r.rows, want.rows) and torch.equal(r.weight, want.weight)
+        assert torch.equal(rb.rows, want_big.rows) and torch.equal(rb.pos, want_big.pos)
+        m.synchronize()
+        del graph
+        m.close()
+    other.close()
