@@ -77,9 +77,12 @@ typedef struct {
  * ESP_ERR_OOM, ESP_ERR_CUDA. */
 esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream);
 
-/* Later calls run on `cuda_stream`, after what the handle queued on the stream it leaves (which must
- * still exist). While either stream is being captured into a graph no such order is added: the program
- * orders the graph's launches after the handle's other work, as they share its work space. */
+/* Later calls run on `cuda_stream`, after what the handle queued on the streams before (the one it
+ * leaves must still exist). Captured calls have no part in that order: the program orders a graph's
+ * launches, and the branches inside one, with the handle's other work, as they share its work space.
+ * Errors: ESP_ERR_STATE, with the handle and its stream as they were, where the order cannot be had: the
+ * stream it leaves is being captured and took the handle's work before its capture began (a call on a
+ * stream whose own capture has ended is refused likewise while that one's runs). */
 esp_status esp_moe_set_stream(esp_moe *m, void *cuda_stream);
 
 /* Routes T tokens over E experts (logits T x E). An expert can be chosen if profit = logit - price
@@ -161,9 +164,11 @@ esp_status esp_moe_combine_backward(esp_moe *m, int32_t dtype, int64_t T, int32_
                                     const void *dout, int64_t ldy, const void *y, const int32_t *pos,
                                     const float *weight, int64_t lddy, void *dy, float *dweight);
 
-/* Waits for the handle's stream and reports a device-side failure of the queued work: ESP_ERR_TIMEOUT
+/* Waits for the handle's work on all streams (not for graphs that the program launches: it waits for
+ * those itself first) and reports a device-side failure of the queued work: ESP_ERR_TIMEOUT
  * when a bounded wait of a product kernel gave up (its results are then undefined and the handle
- * refuses further work with ESP_ERR_STATE), ESP_ERR_CUDA on a CUDA error. */
+ * refuses further work with ESP_ERR_STATE), ESP_ERR_CUDA on a CUDA error, ESP_ERR_STATE while the
+ * handle's stream is being captured (the handle stays usable). */
 esp_status esp_moe_synchronize(esp_moe *m);
 
 /* Kernel launches of the handle's last call. */

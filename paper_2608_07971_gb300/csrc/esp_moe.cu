@@ -38,19 +38,48 @@ bool capturing(cudaStream_t s)
     return status != cudaStreamCaptureStatusNone;
 }
 
-// Common head of every call: the handle, its device current, no launches yet.
-esp_status begin(esp_moe *m)
+// The handle, its device current.
+esp_status check(esp_moe *m)
 {
     if (!m)
         return ESP_ERR_INVALID_ARG;
     if (m->poisoned)
         return ESP_ERR_STATE;
-    m->launches = 0;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || (dev != m->device && cudaSetDevice(m->device) != cudaSuccess))
         return fail(m);
-    m->in_capture = capturing(m->stream);
     return ESP_OK;
+}
+
+// Orders what comes next on the handle's stream, which is not being captured, after all of the handle's earlier work
+// that was not captured: it shares the work space. A stream whose capture began after such work, and still runs,
+// cannot be waited for.
+esp_status join_earlier(esp_moe *m)
+{
+    if (m->has_direct && m->direct != m->stream) {
+        if (!m->marked) {
+            if (capturing(m->direct))
+                return ESP_ERR_STATE;
+            MOE_CUDA(cudaEventRecord(m->handoff, m->direct));
+            m->marked = true;
+        }
+        MOE_CUDA(cudaStreamWaitEvent(m->stream, m->handoff, 0));
+    }
+    m->direct = m->stream;
+    m->has_direct = true;
+    m->marked = false;
+    return ESP_OK;
+}
+
+// Common head of every call that queues work: its place among the earlier ones, no launches yet.
+esp_status begin(esp_moe *m)
+{
+    const esp_status st = check(m);
+    if (st != ESP_OK)
+        return st;
+    m->launches = 0;
+    m->in_capture = capturing(m->stream);
+    return m->in_capture ? ESP_OK : join_earlier(m);
 }
 
 // While one lives, its thread's allocations are neither forbidden by a capture, of this stream or another, nor end it.
@@ -204,19 +233,21 @@ esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream)
 
 esp_status esp_moe_set_stream(esp_moe *m, void *cuda_stream)
 {
-    const esp_status st = begin(m);
+    esp_status st = check(m);
     if (st != ESP_OK)
         return st;
-    const cudaStream_t next = static_cast<cudaStream_t>(cuda_stream);
-    if (next != m->stream) {
-        // an event cannot order a stream that is being captured after one that is not
-        if (!capturing(next) && !capturing(m->stream)) {
-            MOE_CUDA(cudaEventRecord(m->handoff, m->stream));
-            MOE_CUDA(cudaStreamWaitEvent(next, m->handoff, 0));
-        }
-        m->stream = next;
+    const cudaStream_t next = static_cast<cudaStream_t>(cuda_stream), left = m->stream;
+    if (next == left)
+        return ESP_OK;
+    // an event cannot order a stream that is being captured after one that is not, or the other way round
+    if (m->has_direct && m->direct == left && !m->marked && !capturing(left)) {
+        MOE_CUDA(cudaEventRecord(m->handoff, left));
+        m->marked = true;
     }
-    return ESP_OK;
+    m->stream = next;
+    if (!capturing(next) && (st = join_earlier(m)) != ESP_OK)
+        m->stream = left;
+    return st;
 }
 
 esp_status esp_moe_route(esp_moe *m, const esp_moe_gate *gate, int32_t dtype, int64_t T, int32_t E, int32_t k,
@@ -488,8 +519,12 @@ esp_status esp_moe_combine_backward(esp_moe *m, int32_t dtype, int64_t T, int32_
 
 esp_status esp_moe_synchronize(esp_moe *m)
 {
-    const esp_status st = begin(m);
+    esp_status st = check(m);
     if (st != ESP_OK)
+        return st;
+    if (capturing(m->stream))
+        return ESP_ERR_STATE;
+    if ((st = join_earlier(m)) != ESP_OK)
         return st;
     MOE_CUDA(cudaStreamSynchronize(m->stream));
     unsigned int err = 0;
@@ -511,7 +546,7 @@ esp_status esp_moe_last_launch_count(esp_moe *m, int64_t *out)
 
 esp_status esp_moe_debug_set_wait_limit(esp_moe *m, uint32_t limit_ms)
 {
-    const esp_status st = begin(m);
+    const esp_status st = check(m);
     if (st != ESP_OK)
         return st;
     m->wait_ms = limit_ms == 0 ? kMoeWaitMs : limit_ms;
@@ -520,7 +555,7 @@ esp_status esp_moe_debug_set_wait_limit(esp_moe *m, uint32_t limit_ms)
 
 esp_status esp_moe_debug_hold_load(esp_moe *m)
 {
-    const esp_status st = begin(m);
+    const esp_status st = check(m);
     if (st != ESP_OK)
         return st;
     m->hold_load = true;

@@ -13,7 +13,11 @@ constexpr uint32_t kMoeWaitMs = 4000;   // a bounded wait's limit
 struct esp_moe {
     int device = 0;
     cudaStream_t stream = nullptr;
-    cudaEvent_t handoff = nullptr;   // orders a new stream after the one the handle leaves
+    // the stream that took the last work that is not captured (null as a stream means the legacy one: has_direct),
+    // and the event that orders others after it (recorded there since, where marked is set)
+    cudaStream_t direct = nullptr;
+    bool has_direct = false, marked = false;
+    cudaEvent_t handoff = nullptr;
     int sm_count = 0;
     bool poisoned = false;
     int64_t launches = 0;

@@ -297,9 +297,76 @@ void growing_while_captured()
     }
 }
 
+// Work before a capture and work after it share the work space in order, whichever stream comes after.
+void order_across_a_capture()
+{
+    for (int stay = 0; stay < 2; ++stay) {
+        cudaStream_t a = new_stream(), b = new_stream(), c = new_stream();
+        esp_moe *m = open(a);
+        want(route(m, 10), ESP_OK, "call");
+        of(b).capturing = true;
+        want(esp_moe_set_stream(m, b), ESP_OK, "to the captured stream");
+        want(route(m, 10), ESP_OK, "captured call");
+        of(b).capturing = false;
+        if (!stay)
+            want(esp_moe_set_stream(m, c), ESP_OK, "to another stream");
+        want(route(m, 10), ESP_OK, "call after");
+        want(esp_moe_set_stream(m, a), ESP_OK, "back");
+        want(route(m, 10), ESP_OK, "last call");
+        in_graph.clear();
+        esp_moe_destroy(m);
+    }
+}
+
+// A capture that began on the handle's own stream, after work of the handle there: no order can be had until it ends.
+void order_after_a_capture_in_place()
+{
+    cudaStream_t a = new_stream(), b = new_stream();
+    esp_moe *m = open(a);
+    want(route(m, 10), ESP_OK, "call");
+    of(a).capturing = true;
+    want(route(m, 10), ESP_OK, "captured call");
+    want(esp_moe_set_stream(m, b), ESP_ERR_STATE, "to another stream during the capture");
+    want(route(m, 10), ESP_OK, "captured call after the refusal");
+    of(b).capturing = true;
+    want(esp_moe_set_stream(m, b), ESP_OK, "to a captured stream");
+    want(route(m, 10), ESP_OK, "call captured there");
+    of(b).capturing = false;
+    want(route(m, 10), ESP_ERR_STATE, "a call there that nothing orders");
+    of(a).capturing = false;
+    if (of(a).broken || of(b).broken)
+        fault("a capture is broken");
+    want(route(m, 10), ESP_OK, "call after");
+    in_graph.clear();
+    esp_moe_destroy(m);
+}
+
+// Waiting for the handle reaches work on the stream before a capture, and is refused during one.
+void synchronize_across_a_capture()
+{
+    cudaStream_t a = new_stream(), b = new_stream();
+    esp_moe *m = open(a);
+    want(route(m, 10), ESP_OK, "call");
+    of(b).capturing = true;
+    want(esp_moe_set_stream(m, b), ESP_OK, "to the captured stream");
+    want(route(m, 10), ESP_OK, "captured call");
+    want(esp_moe_synchronize(m), ESP_ERR_STATE, "waiting during the capture");
+    if (of(b).broken)
+        fault("the capture is broken");
+    of(b).capturing = false;
+    want(esp_moe_synchronize(m), ESP_OK, "waiting");
+    if (!finished.count(0))
+        fault("work before the capture was not waited for");
+    in_graph.clear();
+    esp_moe_destroy(m);
+}
+
 const std::map<std::string, void (*)()> checks = {
     {"growing_while_captured", growing_while_captured},
     {"graph_keeps_its_block", graph_keeps_its_block},
+    {"order_across_a_capture", order_across_a_capture},
+    {"order_after_a_capture_in_place", order_after_a_capture_in_place},
+    {"synchronize_across_a_capture", synchronize_across_a_capture},
 };
 
 }  // namespace

@@ -11,8 +11,11 @@ from paper_2608_07971_gb300 import build
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 CHECKS = [
-    "growing_while_captured",
     "graph_keeps_its_block",
+    "growing_while_captured",
+    "order_across_a_capture",
+    "order_after_a_capture_in_place",
+    "synchronize_across_a_capture",
 ]
 
 

@@ -77,3 +77,41 @@ def test_captured_call_that_needs_more_work_space(moe):
         del graph
         m.close()
     other.close()
+
+
+def test_order_across_a_capture(moe):
+    """Work on one stream, a capture on a second, work on a third, with no wait of the program's: the calls that are
+    not captured share the work space one after the other."""
+    m, other = moe.Moe(), moe.Moe()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, y, z = (torch.randn(n, 64, generator=g, device="cuda") for n in (40000, 500, 30000))
+    want = [other.route(v, 4) for v in (x, y, z)]
+    a, b, c = (torch.cuda.Stream() for _ in range(3))
+    r = [m.routing(v.shape[0], 64, 4) for v in (x, y, z)]
+    for v, out in zip((x, y, z), r):
+        m.route(v, 4, out=out)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for out in r:
+            for t in (out.rows, out.pos, out.counts):
+                t.zero_()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(a):
+            torch.cuda._sleep(20_000_000)
+            m.route(x, 4, out=r[0])
+        with torch.cuda.stream(b):
+            graph.capture_begin()
+            m.route(y, 4, out=r[1])
+            graph.capture_end()
+        with torch.cuda.stream(c):
+            m.route(z, 4, out=r[2])
+        m.synchronize()
+        for i in (0, 2):
+            assert torch.equal(r[i].rows, want[i].rows) and torch.equal(r[i].pos, want[i].pos)
+            assert torch.equal(r[i].counts, want[i].counts)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(r[1].rows, want[1].rows)
+    m.close()
+    other.close()
