@@ -900,7 +900,7 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const
 {
     using S = Shape<CG, BN>;
     auto kernel = k_gemm<CG, BN, COLS, T>;
-    cudaError_t e = allow_smem<k_gemm<CG, BN, COLS, T>>(S::kSmem, m->device);
+    cudaError_t e = allow_smem<k_gemm<CG, BN, COLS, T>, S::kSmem>(m->device);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};

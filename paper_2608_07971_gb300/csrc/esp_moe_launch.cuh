@@ -1,7 +1,7 @@
 // Launches of the expert layer's kernels. Every one is a dependent launch: it starts while the kernel before
 // it on the stream still runs (once all of that one's CTAs have started, where it says so), sets up what
 // needs no global memory, and then waits for it to finish. That hides a microsecond or so of launch latency
-// behind each kernel. And the shared-memory limit of a kernel, raised once.
+// behind each kernel. And the shared-memory limit of a kernel, set once.
 #pragma once
 
 #include <atomic>
@@ -49,18 +49,20 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
-// Lets a kernel use `bytes` of dynamic shared memory on `device` (the call takes about a microsecond, so the
-// largest amount allowed so far is kept per kernel and device).
-template <auto Kernel>
-inline cudaError_t allow_smem(size_t bytes, int device)
+// Lets a kernel use up to Most bytes of dynamic shared memory on `device`: the most that any of its launches asks for,
+// whatever this one does, so that handles of several threads set the same limit. The default limit counts static
+// memory too. Done once per kernel and device (the call takes about a microsecond).
+template <auto Kernel, size_t Most>
+inline cudaError_t allow_smem(int device)
 {
     constexpr int kDevices = 64;
-    static std::atomic<size_t> allowed[kDevices];
-    if (bytes <= 48 * 1024 || (device < kDevices && allowed[device].load() >= bytes))
+    static std::atomic<bool> done[kDevices];
+    if (device < kDevices && done[device].load())
         return cudaSuccess;
-    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(Kernel),
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Most);
     if (e == cudaSuccess && device < kDevices)
-        allowed[device].store(bytes);
+        done[device].store(true);
     return e;
 }
 

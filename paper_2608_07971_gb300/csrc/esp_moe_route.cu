@@ -220,6 +220,19 @@ __device__ __forceinline__ void store_demand(const RouteArgs &a, int64_t i, int 
 template <int VPT>
 constexpr int kRouteThreads = VPT <= 8 ? 1024 : 512;
 
+// Bytes of dynamic shared memory of k_route and of k_balance for E experts; E is at most 32 VPT.
+template <int VPT>
+constexpr size_t route_smem(int E)
+{
+    return (size_t)(32 * VPT + (kRouteThreads<VPT> / 32 + 2) * E + 1) * sizeof(int);
+}
+
+template <int VPT>
+constexpr size_t balance_smem(int E)
+{
+    return ((size_t)kRouteThreads<VPT> * VPT + E) * sizeof(float);
+}
+
 // A lane's values in descending order of key, equal keys in their order (Batcher's odd-even merge sort), so
 // that a round of the choice looks at the lanes' first values only; packed: the sorted values' places
 // before, four bits each, the first in the lowest.
@@ -957,20 +970,21 @@ cudaError_t launch_route(esp_moe *m, int32_t dtype, const RouteArgs &args)
             using S = RowShape<T, VPT>;
             const bool aligned = rows_aligned(a.logits, a.ld, sizeof(T), S::V * sizeof(T));
             constexpr int kThr = kRouteThreads<VPT>;
-            const size_t route_smem = (size_t)(32 * VPT + (kThr / 32 + 2) * a.E + 1) * sizeof(int);
+            const size_t smem = route_smem<VPT>(a.E);
+            constexpr size_t kMost = route_smem<VPT>(32 * VPT);
             if (fused(a.T, a.k)) {
-                const cudaError_t e = allow_smem<k_route<T, VPT, true>>(route_smem, m->device);
+                const cudaError_t e = allow_smem<k_route<T, VPT, true>, kMost>(m->device);
                 if (e != cudaSuccess)
                     return e;
                 const int warps = std::min(kThr / 32, std::max(4, (int)a.T));
                 m->launches += 1;
-                return launch_after(k_route<T, VPT, true>, dim3(1), 32 * warps, route_smem, m->stream, a, a.T, aligned);
+                return launch_after(k_route<T, VPT, true>, dim3(1), 32 * warps, smem, m->stream, a, a.T, aligned);
             }
             const int64_t chunk = route_chunk(a.T);
             const int nb = (int)ceil_div(a.T, chunk);
-            cudaError_t e = allow_smem<k_route<T, VPT, false>>(route_smem, m->device);
+            cudaError_t e = allow_smem<k_route<T, VPT, false>, kMost>(m->device);
             if (e == cudaSuccess)
-                e = launch_after(k_route<T, VPT, false>, dim3((unsigned)nb), kThr, route_smem, m->stream, a, chunk, aligned);
+                e = launch_after(k_route<T, VPT, false>, dim3((unsigned)nb), kThr, smem, m->stream, a, chunk, aligned);
             if (e != cudaSuccess)
                 return e;
             m->launches += 2;
@@ -995,8 +1009,8 @@ cudaError_t launch_balance(esp_moe *m, int32_t dtype, const BalanceArgs &a)
                 constexpr int VPT = decltype(vpt)::value;
                 using S = RowShape<T, VPT>;
                 constexpr int kThr = kRouteThreads<VPT>;
-                const size_t smem = ((size_t)kThr * VPT + a.E) * sizeof(float);
-                const cudaError_t e2 = allow_smem<k_balance<T, VPT>>(smem, m->device);
+                const size_t smem = balance_smem<VPT>(a.E);
+                const cudaError_t e2 = allow_smem<k_balance<T, VPT>, balance_smem<VPT>(32 * VPT)>(m->device);
                 if (e2 != cudaSuccess)
                     return e2;
                 m->launches += 1;

@@ -1,5 +1,5 @@
 """The expert layer's handle against a fake CUDA runtime (no GPU): work space under captured graphs, the order of work
-across streams (tests/moe_handle_driver.cpp)."""
+across streams (tests/moe_handle_driver.cpp), kernels' shared-memory limits (tests/moe_smem_driver.cpp)."""
 
 import os
 import subprocess
@@ -19,15 +19,18 @@ CHECKS = [
 ]
 
 
-@pytest.fixture(scope="module")
-def driver(tmp_path_factory):
-    out = str(tmp_path_factory.mktemp("moe_handle") / "driver")
+def compiled(out, *sources):
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(build.nvcc()))), "include")
     subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
-                    "-I", build.INCLUDE, "-I", build.CSRC, "-I", cuda, "-x", "c++",
-                    os.path.join(build.CSRC, "esp_moe.cu"), os.path.join(HERE, "moe_handle_driver.cpp"), "-o", out],
+                    "-I", build.INCLUDE, "-I", build.CSRC, "-I", cuda, "-x", "c++", *sources, "-o", out, "-lpthread"],
                    check=True, capture_output=True, text=True)
     return out
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    return compiled(str(tmp_path_factory.mktemp("moe_handle") / "driver"), os.path.join(build.CSRC, "esp_moe.cu"),
+                    os.path.join(HERE, "moe_handle_driver.cpp"))
 
 
 def test_every_check_is_listed(driver):
@@ -38,4 +41,11 @@ def test_every_check_is_listed(driver):
 @pytest.mark.parametrize("name", CHECKS)
 def test_handle(driver, name):
     res = subprocess.run([driver, name], capture_output=True, text=True)
+    assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
+
+
+def test_shared_memory_limit(tmp_path):
+    """One limit per kernel, its greatest, also where two threads set it at once."""
+    out = compiled(str(tmp_path / "driver"), os.path.join(HERE, "moe_smem_driver.cpp"))
+    res = subprocess.run([out], capture_output=True, text=True, timeout=60)
     assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr

@@ -1,6 +1,12 @@
 """Handles of the expert layer on the GPU: captured graphs beside direct calls, streams, work space."""
 
+import os
+import subprocess
+import sys
+
 import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 torch = pytest.importorskip("torch")
 
@@ -115,3 +121,25 @@ def test_order_across_a_capture(moe):
         assert torch.equal(r[1].rows, want[1].rows)
     m.close()
     other.close()
+
+
+def test_first_call_at_the_default_shared_memory_limit(moe):
+    """In a process of their own, the sizes whose dynamic shared memory alone would fit the default limit: static
+    memory counts too (625 experts: 49,100 bytes and 64)."""
+    code = """
+import torch
+from paper_2608_07971_gb300 import moe
+m = moe.Moe()
+for E in (624, 625, 626, 1024, 625):
+    for dt in (torch.float32, torch.bfloat16, torch.float16):
+        z = torch.randn(4, E, device="cuda").to(dt)
+        r = m.route(z, 2)
+        assert torch.equal(r.idx.long(), torch.sort(z, dim=1, descending=True, stable=True)[1][:, :2]), (E, dt)
+        z = torch.randn(600, E, device="cuda").to(dt)
+        b = m.balance(z, m.route(z, 2).idx)
+        assert int(b.counts.sum()) == 1200
+m.synchronize()
+print("ok")
+"""
+    res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=200)
+    assert res.returncode == 0 and res.stdout.strip() == "ok", res.stdout + res.stderr
