@@ -16,6 +16,7 @@ uses the handle's work space, so the handle is kept as long as the graph is repl
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 from typing import Optional, Tuple
@@ -169,7 +170,13 @@ def _ptr(t):
 
 
 class Moe:
-    """One esp_moe handle."""
+    """One esp_moe handle.
+
+    With a ``stream`` of its own all of a call's work is queued there: kernels, fills, copies, and the allocation of
+    results, which belong to that stream in torch's sense. As with any side stream the program orders its inputs before
+    the call and its use of the results after it (``synchronize``, or events), and calls ``record_stream`` where a
+    tensor is freed on one stream while the other still uses it.
+    """
 
     def __init__(self, device=None, stream: Optional[int] = None):
         self.h = None
@@ -186,8 +193,20 @@ class Moe:
         h = ctypes.c_void_p()
         esp._check(self._lib.esp_moe_create(ctypes.byref(h), self.device.index, self._stream or None), "esp_moe_create")
         self.h = h.value
+        self._side = None   # torch's view of a stream of the handle's own
+        if not self._follow:
+            self._side = self._torch_stream(self._stream)
 
     # -- helpers
+
+    def _torch_stream(self, stream: int):
+        if stream == 0:
+            return torch.cuda.default_stream(self.device)
+        return torch.cuda.ExternalStream(stream, device=self.device)
+
+    def _queue(self):
+        """Context in which torch allocates and queues on the handle's stream."""
+        return contextlib.nullcontext() if self._side is None else torch.cuda.stream(self._side)
 
     def _on_stream(self):
         if self.h is None:
@@ -201,6 +220,8 @@ class Moe:
         """Later calls run on the cudaStream_t `stream`, after what was queued before."""
         esp._check(self._lib.esp_moe_set_stream(self.h, stream or None), "esp_moe_set_stream")
         self._stream = stream
+        if not self._follow:
+            self._side = self._torch_stream(stream)
 
     def _need(self, t, name: str, dtype=None, shape=None, optional: bool = False):
         """Checks a dense argument: its device, type, shape."""
@@ -241,7 +262,10 @@ class Moe:
         return code, step if n > 1 else m
 
     def _new(self, shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=self.device)
+        if self._side is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with self._queue():
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     # -- router
 
@@ -377,15 +401,16 @@ class Moe:
         E, N, K = codes.shape
         self._need(codes, "codes", torch.float8_e4m3fn)
         self._need(scale, "scale", torch.float32, (E, -(-N // BLOCK), -(-K // BLOCK)))
-        if K % 16 == 0 and codes.is_contiguous() and codes.data_ptr() % 16 == 0:
-            q = codes.view(torch.uint8)
-        else:
-            q = torch.zeros((E, N, _pad16(K)), dtype=torch.uint8, device=self.device)
-            q[:, :, :K] = codes.view(torch.uint8)
-        qt = None
-        if transposed:
-            qt = torch.zeros((E, K, _pad16(N)), dtype=torch.uint8, device=self.device)
-            qt[:, :, :N] = q[:, :, :K].transpose(1, 2)
+        with self._queue():
+            if K % 16 == 0 and codes.is_contiguous() and codes.data_ptr() % 16 == 0:
+                q = codes.view(torch.uint8)
+            else:
+                q = torch.zeros((E, N, _pad16(K)), dtype=torch.uint8, device=self.device)
+                q[:, :, :K] = codes.view(torch.uint8)
+            qt = None
+            if transposed:
+                qt = torch.zeros((E, K, _pad16(N)), dtype=torch.uint8, device=self.device)
+                qt[:, :, :N] = q[:, :, :K].transpose(1, 2)
         return Weight(E, N, K, q, scale, qt)
 
     def _rows(self, x, weight: Weight, offsets, rows):
@@ -468,7 +493,8 @@ class Moe:
         self._need(weight, "weight", torch.float32, (T, k), optional=True)
         dy, dweight = out
         if dy is None:
-            dy = torch.zeros(y.shape, dtype=y.dtype, device=self.device)
+            with self._queue():
+                dy = torch.zeros(y.shape, dtype=y.dtype, device=self.device)
         _, lddy = self._matrix(dy, "dy", y.shape[0], H, y.dtype)
         if dweight is None:
             dweight = self._new((T, k), torch.float32)

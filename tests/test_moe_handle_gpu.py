@@ -143,3 +143,90 @@ print("ok")
 """
     res = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=200)
     assert res.returncode == 0 and res.stdout.strip() == "ok", res.stdout + res.stderr
+
+
+def delayed(stream):
+    """Keeps `stream` busy for some tens of milliseconds."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+
+
+@pytest.mark.parametrize("busy", ["current", "own"])
+def test_handle_with_a_stream_of_its_own(moe, busy):
+    """What its calls allocate, fill and lay out is ordered with its kernels, whatever the caller's current stream is
+    at; results are those of a handle that follows it."""
+    s = torch.cuda.Stream()
+    m, other = moe.Moe(stream=s.cuda_stream), moe.Moe()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    T, k, H = 600, 4, 512
+    y, d = (torch.randn(n, H, generator=g, device="cuda") for n in (T * k, T))
+    pos = torch.randperm(T * k, generator=g, device="cuda").int().view(T, k)
+    pos[::7, 1] = -1
+    w = torch.rand(T, k, generator=g, device="cuda")
+    q = other.quantize_weight(torch.randn(3, 50, 77, generator=g, device="cuda"), transposed=True)
+    codes = q.codes().contiguous()
+    x, off = torch.randn(9, 77, generator=g, device="cuda"), torch.tensor([0, 2, 2, 9], device="cuda").int()
+    dz = torch.randn(9, 50, generator=g, device="cuda")
+
+    def calls(h):
+        v = h.load_weight(codes, q.scale, transposed=True)
+        return (*h.combine_backward(d, y, pos, w), h.linear(x, v, offsets=off), *h.linear_backward(dz, x, v, offsets=off),
+                h.combine(y, pos, w))
+
+    want = calls(other)
+    calls(m)   # kernels are loaded, memory is there
+    m.synchronize()
+    torch.cuda.synchronize()
+    delayed(torch.cuda.current_stream() if busy == "current" else s)
+    got = calls(m)
+    m.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()   # nothing of the calls was left on the current stream
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    m.close()
+    other.close()
+
+
+def test_results_on_a_stream_of_its_own_share_no_memory_in_use(moe):
+    """Memory freed on the current stream, but read there by queued work, is not a result's on another stream; nor the
+    other way round."""
+    s = torch.cuda.Stream()
+    m = moe.Moe(stream=s.cuda_stream)
+    n = 1 << 16
+    y, pos = torch.full((n, 64), 3.0, device="cuda"), torch.arange(n, device="cuda").int().view(-1, 1)
+    a, out = torch.ones(n, 64, device="cuda"), torch.zeros(n, 64, device="cuda")
+    out.copy_(a)
+    m.combine(y, pos)
+    out.zero_()
+    torch.cuda.synchronize()
+    delayed(torch.cuda.current_stream())
+    out.copy_(a)
+    del a
+    r = m.combine(y, pos)
+    m.synchronize()
+    torch.cuda.synchronize()
+    assert bool((out == 1).all()) and bool((r == 3).all())
+    del r
+    torch.cuda.synchronize()
+    delayed(s)
+    r = m.combine(y, pos)
+    del r
+    b = torch.full((n, 64), 5.0, device="cuda")
+    m.synchronize()
+    torch.cuda.synchronize()
+    assert bool((b == 5).all())
+    m.close()
+
+
+def test_own_streams_by_number(moe):
+    """The legacy stream as 0, and set_stream to another one."""
+    z = torch.randn(100, 8, device="cuda")
+    m = moe.Moe(stream=0)
+    want = m.route(z, 2)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    m.set_stream(s.cuda_stream)
+    r = m.route(z, 2)
+    m.synchronize()
+    assert torch.equal(r.rows, want.rows)
+    m.close()
