@@ -1,8 +1,8 @@
 """Price-routed expert layer on torch CUDA tensors: the binding of include/esp_moe.h.
 
 Argument marshalling only: every step runs in the library's CUDA kernels (there is no CPU fallback). ``Moe``
-holds one handle. Its calls are queued on the stream given at creation, or without one on the caller's
-current torch stream at every call; they return without waiting. Every call takes ``out`` to reuse the
+holds one handle. Its calls are queued on the stream given at creation or to ``set_stream``, or without one on the
+caller's current torch stream at every call; they return without waiting. Every call takes ``out`` to reuse the
 tensors of an earlier one (a serving loop, a CUDA graph), else allocates its results. A graph that captured calls
 uses the handle's work space, so the handle is kept as long as the graph is replayed.
 
@@ -214,14 +214,18 @@ class Moe:
         if self._follow:
             s = _raw_stream(self._index)
             if s != self._stream:
-                self.set_stream(s)
+                self._move(s)
 
-    def set_stream(self, stream: int) -> None:
-        """Later calls run on the cudaStream_t `stream`, after what was queued before."""
+    def _move(self, stream: int) -> None:
         esp._check(self._lib.esp_moe_set_stream(self.h, stream or None), "esp_moe_set_stream")
         self._stream = stream
-        if not self._follow:
-            self._side = self._torch_stream(stream)
+
+    def set_stream(self, stream: int) -> None:
+        """Later calls run on the cudaStream_t `stream`, after what was queued before; the handle no longer follows
+        the current stream."""
+        self._move(stream)
+        self._side = self._torch_stream(stream)
+        self._follow = False
 
     def _need(self, t, name: str, dtype=None, shape=None, optional: bool = False):
         """Checks a dense argument: its device, type, shape."""

@@ -230,3 +230,25 @@ def test_own_streams_by_number(moe):
     m.synchronize()
     assert torch.equal(r.rows, want.rows)
     m.close()
+
+
+def test_set_stream_of_a_handle_that_followed(moe):
+    """After set_stream a handle stays on that stream, whatever the current one is."""
+    m, s = moe.Moe(), torch.cuda.Stream()
+    z = torch.randn(5000, 32, device="cuda")
+    want = m.route(z, 4)
+    torch.cuda.synchronize()
+    m.set_stream(s.cuda_stream)
+    out = m.route(z, 4)
+    m.synchronize()
+    delayed(s)
+    busy = torch.cuda.Event()
+    out.rows.zero_()
+    torch.cuda.current_stream().synchronize()
+    r = m.route(z, 4, out=out)   # waits behind the delay
+    busy.record(s)
+    seen = out.rows.cpu()
+    assert not busy.query() and not bool(seen.any())
+    m.synchronize()
+    assert busy.query() and torch.equal(r.rows, want.rows)
+    m.close()
