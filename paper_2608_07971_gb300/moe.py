@@ -103,7 +103,8 @@ class Gate:
 @dataclasses.dataclass(frozen=True)
 class Routing:
     """Results of ``Moe.route``: idx, weight (T, k); counts (E,); rows (T * k,), pos (T, k), offsets (E + 1,)
-    or None without a plan. `checked` holds (device index, T, E, k) where ``Moe.routing`` made the tensors."""
+    or None without a plan. `checked` holds (device index, T, E, k) where ``Moe.routing`` made the tensors; a copy with
+    other tensors (``dataclasses.replace``) starts without it."""
 
     idx: torch.Tensor
     weight: torch.Tensor
@@ -111,19 +112,19 @@ class Routing:
     rows: Optional[torch.Tensor] = None
     pos: Optional[torch.Tensor] = None
     offsets: Optional[torch.Tensor] = None
-    checked: Optional[tuple] = None
+    checked: Optional[tuple] = dataclasses.field(default=None, init=False, repr=False, compare=False)
 
 
 @dataclasses.dataclass(frozen=True)
 class Balance:
     """Results of ``Moe.balance``: loss (2,) = balance, logit; counts (B, E), share (B, E), tokens (B,). `checked`
-    holds (device index, B, E) where ``Moe.balancing`` made the tensors."""
+    holds (device index, B, E) where ``Moe.balancing`` made the tensors; a copy with other tensors starts without it."""
 
     loss: torch.Tensor
     counts: torch.Tensor
     share: torch.Tensor
     tokens: torch.Tensor
-    checked: Optional[tuple] = None
+    checked: Optional[tuple] = dataclasses.field(default=None, init=False, repr=False, compare=False)
 
 
 @dataclasses.dataclass
@@ -278,8 +279,9 @@ class Moe:
         i32, plan_of = torch.int32, (None, None, None)
         if plan:
             plan_of = (self._new((T * k,), i32), self._new((T, k), i32), self._new((E + 1,), i32))
-        return Routing(self._new((T, k), i32), self._new((T, k), torch.float32), self._new((E,), torch.int64), *plan_of,
-                       checked=(self._index, T, E, k))
+        r = Routing(self._new((T, k), i32), self._new((T, k), torch.float32), self._new((E,), torch.int64), *plan_of)
+        object.__setattr__(r, "checked", (self._index, T, E, k))
+        return r
 
     def route(self, logits, k: int, gate: Gate = Gate(), prices=None, valid=None, plan: bool = True,
               out: Optional[Routing] = None) -> Routing:
@@ -308,8 +310,10 @@ class Moe:
 
     def balancing(self, B: int, E: int) -> Balance:
         """Empty results of ``balance``, to pass as its ``out``."""
-        return Balance(self._new((2,), torch.float32), self._new((B, E), torch.int64), self._new((B, E), torch.float32),
-                       self._new((B,), torch.int64), checked=(self._index, B, E))
+        b = Balance(self._new((2,), torch.float32), self._new((B, E), torch.int64), self._new((B, E), torch.float32),
+                    self._new((B,), torch.int64))
+        object.__setattr__(b, "checked", (self._index, B, E))
+        return b
 
     def balance(self, logits, idx, gate: Gate = Gate(), seq_offsets=None, out: Optional[Balance] = None) -> Balance:
         """Balance and logit losses of the choices idx, over the sequences that seq_offsets (B + 1,) int32 bounds

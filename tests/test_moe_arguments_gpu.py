@@ -1,0 +1,53 @@
+"""Results and weights that a program hands back to the expert layer's calls: what was changed is checked and used."""
+
+import dataclasses
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def moe():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2608_07971_gb300 import build, moe
+    build.build()
+    return moe
+
+
+@pytest.fixture(scope="module")
+def m(moe):
+    h = moe.Moe()
+    yield h
+    h.synchronize()
+    h.close()
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32, device="cuda")
+
+
+def test_replaced_results_are_checked(moe, m):
+    z = torch.randn(40, 8, device="cuda")
+    r, b = m.routing(40, 8, 2), m.balancing(1, 8)
+    m.route(z, 2, out=r)
+    # larger than needed, so that nothing is written out of bounds where the check is missing
+    for change in (dict(idx=i32(50, 2)), dict(rows=i32(100)), dict(pos=i32(40, 3)), dict(offsets=i32(10)),
+                   dict(counts=torch.zeros(9, dtype=torch.int64, device="cuda")),
+                   dict(weight=torch.zeros(40, 2, dtype=torch.float64, device="cuda")), dict(rows=i32(80).long())):
+        with pytest.raises(ValueError):
+            m.route(z, 2, out=dataclasses.replace(r, **change))
+    for change in (dict(loss=torch.zeros(3, device="cuda")), dict(share=torch.zeros(2, 8, device="cuda")),
+                   dict(tokens=torch.zeros(2, dtype=torch.int64, device="cuda"))):
+        with pytest.raises(ValueError):
+            m.balance(z, r.idx, out=dataclasses.replace(b, **change))
+    m.balance(z, r.idx, out=b)
+    with pytest.raises(ValueError):
+        m.route_backward(z, r.idx, balance=dataclasses.replace(b, counts=torch.zeros(1, 9, dtype=torch.int64, device="cuda")),
+                         dloss=torch.ones(2, device="cuda"))
+    # good replacements are taken
+    spare = dataclasses.replace(r, rows=i32(80))
+    assert m.route(z, 2, out=spare) is spare and torch.equal(spare.rows, r.rows)
