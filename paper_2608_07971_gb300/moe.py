@@ -297,7 +297,7 @@ class Moe:
             self._need(out.idx, "out.idx", torch.int32, (T, k))
             self._need(out.weight, "out.weight", torch.float32, (T, k))
             self._need(out.counts, "out.counts", torch.int64, (E,))
-            if out.rows is not None:
+            if out.rows is not None or out.pos is not None or out.offsets is not None:
                 self._need(out.rows, "out.rows", torch.int32, (T * k,))
                 self._need(out.pos, "out.pos", torch.int32, (T, k))
                 self._need(out.offsets, "out.offsets", torch.int32, (E + 1,))

@@ -51,3 +51,12 @@ def test_replaced_results_are_checked(moe, m):
     # good replacements are taken
     spare = dataclasses.replace(r, rows=i32(80))
     assert m.route(z, 2, out=spare) is spare and torch.equal(spare.rows, r.rows)
+
+
+def test_parts_of_a_plan_are_refused(moe, m):
+    """A plan is whole or left out, also where there are no tokens and nothing but offsets would be written."""
+    z, r = torch.randn(0, 8, device="cuda"), m.routing(0, 8, 2)
+    for change in (dict(rows=None, offsets=i32(20)), dict(rows=None, pos=None, offsets=i32(20)), dict(pos=None)):
+        with pytest.raises(ValueError):
+            m.route(z, 2, out=dataclasses.replace(r, **change))
+    assert m.route(z, 2, out=dataclasses.replace(r, rows=None, pos=None, offsets=None)).rows is None
