@@ -149,9 +149,23 @@ class Weight:
         if not codes(q, N, K) or (qt is not None and not codes(qt, K, N)) or scale.dtype is not torch.float32 or \
                 scale.shape != (E, -(-N // BLOCK), -(-K // BLOCK)) or not scale.is_contiguous():
             raise ValueError("8-bit weights: contiguous uint8 codes (E, N, >= K), fp32 scales (E, N / 128, K / 128)")
-        self._c = _CWeight(self.E, self.N, self.K, self.q.shape[2], qt.shape[2] if qt is not None else 0,
-                           self.q.data_ptr(), qt.data_ptr() if qt is not None else None, self.scale.data_ptr())
+        self._c = _CWeight(E, N, K, q.shape[2], qt.shape[2] if qt is not None else 0, *self._places())
         self._ref = ctypes.byref(self._c)
+        self._made_at = self._places()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name[0] != "_":
+            self._ref = None   # checked and made anew by the next call
+
+    def _places(self):
+        return self.q.data_ptr(), _ptr(self.qt), self.scale.data_ptr()
+
+    def _arg(self):
+        """The C argument for the fields as they are, whether assigned since or their memory moved (``.data``)."""
+        if self._ref is None or self._places() != self._made_at:
+            self.__post_init__()
+        return self._ref
 
     def codes(self) -> torch.Tensor:
         """The codes as float8_e4m3fn, (E, N, K)."""
@@ -399,7 +413,7 @@ class Moe:
             raise ValueError(f"out: weights of {(E, N, K)} expected")
         self._need(out.scale, "out")
         self._on_stream()
-        esp._check(self._lib.esp_moe_quantize_weight(self.h, code, w3.data_ptr(), ld, out._ref),
+        esp._check(self._lib.esp_moe_quantize_weight(self.h, code, w3.data_ptr(), ld, out._arg()),
                    "esp_moe_quantize_weight")
         return out
 
@@ -442,7 +456,7 @@ class Moe:
             out = self._new((M, weight.N), x.dtype)
         _, ldy = self._matrix(out, "out", M, weight.N, x.dtype)
         self._on_stream()
-        esp._check(self._lib.esp_moe_linear(self.h, code, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), weight._ref,
+        esp._check(self._lib.esp_moe_linear(self.h, code, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), weight._arg(),
                                             _ptr(offsets), ldy, out.data_ptr()), "esp_moe_linear")
         return out
 
@@ -468,7 +482,7 @@ class Moe:
             self._need(dw, "dw", torch.float32, (weight.E, weight.N, weight.K))
         self._on_stream()
         esp._check(self._lib.esp_moe_linear_backward(
-            self.h, code, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), weight._ref, _ptr(offsets), lddy,
+            self.h, code, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), weight._arg(), _ptr(offsets), lddy,
             dy.data_ptr(), lddx, _ptr(dx) if need[0] else None, weight.K, _ptr(dw) if need[1] else None),
             "esp_moe_linear_backward")
         return dx, dw

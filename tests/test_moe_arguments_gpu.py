@@ -60,3 +60,28 @@ def test_parts_of_a_plan_are_refused(moe, m):
         with pytest.raises(ValueError):
             m.route(z, 2, out=dataclasses.replace(r, **change))
     assert m.route(z, 2, out=dataclasses.replace(r, rows=None, pos=None, offsets=None)).rows is None
+
+
+def test_changed_weights_are_used(moe, m):
+    """Tensors assigned to a weight's fields, or moved under them, are what the next call reads or writes."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    w = [torch.randn(2, 48, 160, generator=g, device="cuda") for _ in range(3)]
+    x, dy = torch.randn(7, 160, generator=g, device="cuda"), torch.randn(7, 48, generator=g, device="cuda")
+    off = torch.tensor([0, 3, 7], device="cuda").int()
+    a, b, c = (m.quantize_weight(v, transposed=True) for v in w)
+    kept = (a.q, a.scale, a.qt)   # the memory before stays there
+    a.q, a.scale, a.qt = b.q, b.scale, b.qt
+    assert torch.equal(m.linear(x, a, offsets=off), m.linear(x, b, offsets=off))
+    assert torch.equal(m.linear_backward(dy, x, a, offsets=off)[0], m.linear_backward(dy, x, b, offsets=off)[0])
+    a.q.data = c.q.clone()
+    a.scale.data = c.scale.clone()
+    assert torch.equal(m.linear(x, a, offsets=off), m.linear(x, c, offsets=off))
+    a.q, a.scale, a.qt = kept
+    m.quantize_weight(w[2], transposed=True, out=a)
+    assert torch.equal(kept[0], c.q) and torch.equal(kept[2], c.qt) and torch.equal(kept[1], c.scale)
+    a.qt = None
+    with pytest.raises(ValueError):
+        m.linear_backward(dy, x, a, offsets=off)
+    a.q = torch.zeros(2, 40, 160, dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        m.linear(x, a, offsets=off)
