@@ -85,6 +85,11 @@ def load_library():
     return lib
 
 
+def _from_fields(self):
+    """Copies and pickles are made of the fields: C arguments and marks of checked tensors belong to one object."""
+    return type(self), tuple(getattr(self, f.name) for f in dataclasses.fields(self) if f.init)
+
+
 @dataclasses.dataclass(frozen=True)
 class Gate:
     """How a chosen expert's weight follows from the logits (esp_moe_gate)."""
@@ -98,6 +103,8 @@ class Gate:
             raise ValueError(f"unknown gate {self.kind!r}")
         object.__setattr__(self, "_c", _CGate(_KINDS[self.kind], int(self.renorm), self.scale))
         object.__setattr__(self, "_ref", ctypes.byref(self._c))
+
+    __reduce__ = _from_fields
 
 
 @dataclasses.dataclass(frozen=True)
@@ -114,6 +121,8 @@ class Routing:
     offsets: Optional[torch.Tensor] = None
     checked: Optional[tuple] = dataclasses.field(default=None, init=False, repr=False, compare=False)
 
+    __reduce__ = _from_fields
+
 
 @dataclasses.dataclass(frozen=True)
 class Balance:
@@ -125,6 +134,8 @@ class Balance:
     share: torch.Tensor
     tokens: torch.Tensor
     checked: Optional[tuple] = dataclasses.field(default=None, init=False, repr=False, compare=False)
+
+    __reduce__ = _from_fields
 
 
 @dataclasses.dataclass
@@ -152,6 +163,8 @@ class Weight:
         self._c = _CWeight(E, N, K, q.shape[2], qt.shape[2] if qt is not None else 0, *self._places())
         self._ref = ctypes.byref(self._c)
         self._made_at = self._places()
+
+    __reduce__ = _from_fields
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
