@@ -22,10 +22,10 @@ def _clean(z):
 
 def choose(logits, k, prices=None, valid=None):
     """(T, k) int: experts of greatest fp32 profit, descending, ties to the lower index; -1: none left."""
-    z = _clean(logits)
+    z = np.asarray(logits, np.float32)
     T, E = z.shape
     out = np.full((T, k), -1, np.int64)
-    with np.errstate(invalid="ignore"):
+    with np.errstate(invalid="ignore", over="ignore"):
         profit = z if prices is None else (z - np.asarray(prices, np.float32)).astype(np.float32)
     for t in range(T):
         if valid is not None and not valid[t]:

@@ -44,10 +44,10 @@ __device__ __forceinline__ float clean(float z)
 }
 
 // What a price adds to a logit: its negative, with +0 for both zeros (then a sum of 0 is +0, whatever the
-// logit's sign) and NaN closing the expert. Clean logits plus it are never NaN.
+// logit's sign).
 __device__ __forceinline__ float price_term(float price)
 {
-    return price == 0.0f ? 0.0f : fminf(fmaxf(-price, -INFINITY), FLT_MAX);
+    return price == 0.0f ? 0.0f : -price;
 }
 
 template <typename T, int VPT>
@@ -65,9 +65,6 @@ __device__ __forceinline__ void load_row(const T *row, int E, bool aligned, int 
                 z[c * S::V + j] = e0 + j < E ? to_f32(row[e0 + j]) : -INFINITY;
         }
     }
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-        z[i] = clean(z[i]);
 }
 
 template <typename T, int VPT>
@@ -361,15 +358,18 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_route(const RouteArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             z[i] = next[i];
-            key[i] = order_key(__fadd_rn(z[i], price[32 * i + lane]));
+            // the logit as it is minus the price; a NaN closes the expert as -inf does
+            key[i] = order_key(fmaxf(__fadd_rn(z[i], price[32 * i + lane]), -INFINITY));
         }
         if (t + 1 < tb)
             load_row<T, VPT>(row + a.ld, E, aligned, lane, next);
         float m = -INFINITY, zsum = 0.0f;
         if (!a.gate.renorm && !a.gate.sigmoid) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
+            for (int i = 0; i < VPT; ++i) {
+                z[i] = clean(z[i]);
                 m = fmaxf(m, z[i]);
+            }
             m = warp_max(m);
             if (m > -INFINITY) {
 #pragma unroll
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kRouteThreads<VPT>) k_balance(const BalanceArg
             float z[VPT], p[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                z[i] = next[i];
+                z[i] = clean(next[i]);
             fetch(t + W);
             if (__shfl_sync(kFull, mine, 0) < 0)
                 continue;
@@ -804,7 +804,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_route_backward(const RouteBackw
         float z[VPT], p[VPT], d[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            z[i] = next[i];
+            z[i] = clean(next[i]);
             d[i] = 0.0f;
         }
         fetch(t + 1);

@@ -91,3 +91,11 @@ def test_combine_gradient_against_differences():
     dy, dw = mo.combine_grad(d, y, pos, w)
     assert np.abs(dy - numeric(lambda v: (mo.combine(v, pos, w) * d).sum(), y)).max() < 1e-8
     assert np.abs(dw - numeric(lambda v: (mo.combine(y, pos, v) * d).sum(), w)).max() < 1e-8
+
+
+def test_choice_reads_infinite_logits_as_they_are():
+    big, inf = np.finfo(np.float32).max, np.inf
+    z = np.array([[big, inf], [inf, inf], [0.0, inf]], np.float32)
+    assert mo.choose(z, 1).tolist() == [[1], [0], [1]]
+    assert mo.choose(z, 2, prices=np.array([1e38, inf], np.float32)).tolist() == [[0, -1], [0, -1], [0, -1]]
+    assert mo.choose(z, 2, prices=np.array([1e38, 1e38], np.float32)).tolist() == [[1, 0], [0, 1], [1, 0]]
