@@ -78,8 +78,10 @@ esp_status begin(esp_moe *m)
     if (st != ESP_OK)
         return st;
     m->launches = 0;
-    m->in_capture = capturing(m->stream);
-    return m->in_capture ? ESP_OK : join_earlier(m);
+    // on the stream that took the last direct work there is nothing to join, captured or not
+    if (m->has_direct && m->direct == m->stream && !m->marked)
+        return ESP_OK;
+    return capturing(m->stream) ? ESP_OK : join_earlier(m);
 }
 
 // While one lives, its thread's allocations are neither forbidden by a capture, of this stream or another, nor end it.
@@ -99,13 +101,16 @@ private:
 // and cannot be waited for.
 esp_status reserve(esp_moe *m, size_t bytes)
 {
+    if (bytes == 0)
+        return ESP_OK;
+    const bool in_capture = capturing(m->stream);
     if (bytes <= m->ws_bytes) {
-        m->ws_captured = m->ws_captured || m->in_capture;
+        m->ws_captured = m->ws_captured || in_capture;
         return ESP_OK;
     }
     const BesideCaptures beside;
     if (m->ws) {
-        if (m->ws_captured || m->in_capture) {
+        if (m->ws_captured || in_capture) {
             esp_moe::Kept *k = new (std::nothrow) esp_moe::Kept{m->ws, m->kept};
             if (!k)
                 return ESP_ERR_OOM;
@@ -124,7 +129,7 @@ esp_status reserve(esp_moe *m, size_t bytes)
     }
     m->ws = static_cast<unsigned char *>(p);
     m->ws_bytes = bytes;
-    m->ws_captured = m->in_capture;
+    m->ws_captured = in_capture;
     return ESP_OK;
 }
 

@@ -24,7 +24,6 @@ struct esp_moe {
     unsigned char *ws = nullptr;     // work space of the call in flight (later calls run after it)
     size_t ws_bytes = 0;
     bool ws_captured = false;        // a captured call uses it: its graph names the block as long as it lives
-    bool in_capture = false;         // the call in flight is being captured
     struct Kept {                    // outgrown blocks that graphs name, freed with the handle
         void *p;
         Kept *next;
