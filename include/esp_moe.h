@@ -164,11 +164,12 @@ esp_status esp_moe_combine_backward(esp_moe *m, int32_t dtype, int64_t T, int32_
                                     const void *dout, int64_t ldy, const void *y, const int32_t *pos,
                                     const float *weight, int64_t lddy, void *dy, float *dweight);
 
-/* Waits for the handle's work on all streams (not for graphs that the program launches: it waits for
- * those itself first) and reports a device-side failure of the queued work: ESP_ERR_TIMEOUT
+/* Waits for the handle's work on all streams (not for graphs that the program launches: it waits
+ * for those itself first) and reports a device-side failure of the queued work: ESP_ERR_TIMEOUT
  * when a bounded wait of a product kernel gave up (its results are then undefined and the handle
- * refuses further work with ESP_ERR_STATE), ESP_ERR_CUDA on a CUDA error, ESP_ERR_STATE while the
- * handle's stream is being captured (the handle stays usable). */
+ * refuses further work with ESP_ERR_STATE; any other call that finds such a failure reports it
+ * instead), ESP_ERR_CUDA on a CUDA error, ESP_ERR_STATE while the handle's stream is being captured
+ * (the handle stays usable). */
 esp_status esp_moe_synchronize(esp_moe *m);
 
 /* Kernel launches of the handle's last call. */

@@ -76,7 +76,7 @@ struct GemmParams {
     void *out;
     int64_t ldo;
     bool wide_store;
-    unsigned int *err;
+    unsigned int *err;               // set to 1 where a wait runs out
     uint32_t wait_ms;
     // parts of every tile's inner axis, each a work item of its own (CG = 1); their sums meet in
     // partial[item][BN / 4][128][4] (lanes hold rows: consecutive rows, four columns each, lie together), and
@@ -188,7 +188,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const G
     if (mbar_try(bar, parity) || mbar_wait_ms(bar, parity, p.wait_ms, dead))
         return true;
     *dead = 1;
-    atomicOr(p.err, 1u);
+    *static_cast<volatile unsigned int *>(p.err) = 1u;   // in host memory
     return false;
 }
 

@@ -38,6 +38,15 @@ bool capturing(cudaStream_t s)
     return status != cudaStreamCaptureStatusNone;
 }
 
+// A wait that ran out in work done so far, reported once.
+esp_status timed_out(esp_moe *m)
+{
+    if (!*m->err)
+        return ESP_OK;
+    m->poisoned = true;
+    return ESP_ERR_TIMEOUT;
+}
+
 // The handle, its device current.
 esp_status check(esp_moe *m)
 {
@@ -45,6 +54,9 @@ esp_status check(esp_moe *m)
         return ESP_ERR_INVALID_ARG;
     if (m->poisoned)
         return ESP_ERR_STATE;
+    const esp_status st = timed_out(m);
+    if (st != ESP_OK)
+        return st;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || (dev != m->device && cudaSetDevice(m->device) != cudaSuccess))
         return fail(m);
@@ -220,18 +232,24 @@ esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream)
     m->device = device;
     m->stream = static_cast<cudaStream_t>(cuda_stream);
     m->sm_count = sms;
-    void *words = nullptr;
-    const size_t bytes = (1 + kTickets) * sizeof(unsigned int);
+    void *words = nullptr, *err = nullptr, *d_err = nullptr;
+    const size_t bytes = kTickets * sizeof(unsigned int);
     if (cudaMalloc(&words, bytes) != cudaSuccess || cudaMemset(words, 0, bytes) != cudaSuccess ||
+        cudaHostAlloc(&err, sizeof(unsigned int), cudaHostAllocMapped) != cudaSuccess ||
+        cudaHostGetDevicePointer(&d_err, err, 0) != cudaSuccess ||
         cudaEventCreateWithFlags(&m->handoff, cudaEventDisableTiming) != cudaSuccess) {
         cudaGetLastError();
         if (words)
             cudaFree(words);
+        if (err)
+            cudaFreeHost(err);
         delete m;
         return ESP_ERR_CUDA;
     }
-    m->d_err = static_cast<unsigned int *>(words);
-    m->d_ticket = m->d_err + 1;
+    m->err = static_cast<volatile unsigned int *>(err);
+    *m->err = 0;
+    m->d_err = static_cast<unsigned int *>(d_err);
+    m->d_ticket = static_cast<unsigned int *>(words);
     *out = m;
     return ESP_OK;
 }
@@ -532,13 +550,7 @@ esp_status esp_moe_synchronize(esp_moe *m)
     if ((st = join_earlier(m)) != ESP_OK)
         return st;
     MOE_CUDA(cudaStreamSynchronize(m->stream));
-    unsigned int err = 0;
-    MOE_CUDA(cudaMemcpy(&err, m->d_err, sizeof(err), cudaMemcpyDeviceToHost));
-    if (err) {
-        m->poisoned = true;
-        return ESP_ERR_TIMEOUT;
-    }
-    return ESP_OK;
+    return timed_out(m);
 }
 
 esp_status esp_moe_last_launch_count(esp_moe *m, int64_t *out)
@@ -580,8 +592,8 @@ void esp_moe_destroy(esp_moe *m)
         cudaFree(k->p);
         delete k;
     }
-    if (m->d_err)
-        cudaFree(m->d_err);
+    cudaFree(m->d_ticket);
+    cudaFreeHost(const_cast<unsigned int *>(m->err));
     if (m->handoff)
         cudaEventDestroy(m->handoff);
     cudaGetLastError();

@@ -28,7 +28,10 @@ struct esp_moe {
         void *p;
         Kept *next;
     } *kept = nullptr;
-    unsigned int *d_err = nullptr;   // device error word (timeouts of the product kernels)
+    // error word (timeouts of the product kernels) in host memory, so that every call can look at it, and its address
+    // on the device
+    volatile unsigned int *err = nullptr;
+    unsigned int *d_err = nullptr;
     unsigned int *d_ticket = nullptr;   // arrival counters, zero between launches
     int max_pairs = 0;               // CTA pairs of the product kernel that run at once (0: not asked yet)
     // failure-detection hooks (esp_moe.h): limit of a bounded wait, and the next

@@ -543,7 +543,8 @@ class Moe:
     # -- handle
 
     def synchronize(self) -> None:
-        """Waits for the queued calls; raises if a product kernel gave up a bounded wait."""
+        """Waits for the queued calls; raises if a product kernel gave up a bounded wait (any later call that finds
+        that raises too, but does not wait)."""
         esp._check(self._lib.esp_moe_synchronize(self.h), "esp_moe_synchronize")
 
     def last_launch_count(self) -> int:

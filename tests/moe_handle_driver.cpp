@@ -134,14 +134,24 @@ cudaError_t cudaFree(void *p)
     free(p);
     return cudaSuccess;
 }
+cudaError_t cudaHostAlloc(void **p, size_t n, unsigned int)
+{
+    *p = calloc(1, n);
+    return cudaSuccess;
+}
+cudaError_t cudaFreeHost(void *p)
+{
+    free(p);
+    return cudaSuccess;
+}
+cudaError_t cudaHostGetDevicePointer(void **d, void *h, unsigned int)
+{
+    *d = h;
+    return cudaSuccess;
+}
 cudaError_t cudaMemset(void *p, int v, size_t n)
 {
     memset(p, v, n);
-    return cudaSuccess;
-}
-cudaError_t cudaMemcpy(void *d, const void *s, size_t n, cudaMemcpyKind)
-{
-    memcpy(d, s, n);
     return cudaSuccess;
 }
 cudaError_t cudaStreamSynchronize(cudaStream_t s)
@@ -261,7 +271,7 @@ void graph_keeps_its_block()
     of(s).capturing = false;
     want(route(m, 5000), ESP_OK, "largest call");
     want(route(m, 9000), ESP_OK, "larger still");   // a block that no graph names goes at once
-    if (memory.size() != 4)                         // the error word and counters, two kept, the present one
+    if (memory.size() != 4)                         // the counters, two kept, the present one
         fault("blocks alive: " + std::to_string(memory.size()));
     in_graph.clear();                               // the graphs end before the handle
     esp_moe_destroy(m);
@@ -361,12 +371,29 @@ void synchronize_across_a_capture()
     esp_moe_destroy(m);
 }
 
+// A wait that ran out is reported by the next call of any kind, once; then the handle refuses work.
+void timeout_is_reported_by_the_next_call()
+{
+    for (int way = 0; way < 3; ++way) {
+        cudaStream_t a = new_stream(), b = new_stream();
+        esp_moe *m = open(a);
+        want(route(m, 10), ESP_OK, "call");
+        *m->d_err = 1u;   // as a kernel does
+        want(way == 0 ? route(m, 10) : way == 1 ? esp_moe_set_stream(m, b) : esp_moe_synchronize(m), ESP_ERR_TIMEOUT,
+             "next call");
+        want(route(m, 10), ESP_ERR_STATE, "call after");
+        want(esp_moe_synchronize(m), ESP_ERR_STATE, "waiting after");
+        esp_moe_destroy(m);
+    }
+}
+
 const std::map<std::string, void (*)()> checks = {
     {"growing_while_captured", growing_while_captured},
     {"graph_keeps_its_block", graph_keeps_its_block},
     {"order_across_a_capture", order_across_a_capture},
     {"order_after_a_capture_in_place", order_after_a_capture_in_place},
     {"synchronize_across_a_capture", synchronize_across_a_capture},
+    {"timeout_is_reported_by_the_next_call", timeout_is_reported_by_the_next_call},
 };
 
 }  // namespace

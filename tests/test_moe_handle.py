@@ -16,6 +16,7 @@ CHECKS = [
     "order_across_a_capture",
     "order_after_a_capture_in_place",
     "synchronize_across_a_capture",
+    "timeout_is_reported_by_the_next_call",
 ]
 
 

@@ -252,3 +252,24 @@ def test_set_stream_of_a_handle_that_followed(moe):
     m.synchronize()
     assert busy.query() and torch.equal(r.rows, want.rows)
     m.close()
+
+
+@pytest.mark.parametrize("M", [40, 2000])
+def test_wait_that_runs_out_is_seen_by_the_next_call(moe, M):
+    """A program that waits for the device by itself learns of a given-up wait from its next call."""
+    from paper_2608_07971_gb300 import esp
+    m = moe.Moe()
+    x, w = torch.randn(M, 1024, device="cuda"), torch.randn(300, 1024, device="cuda")
+    q = m.quantize_weight(w)
+    m.linear(x, q)
+    m.synchronize()
+    lib = moe.load_library()
+    esp._check(lib.esp_moe_debug_set_wait_limit(m.h, 20), "set_wait_limit")
+    esp._check(lib.esp_moe_debug_hold_load(m.h), "hold_load")
+    m.linear(x, q)
+    torch.cuda.synchronize()
+    for status in (esp.ESP_ERR_TIMEOUT, esp.ESP_ERR_STATE, esp.ESP_ERR_STATE):
+        with pytest.raises(esp.EspError) as err:
+            m.route(x[:, :8], 2)
+        assert err.value.status == status
+    m.close()
