@@ -134,16 +134,28 @@ __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// PAIR: a barrier at which another CTA's threads arrive (mbar_arrive); what orders their tensor-memory loads before the
+// MMAs that follow are the tcgen05 fences around a relaxed arrival and wait of the same, cluster, scope.
+template <bool PAIR>
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    if (PAIR)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
     return done != 0;
 }
 
@@ -155,12 +167,13 @@ __device__ __forceinline__ uint64_t global_ns()
 }
 
 // Waits for a phase for at most `ms` milliseconds of the GPU's timer, which is read once in 256 polls.
+template <bool PAIR = false>
 __device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
 {
     uint64_t end = 0;
     for (;;) {
         for (int i = 0; i < 256; ++i)
-            if (mbar_try(bar, parity))
+            if (mbar_try<PAIR>(bar, parity))
                 return true;
         if (dead && *dead)
             return false;
@@ -183,9 +196,10 @@ __device__ __forceinline__ bool elect_one()
 
 // Bounded wait of a role; gives up early once another wait of the CTA did. On running out it sets the CTA's
 // flag and the error word.
+template <bool PAIR = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
 {
-    if (mbar_try(bar, parity) || mbar_wait_ms(bar, parity, p.wait_ms, dead))
+    if (mbar_try<PAIR>(bar, parity) || mbar_wait_ms<PAIR>(bar, parity, p.wait_ms, dead))
         return true;
     *dead = 1;
     *static_cast<volatile unsigned int *>(p.err) = 1u;   // in host memory
@@ -614,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if ((bool)(acc & 1) == odd) {
                         ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * s, ph, p, dead) &&
-                                                         mbar_wait(tempty + 8 * acc, aph, p, dead));
+                                                         mbar_wait<CG == 2>(tempty + 8 * acc, aph, p, dead));
                         if (!ok)
                             break;
                         fence_after();
