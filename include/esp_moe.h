@@ -138,6 +138,7 @@ esp_status esp_moe_quantize_weight(esp_moe *m, int32_t dtype, const void *w, int
  * rows of x are rounded to e4m3 codes with one scale for each 128 of a row (as esp_moe_quantize_weight
  * does); the products of a block are summed in fp32, then scaled and added. x (T x K) and y (M x N)
  * have type dtype; rows outside every expert are not written; a row index outside [0, T) reads zeros.
+ * Offsets that do not ascend leave the rows of y undefined, and touch nothing else.
  * Errors: ESP_ERR_INVALID_ARG (M, T <= 2^31 - 256, at most 2^29 blocks of 128 x 128 in y, the weights or
  * their gradients, 16-byte rules of esp_moe_weight). */
 esp_status esp_moe_linear(esp_moe *m, int32_t dtype, int64_t T, int64_t ldx, const void *x, int64_t M,

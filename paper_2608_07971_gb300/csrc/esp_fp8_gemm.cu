@@ -29,6 +29,7 @@
 
 #include <cuda.h>
 
+#include "esp_fp8_tiles.cuh"
 #include "esp_moe_impl.h"
 #include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
@@ -41,7 +42,6 @@ constexpr int kThreads = 384;                // 8 epilogue warps, loads, MMAs, s
 // registers per thread of the epilogue and of the other warpgroup: 2 * 216 + 72 = 3 * 168, the launch's
 constexpr int kEpilogueRegs = 216, kOtherRegs = 72;
 constexpr int kEpilogueWarps = 8;
-constexpr int kRowsA = 128;                  // rows of A that a CTA holds
 constexpr int kStageA = kRowsA * kBlock;     // bytes
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBoxBytes = 128, kBox = 32 * kBoxBytes;   // a warp's staged store: 128 bytes of 32 rows
@@ -64,27 +64,6 @@ struct Shape {
     static constexpr int kStages = std::min(8, (kSmemLimit - kFixed) / kStage);
     static constexpr int kSmem = kStages * kStage + kFixed;
     static_assert((2 * kStages + 3 * kAcc + 1) * 8 + 16 <= kBars, "barriers");
-};
-
-struct GemmParams {
-    int32_t M, E, N, K;              // rows over all experts; N: the output's columns; K: of the inner axis (FWD)
-    int64_t sa_row, sa_k;            // steps of A's scales by row and block
-    int32_t rows_b;                  // rows of B per expert (FWD)
-    const float *scale_a, *scale_b;
-    int64_t sb_e, sb_n, sb_k;
-    const int32_t *offsets;
-    void *out;
-    int64_t ldo;
-    bool wide_store;
-    unsigned int *err;               // set to 1 where a wait runs out
-    uint32_t wait_ms;
-    // parts of every tile's inner axis, each a work item of its own (CG = 1); their sums meet in
-    // partial[item][BN / 4][128][4] (lanes hold rows: consecutive rows, four columns each, lie together), and
-    // the last part of a tile to arrive adds them up in order
-    int32_t splits;
-    float *partial;
-    unsigned int *tickets;           // one per tile, zero between launches
-    int32_t hold;                    // leave out the CTAs' third load (failure detection)
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p)
@@ -340,80 +319,6 @@ __device__ __forceinline__ bool sync_and(int id, bool v)
     return r != 0;
 }
 
-// Expert e's rows [lo, hi).
-__device__ __forceinline__ void expert_rows(const GemmParams &p, int e, int &lo, int &hi)
-{
-    lo = p.offsets ? max(0, min(p.M, p.offsets[e])) : 0;
-    hi = p.offsets ? max(lo, min(p.M, p.offsets[e + 1])) : p.M;
-}
-
-// One item of the list: rows m0 .. m0 + rows - 1 of expert e (COLS: of its output), columns n0 .., blocks
-// kb0 .. kb1 - 1 (of a tile's, where its inner axis is split).
-struct Tile {
-    int e, m0, rows, n0, kb0, kb1;
-};
-
-// Part number `part` of the tile's blocks.
-template <int CG>
-__device__ __forceinline__ void take_part(const GemmParams &p, int part, Tile &t)
-{
-    if (CG == 2 || p.splits == 1)
-        return;
-    const int first = t.kb0, n = t.kb1 - t.kb0;
-    t.kb0 = first + (int)((int64_t)n * part / p.splits);
-    t.kb1 = first + (int)((int64_t)n * (part + 1) / p.splits);
-}
-
-// table[e]: row tiles (COLS: blocks) of the experts before e. Tiles run over an expert's rows first, so that
-// the tiles in flight share columns of B.
-template <int CG, int BN, bool COLS>
-__device__ __forceinline__ bool tile_at(const GemmParams &p, const int *table, int item, Tile &t)
-{
-    constexpr int BM = kRowsA * CG;
-    int w = item, part = 0;
-    if (CG == 1 && p.splits > 1) {
-        w = item / p.splits;
-        part = item - w * p.splits;
-    }
-    const int nt = (p.N + BN - 1) / BN;
-    if (!COLS) {
-        if (w >= table[p.E] * nt)
-            return false;
-        int lo = 0, hi = p.E;   // the expert whose tiles hold w
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (table[mid] * nt <= w)
-                lo = mid;
-            else
-                hi = mid;
-        }
-        t.e = lo;
-        const int mt = table[lo + 1] - table[lo], i = w - table[lo] * nt;
-        int a, b;
-        expert_rows(p, lo, a, b);
-        t.m0 = a + (i % mt) * BM;
-        t.rows = min(BM, b - t.m0);
-        t.n0 = (i / mt) * BN;
-        t.kb0 = 0;
-        t.kb1 = (p.K + kBlock - 1) / kBlock;
-        take_part<CG>(p, part, t);
-        return true;
-    }
-    const int mt = (p.rows_b + BM - 1) / BM;   // rows_b: output rows per expert
-    const int per = mt * nt;
-    if (w >= per * p.E)
-        return false;
-    t.e = w / per;
-    const int i = w % per;
-    t.m0 = (i % mt) * BM;
-    t.rows = min(BM, p.rows_b - t.m0);
-    t.n0 = (i / mt) * BN;
-    t.kb0 = table[t.e];
-    t.kb1 = table[t.e + 1];
-    take_part<CG>(p, part, t);
-    return true;
-}
-
 // A warp's 32 rows of one box of the output: 128 bytes of every row (a lane holds a row's values), staged in
 // the 128-byte swizzle (16-byte chunk j of row r at place j ^ (r & 7): no bank conflicts). Whole boxes leave
 // by one TMA store, so that the warp goes on while they are written; with a bulk copy for every row instead,
@@ -553,13 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the experts' row tiles (blocks) before each: one warp's scan
         int carry = 0;
         for (int e0 = 0; e0 < p.E; e0 += 32) {
-            int n = 0;
-            if (e0 + lane < p.E) {
-                int lo, hi;
-                expert_rows(p, e0 + lane, lo, hi);
-                constexpr int per = COLS ? kBlock : kRowsA * CG;
-                n = (hi - lo) / per + ((hi - lo) % per != 0);
-            }
+            const int n = e0 + lane < p.E ? tiles_of<CG, COLS>(p, e0 + lane) : 0;
             int s = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -568,8 +467,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     s += y;
             }
             if (e0 + lane < p.E)
-                table[e0 + lane] = carry + s - n;
-            carry += __shfl_sync(0xffffffffu, s, 31);
+                table[e0 + lane] = min(p.most, carry + s - n);
+            carry = min(p.most, carry + __shfl_sync(0xffffffffu, s, 31));
         }
         if (lane == 0)
             table[p.E] = carry;
@@ -1029,10 +928,12 @@ cudaError_t launch_gemm_rows(esp_moe *m, int32_t dtype, const GemmRowsArgs &a)
         p.wide_store = rows_aligned(a.out, a.ldo, sizeof(T), 16);
         p.partial = a.partial;
         // at most this many tiles: every expert with rows has one that is not full
-        const int64_t experts = std::min<int64_t>(a.E, a.M);
-        const int64_t pair = (a.E == 1 ? ceil_div(a.M, 256) : a.M / 256 + experts) * ceil_div(a.N, 256);
-        const int64_t one = (a.E == 1 ? ceil_div(a.M, 128) : a.M / 128 + experts) * ceil_div(a.N, 128);
+        const auto row_tiles = [&](int rows) {
+            return a.E == 1 ? ceil_div(a.M, rows) : a.M / rows + std::min<int64_t>(a.E, a.M);
+        };
+        const int64_t pair = row_tiles(256) * ceil_div(a.N, 256), one = row_tiles(128) * ceil_div(a.N, 128);
         const Choice c = choose_tiles(m, pair, one, ceil_div(a.K, kBlock), a.M / a.E);
+        p.most = (int32_t)row_tiles(c.pair ? 256 : 128);
         if (c.pair)
             return encode_and_launch<2, 256, false, T>(m, a.A, a.M, a.K, a.lda, a.B, (int64_t)a.E * a.N, a.ldb, p, pair);
         p.splits = c.splits;
@@ -1058,7 +959,8 @@ cudaError_t launch_gemm_cols(esp_moe *m, const GemmColsArgs &a)
     p.ldo = a.ldo;
     p.wide_store = rows_aligned(a.out, a.ldo, 4, 16);
     p.partial = a.partial;
-    const int64_t positions = (a.M / kBlock + a.E) * kBlock;
+    p.most = (int32_t)(a.M / kBlock + a.E);
+    const int64_t positions = (int64_t)p.most * kBlock;
     const int64_t pair = (int64_t)a.E * ceil_div(a.N, 256) * ceil_div(a.K, 256);
     const int64_t one = (int64_t)a.E * ceil_div(a.N, 128) * ceil_div(a.K, 128);
     const Choice c = choose_tiles(m, pair, one, ceil_div(a.M, kBlock * a.E), a.N);   // blocks: the experts' mean

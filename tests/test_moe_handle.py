@@ -1,5 +1,6 @@
-"""The expert layer's handle against a fake CUDA runtime (no GPU): work space under captured graphs, the order of work
-across streams (tests/moe_handle_driver.cpp), kernels' shared-memory limits (tests/moe_smem_driver.cpp)."""
+"""The expert layer's host code without a GPU: its handle against a fake CUDA runtime (work space under captured graphs,
+the order of work across streams, failures: tests/moe_handle_driver.cpp), kernels' shared-memory limits
+(tests/moe_smem_driver.cpp), the products' work items (tests/moe_tiles_driver.cpp)."""
 
 import os
 import subprocess
@@ -49,4 +50,11 @@ def test_shared_memory_limit(tmp_path):
     """One limit per kernel, its greatest, also where two threads set it at once."""
     out = compiled(str(tmp_path / "driver"), os.path.join(HERE, "moe_smem_driver.cpp"))
     res = subprocess.run([out], capture_output=True, text=True, timeout=60)
+    assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
+
+
+def test_work_items_stay_in_range(tmp_path):
+    """The products' work items cover every row once, and stay in bounds for offsets that do not ascend."""
+    out = compiled(str(tmp_path / "driver"), os.path.join(HERE, "moe_tiles_driver.cpp"))
+    res = subprocess.run([out], capture_output=True, text=True, timeout=120)
     assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
