@@ -162,15 +162,18 @@ int threads_for(int64_t H, int V)
     return (int)std::min<int64_t>(kMaxThreads, std::max<int64_t>(32, ceil_div(ceil_div(H, V), 32) * 32));
 }
 
-// Calls f(V, KT) for the widest load that every row allows and the rows in flight.
+// Calls f(V): the widest load, or single elements where not every row allows it.
 template <typename T, typename F>
-cudaError_t with_shape(bool wide, int rows, F &&f)
+cudaError_t with_load(bool wide, F &&f)
 {
-    constexpr int W = 16 / (int)sizeof(T);
-    if (!wide)
-        return f(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
-    return rows > 4 ? f(std::integral_constant<int, W>(), std::integral_constant<int, 8>())
-                    : f(std::integral_constant<int, W>(), std::integral_constant<int, 4>());
+    return wide ? f(std::integral_constant<int, 16 / (int)sizeof(T)>()) : f(std::integral_constant<int, 1>());
+}
+
+template <typename T, int V, int KT>
+cudaError_t start_combine(esp_moe *m, const CombineArgs &a)
+{
+    m->launches += 1;
+    return launch_after(k_combine<T, V, KT>, dim3((unsigned)a.T), threads_for(a.H, V), 0, m->stream, a);
 }
 
 }  // namespace
@@ -183,10 +186,12 @@ cudaError_t launch_combine(esp_moe *m, int32_t dtype, const CombineArgs &a)
         using T = decltype(elem);
         const bool wide = rows_aligned(a.y, a.ldy, sizeof(T), 16) && rows_aligned(a.out, a.ldo, sizeof(T), 16) &&
                           a.H * sizeof(T) % 16 == 0;
-        return with_shape<T>(wide, a.k, [&](auto v, auto kt) -> cudaError_t {
-            constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
-            m->launches += 1;
-            return launch_after(k_combine<T, V, KT>, dim3((unsigned)a.T), threads_for(a.H, V), 0, m->stream, a);
+        return with_load<T>(wide, [&](auto v) -> cudaError_t {
+            constexpr int V = decltype(v)::value;
+            if constexpr (V > 1)   // rows in flight
+                if (a.k <= 4)
+                    return start_combine<T, V, 4>(m, a);
+            return start_combine<T, V, 8>(m, a);
         });
     });
 }
@@ -202,8 +207,8 @@ cudaError_t launch_combine_backward(esp_moe *m, int32_t dtype, const CombineArgs
                           rows_aligned(a.dout, a.lddo, sizeof(T), 16) && a.H * sizeof(T) % 16 == 0;
         // four rows in flight: eight take 97 registers and halve the CTAs of an SM (8192 x 8 rows of 4096 bf16:
         // 186 us, 175 with four)
-        return with_shape<T>(wide, 4, [&](auto v, auto kt) -> cudaError_t {
-            constexpr int V = decltype(v)::value, KT = decltype(kt)::value;
+        return with_load<T>(wide, [&](auto v) -> cudaError_t {
+            constexpr int V = decltype(v)::value, KT = V > 1 ? 4 : 8;
             m->launches += 1;
             return launch_after(k_combine_backward<T, V, KT>, dim3((unsigned)a.T), threads_for(a.H, V), 0, m->stream, a);
         });
