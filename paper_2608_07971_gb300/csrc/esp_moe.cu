@@ -232,6 +232,7 @@ esp_status esp_moe_create(esp_moe **out, int device, void *cuda_stream)
     m->device = device;
     m->stream = static_cast<cudaStream_t>(cuda_stream);
     m->sm_count = sms;
+    const BesideCaptures beside;
     void *words = nullptr, *err = nullptr, *d_err = nullptr;
     const size_t bytes = kTickets * sizeof(unsigned int);
     if (cudaMalloc(&words, bytes) != cudaSuccess || cudaMemset(words, 0, bytes) != cudaSuccess ||
@@ -584,6 +585,7 @@ void esp_moe_destroy(esp_moe *m)
     if (!m)
         return;
     cudaSetDevice(m->device);
+    const BesideCaptures beside;
     if (m->ws)
         cudaFree(m->ws);
     while (m->kept) {

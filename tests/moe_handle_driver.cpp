@@ -65,6 +65,16 @@ bool any_capturing()
     return false;
 }
 
+// An allocation or a release now: a capture forbids it, and is ended by it, unless the thread has relaxed that.
+bool breaks_captures()
+{
+    if (!any_capturing() || mode == cudaStreamCaptureModeRelaxed)
+        return false;
+    for (Stream *s : streams)
+        s->broken = s->broken || s->capturing;
+    return true;
+}
+
 // A kernel queued on the handle's stream that uses its work space and counters.
 cudaError_t work(esp_moe *m)
 {
@@ -109,22 +119,16 @@ cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr a, int)
 }
 cudaError_t cudaMalloc(void **p, size_t n)
 {
-    if (any_capturing() && mode != cudaStreamCaptureModeRelaxed) {
-        for (Stream *s : streams)
-            s->broken = s->broken || s->capturing;
+    if (breaks_captures())
         return cudaErrorStreamCaptureUnsupported;
-    }
     *p = calloc(1, n < 4096 ? n : 4096);
     memory[*p] = n;
     return cudaSuccess;
 }
 cudaError_t cudaFree(void *p)
 {
-    if (any_capturing() && mode != cudaStreamCaptureModeRelaxed) {
-        for (Stream *s : streams)
-            s->broken = s->broken || s->capturing;
+    if (breaks_captures())
         return cudaErrorStreamCaptureUnsupported;
-    }
     if (in_graph.count(p))
         fault("memory that a captured graph names is freed");
     if (!memory.erase(p))
@@ -136,11 +140,15 @@ cudaError_t cudaFree(void *p)
 }
 cudaError_t cudaHostAlloc(void **p, size_t n, unsigned int)
 {
+    if (breaks_captures())
+        return cudaErrorStreamCaptureUnsupported;
     *p = calloc(1, n);
     return cudaSuccess;
 }
 cudaError_t cudaFreeHost(void *p)
 {
+    if (breaks_captures())
+        return cudaErrorStreamCaptureUnsupported;
     free(p);
     return cudaSuccess;
 }
@@ -307,6 +315,25 @@ void growing_while_captured()
     }
 }
 
+// A handle made or destroyed (by a garbage collector, say) while some stream is being captured.
+void handles_beside_a_capture()
+{
+    cudaStream_t s = new_stream(), other = new_stream();
+    esp_moe *before = open(s);
+    want(route(before, 10), ESP_OK, "call");
+    of(other).capturing = true;
+    esp_moe *m = open(s);
+    if (m)
+        esp_moe_destroy(m);
+    esp_moe_destroy(before);
+    if (of(other).broken)
+        fault("the capture is broken");
+    if (!memory.empty())
+        fault("memory left after the handles' end");
+    if (mode != cudaStreamCaptureModeGlobal)
+        fault("the thread's capture mode is left changed");
+}
+
 // Work before a capture and work after it share the work space in order, whichever stream comes after.
 void order_across_a_capture()
 {
@@ -390,6 +417,7 @@ void timeout_is_reported_by_the_next_call()
 const std::map<std::string, void (*)()> checks = {
     {"growing_while_captured", growing_while_captured},
     {"graph_keeps_its_block", graph_keeps_its_block},
+    {"handles_beside_a_capture", handles_beside_a_capture},
     {"order_across_a_capture", order_across_a_capture},
     {"order_after_a_capture_in_place", order_after_a_capture_in_place},
     {"synchronize_across_a_capture", synchronize_across_a_capture},

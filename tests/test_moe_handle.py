@@ -14,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CHECKS = [
     "graph_keeps_its_block",
     "growing_while_captured",
+    "handles_beside_a_capture",
     "order_across_a_capture",
     "order_after_a_capture_in_place",
     "synchronize_across_a_capture",

@@ -273,3 +273,24 @@ def test_wait_that_runs_out_is_seen_by_the_next_call(moe, M):
             m.route(x[:, :8], 2)
         assert err.value.status == status
     m.close()
+
+
+def test_handles_made_and_closed_during_a_capture(moe):
+    """Neither ends the capture of another stream's work."""
+    m, spare = moe.Moe(), moe.Moe()
+    z = torch.randn(3000, 32, device="cuda")
+    r, want = m.routing(3000, 32, 3), spare.route(z, 3)
+    m.route(z, 3, out=r)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spare.close()
+        new = moe.Moe()
+        m.route(z, 3, out=r)
+    r.rows.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(r.rows, want.rows) and torch.equal(new.route(z, 3).rows, want.rows)
+    new.close()
+    del graph
+    m.close()
