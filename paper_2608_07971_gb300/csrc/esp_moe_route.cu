@@ -3,10 +3,11 @@
 //
 // A warp holds one token's row in registers, lane l the elements c * 32 V + l V .. + V - 1 of chunk c (V
 // elements = one load of up to 16 bytes), so a row is read once, coalesced, and the statistics are
-// warp reductions. The bytes are few (16384 x 256 bf16: 8.4 MB, 1.3 us); what bounds the choice is
-// instruction issue (about 790 per token at k = 8: 15 us, and 5 of plan), the losses (10 us and 6 to join
-// the parts) and the gradients (8 us from the weights, 12 from the losses) the chain of a warp's tokens, each
-// fetched while the one before is worked on.
+// warp reductions. The bytes are few (16384 x 256 bf16: 8.4 MB, 1.3 us). At that size and k = 8 the choice takes
+// 15 us, its plan 5: 783 warp instructions per token fill 52% of the issue slots, the rest goes to a token's chain of
+// dependent reductions (half of the SM's warps are there to hide it) and to the barriers around a CTA's tokens. The
+// losses (10 us and 6 to join the parts) and the gradients (8 us from the weights, 12 from the losses) are bound by the
+// chain of a warp's tokens, each fetched while the one before is worked on (issue slots 29 to 37% full).
 
 #include <algorithm>
 #include <cfloat>
