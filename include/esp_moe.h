@@ -14,6 +14,9 @@
  *   esp_moe_linear_backward  gradients of the rows and of the weights
  *   esp_moe_combine          the experts' rows, weighted and summed back into their tokens
  *   esp_moe_combine_backward gradients of the rows and of the gate weights
+ *   esp_moe_feed_forward          gated feed-forward blocks of the experts (or one dense block) in 16 bits
+ *   esp_moe_feed_forward_backward gradients of their rows and weights
+ *   esp_moe_clip                  norm of many gradient tensors together, and their clipping
  *
  * Conventions are those of esp.h: every function returns an esp_status and no exception crosses the
  * boundary; every data pointer here is a CUDA device pointer on the handle's device, owned by the
@@ -164,6 +167,65 @@ esp_status esp_moe_combine(esp_moe *m, int32_t dtype, int64_t T, int32_t k, int3
 esp_status esp_moe_combine_backward(esp_moe *m, int32_t dtype, int64_t T, int32_t k, int32_t H, int64_t M, int64_t lddo,
                                     const void *dout, int64_t ldy, const void *y, const int32_t *pos,
                                     const float *weight, int64_t lddy, void *dy, float *dweight);
+
+/* Gated feed-forward blocks of E experts in 16 bits: y = O (act(G x) * (U x)).
+ *   inner  E x 2 F x H: G (F rows), then U (F rows), rows ld_inner elements apart, halves F and experts 2 F rows apart
+ *   outer  E x H x F: O, rows ld_outer elements apart, experts H rows apart
+ * Both are 16-byte aligned, ld_inner and ld_outer multiples of 8; elements between a row's end and the next row are not
+ * read. dtype (ESP_MOE_BF16 or ESP_MOE_F16) is the type of the weights and of all rows. */
+typedef enum { ESP_MOE_SILU = 0, ESP_MOE_GELU = 1, ESP_MOE_GELU_TANH = 2, ESP_MOE_RELU = 3 } esp_moe_activation;
+typedef struct {
+    int32_t dtype, activation;   /* GELU: g Phi(g); GELU_TANH: its approximation by tanh */
+    int32_t E, F, H;
+    int64_t ld_inner, ld_outer;
+    const void *inner, *outer;
+} esp_moe_gated;
+
+/* What a forward pass keeps for its gradients, in memory of the caller, 16-byte aligned; F8 and H8 are F and H rounded up
+ * to a multiple of 8:
+ *   pre     M x 2 x F8: G x and U x        hidden  M x F8: act(G x) * (U x)
+ *   rows    M x H8: the rows, where they are gathered or x is not laid out for the tensor cores' loads (its address a
+ *           multiple of 16 bytes and ldx of 8); may be NULL otherwise
+ *   copied  set by the forward pass: whether it filled `rows` */
+typedef struct {
+    void *pre, *hidden, *rows;
+    int32_t copied;
+} esp_moe_kept;
+
+/* y[i] = O_e (act(G_e x[rows[i]]) * (U_e x[rows[i]])) for the rows i of expert e; x, M, rows, offsets and what is left as
+ * it was as in esp_moe_linear. Both inner products and the hidden row are summed and computed in fp32; the hidden row is
+ * rounded to 16 bits once, as the outer product's operand. kept NULL: nothing is kept. y must not overlap what the call
+ * reads.
+ * Errors: ESP_ERR_INVALID_ARG (F, H <= 2^22; E x F <= 2^30; fp32 rows, as the tensor cores would round them). */
+esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x, int64_t M,
+                                const int32_t *rows, const int32_t *offsets, int64_t ldy, void *y, esp_moe_kept *kept);
+
+/* Gradients of esp_moe_feed_forward at dy (M x H), with the same x, rows, offsets and weights and what that call kept:
+ * dx (M x H, or NULL), one row for each of y's (rows of no expert are not written), dinner (E x 2 F x H, contiguous, or
+ * NULL) and douter (E x H x F, contiguous, or NULL), these two in dw_dtype: the rows' type, or ESP_MOE_F32. An expert
+ * without rows has dinner and douter 0. The gradients of G x and U x are rounded to 16 bits once, as operands. */
+esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x,
+                                         int64_t M, const int32_t *rows, const int32_t *offsets, const esp_moe_kept *kept,
+                                         int64_t lddy, const void *dy, int64_t lddx, void *dx, int32_t dw_dtype,
+                                         void *dinner, void *douter);
+
+/* One of many gradient tensors: n contiguous elements of any alignment of their size; out NULL (counted in the norm, not
+ * written), `grad` itself, or other memory. */
+typedef struct {
+    const void *grad;
+    void *out;
+    int64_t n;
+    int32_t dtype;   /* esp_moe_dtype */
+} esp_moe_tensor;
+
+/* norm (1 fp32, on the device) = scale * sqrt(sum of squares over all elements of all tensors); out = grad * scale *
+ * min(1, max_norm / norm), rounded once. scale is the inverse of a loss scale, 1 without. Where the norm is not finite,
+ * out = grad * scale, and the program skips its step by the norm. The sum is in fp64 (fp32 within a thread's 64
+ * elements); max_norm infinity: no clipping. `tensors` (on the host) is read during the call.
+ * Errors: ESP_ERR_INVALID_ARG (max_norm > 0, scale > 0 and finite, 0 <= n <= 2^40, 2^45 bytes in all; memory that is written
+ * for one tensor and read or written for another). */
+esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, double max_norm, double scale,
+                        float *norm);
 
 /* Waits for the handle's work on all streams (not for graphs that the program launches: it waits
  * for those itself first) and reports a device-side failure of the queued work: ESP_ERR_TIMEOUT

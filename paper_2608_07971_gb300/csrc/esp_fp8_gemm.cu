@@ -27,12 +27,11 @@
 
 #include <algorithm>
 
-#include <cuda.h>
-
 #include "esp_fp8_tiles.cuh"
 #include "esp_moe_impl.h"
 #include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
+#include "esp_tcgen.cuh"
 
 namespace esp_moe_impl {
 
@@ -66,51 +65,11 @@ struct Shape {
     static_assert((2 * kStages + 3 * kAcc + 1) * 8 + 16 <= kBars, "barriers");
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p)
-{
-    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-
-// Address of the same shared-memory location in CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-}
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
 // Arrival on a barrier of this CTA or, through its cluster address, of another. Relaxed: it orders the
 // tensor-memory loads before it, which have completed; a release would wait for unrelated stores.
 __device__ __forceinline__ void mbar_arrive(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
-__device__ __forceinline__ void mbar_arrive_cta(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // PAIR: a barrier at which another CTA's threads arrive (mbar_arrive); what orders their tensor-memory loads before the
@@ -138,13 +97,6 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     return done != 0;
 }
 
-__device__ __forceinline__ uint64_t global_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-
 // Waits for a phase for at most `ms` milliseconds of the GPU's timer, which is read once in 256 polls.
 template <bool PAIR = false>
 __device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
@@ -162,15 +114,6 @@ __device__ __forceinline__ bool mbar_wait_ms(uint32_t bar, uint32_t parity, uint
         else if (now >= end)
             return false;
     }
-}
-
-// One thread of a whole warp, the same at every call. What the warp computes stays in uniform registers, which
-// the MMA and TMA instructions read; a branch on a lane number moves every operand there first.
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
 }
 
 // Bounded wait of a role; gives up early once another wait of the CTA did. On running out it sets the CTA's
@@ -225,63 +168,6 @@ __device__ __forceinline__ void mma_codes(uint32_t d, uint64_t a, uint64_t b, ui
             "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
             "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
             : "memory");
-}
-
-// The barrier (of every CTA that shares the MMAs) completes when the MMAs issued so far have.
-template <int CG>
-__device__ __forceinline__ void mma_commit(uint32_t bar)
-{
-    if (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-                     : "memory");
-    else
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-                bar),
-            "h"((uint16_t)3)
-            : "memory");
-}
-
-__device__ __forceinline__ void fence_after()
-{
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-
-__device__ __forceinline__ void fence_before()
-{
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-
-// Starts the load of 16 consecutive 32-bit columns of this thread's TMEM lane. The registers hold them after
-// tmem_wait, which names them so that no use of theirs moves before it.
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-        "%15}, [%16];"
-        :
-          "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr)
-        : "memory");
-}
-
-__device__ __forceinline__ void pin16(uint32_t (&r)[16])
-{
-    asm volatile(""
-                 :
-                   "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
-                   "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
-                   "+r"(r[14]), "+r"(r[15]));
-}
-
-template <int N>
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[N][16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int h = 0; h < N; ++h)
-        pin16(r[h]);
 }
 
 // (c, d) += (a, b) * (s, t) and (a, b) *= s, each one instruction on pairs of registers.
@@ -767,27 +653,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // ---- launches
-
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// cuTensorMapEncodeTiled of the driver in use (null if it has none).
-EncodeTiled encode_tiled()
-{
-    static const EncodeTiled fn = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) !=
-                cudaSuccess ||
-            found != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return fn;
-}
 
 // Boxes of box_rows rows and 128 bytes of a matrix of elements of 1, 2 or 4 bytes; what a load finds outside
 // is zero, what a store has outside is dropped.

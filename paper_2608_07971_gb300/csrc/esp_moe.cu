@@ -12,9 +12,6 @@ using namespace esp_moe_impl;
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffff00;   // row counts fit int32 with a tile to spare
-constexpr int64_t kMaxTiles = 1 << 29;
-
 esp_status fail(esp_moe *m)
 {
     cudaGetLastError();
@@ -189,7 +186,6 @@ bool good_product(int64_t T, int64_t M, const int32_t *rows, const esp_moe_weigh
     if (!good_weight(w) || T < 0 || M < 0 || T > kMaxRows || M > kMaxRows || (!rows && M != T) ||
         (!offsets && w->E != 1))
         return false;
-    // the kernels number their tiles in int32
     const int64_t nb = ceil_div(w->N, kBlock), kb = ceil_div(w->K, kBlock);
     return (M / kBlock + w->E) * std::max(nb, kb) <= kMaxTiles && w->E * nb * kb <= kMaxTiles;
 }
@@ -200,6 +196,25 @@ int64_t round_up(int64_t v, int64_t to)
 }
 
 }  // namespace
+
+namespace esp_moe_impl {
+
+esp_status begin_call(esp_moe *m)
+{
+    return begin(m);
+}
+
+esp_status reserve_space(esp_moe *m, size_t bytes)
+{
+    return reserve(m, bytes);
+}
+
+esp_status fail_call(esp_moe *m)
+{
+    return fail(m);
+}
+
+}  // namespace esp_moe_impl
 
 extern "C" {
 

@@ -1,0 +1,394 @@
+// Norm of many gradient tensors together and their clipping (include/esp_moe.h: esp_moe_clip).
+//
+// norm = |scale| sqrt(sum g^2) over all elements of all tensors; out = g * factor, factor = scale min(1, max_norm / norm)
+// (scale where the norm is not finite). Two passes, as the factor needs every element: k_norm reads all, k_scale reads
+// again and writes. Bound by HBM. The tensors are cut into chunks of 16-byte groups that the CTAs take in turn; k_scale
+// takes them from the last to the first, so that it begins with what k_norm left in L2.
+//
+// A thread sums the squares of a chunk's groups in fp32 (at most 64 of them), then adds that to its sum in fp64; the
+// threads', CTAs' and launches' sums are joined in a fixed order in fp64. Squares of values that fp32 does not hold
+// (above 2^60, or all below 2^-50) are summed again in fp64.
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "esp_moe_impl.h"
+#include "esp_moe_launch.cuh"
+#include "esp_moe_load.cuh"
+
+namespace esp_moe_impl {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kCtasPerSm = 4;
+constexpr int kBatch = 144;       // tensors of a launch, in its parameters
+constexpr int64_t kMostBytes = (int64_t)1 << 45;   // of all tensors; keeps a launch's chunks in int32
+
+struct ClipTensor {
+    const void *grad;
+    void *out;
+    int64_t n;
+};
+
+struct ClipArgs {
+    ClipTensor t[kBatch];
+    int32_t first[kBatch];        // first chunk of each tensor
+    uint8_t dtype[kBatch];
+    int32_t count, chunks;
+};
+
+struct NormArgs {
+    double *partial;              // one for each CTA of every launch
+    int32_t base, total;          // this launch's first partial; all of them in the last launch, else 0
+    unsigned int *ticket;
+    double max_norm, scale;
+    float *norm;
+    float *factor;
+};
+
+// Elements before the first of a tensor in its first 16-byte group.
+template <typename T>
+__device__ __forceinline__ int lead(const void *p)
+{
+    return (int)(reinterpret_cast<uintptr_t>(p) % 16) / (int)sizeof(T);
+}
+
+template <typename T>
+constexpr int kPer = 16 / (int)sizeof(T);
+
+// The tensor whose chunks hold `chunk`.
+__device__ __forceinline__ int tensor_of(const ClipArgs &a, int chunk)
+{
+    int lo = 0, hi = a.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.first[mid] <= chunk)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// Group g of a tensor (groups are aligned in memory; the first and last may hold fewer elements): zeros where it has none.
+template <typename T>
+__device__ __forceinline__ uint4 load_group(const ClipTensor &t, int64_t g, int skip)
+{
+    uint4 r = make_uint4(0, 0, 0, 0);
+    const int64_t i = g * kPer<T> - skip;   // element
+    const T *p = static_cast<const T *>(t.grad) + i;
+    if (i >= 0 && i + kPer<T> <= t.n) {
+        r = *reinterpret_cast<const uint4 *>(p);
+    } else if (i < t.n) {
+        T v[kPer<T>];
+        memcpy(v, &r, 16);
+#pragma unroll
+        for (int j = 0; j < kPer<T>; ++j)
+            if (i + j >= 0 && i + j < t.n)
+                v[j] = p[j];
+        memcpy(&r, v, 16);
+    }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4 &r, float (&f)[kPer<T>])
+{
+    T v[kPer<T>];
+    memcpy(v, &r, 16);
+#pragma unroll
+    for (int j = 0; j < kPer<T>; ++j)
+        f[j] = to_f32(v[j]);
+}
+
+// This thread's squares in U groups from g0 + threadIdx.x on, kThreads apart.
+template <typename T, int U>
+__device__ __forceinline__ double square_chunk(const ClipTensor &t, int64_t g0)
+{
+    const int skip = lead<T>(t.grad);
+    uint4 r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        r[u] = load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip);
+    float s = 0.0f;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[kPer<T>];
+        unpack<T>(r[u], f);
+        float q = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kPer<T>; ++j)
+            q = fmaf(f[j], f[j], q);
+        s += q;
+        bits |= r[u].x | r[u].y | r[u].z | r[u].w;
+    }
+    bits &= sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
+    if (s < 0x1p120f && (s > 0x1p-90f || bits == 0))
+        return (double)s;
+    double d = 0.0;
+    for (int u = 0; u < U; ++u) {
+        float f[kPer<T>];
+        unpack<T>(load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip), f);
+        for (int j = 0; j < kPer<T>; ++j)
+            d += (double)f[j] * (double)f[j];
+    }
+    return d;
+}
+
+// Sum over the CTA, in thread 0.
+__device__ __forceinline__ double sum_of_cta(double v, double *warps)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        v += __shfl_down_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0)
+        warps[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kThreads / 32; ++w)
+            v += warps[w];
+    return v;
+}
+
+template <int U>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const __grid_constant__ ClipArgs a, const NormArgs n)
+{
+    __shared__ double warps[kThreads / 32];
+    __shared__ bool last;
+    wait_for_launch_before();
+    double sum = 0.0;
+    for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        const int i = tensor_of(a, c);
+        const ClipTensor &t = a.t[i];
+        const int64_t g0 = (int64_t)(c - a.first[i]) * (U * kThreads);
+        sum += a.dtype[i] == ESP_MOE_F32    ? square_chunk<float, U>(t, g0)
+               : a.dtype[i] == ESP_MOE_BF16 ? square_chunk<__nv_bfloat16, U>(t, g0)
+                                            : square_chunk<__half, U>(t, g0);
+    }
+    sum = sum_of_cta(sum, warps);
+    if (threadIdx.x == 0) {
+        n.partial[n.base + blockIdx.x] = sum;
+        last = false;
+        if (n.total > 0) {
+            __threadfence();
+            last = atomicAdd(n.ticket, 1u) == gridDim.x - 1;
+        }
+    }
+    __syncthreads();
+    if (!last)
+        return;
+    __threadfence();
+    sum = 0.0;
+    for (int i = threadIdx.x; i < n.total; i += kThreads)
+        sum += __ldcg(n.partial + i);
+    sum = sum_of_cta(sum, warps);
+    if (threadIdx.x == 0) {
+        *n.ticket = 0u;
+        const double norm = fabs(n.scale) * sqrt(sum);
+        const double less = norm > n.max_norm && norm < (double)INFINITY ? n.max_norm / norm : 1.0;
+        *n.norm = (float)norm;
+        *n.factor = (float)(n.scale * less);
+    }
+}
+
+template <typename T, int U>
+__device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, float by)
+{
+    if (!t.out || (by == 1.0f && t.out == t.grad))
+        return;
+    const int skip = lead<T>(t.grad);
+    const bool same = lead<T>(t.out) == skip;   // groups of `out` are aligned too
+    uint4 r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        r[u] = load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = (g0 + u * kThreads + threadIdx.x) * kPer<T> - skip;
+        if (i >= t.n)
+            break;
+        T *out = static_cast<T *>(t.out) + i;
+        float f[kPer<T>];
+        unpack<T>(r[u], f);
+        T v[kPer<T>];
+#pragma unroll
+        for (int j = 0; j < kPer<T>; ++j)
+            v[j] = from_f32<T>(f[j] * by);
+        if (same && i >= 0 && i + kPer<T> <= t.n) {
+            uint4 w;
+            memcpy(&w, v, 16);
+            *reinterpret_cast<uint4 *>(out) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j)
+                if (i + j >= 0 && i + j < t.n)
+                    out[j] = v[j];
+        }
+    }
+}
+
+template <int U>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_scale(const __grid_constant__ ClipArgs a, const float *factor)
+{
+    wait_for_launch_before();
+    const float by = *factor;
+    for (int c = a.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+        const int i = tensor_of(a, c);
+        const ClipTensor &t = a.t[i];
+        const int64_t g0 = (int64_t)(c - a.first[i]) * (U * kThreads);
+        if (a.dtype[i] == ESP_MOE_F32)
+            scale_chunk<float, U>(t, g0, by);
+        else if (a.dtype[i] == ESP_MOE_BF16)
+            scale_chunk<__nv_bfloat16, U>(t, g0, by);
+        else
+            scale_chunk<__half, U>(t, g0, by);
+    }
+}
+
+int size_of(int32_t dtype)
+{
+    return dtype == ESP_MOE_F32 ? 4 : 2;
+}
+
+// Chunks of a tensor, U groups for each of a CTA's threads.
+int64_t chunks_of(const esp_moe_tensor &t, int U)
+{
+    const int size = size_of(t.dtype);
+    const int64_t skip = (int64_t)(reinterpret_cast<uintptr_t>(t.grad) % 16) / size;
+    return ceil_div(ceil_div(t.n + skip, 16 / size), (int64_t)U * kThreads);
+}
+
+bool good_tensor(const esp_moe_tensor &t)
+{
+    if (t.dtype != ESP_MOE_F32 && t.dtype != ESP_MOE_BF16 && t.dtype != ESP_MOE_F16)
+        return false;
+    const int size = size_of(t.dtype);
+    return t.n >= 0 && t.n <= (int64_t)1 << 40 && (t.n == 0 || t.grad) &&
+           reinterpret_cast<uintptr_t>(t.grad) % size == 0 && reinterpret_cast<uintptr_t>(t.out) % size == 0;
+}
+
+// Whether some memory is written for one tensor and read or written for another.
+bool overlapping(int32_t count, const esp_moe_tensor *tensors)
+{
+    struct Range {
+        uintptr_t lo, hi;
+        bool written;
+    };
+    std::vector<Range> all;
+    all.reserve(2 * (size_t)count);
+    for (int32_t i = 0; i < count; ++i) {
+        const esp_moe_tensor &t = tensors[i];
+        if (t.n == 0)
+            continue;
+        const uintptr_t bytes = (uintptr_t)t.n * size_of(t.dtype);
+        const uintptr_t g = reinterpret_cast<uintptr_t>(t.grad), o = reinterpret_cast<uintptr_t>(t.out);
+        all.push_back(Range{g, g + bytes, g == o});
+        if (o && o != g)
+            all.push_back(Range{o, o + bytes, true});
+    }
+    std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+    // ends of what came before: of all of it, and of what is written
+    uintptr_t end = 0, end_written = 0;
+    for (const Range &r : all) {
+        if (r.lo < end_written || (r.written && r.lo < end))
+            return true;
+        end = std::max(end, r.hi);
+        if (r.written)
+            end_written = std::max(end_written, r.hi);
+    }
+    return false;
+}
+
+template <int U>
+cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, NormArgs n, bool write)
+{
+    const int most = kCtasPerSm * m->sm_count;
+    ClipArgs a;
+    for (int pass = 0; pass < (write ? 2 : 1); ++pass) {
+        n.base = 0;
+        int32_t at = 0;
+        for (bool more = true; more;) {
+            a.count = a.chunks = 0;
+            for (; at < count && a.count < kBatch; ++at) {
+                const esp_moe_tensor &t = tensors[at];
+                const int64_t chunks = t.n == 0 || (pass == 1 && !t.out) ? 0 : chunks_of(t, U);
+                if (chunks == 0)
+                    continue;
+                a.t[a.count] = ClipTensor{t.grad, t.out, t.n};
+                a.first[a.count] = a.chunks;
+                a.dtype[a.count] = (uint8_t)t.dtype;
+                a.chunks += (int32_t)chunks;
+                a.count += 1;
+            }
+            more = at < count;
+            if (pass == 1 && a.chunks == 0)
+                break;
+            const int grid = std::max(1, std::min(most, a.chunks));
+            n.total = pass == 0 && !more ? n.base + grid : 0;
+            m->launches += 1;
+            const cudaError_t e = pass == 0 ? launch_after(k_norm<U>, dim3(grid), kThreads, 0, m->stream, a, n)
+                                            : launch_after(k_scale<U>, dim3(grid), kThreads, 0, m->stream, a,
+                                                           (const float *)n.factor);
+            if (e != cudaSuccess)
+                return e;
+            n.base += grid;
+        }
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+}  // namespace esp_moe_impl
+
+using namespace esp_moe_impl;
+
+extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, double max_norm, double scale,
+                                   float *norm)
+{
+    esp_status st = begin_call(m);
+    if (st != ESP_OK)
+        return st;
+    if (count < 0 || (count > 0 && !tensors) || !norm || !(max_norm > 0.0) || !(scale > 0.0) || !std::isfinite(scale))
+        return ESP_ERR_INVALID_ARG;
+    bool write = false;
+    int64_t bytes = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (!good_tensor(tensors[i]))
+            return ESP_ERR_INVALID_ARG;
+        write = write || (tensors[i].out && tensors[i].n > 0);
+        bytes += tensors[i].n * size_of(tensors[i].dtype);
+        if (bytes > kMostBytes)
+            return ESP_ERR_INVALID_ARG;
+    }
+    try {
+        if (write && overlapping(count, tensors))
+            return ESP_ERR_INVALID_ARG;
+    } catch (const std::bad_alloc &) {
+        return ESP_ERR_OOM;
+    }
+    NormArgs n{};
+    const size_t launches = (size_t)count / kBatch + 1;
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        n.factor = c.take<float>(1);
+        n.partial = c.take<double>((size_t)kCtasPerSm * m->sm_count * launches);
+        if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
+            return st;
+    }
+    n.ticket = m->d_ticket;
+    n.max_norm = max_norm;
+    n.scale = scale;
+    n.norm = norm;
+    // few bytes: two groups a thread, so that every SM has some; else eight in flight
+    const bool few = bytes < (int64_t)m->sm_count * kCtasPerSm * kThreads * 8 * 16;
+    const cudaError_t e = few ? launch_clip<2>(m, count, tensors, n, write) : launch_clip<8>(m, count, tensors, n, write);
+    return e == cudaSuccess ? ESP_OK : fail_call(m);
+}

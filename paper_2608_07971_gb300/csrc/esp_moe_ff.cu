@@ -1,0 +1,203 @@
+// C entry points of the gated feed-forward blocks (include/esp_moe.h), and the copy of rows that tensor maps cannot read
+// where they lie.
+
+#include <algorithm>
+
+#include "esp_moe_ff_impl.h"
+#include "esp_moe_launch.cuh"
+#include "esp_moe_load.cuh"
+
+namespace esp_moe_impl {
+
+namespace {
+
+constexpr int kCopyThreads = 256;
+
+// A CTA copies a row's 16-byte groups; bound by HBM. V: elements that a source row allows to load at once.
+template <int V>
+__global__ void __launch_bounds__(kCopyThreads) k_copy_rows(const CopyRowsArgs a)
+{
+    let_next_launch_start();
+    wait_for_launch_before();
+    const int64_t i = blockIdx.x;
+    const int64_t from = a.rows ? a.rows[i] : i;
+    const bool there = from >= 0 && from < a.T;
+    const uint16_t *x = static_cast<const uint16_t *>(a.x) + from * a.ldx;
+    uint16_t *out = static_cast<uint16_t *>(a.out) + i * a.ldo;
+    for (int h = (blockIdx.y * kCopyThreads + threadIdx.x) * 8; h < a.H; h += gridDim.y * kCopyThreads * 8) {
+        Pack<uint16_t, 8> r = {};
+        if (there) {
+            if constexpr (V == 8) {
+                r = *reinterpret_cast<const Pack<uint16_t, 8> *>(x + h);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (h + j < a.H)
+                        r.v[j] = x[h + j];
+            }
+        }
+        *reinterpret_cast<Pack<uint16_t, 8> *>(out + h) = r;   // a row of `out` is whole groups of 8
+    }
+}
+
+int64_t up8(int64_t n)
+{
+    return (n + 7) / 8 * 8;
+}
+
+bool aligned_to(const void *p, size_t bytes)
+{
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0;
+}
+
+bool good_blocks(const esp_moe_gated *w)
+{
+    constexpr int64_t kMostBytes = (int64_t)1 << 40;   // steps of a tensor map
+    return w && (w->dtype == ESP_MOE_BF16 || w->dtype == ESP_MOE_F16) && w->activation >= ESP_MOE_SILU &&
+           w->activation <= ESP_MOE_RELU && w->E >= 1 && w->E <= ESP_MOE_MAX_EXPERTS && w->F >= 1 && w->H >= 1 &&
+           w->F <= (1 << 22) && w->H <= (1 << 22) && (int64_t)w->E * w->F <= kMaxRows / 2 &&
+           (int64_t)w->E * w->H <= kMaxRows && w->inner && w->outer && w->ld_inner >= w->H && w->ld_outer >= w->F &&
+           w->ld_inner % 8 == 0 && w->ld_outer % 8 == 0 && aligned_to(w->inner, 16) && aligned_to(w->outer, 16) &&
+           w->ld_inner < kMostBytes / 2 / w->F && w->ld_outer < kMostBytes / 2 / w->H;
+}
+
+bool good_rows(const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x, int64_t M, const int32_t *rows,
+               const int32_t *offsets)
+{
+    if (!good_blocks(w) || T < 0 || M < 0 || T > kMaxRows || M > kMaxRows || (!rows && M != T) ||
+        (!offsets && w->E != 1) || ldx < w->H || ldx >= (int64_t)1 << 39 || (M > 0 && T > 0 && !x) || !aligned_to(x, 2))
+        return false;
+    return (M / 256 + w->E) * ceil_div(std::max(w->F, w->H), 128) <= kMaxTiles &&
+           2 * (int64_t)w->E * ceil_div(w->F, 256) * ceil_div(w->H, 256) <= kMaxTiles;
+}
+
+bool good_kept(const esp_moe_kept *k, bool copied)
+{
+    return k->pre && k->hidden && aligned_to(k->pre, 16) && aligned_to(k->hidden, 16) &&
+           (!copied || (k->rows && aligned_to(k->rows, 16)));
+}
+
+// Whether a tensor map can read the rows in place.
+bool mappable(const void *x, int64_t ldx)
+{
+    return rows_aligned(x, ldx, 2, 16);
+}
+
+FfShape shape_of(const esp_moe_gated *w, int64_t M, const int32_t *offsets)
+{
+    return FfShape{w->dtype, w->activation, w->E, w->F, w->H, M, offsets, w->inner, w->outer, w->ld_inner, w->ld_outer,
+                   up8(w->F)};
+}
+
+}  // namespace
+
+cudaError_t launch_copy_rows(esp_moe *m, const CopyRowsArgs &a)
+{
+    if (a.M == 0)
+        return cudaSuccess;
+    const bool wide = rows_aligned(a.x, a.ldx, 2, 16) && a.H % 8 == 0;
+    const dim3 grid((unsigned)a.M, (unsigned)std::min<int64_t>(64, ceil_div(a.H, 8 * kCopyThreads)));
+    m->launches += 1;
+    return wide ? launch_after(k_copy_rows<8>, grid, kCopyThreads, 0, m->stream, a)
+                : launch_after(k_copy_rows<1>, grid, kCopyThreads, 0, m->stream, a);
+}
+
+}  // namespace esp_moe_impl
+
+using namespace esp_moe_impl;
+
+#define MOE_CUDA(call)               \
+    do {                             \
+        if ((call) != cudaSuccess)   \
+            return fail_call(m);     \
+    } while (0)
+
+extern "C" {
+
+esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x, int64_t M,
+                                const int32_t *rows, const int32_t *offsets, int64_t ldy, void *y, esp_moe_kept *kept)
+{
+    esp_status st = begin_call(m);
+    if (st != ESP_OK)
+        return st;
+    const bool copied = rows || !mappable(x, ldx);
+    if (!good_rows(w, T, ldx, x, M, rows, offsets) || ldy < w->H || ldy >= (int64_t)1 << 39 || (M > 0 && !y) ||
+        !aligned_to(y, 2) || (kept && M > 0 && !good_kept(kept, copied)))
+        return ESP_ERR_INVALID_ARG;
+    if (kept)
+        kept->copied = copied;
+    if (M == 0)
+        return ESP_OK;
+    const FfShape s = shape_of(w, M, offsets);
+    const int64_t hp = up8(w->H);
+    void *hidden = nullptr, *gathered = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        hidden = kept ? kept->hidden : c.take<uint16_t>((size_t)(M * s.fp));
+        if (copied)
+            gathered = kept ? kept->rows : c.take<uint16_t>((size_t)(M * hp));
+        if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
+            return st;
+    }
+    if (copied)
+        MOE_CUDA(launch_copy_rows(m, CopyRowsArgs{M, T, ldx, hp, w->H, x, rows, gathered}));
+    MOE_CUDA(launch_ff_hidden(m, s, copied ? gathered : x, copied ? hp : ldx, hidden, kept ? kept->pre : nullptr));
+    MOE_CUDA(launch_ff_out(m, s, hidden, y, ldy));
+    return ESP_OK;
+}
+
+esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x,
+                                         int64_t M, const int32_t *rows, const int32_t *offsets, const esp_moe_kept *kept,
+                                         int64_t lddy, const void *dy, int64_t lddx, void *dx, int32_t dw_dtype,
+                                         void *dinner, void *douter)
+{
+    esp_status st = begin_call(m);
+    if (st != ESP_OK)
+        return st;
+    const bool copied = kept && kept->copied;
+    if (!good_rows(w, T, ldx, x, M, rows, offsets) || !kept || (M > 0 && !good_kept(kept, copied)) ||
+        (M > 0 && !copied && (rows || !mappable(x, ldx))) || lddy < w->H || lddy >= (int64_t)1 << 39 || (M > 0 && !dy) ||
+        !aligned_to(dy, 2) || (dx && (lddx < w->H || lddx >= (int64_t)1 << 39 || !aligned_to(dx, 2))) ||
+        (dw_dtype != w->dtype && dw_dtype != ESP_MOE_F32))
+        return ESP_ERR_INVALID_ARG;
+    const bool f32 = dw_dtype == ESP_MOE_F32;
+    if (!aligned_to(dinner, f32 ? 4 : 2) || !aligned_to(douter, f32 ? 4 : 2))
+        return ESP_ERR_INVALID_ARG;
+    if (M == 0) {
+        const size_t n = (size_t)w->E * w->F * w->H * (f32 ? 4 : 2);
+        if (dinner)
+            MOE_CUDA(cudaMemsetAsync(dinner, 0, 2 * n, m->stream));
+        if (douter)
+            MOE_CUDA(cudaMemsetAsync(douter, 0, n, m->stream));
+        return ESP_OK;
+    }
+    const FfShape s = shape_of(w, M, offsets);
+    const int64_t hp = up8(w->H);
+    const bool copy_dy = !mappable(dy, lddy), want_dpre = dx || dinner;
+    void *dpre = nullptr, *dy_copy = nullptr;
+    for (int pass = 0; pass < 2; ++pass) {
+        Carver c(m->ws);
+        if (want_dpre)
+            dpre = c.take<uint16_t>((size_t)(2 * M * s.fp));
+        if (copy_dy)
+            dy_copy = c.take<uint16_t>((size_t)(M * hp));
+        if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
+            return st;
+    }
+    if (copy_dy) {
+        MOE_CUDA(launch_copy_rows(m, CopyRowsArgs{M, M, lddy, hp, w->H, dy, nullptr, dy_copy}));
+        dy = dy_copy;
+        lddy = hp;
+    }
+    if (want_dpre)
+        MOE_CUDA(launch_ff_dpre(m, s, dy, lddy, kept->pre, dpre));
+    if (dx)
+        MOE_CUDA(launch_ff_dx(m, s, dpre, dx, lddx));
+    if (dinner)
+        MOE_CUDA(launch_ff_dinner(m, s, dpre, copied ? kept->rows : x, copied ? hp : ldx, dinner, f32));
+    if (douter)
+        MOE_CUDA(launch_ff_douter(m, s, dy, lddy, kept->hidden, douter, f32));
+    return ESP_OK;
+}
+
+}  // extern "C"

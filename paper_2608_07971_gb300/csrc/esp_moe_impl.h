@@ -43,6 +43,16 @@ struct esp_moe {
 namespace esp_moe_impl {
 
 constexpr int kBlock = ESP_MOE_BLOCK;
+constexpr int64_t kMaxRows = 0x7fffff00;   // row counts fit int32 with a tile to spare
+constexpr int64_t kMaxTiles = 1 << 29;     // the kernels number their tiles in int32
+
+// ---- esp_moe.cu, for the entry points in other files
+// Head of a call that queues work: the handle's state, its place among the earlier calls, no launches yet.
+esp_status begin_call(esp_moe *m);
+// At least `bytes` of work space at m->ws.
+esp_status reserve_space(esp_moe *m, size_t bytes);
+// A CUDA call failed: the handle takes no more work.
+esp_status fail_call(esp_moe *m);
 constexpr int kTickets = 1 + 256;   // the losses', and one per tile of a split product (fewer tiles than SMs)
 
 // Carves the handle's work space into 256-byte aligned parts.

@@ -12,6 +12,14 @@ uses the handle's work space, so the handle is kept as long as the graph is repl
     y = m.linear(act(h), w2, offsets=r.offsets)
     out = m.combine(y, r.pos, r.weight)
     m.step_prices(prices, r.counts, eta=0.02)
+
+or, with 16-bit weights and a gated block for each expert, and for a training step:
+
+    w = m.gated_weight(inner, outer, "silu")                         # (E, 2 F, H) and (E, H, F)
+    kept = m.keep(r.rows.shape[0], w)
+    y = m.feed_forward(x, w, offsets=r.offsets, rows=r.rows, keep=kept)
+    dx, dinner, douter = m.feed_forward_backward(dy, x, w, kept, offsets=r.offsets, rows=r.rows)
+    norm = m.clip([dinner, douter, drouter], max_norm=1.0)           # in place
 """
 
 from __future__ import annotations
@@ -19,6 +27,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import dataclasses
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -32,11 +41,13 @@ EXPORTED = [
     "esp_moe_create", "esp_moe_set_stream", "esp_moe_route", "esp_moe_balance", "esp_moe_route_backward",
     "esp_moe_step_prices", "esp_moe_quantize_weight", "esp_moe_linear", "esp_moe_linear_backward", "esp_moe_combine",
     "esp_moe_combine_backward", "esp_moe_synchronize", "esp_moe_last_launch_count", "esp_moe_destroy",
-    "esp_moe_debug_set_wait_limit", "esp_moe_debug_hold_load",
+    "esp_moe_debug_set_wait_limit", "esp_moe_debug_hold_load", "esp_moe_feed_forward", "esp_moe_feed_forward_backward",
+    "esp_moe_clip",
 ]
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _KINDS = {"softmax": 0, "sigmoid": 1}
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 
 
 class _CGate(ctypes.Structure):
@@ -46,6 +57,20 @@ class _CGate(ctypes.Structure):
 class _CWeight(ctypes.Structure):
     _fields_ = [("E", ctypes.c_int32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("ld", ctypes.c_int64),
                 ("ldt", ctypes.c_int64), ("q", ctypes.c_void_p), ("qt", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class _CGated(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("E", ctypes.c_int32), ("F", ctypes.c_int32),
+                ("H", ctypes.c_int32), ("ld_inner", ctypes.c_int64), ("ld_outer", ctypes.c_int64),
+                ("inner", ctypes.c_void_p), ("outer", ctypes.c_void_p)]
+
+
+class _CKept(ctypes.Structure):
+    _fields_ = [("pre", ctypes.c_void_p), ("hidden", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("copied", ctypes.c_int32)]
+
+
+class _CTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
 
 
 _bound = None
@@ -59,6 +84,7 @@ def load_library():
         return lib
     vp, i32, i64, f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
     st, gate, weight = ctypes.c_int, ctypes.POINTER(_CGate), ctypes.POINTER(_CWeight)
+    gated, kept = ctypes.POINTER(_CGated), ctypes.POINTER(_CKept)
     sig = {
         "esp_moe_create": ([ctypes.POINTER(vp), ctypes.c_int, vp], st),
         "esp_moe_set_stream": ([vp, vp], st),
@@ -71,6 +97,9 @@ def load_library():
         "esp_moe_linear_backward": ([vp, i32, i64, i64, vp, i64, vp, weight, vp, i64, vp, i64, vp, i64, vp], st),
         "esp_moe_combine": ([vp, i32, i64, i32, i32, i64, i64, vp, vp, vp, i64, vp], st),
         "esp_moe_combine_backward": ([vp, i32, i64, i32, i32, i64, i64, vp, i64, vp, vp, vp, i64, vp, vp], st),
+        "esp_moe_feed_forward": ([vp, gated, i64, i64, vp, i64, vp, vp, i64, vp, kept], st),
+        "esp_moe_feed_forward_backward": ([vp, gated, i64, i64, vp, i64, vp, vp, kept, i64, vp, i64, vp, i32, vp, vp], st),
+        "esp_moe_clip": ([vp, i32, ctypes.POINTER(_CTensor), f64, f64, vp], st),
         "esp_moe_synchronize": ([vp], st),
         "esp_moe_last_launch_count": ([vp, ctypes.POINTER(i64)], st),
         "esp_moe_destroy": ([vp], None),
@@ -185,12 +214,106 @@ class Weight:
         return self.q.view(torch.float8_e4m3fn)[:, :, :self.K]
 
 
+@dataclasses.dataclass
+class GatedWeight:
+    """16-bit weights of E gated feed-forward blocks: inner (E, 2 F, H), gate rows before up rows, and outer (E, H, F),
+    whose rows start at multiples of 16 bytes (``Moe.gated_weight`` lays out others). Both may be written to between calls."""
+
+    inner: torch.Tensor
+    outer: torch.Tensor
+    activation: str = "silu"
+
+    def __post_init__(self):
+        a, b = self.inner, self.outer
+        if self.activation not in _ACTIVATIONS:
+            raise ValueError(f"unknown activation {self.activation!r}")
+        if a.dim() != 3 or b.dim() != 3 or a.dtype not in (torch.bfloat16, torch.float16) or b.dtype is not a.dtype or \
+                a.device != b.device or a.shape[1] % 2 or b.shape != (a.shape[0], a.shape[2], a.shape[1] // 2) or \
+                a.numel() == 0 or not (_rows16(a) and _rows16(b)):
+            raise ValueError("gated weights: bf16 or fp16, inner (E, 2 F, H) and outer (E, H, F), rows on multiples of 16 bytes")
+        self.E, self.F, self.H = a.shape[0], b.shape[2], a.shape[2]
+        self._c = _CGated(_DTYPES[a.dtype], _ACTIVATIONS[self.activation], self.E, self.F, self.H, a.stride(1), b.stride(1),
+                          *self._places())
+        self._ref = ctypes.byref(self._c)
+        self._made_at = self._places()
+
+    __reduce__ = _from_fields
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name in ("inner", "outer", "activation"):
+            self._ref = None   # checked and made anew by the next call
+
+    def _places(self):
+        return self.inner.data_ptr(), self.outer.data_ptr()
+
+    def _arg(self):
+        if self._ref is None or self._places() != self._made_at:
+            self.__post_init__()
+        return self._ref
+
+
+@dataclasses.dataclass
+class Kept:
+    """What ``Moe.feed_forward`` keeps for its gradients (esp_moe_kept): pre (M, 2, F8), hidden (M, F8), rows (M, H8), with F
+    and H rounded up to multiples of 8. Made by ``Moe.keep``."""
+
+    pre: torch.Tensor
+    hidden: torch.Tensor
+    rows: torch.Tensor
+    copied: bool = False
+
+    def _arg(self):
+        return _CKept(self.pre.data_ptr(), self.hidden.data_ptr(), self.rows.data_ptr(), int(self.copied))
+
+
+class Gradients:
+    """A list of gradient tensors laid out for ``Moe.clip``: made once by ``Moe.gradients`` where the tensors stay the same
+    from step to step."""
+
+    def __init__(self, tensors, out, index: int):
+        self.tensors, self.out = list(tensors), None if out is None else list(out)
+        if self.out is not None and len(self.out) != len(self.tensors):
+            raise ValueError("out: one tensor for each gradient expected")
+        outs = self.tensors if self.out is None else self.out
+        for t, o in zip(self.tensors, outs):
+            for v in (t, o):
+                if v.get_device() != index:
+                    raise ValueError(f"a gradient is on {v.device}, the handle on cuda:{index}")
+                if v.dtype not in _DTYPES or v.dtype is not t.dtype:
+                    raise ValueError(f"gradients: type {v.dtype} not taken here")
+                if v.shape != t.shape or not v.is_contiguous():
+                    raise ValueError("gradients: contiguous tensors expected, out of the same shapes")
+        self.index = index
+        self._made_at = self._places()
+        self._c = (_CTensor * len(self.tensors))(*(
+            (t.data_ptr(), o.data_ptr(), t.numel(), _DTYPES[t.dtype]) for t, o in zip(self.tensors, outs)))
+
+    def _places(self):
+        return [t.data_ptr() for t in self.tensors] + [t.data_ptr() for t in self.out or ()]
+
+    def _arg(self):
+        if self._places() != self._made_at:   # memory moved (``.data``)
+            self.__init__(self.tensors, self.out, self.index)
+        return self._c
+
+
 # the current stream's handle without a Stream object around it (0.1 instead of 2 us per call)
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _pad16(n: int) -> int:
     return (n + 15) // 16 * 16
+
+
+def _pad8(n: int) -> int:
+    return (n + 7) // 8 * 8
+
+
+def _rows16(t) -> bool:
+    """Whether the rows of a 3-D 16-bit tensor start at multiples of 16 bytes, planes following one another."""
+    return t.stride(2) == 1 and t.stride(1) % 8 == 0 and t.stride(1) >= t.shape[2] and t.data_ptr() % 16 == 0 and \
+        (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1))
 
 
 def _ptr(t):
@@ -499,6 +622,126 @@ class Moe:
             dy.data_ptr(), lddx, _ptr(dx) if need[0] else None, weight.K, _ptr(dw) if need[1] else None),
             "esp_moe_linear_backward")
         return dx, dw
+
+    # -- gated feed-forward blocks
+
+    def gated_weight(self, inner, outer, activation: str = "silu") -> GatedWeight:
+        """16-bit weights of gated blocks, inner (E, 2 F, H) and outer (E, H, F), or of one block without E. Tensors whose
+        rows start at multiples of 16 bytes are used as they are, others are laid out anew (new values then go to the
+        result's ``inner`` and ``outer``). Activations: silu, gelu, gelu_tanh, relu."""
+        with self._queue():
+            a, b = (self._laid_out(t, name) for t, name in ((inner, "inner"), (outer, "outer")))
+        return GatedWeight(a, b, activation)
+
+    def _laid_out(self, w, name: str):
+        self._need(w, name)
+        w = w if w.dim() == 3 else w[None]
+        if w.dim() != 3:
+            raise ValueError(f"{name}: a matrix for each expert expected")
+        if w.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"{name}: type {w.dtype} not taken here")
+        E, n, k = w.shape
+        if _rows16(w):
+            return w
+        room = torch.zeros((E, n, _pad8(k)), dtype=w.dtype, device=self.device)[:, :, :k]
+        room.copy_(w)
+        return room
+
+    def keep(self, M: int, weight: GatedWeight) -> Kept:
+        """Room for what ``feed_forward`` keeps of M rows for their gradients."""
+        F8, dt = _pad8(weight.F), weight.inner.dtype
+        return Kept(self._new((M, 2, F8), dt), self._new((M, F8), dt), self._new((M, _pad8(weight.H)), dt))
+
+    def _need_kept(self, kept: Kept, M: int, weight: GatedWeight):
+        F8, dt = _pad8(weight.F), weight.inner.dtype
+        self._need(kept.pre, "pre", dt, (M, 2, F8))
+        self._need(kept.hidden, "hidden", dt, (M, F8))
+        self._need(kept.rows, "rows", dt, (M, _pad8(weight.H)))
+
+    def _block_rows(self, x, weight: GatedWeight, offsets, rows):
+        self._need(weight.inner, "weight")
+        code, ldx = self._matrix(x, "x", cols=weight.H, dtype=weight.inner.dtype)
+        if offsets is not None:
+            self._need(offsets, "offsets", torch.int32, (weight.E + 1,))
+        elif weight.E != 1:
+            raise ValueError("offsets: needed for more than one expert")
+        M = x.shape[0]
+        if rows is not None:
+            M = rows.shape[0]
+            self._need(rows, "rows", torch.int32, (M,))
+        return M, ldx
+
+    def feed_forward(self, x, weight: GatedWeight, offsets=None, rows=None, keep: Optional[Kept] = None, out=None):
+        """y (M, H): row i of expert e is O_e (act(G_e v) * (U_e v)), v = x[rows[i]] or x[i] (esp_moe_feed_forward). Rows
+        outside every expert are left as they are. keep: room that takes what the gradients need."""
+        M, ldx = self._block_rows(x, weight, offsets, rows)
+        if out is None:
+            out = self._new((M, weight.H), x.dtype)
+        _, ldy = self._matrix(out, "out", M, weight.H, x.dtype)
+        kept = None
+        if keep is not None:
+            self._need_kept(keep, M, weight)
+            kept = keep._arg()
+        self._on_stream()
+        esp._check(self._lib.esp_moe_feed_forward(
+            self.h, weight._arg(), x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ldy, out.data_ptr(),
+            None if kept is None else ctypes.byref(kept)), "esp_moe_feed_forward")
+        if keep is not None:
+            keep.copied = bool(kept.copied)
+        return out
+
+    def feed_forward_backward(self, dy, x, weight: GatedWeight, kept: Kept, offsets=None, rows=None,
+                              need=(True, True, True), out=(None, None, None), dtype=None):
+        """(dx, dinner, douter) of ``feed_forward`` at dy (M, H), called with the same arguments before: dx (M, H), dinner
+        (E, 2 F, H), douter (E, H, F); need: which of them (esp_moe_feed_forward_backward). dtype: the weights' gradients'
+        type where they are allocated here, the rows' or fp32."""
+        M, ldx = self._block_rows(x, weight, offsets, rows)
+        _, lddy = self._matrix(dy, "dy", M, weight.H, x.dtype)
+        self._need_kept(kept, M, weight)
+        dx, dinner, douter = (t if n else None for t, n in zip(out, need))
+        dt = dtype or next((t.dtype for t in (dinner, douter) if t is not None), x.dtype)
+        if dt is not x.dtype and dt is not torch.float32:
+            raise ValueError(f"the weights' gradients: {x.dtype} or fp32 expected, not {dt}")
+        E, F, H = weight.E, weight.F, weight.H
+        lddx = H
+        if need[0]:
+            dx = self._new((M, H), x.dtype) if dx is None else dx
+            _, lddx = self._matrix(dx, "dx", M, H, x.dtype)
+        if need[1]:
+            dinner = self._new((E, 2 * F, H), dt) if dinner is None else dinner
+            self._need(dinner, "dinner", dt, (E, 2 * F, H))
+        if need[2]:
+            douter = self._new((E, H, F), dt) if douter is None else douter
+            self._need(douter, "douter", dt, (E, H, F))
+        self._on_stream()
+        esp._check(self._lib.esp_moe_feed_forward_backward(
+            self.h, weight._arg(), x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ctypes.byref(kept._arg()),
+            lddy, dy.data_ptr(), lddx, _ptr(dx), _DTYPES[dt], _ptr(dinner), _ptr(douter)),
+            "esp_moe_feed_forward_backward")
+        return dx, dinner, douter
+
+    # -- gradients together
+
+    def gradients(self, tensors, out=None) -> Gradients:
+        """A list of gradients for ``clip``; out: tensors of the same shapes and types that take the results."""
+        return Gradients(tensors, out, self._index)
+
+    def clip(self, gradients, max_norm: float = math.inf, scale: float = 1.0, norm=None):
+        """The norm (fp32, on the device) of scale times all the gradients together, which become, in place or in their
+        list's ``out``, gradient * scale * min(1, max_norm / norm) (esp_moe_clip). Where the norm is not finite they are
+        scaled only. gradients: contiguous tensors, or what ``Moe.gradients`` made of them."""
+        g = gradients if isinstance(gradients, Gradients) else Gradients(gradients, None, self._index)
+        if g.index != self._index:
+            raise ValueError(f"the gradients are on cuda:{g.index}, the handle on {self.device}")
+        if norm is None:
+            norm = self._new((), torch.float32)
+        elif norm.numel() != 1:
+            raise ValueError("norm: one element expected")
+        self._need(norm, "norm", torch.float32, norm.shape)
+        c = g._arg()
+        self._on_stream()
+        esp._check(self._lib.esp_moe_clip(self.h, len(c), c, max_norm, scale, norm.data_ptr()), "esp_moe_clip")
+        return norm
 
     # -- return of the rows
 

@@ -1,0 +1,507 @@
+"""Gated feed-forward blocks (include/esp_moe.h: esp_moe_feed_forward and its gradients) against the formulas in 64 bits.
+
+Bounds, element by element, with u = 2^-24 and r the rounding unit of the 16-bit type (bf16 2^-8, half a step relative to
+the value; fp16 2^-11, and 2^-25 absolute below its normal range), |.| of matrices by element:
+  a sum of n products      2 n u sum |a b| (a truncating adder), each added operand's error times the other operand
+  g, u = x G^T, x U^T      e_g = 2 H u |x||G|^T, e_u likewise
+  act(g)                   slope below 1.13: 1.13 e_g, and its own arithmetic 16 u (|g| + 16) (|g| + 1)
+  h = act(g) u             |u| e_act + |act| e_u + e_act e_u, then r |h|
+  y = h O^T                e_h |O|^T + 2 F u |h||O|^T, then r |y|
+  dh = dy O                2 H u |dy||O|
+  dg = dh u act'(g)        g and u as kept, r |g| and r |u| more; act'' below 1 (relu: 1 where g is within its error of 0),
+                           act' itself 16 u (|g| + 16); the product rule, then r |dg|; du = dh act(g) likewise
+  dx, dG, dU, dO           as y, from the errors of their operands
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+UNIT = {"bf16": (2.0 ** -8, 2.0 ** -134), "f16": (2.0 ** -11, 2.0 ** -25), "f32": (U, 2.0 ** -149)}
+ACTS = ["silu", "gelu", "gelu_tanh", "relu"]
+
+
+@pytest.fixture(scope="module")
+def mm():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2608_07971_gb300 import build, moe
+    build.build()
+    m = moe.Moe()
+    yield m
+    m.synchronize()
+    m.close()
+
+
+def rand(*shape, dt, seed, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * size).to(DT[dt])
+
+
+def act(g, kind):
+    """The activation and its slope, in 64 bits."""
+    if kind == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    if kind == "gelu":
+        c = 0.5 * (1 + torch.erf(g / math.sqrt(2)))
+        return g * c, c + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    if kind == "gelu_tanh":
+        a = math.sqrt(2 / math.pi)
+        t = torch.tanh(a * (g + 0.044715 * g ** 3))
+        return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * a * (1 + 3 * 0.044715 * g * g)
+    return torch.clamp(g, min=0), (g > 0).double()
+
+
+def product(a, ea, b, eb, n):
+    """a b and the bound of its error."""
+    return a @ b, ea @ b.abs() + a.abs() @ eb + ea @ eb + 2 * n * U * (a.abs() @ b.abs())
+
+
+def expert(x, w, o, kind, dt, dy=None):
+    """{name: (value, bound)} of one expert's rows; the bounds leave out the results' own rounding."""
+    r, tiny = UNIT[dt]
+    F, H = o.shape[1], o.shape[0]
+    zero = torch.zeros_like
+    G, Up = w[:F], w[F:]
+    g, eg = product(x, zero(x), G.t(), zero(G.t()), H)
+    u, eu = product(x, zero(x), Up.t(), zero(Up.t()), H)
+    a, slope = act(g, kind)
+    ea = 1.13 * eg + 16 * U * (g.abs() + 16) * (g.abs() + 1)
+    h = a * u
+    eh = u.abs() * ea + a.abs() * eu + ea * eu
+    eh = eh + r * (h.abs() + eh) + tiny
+    out = dict(y=product(h, eh, o.t(), zero(o.t()), F))
+    if dy is None:
+        return out
+    dh, edh = product(dy, zero(dy), o, zero(o), H)
+    egk, euk = eg + r * (g.abs() + eg) + tiny, eu + r * (u.abs() + eu) + tiny
+    es = egk + 16 * U * (g.abs() + 16) if kind != "relu" else (g.abs() <= egk).double()
+    eak = 1.13 * egk + 16 * U * (g.abs() + 16) * (g.abs() + 1)
+    dg, du = dh * u * slope, dh * a
+    edg = (dh.abs() + edh) * (u.abs() + euk) * (slope.abs() + es) - dg.abs()
+    edu = (dh.abs() + edh) * (a.abs() + eak) - du.abs()
+    edg, edu = (e + r * (d.abs() + e) + tiny for e, d in ((edg, dg), (edu, du)))
+    dp, edp = torch.cat([dg, du], 1), torch.cat([edg, edu], 1)
+    out["dx"] = product(dp, edp, w, zero(w), 2 * F)
+    n = x.shape[0]
+    out["dinner"] = product(dp.t(), edp.t(), x, zero(x), n)
+    out["douter"] = product(dy.t(), zero(dy.t()), h, eh, n)
+    return out
+
+
+def close(got, want, bound, dt):
+    rel, absolute = UNIT[dt]
+    got = got.double()
+    lim = bound + rel * (want.abs() + bound) + absolute
+    bad = ~((got - want).abs() <= lim)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {float(((got - want).abs() / lim).max()):.3g} of the bound"
+
+
+def check(mm, sizes, H, F, dt, kind, gathered=False, spare=0, dw_dtype=None, seed=0):
+    """One block with gradients against the formulas; `spare` rows belong to no expert."""
+    E, n = len(sizes), sum(sizes)
+    M = n + spare
+    T = max(1, n // 2) if gathered else M
+    x = rand(T, H, dt=dt, seed=seed)
+    inner, outer = rand(E, 2 * F, H, dt=dt, seed=seed + 1, size=H ** -0.5), rand(E, H, F, dt=dt, seed=seed + 2, size=F ** -0.5)
+    dy = rand(M, H, dt=dt, seed=seed + 3)
+    w = mm.gated_weight(inner, outer, kind)
+    rows = None
+    if gathered:
+        rows = torch.as_tensor(np.random.default_rng(seed).integers(0, T, M).astype(np.int32)).cuda()
+        rows[n:] = -1
+    offsets = torch.tensor([0, *np.cumsum(sizes)], dtype=torch.int32, device="cuda") if E > 1 or spare else None
+    plan = dict(offsets=offsets, rows=rows)
+    kept = mm.keep(M, w)
+    y0, dx0 = torch.full((M, H), 7.0, dtype=DT[dt], device="cuda"), torch.full((M, H), 9.0, dtype=DT[dt], device="cuda")
+    y = mm.feed_forward(x, w, keep=kept, out=y0, **plan)
+    dx, dinner, douter = mm.feed_forward_backward(dy, x, w, kept, out=(dx0, None, None), dtype=dw_dtype, **plan)
+    assert (y[n:] == 7.0).all() and (dx[n:] == 9.0).all()
+    bare = mm.feed_forward(x, w, **plan)
+    assert torch.equal(bare[:n], y[:n])
+    wt = "f32" if dw_dtype is torch.float32 else dt
+    assert dinner.dtype is douter.dtype is (dw_dtype or DT[dt])
+    a = 0
+    for e, k in enumerate(sizes):
+        at = slice(a, a + k)
+        xe = (x[rows[at].long()] if gathered else x[at]).double()
+        ref = expert(xe, inner[e].double(), outer[e].double(), kind, dt, dy[at].double())
+        close(y[at], *ref["y"], dt)
+        close(dx[at], *ref["dx"], dt)
+        close(dinner[e], *ref["dinner"], wt)
+        close(douter[e], *ref["douter"], wt)
+        a += k
+
+
+SHAPES = [  # rows of each expert, H, F, type, activation, gathered, rows of no expert
+    ([1], 64, 64, "bf16", "silu", False, 0),
+    ([1], 8, 8, "f16", "gelu", False, 0),
+    ([3], 1, 1, "bf16", "relu", False, 0),
+    ([128], 128, 128, "bf16", "silu", False, 0),
+    ([256], 256, 256, "f16", "gelu_tanh", False, 0),
+    ([257], 200, 136, "bf16", "gelu", False, 0),
+    ([300], 77, 129, "f16", "silu", False, 0),
+    ([65, 0, 1, 63], 130, 67, "bf16", "silu", True, 5),
+    ([0, 0, 0], 64, 72, "bf16", "silu", False, 4),
+    ([64, 128, 256], 264, 320, "f16", "relu", False, 0),
+    ([513, 1, 700], 136, 520, "bf16", "gelu_tanh", True, 0),
+    ([31] * 40, 96, 33, "bf16", "gelu", True, 17),
+    ([1999], 1001, 515, "bf16", "silu", False, 0),
+    ([2] * 130, 72, 40, "f16", "silu", True, 0),
+]
+
+
+@pytest.mark.parametrize("sizes,H,F,dt,kind,gathered,spare", SHAPES)
+def test_block_and_its_gradients(mm, sizes, H, F, dt, kind, gathered, spare):
+    check(mm, sizes, H, F, dt, kind, gathered, spare, seed=sum(sizes) + H)
+
+
+@pytest.mark.parametrize("kind", ACTS)
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_activations(mm, kind, dt):
+    check(mm, [90, 40], 200, 144, dt, kind, True, 3, seed=5)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_weight_gradients_in_32_bits(mm, dt):
+    check(mm, [70, 0, 333], 136, 100, dt, "silu", True, 0, dw_dtype=torch.float32)
+
+
+def test_long_inner_axes(mm):
+    check(mm, [40, 300], 2050, 999, "f16", "gelu", False, 0)
+    check(mm, [260], 72, 4100, "bf16", "silu", False, 0)
+
+
+def test_activations_far_out(mm):
+    """Gate values of hundreds: the activations' tails and their slopes stay finite."""
+    for kind in ACTS:
+        x = torch.tensor([[-300.0, 1.0], [300.0, 1.0], [-30.0, 1.0], [30.0, 1.0], [0.0, 1.0]], device="cuda").bfloat16()
+        inner = torch.eye(2, device="cuda").bfloat16()                       # g = x0, u = x1
+        outer = torch.tensor([[1.0], [0.0]], device="cuda").bfloat16()
+        w = mm.gated_weight(inner, outer, kind)
+        kept = mm.keep(5, w)
+        y = mm.feed_forward(x, w, keep=kept)
+        dx, _, _ = mm.feed_forward_backward(torch.tensor([[1.0, 0.0]] * 5, device="cuda").bfloat16(), x, w, kept)
+        a, slope = act(x[:, 0].double(), kind)
+        assert ((y[:, 0].double() - a).abs() <= 2.0 ** -7 * a.abs() + 1e-6).all()
+        assert ((dx[:, 0].double() - slope).abs() <= 2.0 ** -6 * slope.abs() + 1e-6).all()
+
+
+def test_rows_of_others_do_not_reach_a_gradient(mm):
+    """NaN and infinities in one expert's rows, and in the rows of none, stay there."""
+    sizes = [70, 33, 129]
+    n, H, F = sum(sizes), 128, 192
+    x, dy = rand(n + 40, H, dt="bf16", seed=1), rand(n + 40, H, dt="bf16", seed=2)
+    w = mm.gated_weight(rand(3, 2 * F, H, dt="bf16", seed=3, size=0.1), rand(3, H, F, dt="bf16", seed=4, size=0.1))
+    offsets = torch.tensor([0, 70, 103, n], dtype=torch.int32, device="cuda")
+
+    def both(x, dy):
+        kept = mm.keep(n + 40, w)
+        y = mm.feed_forward(x, w, offsets=offsets, keep=kept)
+        return (y, *mm.feed_forward_backward(dy, x, w, kept, offsets=offsets))
+
+    want = both(x, dy)
+    x2, dy2 = x.clone(), dy.clone()
+    x2[70:103], dy2[70:103] = math.nan, math.inf
+    x2[n:], dy2[n:] = math.inf, math.nan
+    got = both(x2, dy2)
+    for a, b in zip(want[:2], got[:2]):
+        assert torch.equal(a[:70], b[:70]) and torch.equal(a[103:n], b[103:n])
+    for a, b in zip(want[2:], got[2:]):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2]) and b[1].isnan().any()
+
+
+def test_gradients_against_differences(mm):
+    """Along random directions, the loss <y, c> in 64 bits changes as the gradients say."""
+    sizes, H, F = [9, 14], 40, 56
+    n = sum(sizes)
+    x, c = rand(n, H, dt="f16", seed=1), rand(n, H, dt="f16", seed=2)
+    inner, outer = rand(2, 2 * F, H, dt="f16", seed=3, size=0.2), rand(2, H, F, dt="f16", seed=4, size=0.2)
+    offsets = torch.tensor([0, 9, n], dtype=torch.int32, device="cuda")
+    for kind in ACTS[:3]:
+        w = mm.gated_weight(inner, outer, kind)
+        kept = mm.keep(n, w)
+        mm.feed_forward(x, w, offsets=offsets, keep=kept)
+        grads = mm.feed_forward_backward(c, x, w, kept, offsets=offsets)
+
+        def loss(x, inner, outer):
+            total = 0.0
+            for e, at in enumerate((slice(0, 9), slice(9, n))):
+                p = x[at] @ inner[e].t()
+                total += float(((act(p[:, :F], kind)[0] * p[:, F:]) @ outer[e].t() * c[at].double()).sum())
+            return total
+
+        at = [t.double() for t in (x, inner, outer)]
+        for i, g in enumerate(grads):
+            d = torch.randn(at[i].shape, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda").double()
+            step = 1e-4
+            hi, lo = ([t + s * step * d if j == i else t for j, t in enumerate(at)] for s in (1, -1))
+            slope = (loss(*hi) - loss(*lo)) / (2 * step)
+            # each product of the gradient carries at most four roundings to fp16 (2^-11), in either direction
+            size = float((g.double().abs() * d.abs()).sum())
+            assert abs(float((g.double() * d).sum()) - slope) <= 4 * 2.0 ** -11 * size + 1e-5 * size
+
+
+def test_strided_and_misaligned(mm):
+    """Views into wider buffers, and weights whose rows are not on 16 bytes, give what their copies give."""
+    for dt in DT:
+        base = rand(50, 333, dt=dt, seed=1)
+        inner, outer = rand(130, 131, dt=dt, seed=2, size=0.1), rand(131, 65, dt=dt, seed=3, size=0.1)
+        w = mm.gated_weight(inner, outer)
+        assert w.inner.shape == (1, 130, 131) and torch.equal(w.inner[0], inner) and torch.equal(w.outer[0], outer)
+        for at in (slice(5, 136), slice(8, 139)):
+            x = base[:, at]
+            wide = torch.zeros(50, 200, dtype=DT[dt], device="cuda")
+            k1, k2 = mm.keep(50, w), mm.keep(50, w)
+            y = mm.feed_forward(x, w, out=wide[:, 3:134], keep=k1)
+            y2 = mm.feed_forward(x.contiguous(), w, keep=k2)
+            assert torch.equal(y, y2) and not wide[:, :3].any() and not wide[:, 134:].any()
+            dwide = torch.zeros(50, 200, dtype=DT[dt], device="cuda")
+            g1 = mm.feed_forward_backward(y, x, w, k1, out=(dwide[:, 8:139], None, None))
+            g2 = mm.feed_forward_backward(y2, x.contiguous(), w, k2)
+            assert all(torch.equal(a, b) for a, b in zip(g1, g2)) and not dwide[:, :8].any() and not dwide[:, 139:].any()
+            # results that start at an odd element
+            room = torch.zeros(2 * 65 * 131 + 3, dtype=DT[dt], device="cuda")
+            g3 = mm.feed_forward_backward(y2, x.contiguous(), w, k2, need=(False, True, False),
+                                          out=(None, room[1:-2].view(1, 130, 131), None))
+            assert torch.equal(g3[1], g2[1]) and g3[0] is None and g3[2] is None and not room[0] and not room[-2:].any()
+
+
+def test_changed_weights_are_used(mm):
+    x = rand(40, 128, dt="bf16", seed=1)
+    w = mm.gated_weight(rand(2, 64, 128, dt="bf16", seed=2), rand(2, 128, 32, dt="bf16", seed=3))
+    off = torch.tensor([0, 20, 40], dtype=torch.int32, device="cuda")
+    first = mm.feed_forward(x, w, offsets=off)
+    fresh = rand(2, 64, 128, dt="bf16", seed=4)
+    w.inner = fresh
+    second = mm.feed_forward(x, w, offsets=off)
+    assert not torch.equal(first, second)
+    w.inner.copy_(rand(2, 64, 128, dt="bf16", seed=2))
+    assert torch.equal(mm.feed_forward(x, w, offsets=off), first)
+    w.activation = "relu"
+    assert not torch.equal(mm.feed_forward(x, w, offsets=off), first)
+    with pytest.raises(ValueError):
+        w.outer = fresh
+        mm.feed_forward(x, w, offsets=off)
+
+
+def test_offsets_past_32_bits(mm):
+    """Rows whose element offsets pass 2^31, in place and gathered."""
+    base = torch.empty(2100, 1 << 20, dtype=torch.bfloat16, device="cuda")
+    x, out = base[:, 8:72], base[:, 128:192]
+    x.copy_(torch.randn(2100, 64, device="cuda"))
+    w = mm.gated_weight(rand(96, 64, dt="bf16", seed=1), rand(64, 48, dt="bf16", seed=2))
+    want = mm.feed_forward(x.contiguous(), w)
+    assert torch.equal(mm.feed_forward(x, w, out=out), want)
+    rows = torch.arange(2099, -1, -1, dtype=torch.int32, device="cuda")
+    assert torch.equal(mm.feed_forward(x, w, rows=rows), want.flip(0))
+
+
+def test_empty(mm):
+    w = mm.gated_weight(rand(2, 64, 32, dt="bf16", seed=1), rand(2, 32, 32, dt="bf16", seed=2))
+    x, off = torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    kept = mm.keep(0, w)
+    y = mm.feed_forward(x, w, offsets=off, keep=kept)
+    dx, dinner, douter = mm.feed_forward_backward(y, x, w, kept, offsets=off)
+    assert y.shape == dx.shape == (0, 32) and not dinner.any() and not douter.any()
+
+
+def test_rows_out_of_range_read_zeros(mm):
+    w = mm.gated_weight(rand(64, 32, dt="bf16", seed=1), rand(32, 32, dt="bf16", seed=2))
+    x = rand(6, 32, dt="bf16", seed=3)
+    rows = torch.tensor([0, -1, 5, 6, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    y = mm.feed_forward(x, w, rows=rows)
+    assert torch.equal(y[[0, 2]], mm.feed_forward(x[[0, 5]], w)) and not y[[1, 3, 4, 5]].any()
+
+
+def test_offsets_that_do_not_ascend_stay_in_range(mm):
+    """Nothing outside the rows and gradients is written."""
+    w = mm.gated_weight(rand(4, 64, 64, dt="bf16", seed=1), rand(4, 64, 32, dt="bf16", seed=2))
+    x = rand(300, 64, dt="bf16", seed=3)
+    want = mm.feed_forward(x[:100], w, offsets=torch.tensor([0, 25, 50, 75, 100], dtype=torch.int32, device="cuda"))
+    for off in ([0, 300, 0, 300, 300], [-5, 900, 10, 2 ** 31 - 1, 3], [300, 200, 100, 50, 0]):
+        room = torch.full((302, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+        offsets = torch.tensor(off, dtype=torch.int32, device="cuda")
+        kept = mm.keep(300, w)
+        mm.feed_forward(x, w, offsets=offsets, out=room[1:301], keep=kept)
+        mm.feed_forward_backward(x, x, w, kept, offsets=offsets)
+        assert (room[0] == 5.0).all() and (room[301] == 5.0).all()
+    assert torch.equal(mm.feed_forward(x[:100], w, offsets=torch.tensor([0, 25, 50, 75, 100], dtype=torch.int32, device="cuda")), want)
+
+
+def test_repeatable_on_streams_and_in_graphs(mm):
+    """The same bits on every run, on other streams, and from a replayed graph whose inputs changed."""
+    from paper_2608_07971_gb300 import moe
+    m = moe.Moe()
+    sizes = torch.tensor([0, 100, 100, 350, 400], dtype=torch.int32, device="cuda")
+    w = m.gated_weight(rand(4, 256, 136, dt="bf16", seed=1, size=0.1), rand(4, 136, 128, dt="bf16", seed=2, size=0.1))
+    x = [rand(200, 136, dt="bf16", seed=s) for s in (3, 4)]
+    rows = torch.randint(0, 200, (400,), device="cuda").int()
+    dy = rand(400, 136, dt="bf16", seed=5)
+
+    def step(m, x, kept, out=None, grads=(None, None, None)):
+        y = m.feed_forward(x, w, offsets=sizes, rows=rows, keep=kept, out=out)
+        return (y, *m.feed_forward_backward(dy, x, w, kept, offsets=sizes, rows=rows, out=grads))
+
+    want = [[t.clone() for t in step(m, v, m.keep(400, w))] for v in x]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    kept = [m.keep(400, w) for _ in range(2)]
+    got = []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            got.append((i % 2, step(m, x[i % 2], kept[i % 2])))
+    m.synchronize()
+    torch.cuda.synchronize()
+    for i, g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+    buf, keep = x[0].clone(), m.keep(400, w)
+    out = [torch.empty_like(t) for t in want[0]]
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=streams[0]):
+        step(m, buf, keep, out[0], tuple(out[1:]))
+    for i in (1, 0, 1):
+        buf.copy_(x[i])
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+    m.close()
+
+
+def test_copies_of_weights_and_kept(mm):
+    import copy
+    import pickle
+    x = rand(30, 64, dt="bf16", seed=1)
+    w = mm.gated_weight(rand(1, 64, 64, dt="bf16", seed=2), rand(1, 64, 32, dt="bf16", seed=3), "gelu")
+    want = mm.feed_forward(x, w)
+    for v in (copy.copy(w), copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
+        assert v.activation == "gelu" and torch.equal(mm.feed_forward(x, v), want)
+
+
+@pytest.mark.parametrize("which", ["forward", "dx", "weights"])
+def test_wait_that_runs_out_is_reported(mm, which):
+    """A product whose load never comes ends by its bounded waits; the handle then refuses work."""
+    from paper_2608_07971_gb300 import esp, moe
+    m = moe.Moe()
+    sizes = torch.tensor([0, 700, 1010], dtype=torch.int32, device="cuda")
+    x, dy = rand(1010, 512, dt="bf16", seed=1), rand(1010, 512, dt="bf16", seed=2)
+    w = m.gated_weight(rand(2, 640, 512, dt="bf16", seed=3), rand(2, 512, 320, dt="bf16", seed=4))
+    kept = m.keep(1010, w)
+    want = m.feed_forward(x, w, offsets=sizes, keep=kept)
+    m.synchronize()
+    lib = moe.load_library()
+    esp._check(lib.esp_moe_debug_set_wait_limit(m.h, 20), "set_wait_limit")
+    esp._check(lib.esp_moe_debug_hold_load(m.h), "hold_load")
+    if which == "forward":
+        m.feed_forward(x, w, offsets=sizes, keep=kept)
+    else:   # the first product of the call
+        m.feed_forward_backward(dy, x, w, kept, offsets=sizes, need=(True, False, False) if which == "dx" else (False, False, True))
+    with pytest.raises(esp.EspError) as err:
+        m.synchronize()
+    assert err.value.status == esp.ESP_ERR_TIMEOUT
+    with pytest.raises(esp.EspError) as err:
+        m.feed_forward(x, w, offsets=sizes)
+    assert err.value.status == esp.ESP_ERR_STATE
+    m.close()
+    assert torch.equal(mm.feed_forward(x, w, offsets=sizes), want)   # another handle works on
+
+
+def test_refusals(mm):
+    from paper_2608_07971_gb300 import esp, moe
+    x = rand(4, 32, dt="bf16", seed=1)
+    inner, outer = rand(2, 48, 32, dt="bf16", seed=2), rand(2, 32, 24, dt="bf16", seed=3)
+    w = mm.gated_weight(inner, outer)
+    off = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    kept = mm.keep(4, w)
+    y = mm.feed_forward(x, w, offsets=off, keep=kept)
+    bad = [
+        lambda: mm.gated_weight(inner.float(), outer.float()),
+        lambda: mm.gated_weight(inner, outer.half()),
+        lambda: mm.gated_weight(inner[:, :47], outer),
+        lambda: mm.gated_weight(inner, outer[:, :, :23]),
+        lambda: mm.gated_weight(inner, outer, "tanh"),
+        lambda: mm.gated_weight(inner.cpu(), outer.cpu()),
+        lambda: mm.feed_forward(x, w),
+        lambda: mm.feed_forward(x.half(), w, offsets=off),
+        lambda: mm.feed_forward(x.float(), w, offsets=off),
+        lambda: mm.feed_forward(x[:, :31], w, offsets=off),
+        lambda: mm.feed_forward(x.cpu(), w, offsets=off),
+        lambda: mm.feed_forward(x, w, offsets=off.long()),
+        lambda: mm.feed_forward(x, w, offsets=off[:2]),
+        lambda: mm.feed_forward(x, w, offsets=off, rows=torch.zeros(3, device="cuda")),
+        lambda: mm.feed_forward(x, w, offsets=off, out=torch.empty(4, 31, dtype=torch.bfloat16, device="cuda")),
+        lambda: mm.feed_forward(x, w, offsets=off, keep=mm.keep(5, w)),
+        lambda: mm.feed_forward_backward(y[:3], x, w, kept, offsets=off),
+        lambda: mm.feed_forward_backward(y.half(), x, w, kept, offsets=off),
+        lambda: mm.feed_forward_backward(y, x, w, mm.keep(3, w), offsets=off),
+        lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, dtype=torch.float16),
+        lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, out=(None, torch.empty(2, 47, 32, device="cuda"), None)),
+        lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, out=(
+            None, torch.empty(2, 48, 32, device="cuda"), torch.empty(2, 32, 24, dtype=torch.bfloat16, device="cuda"))),
+    ]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    # gathered rows, but kept from a pass over rows in place; rows that overlap one another
+    for f in (lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, rows=torch.zeros(4, dtype=torch.int32, device="cuda")),
+              lambda: mm.feed_forward(x[:1].expand(4, 32), w, offsets=off)):
+        with pytest.raises(esp.EspError) as err:
+            f()
+        assert err.value.status == esp.ESP_ERR_INVALID_ARG
+    assert torch.equal(mm.feed_forward(x, w, offsets=off), y)   # a refusal leaves the handle usable
+    mm.synchronize()
+    assert isinstance(moe.GatedWeight(inner, outer), moe.GatedWeight)
+
+
+def test_a_layer_as_it_is_used(mm):
+    """Routing, blocks, weighted return, all gradients, clipping: a training step against the same in 64 bits."""
+    from paper_2608_07971_gb300 import moe
+    T, E, k, H, F = 150, 6, 2, 96, 80
+    x = rand(T, H, dt="bf16", seed=1)
+    wr = rand(E, H, dt="bf16", seed=2, size=H ** -0.5)
+    inner, outer = rand(E, 2 * F, H, dt="bf16", seed=3, size=H ** -0.5), rand(E, H, F, dt="bf16", seed=4, size=F ** -0.5)
+    w = mm.gated_weight(inner, outer)
+    logits = x.float() @ wr.float().t()
+    r = mm.route(logits, k, gate=moe.Gate("softmax"))
+    kept = mm.keep(T * k, w)
+    y = mm.feed_forward(x, w, offsets=r.offsets, rows=r.rows, keep=kept)
+    out = mm.combine(y, r.pos, r.weight)
+    dout = rand(T, H, dt="bf16", seed=5)
+    dy, dweight = mm.combine_backward(dout, y, r.pos, r.weight)
+    dx, dinner, douter = mm.feed_forward_backward(dy, x, w, kept, offsets=r.offsets, rows=r.rows)
+    dtoken = mm.combine(dx, r.pos)
+    dwr = (mm.route_backward(logits, r.idx, dweight=dweight).t() @ x.float())
+    grads = [dinner, douter, dwr]
+    before = [g.clone() for g in grads]
+    norm = mm.clip(grads, max_norm=0.5)
+
+    v = [t.double().requires_grad_() for t in (x, wr, inner, outer)]
+    z = v[0] @ v[1].t()
+    p = torch.softmax(torch.gather(z, 1, r.idx.long()), -1)
+    total = 0.0
+    for e in range(E):
+        t, j = torch.nonzero(r.idx == e, as_tuple=True)
+        q = v[0][t] @ v[2][e].t()
+        ye = (torch.nn.functional.silu(q[:, :F]) * q[:, F:]) @ v[3][e].t()
+        total = total + torch.zeros(T, H, dtype=torch.float64, device="cuda").index_add(0, t, ye * p[t, j][:, None])
+    total.backward(dout.double())
+    # 16-bit roundings of h, y, dy, the gradients of the inner rows and the results: at most 8 of 2^-8 each, on sums of
+    # hundreds of terms of either sign; 2 percent of a result's norm
+    for got, want in ((out, total.detach()), (before[0], v[2].grad), (before[1], v[3].grad), (before[2], v[1].grad)):
+        assert float((got.double() - want).norm() / want.norm()) < 0.02
+    assert dtoken.shape == (T, H)
+    n = math.sqrt(sum(float(g.double().square().sum()) for g in before))
+    assert abs(float(norm) - n) <= 1e-6 * n
+    for g, b in zip(grads, before):
+        want = b.double() * (0.5 / n)
+        unit = 2.0 ** -8 if g.dtype is torch.bfloat16 else U
+        assert ((g.double() - want).abs() <= (unit + 1e-6) * want.abs() + 2.0 ** -134).all()
