@@ -1,0 +1,222 @@
+// What the products of the gated feed-forward blocks share (esp_ff_gemm.cu: many rows, esp_ff_few.cu: few): parameters,
+// bounded waits, operand descriptors, activations, tensor maps.
+#pragma once
+
+#include <type_traits>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "esp_fp8_tiles.cuh"
+#include "esp_moe_ff_impl.h"
+#include "esp_tcgen.cuh"
+
+namespace esp_moe_impl {
+
+namespace {
+
+enum Kind { HIDDEN, OUT, DPRE, DX, DW };
+
+constexpr int kHalfTile = 64 * 128;   // MN-major: 64 inner indices of 64 outer elements
+
+struct FfParams {
+    GemmParams g;             // rows, experts, N (columns of the output), waits
+    int32_t blocks, halves;   // blocks of the inner axis in a half, halves (DX: G and U)
+    int32_t planes;           // DW: outputs of an expert (G and U, or O), each of out_rows x N
+    int32_t out_rows;
+    int32_t act;
+    int32_t half_f16;         // operands are fp16 (else bf16)
+    const void *pre;          // DPRE
+    int64_t fp;
+    void *out2;               // HIDDEN: pre (or null)
+};
+
+// ---- waits: as wait_phase's scope says, a barrier at which this CTA's copies and threads arrive, at which another CTA's
+// warps hand tensor memory back (relaxed: the tcgen05 fences order it), or for which another CTA's warp wrote memory.
+enum Scope { OWN, HANDBACK, PAIR };
+
+template <int SCOPE>
+__device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    if (SCOPE == OWN)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else if (SCOPE == HANDBACK)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+
+// Waits for at most `ms` milliseconds of the GPU's timer, which is read once in 256 polls.
+template <int SCOPE>
+__device__ __forceinline__ bool wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
+{
+    uint64_t end = 0;
+    for (;;) {
+        for (int i = 0; i < 256; ++i)
+            if (phase_done<SCOPE>(bar, parity))
+                return true;
+        if (dead && *dead)
+            return false;
+        const uint64_t now = global_ns();
+        if (end == 0)
+            end = now + (uint64_t)ms * 1000000ull;
+        else if (now >= end)
+            return false;
+    }
+}
+
+// Bounded wait of a whole warp; one that runs out ends the CTA's other waits and sets the error word.
+template <int SCOPE = OWN>
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
+{
+    bool ok = phase_done<SCOPE>(bar, parity) || wait_ms<SCOPE>(bar, parity, p.wait_ms, dead);
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) {
+        *dead = 1;
+        *static_cast<volatile unsigned int *>(p.err) = 1u;   // in host memory
+    }
+    return ok;
+}
+
+__device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+__device__ __forceinline__ void arrive_release(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// Operand descriptors (version 1 in bits 46-47, 128-byte swizzle in bits 61-63). K-major: groups of 8 rows 1024 bytes
+// apart; an MMA's 16 inner elements are 32 bytes. MN-major: 64 outer elements a row, the next 64 a half tile further
+// (leading offset), groups of 8 inner indices 1024 bytes apart; 16 inner indices are 2048 bytes.
+template <bool MN>
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(MN ? kHalfTile >> 4 : 1) << 16) |
+           ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+template <bool MN>
+constexpr int kOperandStep = (MN ? 2048 : 32) >> 4;
+
+// ---- activations: a = act(g), d = act'(g). The fast exponential's error (2 ulp and |x| 2^-24) and division (2 ulp) are
+// far below the one rounding to 16 bits that follows.
+__device__ __forceinline__ float logistic(float g)
+{
+    return __fdividef(1.0f, 1.0f + __expf(-g));
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float g)
+{
+    if (ACT == ESP_MOE_SILU)
+        return g * logistic(g);
+    if (ACT == ESP_MOE_GELU)
+        return 0.5f * g * (1.0f + erff(g * 0.70710678f));
+    if (ACT == ESP_MOE_GELU_TANH)   // (1 + tanh t) / 2 = logistic(2 t)
+        return g * logistic(1.59576912f * (g + 0.044715f * g * g * g));
+    return fmaxf(g, 0.0f);
+}
+
+template <int ACT>
+__device__ __forceinline__ void act_and_slope(float g, float &a, float &d)
+{
+    if (ACT == ESP_MOE_SILU) {
+        const float s = logistic(g);
+        a = g * s;
+        d = s * (1.0f + g * (1.0f - s));
+    } else if (ACT == ESP_MOE_GELU) {
+        const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
+        a = g * c;
+        d = c + g * 0.39894228f * __expf(-0.5f * g * g);
+    } else if (ACT == ESP_MOE_GELU_TANH) {
+        const float s = logistic(1.59576912f * (g + 0.044715f * g * g * g));
+        a = g * s;
+        d = s + a * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * g * g);
+    } else {
+        a = fmaxf(g, 0.0f);
+        d = g > 0.0f ? 1.0f : 0.0f;
+    }
+}
+
+// Calls f with the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F &&f)
+{
+    if (act == ESP_MOE_SILU)
+        f(std::integral_constant<int, ESP_MOE_SILU>());
+    else if (act == ESP_MOE_GELU)
+        f(std::integral_constant<int, ESP_MOE_GELU>());
+    else if (act == ESP_MOE_GELU_TANH)
+        f(std::integral_constant<int, ESP_MOE_GELU_TANH>());
+    else
+        f(std::integral_constant<int, ESP_MOE_RELU>());
+}
+
+// Boxes of 128 bytes and `rows` of the second axis of a tensor of 2- or 4-byte elements: x elements contiguous, y and z
+// ldy and ldz elements apart. What a load finds outside is zero, what a store has outside is dropped.
+cudaError_t box_map3(CUtensorMap *map, const void *p, int size, int64_t x, int64_t y, int64_t ldy, int64_t z, int64_t ldz,
+                     int rows)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode)
+        return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
+    const cuuint64_t strides[2] = {(cuuint64_t)ldy * size, (cuuint64_t)(z > 1 ? ldz : ldy) * size};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)rows, 1}, step[3] = {1, 1, 1};
+    const CUresult r = encode(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 3,
+                              const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// Calls f(T()) for a 16-bit type.
+template <typename F>
+cudaError_t with_16(int32_t dtype, F &&f)
+{
+    return dtype == ESP_MOE_BF16 ? f(__nv_bfloat16()) : f(__half());
+}
+
+FfParams common(esp_moe *m, const FfShape &s)
+{
+    FfParams p{};
+    p.g.err = m->d_err;
+    p.g.wait_ms = m->wait_ms;
+    p.g.hold = m->hold_load ? 1 : 0;
+    m->hold_load = false;   // the hook holds one launch only
+    p.g.splits = 1;
+    p.g.partial = s.partial;
+    p.g.tickets = m->d_ticket + 1;
+    p.g.M = (int32_t)s.M;
+    p.g.E = s.E;
+    p.g.offsets = s.offsets;
+    p.halves = 1;
+    p.act = s.act;
+    p.half_f16 = s.dtype == ESP_MOE_F16;
+    p.fp = s.fp;
+    return p;
+}
+
+#define FF_TRY(call)                  \
+    do {                              \
+        const cudaError_t e_ = call;  \
+        if (e_ != cudaSuccess)        \
+            return e_;                \
+    } while (0)
+
+}  // namespace
+
+}  // namespace esp_moe_impl

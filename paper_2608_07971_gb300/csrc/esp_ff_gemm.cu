@@ -21,24 +21,19 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "esp_fp8_tiles.cuh"
-#include "esp_moe_ff_impl.h"
+#include "esp_ff.cuh"
 #include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
-#include "esp_tcgen.cuh"
 
 namespace esp_moe_impl {
 
 namespace {
-
-enum Kind { HIDDEN, OUT, DPRE, DX, DW };
 
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr int kStages = 5;
 constexpr int kTileBytes = kRowsA * 128;             // one operand's share of a stage in a CTA
 constexpr int kStage = 2 * kTileBytes;
-constexpr int kHalfTile = kTileBytes / 2;            // MN-major: 64 outer elements x 64 inner indices
 constexpr int kBoxBytes = 128, kBox = 32 * kBoxBytes;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kAccCols = 256;
@@ -47,19 +42,6 @@ constexpr int kBars = 192;
 constexpr int kSmem = kStages * kStage + kEpilogueWarps * kBox + kTable + kBars + 1024;
 static_assert((3 * kStages + 2 * 2 + 1) * 8 + 16 <= kBars, "barriers");
 static_assert(kSmem <= 232448, "shared memory");
-
-struct FfParams {
-    GemmParams g;             // rows, experts, N (columns of the output), waits
-    int32_t blocks, halves;   // blocks of the inner axis in a half, halves (DX: G and U)
-    int32_t planes;           // DW: outputs of an expert (G and U, or O), each of out_rows x N
-    int32_t out_rows;
-    int32_t act;
-    int32_t half_f16;         // operands are fp16 (else bf16)
-    const void *pre;          // DPRE
-    int64_t fp;
-    void *out2;               // HIDDEN: pre (or null)
-    bool wide2;
-};
 
 // One item of the list. Row kinds: rows m0 .. m0 + rows - 1 of expert e, columns n0 ..; DW: output rows m0 .. of plane z,
 // over the rows lo .. hi - 1.
@@ -99,73 +81,6 @@ __device__ __forceinline__ bool ff_tile(const FfParams &p, const int *table, int
     return true;
 }
 
-// ---- waits: as wait_phase's scope says, a barrier at which this CTA's copies and threads arrive, at which another CTA's
-// warps hand tensor memory back (relaxed: the tcgen05 fences order it), or for which another CTA's warp wrote memory.
-enum Scope { OWN, HANDBACK, PAIR };
-
-template <int SCOPE>
-__device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    if (SCOPE == OWN)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    else if (SCOPE == HANDBACK)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-
-// Waits for at most `ms` milliseconds of the GPU's timer, which is read once in 256 polls.
-template <int SCOPE>
-__device__ __forceinline__ bool wait_ms(uint32_t bar, uint32_t parity, uint32_t ms, volatile int *dead)
-{
-    uint64_t end = 0;
-    for (;;) {
-        for (int i = 0; i < 256; ++i)
-            if (phase_done<SCOPE>(bar, parity))
-                return true;
-        if (dead && *dead)
-            return false;
-        const uint64_t now = global_ns();
-        if (end == 0)
-            end = now + (uint64_t)ms * 1000000ull;
-        else if (now >= end)
-            return false;
-    }
-}
-
-// Bounded wait of a whole warp; one that runs out ends the CTA's other waits and sets the error word.
-template <int SCOPE = OWN>
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const GemmParams &p, volatile int *dead)
-{
-    bool ok = phase_done<SCOPE>(bar, parity) || wait_ms<SCOPE>(bar, parity, p.wait_ms, dead);
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) {
-        *dead = 1;
-        *static_cast<volatile unsigned int *>(p.err) = 1u;   // in host memory
-    }
-    return ok;
-}
-
-__device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
-__device__ __forceinline__ void arrive_release(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
 // A box into this CTA's shared memory; its bytes arrive at a barrier of either CTA of the pair.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
@@ -176,19 +91,6 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, i
         : "memory");
 }
 
-// Operand descriptors (version 1 in bits 46-47, 128-byte swizzle in bits 61-63). K-major: groups of 8 rows 1024 bytes
-// apart; an MMA's 16 inner elements are 32 bytes. MN-major: 64 outer elements a row, the next 64 a half tile further
-// (leading offset), groups of 8 inner indices 1024 bytes apart; 16 inner indices are 2048 bytes.
-template <bool MN>
-__device__ __forceinline__ uint64_t operand(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(MN ? kHalfTile >> 4 : 1) << 16) |
-           ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-
-template <bool MN>
-constexpr int kOperandStep = (MN ? 2048 : 32) >> 4;
-
 __device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -196,60 +98,6 @@ __device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
-}
-
-// ---- activations: a = act(g), d = act'(g). The fast exponential's error (2 ulp and |x| 2^-24) and division (2 ulp) are
-// far below the one rounding to 16 bits that follows.
-__device__ __forceinline__ float logistic(float g)
-{
-    return __fdividef(1.0f, 1.0f + __expf(-g));
-}
-
-template <int ACT>
-__device__ __forceinline__ float act_of(float g)
-{
-    if (ACT == ESP_MOE_SILU)
-        return g * logistic(g);
-    if (ACT == ESP_MOE_GELU)
-        return 0.5f * g * (1.0f + erff(g * 0.70710678f));
-    if (ACT == ESP_MOE_GELU_TANH)   // (1 + tanh t) / 2 = logistic(2 t)
-        return g * logistic(1.59576912f * (g + 0.044715f * g * g * g));
-    return fmaxf(g, 0.0f);
-}
-
-template <int ACT>
-__device__ __forceinline__ void act_and_slope(float g, float &a, float &d)
-{
-    if (ACT == ESP_MOE_SILU) {
-        const float s = logistic(g);
-        a = g * s;
-        d = s * (1.0f + g * (1.0f - s));
-    } else if (ACT == ESP_MOE_GELU) {
-        const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
-        a = g * c;
-        d = c + g * 0.39894228f * __expf(-0.5f * g * g);
-    } else if (ACT == ESP_MOE_GELU_TANH) {
-        const float s = logistic(1.59576912f * (g + 0.044715f * g * g * g));
-        a = g * s;
-        d = s + a * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * g * g);
-    } else {
-        a = fmaxf(g, 0.0f);
-        d = g > 0.0f ? 1.0f : 0.0f;
-    }
-}
-
-// Calls f with the activation as a constant.
-template <typename F>
-__device__ __forceinline__ void with_act(int act, F &&f)
-{
-    if (act == ESP_MOE_SILU)
-        f(std::integral_constant<int, ESP_MOE_SILU>());
-    else if (act == ESP_MOE_GELU)
-        f(std::integral_constant<int, ESP_MOE_GELU>());
-    else if (act == ESP_MOE_GELU_TANH)
-        f(std::integral_constant<int, ESP_MOE_GELU_TANH>());
-    else
-        f(std::integral_constant<int, ESP_MOE_RELU>());
 }
 
 // ---- a warp's staged box: 128 bytes of 32 rows, 16-byte chunk j of row r at place j ^ (r & 7).
@@ -514,15 +362,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const int c = 64 * wg, n = t.n0 + c, cols = p.g.N - n;
                     if (cols > 0) {
                         if (p.out2) {
-                            for (int half = 0; half < 2; ++half) {
-                                tmem_ld64(src + 128 * half + c, v);
+                            for (int part = 0; part < 4; ++part) {   // 32 columns of g, 32 more, and of u
+                                const int half = part >> 1, off = 32 * (part & 1);
+                                if (off >= cols)
+                                    continue;
+                                tmem_ld16(src + 128 * half + c + off, v[0]);
+                                tmem_ld16(src + 128 * half + c + off + 16, v[1]);
                                 tmem_wait(v);
                                 box_free();
 #pragma unroll
                                 for (int j = 0; j < 8; ++j)
-                                    box_put<T>(box, lane, j, reinterpret_cast<const float *>(&v[j / 2][8 * (j & 1)]));
-                                box_store<T>(&map_out2, n, y, half, static_cast<T *>(p.out2) + y * 2 * p.fp + half * p.fp + n,
-                                             2 * p.fp, rows, cols, true, box, lane);
+                                    box_put<float>(box, lane, j, reinterpret_cast<const float *>(&v[j / 4][4 * (j & 3)]));
+                                box_store<float>(&map_out2, n + off, y, half,
+                                                 static_cast<float *>(p.out2) + y * 2 * p.fp + half * p.fp + n + off, 2 * p.fp,
+                                                 rows, cols - off, true, box, lane);
                             }
                         }
                         box_free();
@@ -552,7 +405,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int c = 128 * wg; c < 128 * wg + 128 && t.n0 + c < p.g.N; c += 64) {
                         const int n = t.n0 + c, cols = p.g.N - n;
                         tmem_ld64(src + c, v);
-                        const T *g = static_cast<const T *>(p.pre) + (y + min(lane, rows - 1)) * 2 * p.fp + n, *u = g + p.fp;
+                        const float *g = static_cast<const float *>(p.pre) + (y + min(lane, rows - 1)) * 2 * p.fp + n;
+                        const float *u = g + p.fp;
                         tmem_wait(v);
                         box_free();
                         with_act(p.act, [&](auto kind) {
@@ -560,8 +414,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             for (int j = 0; j < 8; ++j) {
                                 float gv[8] = {}, uv[8] = {}, dg[8];
                                 if (8 * j < cols) {   // a half's rows are whole groups of 8
-                                    load_pack<T, 8>(g + 8 * j, gv);
-                                    load_pack<T, 8>(u + 8 * j, uv);
+                                    load_pack<float, 4>(g + 8 * j, gv);
+                                    load_pack<float, 4>(g + 8 * j + 4, gv + 4);
+                                    load_pack<float, 4>(u + 8 * j, uv);
+                                    load_pack<float, 4>(u + 8 * j + 4, uv + 4);
                                 }
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) {
@@ -656,49 +512,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---- launches
 
-// Boxes of 128 bytes and `rows` of the second axis of a tensor of 2- or 4-byte elements: x elements contiguous, y and z
-// ldy and ldz elements apart. What a load finds outside is zero, what a store has outside is dropped.
-cudaError_t box_map3(CUtensorMap *map, const void *p, int size, int64_t x, int64_t y, int64_t ldy, int64_t z, int64_t ldz,
-                     int rows)
-{
-    const EncodeTiled encode = encode_tiled();
-    if (!encode)
-        return cudaErrorNotSupported;
-    const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
-    const cuuint64_t strides[2] = {(cuuint64_t)ldy * size, (cuuint64_t)(z > 1 ? ldz : ldy) * size};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)rows, 1}, step[3] = {1, 1, 1};
-    const CUresult r = encode(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 3,
-                              const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
-}
-
-// Calls f(T()) for a 16-bit type.
-template <typename F>
-cudaError_t with_16(int32_t dtype, F &&f)
-{
-    return dtype == ESP_MOE_BF16 ? f(__nv_bfloat16()) : f(__half());
-}
-
-FfParams common(esp_moe *m, const FfShape &s)
-{
-    FfParams p{};
-    p.g.err = m->d_err;
-    p.g.wait_ms = m->wait_ms;
-    p.g.hold = m->hold_load ? 1 : 0;
-    m->hold_load = false;   // the hook holds one launch only
-    p.g.splits = 1;
-    p.g.M = (int32_t)s.M;
-    p.g.E = s.E;
-    p.g.offsets = s.offsets;
-    p.halves = 1;
-    p.act = s.act;
-    p.half_f16 = s.dtype == ESP_MOE_F16;
-    p.fp = s.fp;
-    return p;
-}
-
 // Row tiles of 256 over all experts, at most: each with rows has one that is not full.
 int64_t row_tiles(const FfShape &s)
 {
@@ -735,13 +548,6 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const
     return cudaLaunchKernelEx(&cfg, kernel, a, b, o, o2, p);
 }
 
-#define FF_TRY(call)                  \
-    do {                              \
-        const cudaError_t e_ = call;  \
-        if (e_ != cudaSuccess)        \
-            return e_;                \
-    } while (0)
-
 template <int KIND, typename T>
 cudaError_t rows_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o,
                         const CUtensorMap &o2, FfParams &p)
@@ -771,6 +577,12 @@ cudaError_t weights_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, c
 
 }  // namespace
 
+int few_chunk(const esp_moe *m, int64_t M, int32_t E)
+{
+    const int64_t rows = ceil_div(M, E);
+    return rows > 128 ? 0 : rows > 64 ? 128 : rows > 32 ? 64 : rows > 16 ? 32 : 16;
+}
+
 cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, void *hidden, void *pre)
 {
     FfParams p = common(m, s);
@@ -781,12 +593,14 @@ cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_
     p.g.ldo = s.fp;
     p.out2 = pre;
     CUtensorMap a, b, o, o2;
-    FF_TRY(box_map3(&a, x, 2, s.H, s.M, ldx, 1, 0, kRowsA));
+    FF_TRY(box_map3(&a, x, 2, s.H, s.M, ldx, 1, 0, s.chunk ? s.chunk : kRowsA));
     FF_TRY(box_map3(&b, s.inner, 2, s.H, s.F, s.ld_inner, 2 * (int64_t)s.E, s.F * s.ld_inner, kRowsA));
+    if (s.chunk)
+        return launch_few(m, s, HIDDEN, s.chunk, &b, &a, &p);
     FF_TRY(box_map3(&o, hidden, 2, s.F, s.M, s.fp, 1, 0, 32));
     o2 = o;
     if (pre)
-        FF_TRY(box_map3(&o2, pre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, 32));
+        FF_TRY(box_map3(&o2, pre, 4, s.F, s.M, 2 * s.fp, 2, s.fp, 32));
     return with_16(s.dtype, [&](auto elem) { return rows_launch<HIDDEN, decltype(elem)>(m, s, a, b, o, o2, p); });
 }
 
@@ -800,8 +614,10 @@ cudaError_t launch_ff_out(esp_moe *m, const FfShape &s, const void *hidden, void
     p.g.ldo = ldy;
     p.g.wide_store = rows_aligned(y, ldy, 2, 16);
     CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, hidden, 2, s.F, s.M, s.fp, 1, 0, kRowsA));
+    FF_TRY(box_map3(&a, hidden, 2, s.F, s.M, s.fp, 1, 0, s.chunk ? s.chunk : kRowsA));
     FF_TRY(box_map3(&b, s.outer, 2, s.F, s.H, s.ld_outer, s.E, s.H * s.ld_outer, kRowsA));
+    if (s.chunk)
+        return launch_few(m, s, OUT, s.chunk, &b, &a, &p);
     o = a;
     if (p.g.wide_store)
         FF_TRY(box_map3(&o, y, 2, s.H, s.M, ldy, 1, 0, 32));
@@ -818,8 +634,10 @@ cudaError_t launch_ff_dpre(esp_moe *m, const FfShape &s, const void *dy, int64_t
     p.g.ldo = 2 * s.fp;
     p.pre = pre;
     CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, kRowsA));
+    FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, s.chunk ? s.chunk : kRowsA));
     FF_TRY(box_map3(&b, s.outer, 2, s.F, s.H, s.ld_outer, s.E, s.H * s.ld_outer, kInner));
+    if (s.chunk)
+        return launch_few(m, s, DPRE, s.chunk, &b, &a, &p);
     FF_TRY(box_map3(&o, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, 32));
     return with_16(s.dtype, [&](auto elem) { return rows_launch<DPRE, decltype(elem)>(m, s, a, b, o, o, p); });
 }
@@ -835,8 +653,10 @@ cudaError_t launch_ff_dx(esp_moe *m, const FfShape &s, const void *dpre, void *d
     p.g.ldo = lddx;
     p.g.wide_store = rows_aligned(dx, lddx, 2, 16);
     CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kRowsA));
+    FF_TRY(box_map3(&a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, s.chunk ? s.chunk : kRowsA));
     FF_TRY(box_map3(&b, s.inner, 2, s.H, s.F, s.ld_inner, 2 * (int64_t)s.E, s.F * s.ld_inner, kInner));
+    if (s.chunk)
+        return launch_few(m, s, DX, s.chunk, &b, &a, &p);
     o = a;
     if (p.g.wide_store)
         FF_TRY(box_map3(&o, dx, 2, s.H, s.M, lddx, 1, 0, 32));

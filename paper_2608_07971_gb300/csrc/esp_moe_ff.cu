@@ -83,10 +83,10 @@ bool mappable(const void *x, int64_t ldx)
     return rows_aligned(x, ldx, 2, 16);
 }
 
-FfShape shape_of(const esp_moe_gated *w, int64_t M, const int32_t *offsets)
+FfShape shape_of(const esp_moe *m, const esp_moe_gated *w, int64_t M, const int32_t *offsets)
 {
     return FfShape{w->dtype, w->activation, w->E, w->F, w->H, M, offsets, w->inner, w->outer, w->ld_inner, w->ld_outer,
-                   up8(w->F)};
+                   nullptr, few_chunk(m, M, w->E), up8(w->F)};
 }
 
 }  // namespace
@@ -128,11 +128,13 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
         kept->copied = copied;
     if (M == 0)
         return ESP_OK;
-    const FfShape s = shape_of(w, M, offsets);
+    FfShape s = shape_of(m, w, M, offsets);
     const int64_t hp = up8(w->H);
     void *hidden = nullptr, *gathered = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
+        if (s.chunk)
+            s.partial = c.take<float>(few_partial_floats(m, s.chunk));
         hidden = kept ? kept->hidden : c.take<uint16_t>((size_t)(M * s.fp));
         if (copied)
             gathered = kept ? kept->rows : c.take<uint16_t>((size_t)(M * hp));
@@ -171,12 +173,14 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
             MOE_CUDA(cudaMemsetAsync(douter, 0, n, m->stream));
         return ESP_OK;
     }
-    const FfShape s = shape_of(w, M, offsets);
+    FfShape s = shape_of(m, w, M, offsets);
     const int64_t hp = up8(w->H);
     const bool copy_dy = !mappable(dy, lddy), want_dpre = dx || dinner;
     void *dpre = nullptr, *dy_copy = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
+        if (s.chunk)
+            s.partial = c.take<float>(few_partial_floats(m, s.chunk));
         if (want_dpre)
             dpre = c.take<uint16_t>((size_t)(2 * M * s.fp));
         if (copy_dy)

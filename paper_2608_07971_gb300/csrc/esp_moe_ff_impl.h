@@ -25,10 +25,21 @@ struct FfShape {
     const int32_t *offsets;
     const void *inner, *outer;
     int64_t ld_inner, ld_outer;
-    int64_t fp;               // elements between the rows of a half of `pre`, `dpre` and `hidden`: F rounded up to 8
+    float *partial;           // work space: few_partial_floats
+    int chunk;                // rows of a tile (few_chunk), 0: tiles of many rows
+    int64_t fp;               // elements of a row of a half of `pre` and `dpre`, and of `hidden`: F rounded up to 8
 };
 
-// hidden (M x fp) = act(gate) * up; pre (M x 2 x fp: gate, up) is written too where it is given.
+// ---- esp_ff_few.cu
+int few_ctas(const esp_moe *m);
+size_t few_partial_floats(const esp_moe *m, int chunk);
+// kind, w, x, params: esp_ff.cuh's Kind, tensor maps of the weights and of the rows, FfParams.
+cudaError_t launch_few(esp_moe *m, const FfShape &s, int kind, int chunk, const void *w, const void *x, const void *params);
+
+// ---- esp_ff_gemm.cu
+// Rows of a tile of a product over these rows: 0 (pairs of CTAs, 256 rows), or 16 to 128 (esp_ff_few.cu).
+int few_chunk(const esp_moe *m, int64_t M, int32_t E);
+// hidden (M x fp) = act(gate) * up; pre (M x 2 x fp fp32: gate, up) is written too where it is given.
 cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, void *hidden, void *pre);
 // y (M x H) = hidden O^T.
 cudaError_t launch_ff_out(esp_moe *m, const FfShape &s, const void *hidden, void *y, int64_t ldy);

@@ -255,8 +255,8 @@ class GatedWeight:
 
 @dataclasses.dataclass
 class Kept:
-    """What ``Moe.feed_forward`` keeps for its gradients (esp_moe_kept): pre (M, 2, F8), hidden (M, F8), rows (M, H8), with F
-    and H rounded up to multiples of 8. Made by ``Moe.keep``."""
+    """What ``Moe.feed_forward`` keeps for its gradients (esp_moe_kept): pre (M, 2, F8) fp32, hidden (M, F8), rows (M, H8),
+    with F and H rounded up to multiples of 8. Made by ``Moe.keep``."""
 
     pre: torch.Tensor
     hidden: torch.Tensor
@@ -650,11 +650,11 @@ class Moe:
     def keep(self, M: int, weight: GatedWeight) -> Kept:
         """Room for what ``feed_forward`` keeps of M rows for their gradients."""
         F8, dt = _pad8(weight.F), weight.inner.dtype
-        return Kept(self._new((M, 2, F8), dt), self._new((M, F8), dt), self._new((M, _pad8(weight.H)), dt))
+        return Kept(self._new((M, 2, F8), torch.float32), self._new((M, F8), dt), self._new((M, _pad8(weight.H)), dt))
 
     def _need_kept(self, kept: Kept, M: int, weight: GatedWeight):
         F8, dt = _pad8(weight.F), weight.inner.dtype
-        self._need(kept.pre, "pre", dt, (M, 2, F8))
+        self._need(kept.pre, "pre", torch.float32, (M, 2, F8))
         self._need(kept.hidden, "hidden", dt, (M, F8))
         self._need(kept.rows, "rows", dt, (M, _pad8(weight.H)))
 

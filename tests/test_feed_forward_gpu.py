@@ -8,7 +8,7 @@ the value; fp16 2^-11, and 2^-25 absolute below its normal range), |.| of matric
   h = act(g) u             |u| e_act + |act| e_u + e_act e_u, then r |h|
   y = h O^T                e_h |O|^T + 2 F u |h||O|^T, then r |y|
   dh = dy O                2 H u |dy||O|
-  dg = dh u act'(g)        g and u as kept, r |g| and r |u| more; act'' below 1 (relu: 1 where g is within its error of 0),
+  dg = dh u act'(g)        g and u as kept, in 32 bits; act'' below 1 (relu: 1 where g is within its error of 0),
                            act' itself 16 u (|g| + 16); the product rule, then r |dg|; du = dh act(g) likewise
   dx, dG, dU, dO           as y, from the errors of their operands
 """
@@ -82,12 +82,10 @@ def expert(x, w, o, kind, dt, dy=None):
     if dy is None:
         return out
     dh, edh = product(dy, zero(dy), o, zero(o), H)
-    egk, euk = eg + r * (g.abs() + eg) + tiny, eu + r * (u.abs() + eu) + tiny
-    es = egk + 16 * U * (g.abs() + 16) if kind != "relu" else (g.abs() <= egk).double()
-    eak = 1.13 * egk + 16 * U * (g.abs() + 16) * (g.abs() + 1)
+    es = eg + 16 * U * (g.abs() + 16) if kind != "relu" else (g.abs() <= eg).double()
     dg, du = dh * u * slope, dh * a
-    edg = (dh.abs() + edh) * (u.abs() + euk) * (slope.abs() + es) - dg.abs()
-    edu = (dh.abs() + edh) * (a.abs() + eak) - du.abs()
+    edg = (dh.abs() + edh) * (u.abs() + eu) * (slope.abs() + es) - dg.abs()
+    edu = (dh.abs() + edh) * (a.abs() + ea) - du.abs()
     edg, edu = (e + r * (d.abs() + e) + tiny for e, d in ((edg, dg), (edu, du)))
     dp, edp = torch.cat([dg, du], 1), torch.cat([edg, edu], 1)
     out["dx"] = product(dp, edp, w, zero(w), 2 * F)
