@@ -181,10 +181,10 @@ typedef struct {
     const void *inner, *outer;
 } esp_moe_gated;
 
-/* What a forward pass keeps for its gradients, in memory of the caller, 16-byte aligned; F8 and H8 are F and H rounded up
- * to a multiple of 8:
- *   pre     M x 2 x F8 fp32: G x and U x        hidden  M x F8: act(G x) * (U x)
- *   rows    M x H8: the rows, where they are gathered or x is not laid out for the tensor cores' loads (its address a
+/* What a forward pass keeps for its gradients, in memory of the caller, 16-byte aligned; F64 and H64 are F and H rounded
+ * up to a multiple of 64:
+ *   pre     M x 2 x F64 fp32: G x and U x        hidden  M x F64: act(G x) * (U x)
+ *   rows    M x H64: the rows, where they are gathered or x is not laid out for the tensor cores' loads (its address a
  *           multiple of 16 bytes and ldx of 8); may be NULL otherwise
  *   copied  set by the forward pass: whether it filled `rows` */
 typedef struct {

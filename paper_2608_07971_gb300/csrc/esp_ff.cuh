@@ -1,4 +1,4 @@
-// What the products of the gated feed-forward blocks share (esp_ff_gemm.cu: many rows, esp_ff_few.cu: few): parameters,
+// What the products of the gated feed-forward blocks share (esp_ff_gemm.cu; esp_ff_vec.cu for single rows): parameters,
 // bounded waits, operand descriptors, activations, tensor maps.
 #pragma once
 
@@ -24,6 +24,7 @@ struct FfParams {
     int32_t blocks, halves;   // blocks of the inner axis in a half, halves (DX: G and U)
     int32_t planes;           // DW: outputs of an expert (G and U, or O), each of out_rows x N
     int32_t out_rows;
+    bool tails;               // DW: a block that an expert's rows do not fill is read from the tails
     int32_t act;
     int32_t half_f16;         // operands are fp16 (else bf16)
     const void *pre;          // DPRE
@@ -31,9 +32,9 @@ struct FfParams {
     void *out2;               // HIDDEN: pre (or null)
 };
 
-// ---- waits: as wait_phase's scope says, a barrier at which this CTA's copies and threads arrive, at which another CTA's
-// warps hand tensor memory back (relaxed: the tcgen05 fences order it), or for which another CTA's warp wrote memory.
-enum Scope { OWN, HANDBACK, PAIR };
+// ---- waits, by the barrier's scope: one at which this CTA's copies, MMAs and threads arrive, or at which another CTA's
+// warps hand tensor memory back (both sides relaxed at cluster scope: the tcgen05 fences around them order it).
+enum Scope { OWN, HANDBACK };
 
 template <int SCOPE>
 __device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity)
@@ -43,14 +44,9 @@ __device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity)
         asm volatile(
             "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    else if (SCOPE == HANDBACK)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     else
         asm volatile(
-            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
             "selp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
@@ -91,11 +87,6 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, const 
 __device__ __forceinline__ void arrive_relaxed(uint32_t cluster_addr)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
-}
-
-__device__ __forceinline__ void arrive_release(uint32_t cluster_addr)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
 // Operand descriptors (version 1 in bits 46-47, 128-byte swizzle in bits 61-63). K-major: groups of 8 rows 1024 bytes
@@ -165,20 +156,20 @@ __device__ __forceinline__ void with_act(int act, F &&f)
         f(std::integral_constant<int, ESP_MOE_RELU>());
 }
 
-// Boxes of 128 bytes and `rows` of the second axis of a tensor of 2- or 4-byte elements: x elements contiguous, y and z
+// Boxes of `bytes` (128 or 64) and `rows` of the second axis of a tensor of 2- or 4-byte elements: x elements contiguous, y and z
 // ldy and ldz elements apart. What a load finds outside is zero, what a store has outside is dropped.
 cudaError_t box_map3(CUtensorMap *map, const void *p, int size, int64_t x, int64_t y, int64_t ldy, int64_t z, int64_t ldz,
-                     int rows)
+                     int rows, int bytes = 128)
 {
     const EncodeTiled encode = encode_tiled();
     if (!encode)
         return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {(cuuint64_t)x, (cuuint64_t)y, (cuuint64_t)z};
     const cuuint64_t strides[2] = {(cuuint64_t)ldy * size, (cuuint64_t)(z > 1 ? ldz : ldy) * size};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)rows, 1}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)(bytes / size), (cuuint32_t)rows, 1}, step[3] = {1, 1, 1};
     const CUresult r = encode(map, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 3,
                               const_cast<void *>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

@@ -5,7 +5,9 @@
 //   OUT     hidden x O^T
 //   DPRE    dy x O, and from it and the kept g, u the gradients of g and u
 //   DX      dpre x [G; U]
-//   DW      dpre^T x rows and dy^T x hidden: the inner axis is an expert's rows
+//   DW      dpre^T x rows and dy^T x hidden: the inner axis is an expert's rows; its last ones, where they do not fill a
+//           block of 64, come from copies padded with zeros (Tails), so that no other expert's rows, NaN included, reach
+//           the sums
 //
 // Every operand is read as it lies in memory: where the inner axis is the contiguous one, a tile is K-major (rows of 64
 // inner elements, 128 bytes, 128-byte swizzle), else MN-major (rows of 64 outer elements, one for each inner index; an
@@ -14,11 +16,12 @@
 // A tile is 256 rows of two CTAs (cta_group::2, each holding 128 rows of A and half of B's 256 columns; HIDDEN: one CTA
 // loads 128 columns of G, the other the same ones of U, so that both halves of a hidden element meet in one thread).
 // Two accumulators of 256 columns: warps 0-7 empty one while the tensor core fills the other. Warp 8 loads by TMA,
-// warp 9 issues the MMAs, warp 10 clears the rows behind an expert's last in its last block (DW). CTAs are persistent.
+// warp 9 issues the MMAs. CTAs are persistent.
 //
 // Every wait is bounded, as in esp_fp8_gemm.cu.
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "esp_ff.cuh"
@@ -29,100 +32,200 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 320;
 constexpr int kEpilogueWarps = 8;
-constexpr int kStages = 5;
-constexpr int kTileBytes = kRowsA * 128;             // one operand's share of a stage in a CTA
-constexpr int kStage = 2 * kTileBytes;
+constexpr int kTileBytes = kRowsA * 128;             // 128 rows of one operand in a stage
 constexpr int kBoxBytes = 128, kBox = 32 * kBoxBytes;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kAccCols = 256;
-constexpr int kTable = (ESP_MOE_MAX_EXPERTS + 1) * 4 + 12;
-constexpr int kBars = 192;
-constexpr int kSmem = kStages * kStage + kEpilogueWarps * kBox + kTable + kBars + 1024;
-static_assert((3 * kStages + 2 * 2 + 1) * 8 + 16 <= kBars, "barriers");
-static_assert(kSmem <= 232448, "shared memory");
+constexpr int kBars = 256;
 
-// One item of the list. Row kinds: rows m0 .. m0 + rows - 1 of expert e, columns n0 ..; DW: output rows m0 .. of plane z,
-// over the rows lo .. hi - 1.
+// CG: CTAs that share a tile. An epilogue warp stages its stores in boxes; DPRE's g and u arrive in two (a third one, for
+// the next g and u, at the cost of a stage of the operands: 16384 x 2048 x 4096 234 us, 210 with two).
+template <int CG, int KIND>
+struct Shape {
+    static constexpr int kRows = 128 * CG;                        // of a tile
+    static constexpr int kStageB = CG == 2 ? kTileBytes : 2 * kTileBytes;
+    static constexpr int kStage = kTileBytes + kStageB;
+    static constexpr int kStages = (CG == 2 ? 5 : 4) - (KIND == DPRE && CG == 1 ? 1 : 0);
+    static constexpr int kBoxes = KIND == DPRE || CG == 2 ? 2 : 1;
+    static constexpr int kSmem = kStages * kStage + kEpilogueWarps * kBoxes * kBox + kBars + 1024;
+    static_assert((2 * kStages + 2 * 2 + 1 + kEpilogueWarps) * 8 + 16 <= kBars, "barriers");
+    static_assert(kSmem <= 232448, "shared memory");
+};
+
+// One item of the list: blocks k0 .. k1 - 1 of the inner axis of a tile. Row kinds: rows m0 .. m0 + rows - 1 of expert e,
+// columns n0 ..; DW: output rows m0 .. of plane z, over the rows lo .. hi - 1, the last block from the tails where `cut` is set.
 struct FfTile {
-    int e, m0, rows, n0, blocks, z, lo, hi;
+    int item, e, m0, rows, n0, k0, k1, z, lo, hi;
+    bool cut;
 };
 
 template <int KIND>
 constexpr int kTileCols = KIND == HIDDEN ? 128 : 256;
 
-template <int KIND>
-__device__ __forceinline__ bool ff_tile(const FfParams &p, const int *table, int item, FfTile &t)
-{
-    if (KIND != DW) {
-        Tile r;
-        if (!tile_at<2, kTileCols<KIND>, false>(p.g, table, item, r))
+// A role's way through the list, in rounds of an item for every CTA (pair), every second round backwards, so that nobody
+// gets the longer item of every round (experts' rows differ). Tiles run over an expert's rows first, so that the tiles in
+// flight share columns of B. Items ascend: the row kinds' expert is kept from one to the next.
+template <int CG, int KIND>
+class Walk {
+public:
+    __device__ __forceinline__ bool next(const FfParams &p, FfTile &t)
+    {
+        const int n = gridDim.x / CG, me = blockIdx.x / CG, item = round_ * n + (round_ & 1 ? n - 1 - me : me);
+        ++round_;
+        t.item = item;
+        if (CG == 2 || p.g.splits == 1)
+            return tile(p, item, t);
+        const int part = item % p.g.splits;
+        if (!tile(p, item / p.g.splits, t))
             return false;
-        t.e = r.e;
-        t.m0 = r.m0;
-        t.rows = r.rows;
-        t.n0 = r.n0;
-        t.blocks = p.blocks * p.halves;
+        const int blocks = t.k1;
+        t.k0 = (int)((int64_t)blocks * part / p.g.splits);
+        t.k1 = (int)((int64_t)blocks * (part + 1) / p.g.splits);
+        t.cut = t.cut && t.k0 < t.k1 && t.k1 == blocks;
         return true;
     }
-    const int mt = (p.out_rows + 255) / 256, nt = (p.g.N + 255) / 256, per = mt * nt * p.planes;
-    if (item >= per * p.g.E)
-        return false;
-    t.e = item / per;
-    int i = item - t.e * per;
-    t.z = i / (mt * nt);
-    i -= t.z * (mt * nt);
-    t.m0 = (i % mt) * 256;
-    t.n0 = (i / mt) * 256;
-    t.rows = min(256, p.out_rows - t.m0);
-    expert_rows(p.g, t.e, t.lo, t.hi);
-    t.blocks = (t.hi - t.lo) / kInner + ((t.hi - t.lo) % kInner != 0);
-    return true;
-}
 
-// A box into this CTA's shared memory; its bytes arrive at a barrier of either CTA of the pair.
+private:
+    __device__ __forceinline__ bool tile(const FfParams &p, int item, FfTile &t)
+    {
+        constexpr int kRows = Shape<CG, KIND>::kRows;
+        t.k0 = 0;
+        t.cut = false;
+        if (KIND != DW) {
+            const int nt = (p.g.N + kTileCols<KIND> - 1) / kTileCols<KIND>;
+            while (item >= (before_ + tiles_) * nt) {
+                before_ += tiles_;
+                if (++e_ >= p.g.E)
+                    return false;
+                expert_rows(p.g, e_, lo_, hi_);
+                // offsets that do not ascend have more tiles than the list
+                tiles_ = min((hi_ - lo_) / kRows + ((hi_ - lo_) % kRows != 0), p.g.most - before_);
+            }
+            const int i = item - before_ * nt;
+            t.e = e_;
+            t.m0 = lo_ + (i % tiles_) * kRows;
+            t.rows = min(kRows, hi_ - t.m0);
+            t.n0 = (i / tiles_) * kTileCols<KIND>;
+            t.k1 = p.blocks * p.halves;
+            return true;
+        }
+        const int mt = (p.out_rows + kRows - 1) / kRows, nt = (p.g.N + 255) / 256, per = mt * nt * p.planes;
+        if (item >= per * p.g.E)
+            return false;
+        t.e = item / per;
+        int i = item - t.e * per;
+        t.z = i / (mt * nt);
+        i -= t.z * (mt * nt);
+        t.m0 = (i % mt) * kRows;
+        t.n0 = (i / mt) * 256;
+        t.rows = min(kRows, p.out_rows - t.m0);
+        expert_rows(p.g, t.e, t.lo, t.hi);
+        const bool part = (t.hi - t.lo) % kInner != 0;   // without tails, what follows the last row is outside: zeros
+        t.cut = part && p.tails;
+        t.k1 = (t.hi - t.lo) / kInner + part;
+        return true;
+    }
+
+    int round_ = 0;
+    int e_ = -1, before_ = 0, tiles_ = 0, lo_ = 0, hi_ = 0;   // expert, row tiles of those before it, its own, its rows
+};
+
+// A box into this CTA's shared memory; its bytes arrive at a barrier of this CTA or of the other one of a pair.
+template <int CG>
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
-        "%3, %4}], [%5];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
+    if (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, "
+            "{%2, %3, %4}], [%5];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+            "[%5];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
 }
 
+template <int CG>
 __device__ __forceinline__ void mma16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
+    if (CG == 2)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
 }
 
-// ---- a warp's staged box: 128 bytes of 32 rows, 16-byte chunk j of row r at place j ^ (r & 7).
-
-// Waits until the box's last store has been read.
-__device__ __forceinline__ void box_free()
+// ---- a warp's staged box: 128 bytes of 32 rows, 16-byte chunk j of row r at place j ^ (r & 7) (the 128-byte swizzle), or
+// half a box: 64 bytes of 32 rows, chunk j at place j ^ (r / 2 & 3) (the 64-byte swizzle).
+template <int BYTES>
+__device__ __forceinline__ int box_place(int r, int j)
 {
-    asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
-    __syncwarp();
+    return r * BYTES + (BYTES == 128 ? j ^ (r & 7) : j ^ (r >> 1 & 3)) * 16;
 }
 
-// V values of this lane's row into chunk j.
-template <typename T>
+// N boxes, used in turn.
+template <int N>
+class Staging {
+public:
+    __device__ explicit Staging(unsigned char *at) : at_(at) {}
+    // The next box, once its last store has been read (each box's stores are one bulk group).
+    __device__ __forceinline__ unsigned char *next()
+    {
+        asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read %0;" ::"n"(N - 1) : "memory");
+        __syncwarp();
+        turn_ = turn_ == N - 1 ? 0 : turn_ + 1;
+        return at_ + turn_ * kBox;
+    }
+
+    // Waits until the stores of all boxes have been read.
+    __device__ __forceinline__ void drain()
+    {
+        asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+
+private:
+    unsigned char *at_;
+    int turn_ = 0;
+};
+
+// Values of this lane's row into and out of chunk j.
+template <typename T, int BYTES>
 __device__ __forceinline__ void box_put(unsigned char *box, int lane, int j, const float *v)
 {
-    store_pack<T, 16 / (int)sizeof(T)>(reinterpret_cast<T *>(box + lane * kBoxBytes + ((j ^ (lane & 7)) * 16)), v);
+    store_pack<T, 16 / (int)sizeof(T)>(reinterpret_cast<T *>(box + box_place<BYTES>(lane, j)), v);
+}
+
+__device__ __forceinline__ void box_get(const unsigned char *box, int lane, int j, float *v)
+{
+    load_pack<float, 4>(reinterpret_cast<const float *>(box + box_place<128>(lane, j)), v);
+}
+
+template <typename T>
+__device__ __forceinline__ bool rows_aligned4(const T *p, int64_t ld)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld * sizeof(T)) & 3) == 0;
 }
 
 // The box leaves: by one TMA store where all its rows are there to be written (columns past the matrix are dropped by the
 // store), else by the lanes: rows at or past `rows`, columns at or past `cols` are dropped.
-template <typename T>
+template <typename T, int BYTES>
 __device__ __forceinline__ void box_store(const CUtensorMap *map, int x, int y, int z, T *out, int64_t ldo, int rows,
                                           int cols, bool wide, const unsigned char *box, int lane)
 {
-    constexpr int V = 16 / (int)sizeof(T), C = kBoxBytes / (int)sizeof(T);
+    constexpr int V = 16 / (int)sizeof(T), C = BYTES / (int)sizeof(T), J = BYTES / 16;
     if (wide && rows >= 32) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -134,144 +237,154 @@ __device__ __forceinline__ void box_store(const CUtensorMap *map, int x, int y, 
     }
     __syncwarp();
     if (wide && cols >= C) {
-        const int j = lane & 7;
-        for (int r = lane >> 3; r < 32 && r < rows; r += 4)
-            *reinterpret_cast<uint4 *>(out + r * ldo + j * V) =
-                *reinterpret_cast<const uint4 *>(box + r * kBoxBytes + ((j ^ (r & 7)) * 16));
+        const int j = lane % J;
+#pragma unroll
+        for (int i = 0; i < J; ++i) {
+            const int r = lane / J + i * (32 / J);
+            if (r < rows)
+                *reinterpret_cast<uint4 *>(out + r * ldo + j * V) =
+                    *reinterpret_cast<const uint4 *>(box + box_place<BYTES>(r, j));
+        }
+    } else if (BYTES == 128 && cols >= C && rows_aligned4(out, ldo)) {   // a lane 4 bytes of every row
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r)
+            if (r < rows)
+                reinterpret_cast<uint32_t *>(out + r * ldo)[lane] =
+                    *reinterpret_cast<const uint32_t *>(box + box_place<BYTES>(r, lane / 4) + lane % 4 * 4);
     } else {
-        for (int r = 0; r < 32 && r < rows; ++r)
-            for (int c = lane; c < C && c < cols; c += 32)
-                out[r * ldo + c] =
-                    reinterpret_cast<const T *>(box + r * kBoxBytes + (((c / V) ^ (r & 7)) * 16))[c % V];
+#pragma unroll
+        for (int c0 = 0; c0 < C; c0 += 32) {
+            const int c = c0 + lane;
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r)
+                if (r < rows && c < cols)
+                    out[r * ldo + c] = reinterpret_cast<const T *>(box + box_place<BYTES>(r, c / V))[c % V];
+        }
     }
     __syncwarp();
 }
 
-// 64 columns of this thread's lane of tensor memory.
-__device__ __forceinline__ void tmem_ld64(uint32_t addr, uint32_t (&v)[4][16])
+// Barrier of the epilogue's threads that also ANDs a predicate over them.
+__device__ __forceinline__ bool all_of_epilogue(bool v)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        tmem_ld16(addr + 16 * i, v[i]);
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)v), "n"(32 * kEpilogueWarps)
+        : "memory");
+    return r != 0;
 }
 
-// T: operands; O: output.
-template <int KIND, typename T, typename O>
+// T: operands; O: output. map_a2, map_b2: DW's tails; map_a2: HIDDEN's and DPRE's pre.
+template <int CG, int KIND, typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 1)
     k_ff(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-         const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_out2, const FfParams p)
+         const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_a2,
+         const __grid_constant__ CUtensorMap map_b2, const FfParams p)
 {
+    using S = Shape<CG, KIND>;
+    constexpr int kStages = S::kStages, kStage = S::kStage;
     constexpr bool A_MN = KIND == DW, B_MN = KIND == DPRE || KIND == DX || KIND == DW;
     extern __shared__ unsigned char smem_raw[];
     unsigned char *sm = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                                           ~static_cast<uintptr_t>(1023));
     unsigned char *staging = sm + kStages * kStage;
-    int *table = reinterpret_cast<int *>(staging + kEpilogueWarps * kBox);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(reinterpret_cast<unsigned char *>(table) + kTable);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kEpilogueWarps * S::kBoxes * kBox);
     const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, tfull = empty + 8 * kStages, tempty = tfull + 16,
-                   tail = tempty + 16, drain = tail + 8 * kStages;
-    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 3 * kStages + 5);
-    volatile int *dead = reinterpret_cast<volatile int *>(slot + 1);
+                   drain = tempty + 16, landed = drain + 8;
+    uint32_t *slot = reinterpret_cast<uint32_t *>(bars + 2 * kStages + 5 + kEpilogueWarps);
+    volatile int *dead = reinterpret_cast<volatile int *>(slot + 1), *last = dead + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
+    const uint32_t rank = CG == 1 ? 0 : cluster_rank();
 
     if (threadIdx.x == 0) {
         *dead = 0;
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(full + 8 * i, KIND == DW ? 2 : 1);   // DW: one arrival of each CTA
+            mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
-            mbar_init(tail + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(tfull + 8 * i, 1);
-            mbar_init(tempty + 8 * i, 2 * kEpilogueWarps);
+            mbar_init(tempty + 8 * i, CG * kEpilogueWarps);
         }
         mbar_init(drain, 1);
+        for (int i = 0; i < kEpilogueWarps; ++i)
+            mbar_init(landed + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
-                     "r"(kTmemCols)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-    wait_for_launch_before();
-    if (KIND != DW && warp == 8) {
-        // the experts' row tiles before each: one warp's scan
-        int carry = 0;
-        for (int e0 = 0; e0 < p.g.E; e0 += 32) {
-            const int n = e0 + lane < p.g.E ? tiles_of<2, false>(p.g, e0 + lane) : 0;
-            int s = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, s, o);
-                if (lane >= o)
-                    s += y;
-            }
-            if (e0 + lane < p.g.E)
-                table[e0 + lane] = min(p.g.most, carry + s - n);
-            carry = min(p.g.most, carry + __shfl_sync(0xffffffffu, s, 31));
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)),
+                         "r"(kTmemCols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
-        if (lane == 0)
-            table[p.g.E] = carry;
     }
     fence_before();
     __syncthreads();
-    cluster_sync();
+    if (CG == 2)
+        cluster_sync();
     fence_after();
+    wait_for_launch_before();
     const uint32_t tmem = *slot;
-    const int w0 = blockIdx.x / 2, dw = gridDim.x / 2;
-    // of this CTA's loading warp: its loads, the stages whose tail barrier it used, and those barriers' next phases
-    uint32_t issued = 0, tail_used = 0, tail_phase = 0;
+    uint32_t issued = 0;   // loads of this CTA's loading warp
     FfTile t;
+    Walk<CG, KIND> walk;
 
     if (warp == 8) {
-        const uint32_t full0 = map_rank(full, 0);
+        const uint32_t full0 = CG == 1 ? full : map_rank(full, 0);
         int s = 0;
         uint32_t ph = 1;
         bool ok = true;
-        for (int w = w0; ok && ff_tile<KIND>(p, table, w, t); w += dw) {
+        while (ok && walk.next(p, t)) {
             const int outer_a = t.m0 + (int)rank * kRowsA;
-            const int outer_b = t.n0 + (KIND == HIDDEN ? 0 : (int)rank * kRowsA);
-            for (int kb = 0; kb < t.blocks; ++kb) {
+            const int outer_b = t.n0 + (KIND == HIDDEN ? 0 : (int)rank * 128);
+            for (int kb = t.k0; kb < t.k1; ++kb) {
                 if (!(ok = wait_phase(empty + 8 * s, ph, p.g, dead)))
                     break;
                 const uint32_t a = smem_u32(sm + s * kStage), b = a + kTileBytes;
                 const int half = KIND == DX && kb >= p.blocks ? 1 : 0, k = (kb - half * p.blocks) * kInner;
-                const bool cut = KIND == DW && kb == t.blocks - 1 && (t.hi - t.lo) % kInner != 0;
+                const bool cut = KIND == DW && t.cut && kb == t.k1 - 1;
                 if (elect_one()) {
-                    uint32_t bar = full0 + 8 * s;
-                    if (cut) {   // arrives here first: warp 10 clears what is not the expert's
-                        bar = map_rank(tail + 8 * s, rank);
-                        mbar_expect(tail + 8 * s, kStage);
-                    } else if (rank == 0) {
-                        mbar_expect(full + 8 * s, 2 * kStage);
-                    } else if (KIND == DW) {
-                        arrive_relaxed(bar);
-                    }
+                    const uint32_t bar = full0 + 8 * s;
+                    if (rank == 0)
+                        mbar_expect(full + 8 * s, CG * kStage);
                     if (!(p.g.hold && issued == 2)) {
+                        constexpr int kHalves = S::kStageB / kHalfTile;   // MN-major halves of B
+                        // DW: the inner axis' first row, and the tensors that hold it
+                        const int y = KIND == DW ? (cut ? t.e * kInner : t.lo + k) : k;
+                        const CUtensorMap *const a_map = KIND == DW && cut ? &map_a2 : &map_a;
+                        const CUtensorMap *const b_map = KIND == DW && cut ? &map_b2 : &map_b;
                         if (A_MN) {
-                            load_box(a, &map_a, outer_a, t.lo + k, t.z, bar);
-                            load_box(a + kHalfTile, &map_a, outer_a + 64, t.lo + k, t.z, bar);
+                            load_box<CG>(a, a_map, outer_a, y, t.z, bar);
+                            load_box<CG>(a + kHalfTile, a_map, outer_a + 64, y, t.z, bar);
                         } else {
-                            load_box(a, &map_a, k, outer_a, half, bar);
+                            load_box<CG>(a, &map_a, k, outer_a, half, bar);
                         }
-                        if (KIND == DW) {
-                            load_box(b, &map_b, outer_b, t.lo + k, 0, bar);
-                            load_box(b + kHalfTile, &map_b, outer_b + 64, t.lo + k, 0, bar);
-                        } else if (B_MN) {
-                            const int z = KIND == DX ? 2 * t.e + half : t.e;
-                            load_box(b, &map_b, outer_b, k, z, bar);
-                            load_box(b + kHalfTile, &map_b, outer_b + 64, k, z, bar);
+                        if (B_MN) {
+                            const int z = KIND == DW ? 0 : KIND == DX ? 2 * t.e + half : t.e;
+#pragma unroll
+                            for (int i = 0; i < kHalves; ++i)
+                                load_box<CG>(b + i * kHalfTile, b_map, outer_b + 64 * i, y, z, bar);
+                        } else if (KIND == HIDDEN) {
+                            load_box<CG>(b, &map_b, k, outer_b, 2 * t.e + (int)rank, bar);
+                            if (CG == 1)
+                                load_box<CG>(b + kTileBytes, &map_b, k, outer_b, 2 * t.e + 1, bar);
                         } else {
-                            load_box(b, &map_b, k, outer_b, KIND == HIDDEN ? 2 * t.e + (int)rank : t.e, bar);
+                            load_box<CG>(b, &map_b, k, outer_b, t.e, bar);
+                            if (CG == 1)
+                                load_box<CG>(b + kTileBytes, &map_b, k, outer_b + 128, t.e, bar);
                         }
                     }
                 }
                 __syncwarp();
                 ++issued;
-                tail_used |= (uint32_t)cut << s;
-                tail_phase ^= (uint32_t)cut << s;
                 if (++s == kStages) {
                     s = 0;
                     ph ^= 1;
@@ -282,17 +395,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (rank == 0) {
             const uint32_t format = p.half_f16 ? 0u : (1u << 7) | (1u << 10);
             const uint32_t idesc = (1u << 4) | format | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) |
-                                   ((uint32_t)(kAccCols >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+                                   ((uint32_t)(kAccCols >> 3) << 17) | ((uint32_t)(128 * CG >> 4) << 24);
             int s = 0, acc = 0;
             uint32_t ph = 0, aph = 1;
             bool ok = true;
-            for (int w = w0; ok && ff_tile<KIND>(p, table, w, t); w += dw) {
-                if (t.blocks == 0)
+            while (ok && walk.next(p, t)) {
+                if (t.k0 == t.k1)
                     continue;
-                if (!(ok = wait_phase<HANDBACK>(tempty + 8 * acc, aph, p.g, dead)))
+                if (!(ok = wait_phase<CG == 2 ? HANDBACK : OWN>(tempty + 8 * acc, aph, p.g, dead)))
                     break;
-                for (int kb = 0; kb < t.blocks; ++kb) {
-                    if (!(ok = wait_phase<KIND == DW ? PAIR : OWN>(full + 8 * s, ph, p.g, dead)))
+                for (int kb = t.k0; kb < t.k1; ++kb) {
+                    if (!(ok = wait_phase(full + 8 * s, ph, p.g, dead)))
                         break;
                     fence_after();
                     const uint64_t a = operand<A_MN>(smem_u32(sm + s * kStage));
@@ -300,11 +413,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < kInner / 16; ++k)
-                            mma16(tmem + acc * kAccCols, a + k * kOperandStep<A_MN>, b + k * kOperandStep<B_MN>, idesc,
-                                  kb > 0 || k > 0);
-                        mma_commit<2>(empty + 8 * s);
-                        if (kb == t.blocks - 1)
-                            mma_commit<2>(tfull + 8 * acc);
+                            mma16<CG>(tmem + acc * kAccCols, a + k * kOperandStep<A_MN>, b + k * kOperandStep<B_MN>, idesc,
+                                  kb > t.k0 || k > 0);
+                        mma_commit<CG>(empty + 8 * s);
+                        if (kb == t.k1 - 1)
+                            mma_commit<CG>(tfull + 8 * acc);
                     }
                     __syncwarp();
                     if (++s == kStages) {
@@ -316,77 +429,144 @@ __global__ void __launch_bounds__(kThreads, 1)
                 aph ^= acc == 0;
             }
         }
-    } else if (KIND == DW && warp == 10) {
-        // rows of the next expert in this one's last block: zeros in both operands, so that nothing of theirs, NaN
-        // included, reaches the sums
-        const uint32_t full0 = map_rank(full, 0);
-        int s = 0;
-        uint32_t tph = 0;   // a bit for each stage
-        for (int w = w0; ff_tile<KIND>(p, table, w, t); w += dw) {
-            const int rows = (t.hi - t.lo) % kInner;
-            if (rows != 0) {
-                const int at = (s + t.blocks - 1) % kStages;
-                if (!wait_phase(tail + 8 * at, tph >> at & 1, p.g, dead))
-                    break;
-                tph ^= 1u << at;
-                unsigned char *stage = sm + at * kStage;
-                for (int i = lane; i < 4 * (kInner - rows) * 8; i += 32) {
-                    const int part = i & 3, chunk = (i >> 2) & 7, row = rows + (i >> 5);
-                    *reinterpret_cast<uint4 *>(stage + part * kHalfTile + row * 128 + chunk * 16) = make_uint4(0, 0, 0, 0);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0)
-                    arrive_release(full0 + 8 * at);
-            }
-            s = (s + t.blocks) % kStages;
-        }
     } else if (warp < kEpilogueWarps) {
         const int wg = warp >> 2, quarter = warp & 3;
-        const uint32_t tempty0 = map_rank(tempty, 0);
-        unsigned char *box = staging + warp * kBox;
+        const uint32_t tempty0 = CG == 1 ? tempty : map_rank(tempty, 0);
+        unsigned char *const gbox = staging + warp * S::kBoxes * kBox, *const ubox = gbox + kBox;   // DPRE
+        Staging<S::kBoxes> boxes(gbox);
         int acc = 0;
-        uint32_t aph = 0;
-        for (int w = w0; ff_tile<KIND>(p, table, w, t); w += dw) {
+        uint32_t aph = 0, lph = 0;
+        bool loading = false;   // DPRE: g and u are on their way to the staging boxes
+        while (walk.next(p, t)) {
             const int rows = t.rows - (int)rank * kRowsA - 32 * quarter;   // of this warp's 32 that exist, from the first
             const int y = t.m0 + (int)rank * kRowsA + 32 * quarter;        // the first
-            if (t.blocks > 0) {
-                if (!wait_phase(tfull + 8 * acc, aph, p.g, dead))
-                    break;
-                fence_after();
-            }
+            const bool split = CG == 1 && p.g.splits > 1, some = t.k0 < t.k1;
             const uint32_t src = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(acc * kAccCols);
-            if (rows > 0) {
-                uint32_t v[4][16];
+            // DPRE: 32 columns of g and u at a time, from column c of the tile on, into two boxes; they arrive together
+            const auto load_pre = [&](int c) {
+                if (lane == 0) {
+                    mbar_expect(landed + 8 * warp, 2 * kBox);
+                    load_box<CG>(smem_u32(gbox), &map_a2, t.n0 + c, y, 0, landed + 8 * warp);
+                    load_box<CG>(smem_u32(ubox), &map_a2, t.n0 + c, y, 1, landed + 8 * warp);
+                }
+                loading = true;
+            };
+            const int first = 128 * wg, columns = min(128, p.g.N - t.n0 - first);   // of this warp (not HIDDEN)
+            if (KIND == DPRE && !split && rows > 0 && columns > 0) {
+                boxes.drain();
+                load_pre(first);
+            }
+            bool ok = !some || wait_phase(tfull + 8 * acc, aph, p.g, dead);
+            if (split)   // all warps go on, or none: those that join a tile meet at a barrier
+                ok = all_of_epilogue(ok);
+            if (!ok)
+                break;
+            fence_after();
+            bool joined = false, skip = rows <= 0;
+            // 16 columns of this thread's row from each of four places
+            const float *parts = nullptr;
+            uint32_t v[4][16];
+            const auto fetch = [&](int c0, int c1, int c2, int c3) {
+                const int c[4] = {c0, c1, c2, c3};
+                if (joined) {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        v[i / 16][i % 16] = 0u;
+                    for (int q = 0; q < p.g.splits; ++q) {
+                        float one[64];   // all on their way before the first is added
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            one[i] = __ldcg(parts + ((int64_t)q * kAccCols + c[i / 16] + i % 16) * kRowsA);
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            v[i / 16][i % 16] = __float_as_uint(__uint_as_float(v[i / 16][i % 16]) + one[i]);
+                    }
+                } else if (some) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        tmem_ld16(src + c[i], v[i]);
+                    tmem_wait(v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        v[i / 16][i % 16] = 0u;
+                }
+            };
+            const auto release = [&] {   // the accumulator has been read
+                if (!some)
+                    return;
+                fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2)
+                        arrive_relaxed(tempty0 + 8 * acc);
+                    else
+                        mbar_arrive_cta(tempty0 + 8 * acc);
+                }
+            };
+            if (split) {
+                // this part's sums go to memory; the last part of the tile to arrive adds all of them up, in order
+                const int tile = t.item / p.g.splits;
+                float *const of_tile =
+                    p.g.partial + (int64_t)tile * p.g.splits * kAccCols * kRowsA + 32 * quarter + lane;
+                float *const mine = of_tile + (int64_t)(t.item - tile * p.g.splits) * kAccCols * kRowsA;
+                if (!skip)
+                    for (int b = 0; b < 2; ++b) {
+                        const int c = KIND == HIDDEN ? 128 * b + 64 * wg : first + 64 * b;
+                        fetch(c, c + 16, c + 32, c + 48);
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            __stcg(mine + (int64_t)(c + i) * kRowsA, __uint_as_float(v[i / 16][i % 16]));
+                    }
+                release();
+                __threadfence();
+                all_of_epilogue(true);
+                if (threadIdx.x == 0) {
+                    const bool l = atomicAdd(p.g.tickets + tile, 1u) == (unsigned)p.g.splits - 1;
+                    if (l)
+                        p.g.tickets[tile] = 0u;
+                    *last = l;
+                    __threadfence();
+                }
+                all_of_epilogue(true);
+                joined = true;
+                parts = of_tile;
+                skip = skip || !*last;
+                all_of_epilogue(true);   // `last` has been read
+                if (KIND == DPRE && !skip && columns > 0) {
+                    boxes.drain();
+                    load_pre(first);
+                }
+            }
+            if (!skip) {
                 if (KIND == HIDDEN) {
                     const int c = 64 * wg, n = t.n0 + c, cols = p.g.N - n;
                     if (cols > 0) {
                         if (p.out2) {
-                            for (int part = 0; part < 4; ++part) {   // 32 columns of g, 32 more, and of u
-                                const int half = part >> 1, off = 32 * (part & 1);
-                                if (off >= cols)
-                                    continue;
-                                tmem_ld16(src + 128 * half + c + off, v[0]);
-                                tmem_ld16(src + 128 * half + c + off + 16, v[1]);
-                                tmem_wait(v);
-                                box_free();
+                            for (int half = 0; half < 2; ++half) {   // g, u
+                                const int at = 128 * half + c;
+                                fetch(at, at + 16, at + 32, at + 48);
 #pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    box_put<float>(box, lane, j, reinterpret_cast<const float *>(&v[j / 4][4 * (j & 3)]));
-                                box_store<float>(&map_out2, n + off, y, half,
-                                                 static_cast<float *>(p.out2) + y * 2 * p.fp + half * p.fp + n + off, 2 * p.fp,
-                                                 rows, cols - off, true, box, lane);
+                                for (int b = 0; b < 2; ++b) {
+                                    if (32 * b >= cols)
+                                        break;
+                                    unsigned char *box = boxes.next();
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j)
+                                        box_put<float, 128>(box, lane, j,
+                                                            reinterpret_cast<const float *>(&v[2 * b + j / 4][4 * (j & 3)]));
+                                    box_store<float, 128>(
+                                        &map_a2, n + 32 * b, y, half,
+                                        static_cast<float *>(p.out2) + y * 2 * p.fp + half * p.fp + n + 32 * b, 2 * p.fp, rows,
+                                        cols - 32 * b, true, box, lane);
+                                }
                             }
                         }
-                        box_free();
+                        unsigned char *box = boxes.next();
                         with_act(p.act, [&](auto kind) {
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                tmem_ld16(src + c + 32 * h, v[0]);
-                                tmem_ld16(src + c + 32 * h + 16, v[1]);
-                                tmem_ld16(src + 128 + c + 32 * h, v[2]);
-                                tmem_ld16(src + 128 + c + 32 * h + 16, v[3]);
-                                tmem_wait(v);
+                                fetch(c + 32 * h, c + 32 * h + 16, 128 + c + 32 * h, 128 + c + 32 * h + 16);
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
                                     float r[8];
@@ -394,94 +574,90 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     for (int i = 0; i < 8; ++i)
                                         r[i] = act_of<decltype(kind)::value>(__uint_as_float(v[j / 2][8 * (j & 1) + i])) *
                                                __uint_as_float(v[2 + j / 2][8 * (j & 1) + i]);
-                                    box_put<T>(box, lane, 4 * h + j, r);
+                                    box_put<T, 128>(box, lane, 4 * h + j, r);
                                 }
                             }
                         });
-                        box_store<T>(&map_out, n, y, 0, static_cast<T *>(p.g.out) + y * p.g.ldo + n, p.g.ldo, rows, cols, true,
-                                     box, lane);
+                        box_store<T, 128>(&map_out, n, y, 0, static_cast<T *>(p.g.out) + y * p.g.ldo + n, p.g.ldo, rows, cols,
+                                          true, box, lane);
                     }
                 } else if (KIND == DPRE) {
-                    for (int c = 128 * wg; c < 128 * wg + 128 && t.n0 + c < p.g.N; c += 64) {
-                        const int n = t.n0 + c, cols = p.g.N - n;
-                        tmem_ld64(src + c, v);
-                        const float *g = static_cast<const float *>(p.pre) + (y + min(lane, rows - 1)) * 2 * p.fp + n;
-                        const float *u = g + p.fp;
-                        tmem_wait(v);
-                        box_free();
+                    bool landed_all = true;
+                    for (int c = first; c < first + columns; c += 32) {
+                        const int h = (c - first) & 32;   // columns come 64 at a time
+                        if (h == 0)
+                            fetch(c, c + 16, c + 32, c + 48);
+                        if (!(landed_all = wait_phase(landed + 8 * warp, lph, p.g, dead)))
+                            break;
+                        loading = false;
+                        lph ^= 1;
+                        float g[32], u[32];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            box_get(gbox, lane, j, g + 4 * j);
+                            box_get(ubox, lane, j, u + 4 * j);
+                        }
+                        __syncwarp();
                         with_act(p.act, [&](auto kind) {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                float gv[8] = {}, uv[8] = {}, dg[8];
-                                if (8 * j < cols) {   // a half's rows are whole groups of 8
-                                    load_pack<float, 4>(g + 8 * j, gv);
-                                    load_pack<float, 4>(g + 8 * j + 4, gv + 4);
-                                    load_pack<float, 4>(u + 8 * j, uv);
-                                    load_pack<float, 4>(u + 8 * j + 4, uv + 4);
-                                }
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    uint32_t &d = v[j / 2][8 * (j & 1) + i];
-                                    const float dh = __uint_as_float(d);
-                                    float a, slope;
-                                    act_and_slope<decltype(kind)::value>(gv[i], a, slope);
-                                    dg[i] = dh * uv[i] * slope;
-                                    d = __float_as_uint(dh * a);
-                                }
-                                box_put<T>(box, lane, j, dg);
+                            for (int i = 0; i < 32; ++i) {
+                                const float dh = __uint_as_float(h == 0 ? v[i / 16][i % 16] : v[2 + i / 16][i % 16]);
+                                float a, slope;
+                                act_and_slope<decltype(kind)::value>(g[i], a, slope);
+                                g[i] = dh * u[i] * slope;
+                                u[i] = dh * a;
                             }
                         });
-                        for (int half = 0; half < 2; ++half) {
-                            if (half == 1) {
-                                box_free();
+                        // both results, 64 bytes of every row, in the box that u came in
+                        const int n = t.n0 + c;
 #pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    box_put<T>(box, lane, j, reinterpret_cast<const float *>(&v[j / 2][8 * (j & 1)]));
-                            }
-                            box_store<T>(&map_out, n, y, half, static_cast<T *>(p.g.out) + y * 2 * p.fp + half * p.fp + n,
-                                         2 * p.fp, rows, cols, true, box, lane);
+                        for (int j = 0; j < 4; ++j) {
+                            box_put<T, 64>(ubox, lane, j, g + 8 * j);
+                            box_put<T, 64>(ubox + kBox / 2, lane, j, u + 8 * j);
+                        }
+                        T *out = static_cast<T *>(p.g.out) + y * 2 * p.fp + n;
+                        box_store<T, 64>(&map_out, n, y, 0, out, 2 * p.fp, rows, p.g.N - n, true, ubox, lane);
+                        box_store<T, 64>(&map_out, n, y, 1, out + p.fp, 2 * p.fp, rows, p.g.N - n, true, ubox + kBox / 2, lane);
+                        if (c + 32 < first + columns) {
+                            boxes.drain();
+                            load_pre(c + 32);
                         }
                     }
+                    if (!landed_all)
+                        break;
                 } else {
                     constexpr int C = kBoxBytes / (int)sizeof(O), V = 16 / (int)sizeof(O);
                     const int z = KIND == DW ? t.e * p.planes + t.z : 0;
                     O *out = static_cast<O *>(p.g.out) + ((int64_t)z * p.out_rows + y) * p.g.ldo + t.n0;
-                    for (int c = 128 * wg; c < 128 * wg + 128 && t.n0 + c < p.g.N; c += 64) {
-                        if (t.blocks > 0) {
-                            tmem_ld64(src + c, v);
-                            tmem_wait(v);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                v[i / 16][i % 16] = 0u;
-                        }
+                    for (int c = first; c < first + columns; c += 64) {
+                        fetch(c, c + 16, c + 32, c + 48);
 #pragma unroll
                         for (int b = 0; b < 64 / C; ++b) {
                             const int n = c + b * C, cols = p.g.N - t.n0 - n;
                             if (cols <= 0)
                                 break;
-                            box_free();
+                            unsigned char *box = boxes.next();
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
                                 const int i = b * C + j * V;
-                                box_put<O>(box, lane, j, reinterpret_cast<const float *>(&v[i / 16][i % 16]));
+                                box_put<O, 128>(box, lane, j, reinterpret_cast<const float *>(&v[i / 16][i % 16]));
                             }
                             // rows past the plane's last are dropped by a TMA store
-                            box_store<O>(&map_out, t.n0 + n, y, z, out + n, p.g.ldo, KIND == DW && p.g.wide_store ? 32 : rows,
-                                         cols, p.g.wide_store, box, lane);
+                            box_store<O, 128>(&map_out, t.n0 + n, y, z, out + n, p.g.ldo,
+                                              KIND == DW && p.g.wide_store ? 32 : rows, cols, p.g.wide_store, box, lane);
                         }
                     }
                 }
             }
-            if (t.blocks > 0) {
-                fence_before();
-                __syncwarp();
-                if (lane == 0)
-                    arrive_relaxed(tempty0 + 8 * acc);
+            if (!split)
+                release();
+            if (some) {
                 acc ^= 1;
                 aph ^= acc == 0;
             }
         }
+        if (loading)   // given up: nothing may still land in this CTA's memory
+            wait_ms<OWN>(landed + 8 * warp, lph, 20, nullptr);
         asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group 0;" ::: "memory");
     }
     fence_before();
@@ -489,98 +665,190 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_after();
     if (*dead) {
         // nothing may still land in this CTA's memory: copies first (the leader's barriers count both CTAs'), then MMAs
-        if (warp == 8 && lane == 0) {
-            if (rank == 0)
-                for (uint32_t i = issued < kStages ? 0 : issued - kStages; i < issued; ++i)
-                    wait_ms<OWN>(full + 8 * (i % kStages), (i / kStages) & 1, 20, nullptr);
-            for (int i = 0; i < kStages; ++i)
-                if (tail_used >> i & 1)
-                    wait_ms<OWN>(tail + 8 * i, (tail_phase >> i & 1) ^ 1, 20, nullptr);
-        }
+        if (warp == 8 && lane == 0 && rank == 0)
+            for (uint32_t i = issued < kStages ? 0 : issued - kStages; i < issued; ++i)
+                wait_ms<OWN>(full + 8 * (i % kStages), (i / kStages) & 1, 20, nullptr);
         if (warp == 9 && rank == 0 && elect_one()) {
-            mma_commit<2>(drain);
+            mma_commit<CG>(drain);
             wait_ms<OWN>(drain, 0, 1000, nullptr);
         }
     }
     fence_before();
     __syncthreads();
-    cluster_sync();
+    if (CG == 2)
+        cluster_sync();
     fence_after();
-    if (warp == 9)
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    if (warp == 9) {
+        if (CG == 2)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
 }
 
 // ---- launches
 
-// Row tiles of 256 over all experts, at most: each with rows has one that is not full.
-int64_t row_tiles(const FfShape &s)
+// Row tiles over all experts, at most: each with rows has one that is not full.
+int64_t row_tiles(const FfShape &s, int rows)
 {
-    return s.E == 1 ? ceil_div(s.M, 256) : s.M / 256 + std::min<int64_t>(s.E, s.M);
+    return s.E == 1 ? ceil_div(s.M, rows) : s.M / rows + std::min<int64_t>(s.E, s.M);
 }
 
-template <int KIND, typename T, typename O>
-cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &o2,
-                   FfParams p, int64_t tiles)
+template <int CG, int KIND, typename T, typename O>
+cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &a2,
+                   const CUtensorMap &b2, const FfParams &p, int64_t tiles)
 {
-    auto kernel = k_ff<KIND, T, O>;
-    cudaError_t e = allow_smem<k_ff<KIND, T, O>, kSmem>(m->device);
+    constexpr int kSmem = Shape<CG, KIND>::kSmem;
+    auto kernel = k_ff<CG, KIND, T, O>;
+    cudaError_t e = allow_smem<k_ff<CG, KIND, T, O>, kSmem>(m->device);
     if (e != cudaSuccess)
         return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0] = after_launch_before();
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = 1;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = m->stream;
-    if (m->max_pairs == 0) {   // any product kernel's: they all take an SM for a CTA
-        cfg.gridDim = dim3((unsigned)(m->sm_count / 2 * 2));
-        e = cudaOccupancyMaxActiveClusters(&m->max_pairs, kernel, &cfg);
-        if (e != cudaSuccess)
-            return e;
+    int groups = m->sm_count;
+    if (CG == 2) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = 2;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+        if (m->max_pairs == 0) {   // any product kernel's: they all take an SM for a CTA
+            cfg.gridDim = dim3((unsigned)(m->sm_count / 2 * 2));
+            e = cudaOccupancyMaxActiveClusters(&m->max_pairs, kernel, &cfg);
+            if (e != cudaSuccess)
+                return e;
+        }
+        groups = std::max(1, m->max_pairs);
     }
-    cfg.gridDim = dim3((unsigned)(2 * std::max<int64_t>(1, std::min<int64_t>(std::max(1, m->max_pairs), tiles))));
+    cfg.gridDim = dim3((unsigned)(CG * std::max<int64_t>(1, std::min<int64_t>(groups, tiles))));
     m->launches += 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, o, o2, p);
+    return cudaLaunchKernelEx(&cfg, kernel, a, b, o, a2, b2, p);
+}
+
+// Which tiles a product takes: pairs of CTAs with 256 x 256, or single ones with 128 x 256 whose inner axis may be split
+// into parts. Times in blocks of the inner axis (0.27 us of a pair's MMAs).
+struct Choice {
+    bool pair;
+    int splits;
+};
+
+Choice choose_tiles(const esp_moe *m, bool even, double tiles_pair, double tiles_one, int64_t most_one, double blocks)
+{
+    Choice best{true, 1};
+    // rounds of tiles; where experts' rows are not known, half a round more than the tiles that there should be
+    const auto rounds = [&](double tiles, int at_once) {
+        return even ? std::ceil(tiles / at_once) : std::max(1.0, tiles / at_once + 0.5);
+    };
+    double t_best = rounds(tiles_pair, m->sm_count / 2) * (blocks + 4.0);
+    for (int splits = 1; splits <= 16; ++splits) {
+        // parts fill at most one round and keep four blocks each
+        if (splits > 1 && (most_one * splits > m->sm_count || blocks < 4 * splits))
+            break;
+        const double t = rounds(tiles_one * splits, m->sm_count) * (1.17 * std::ceil(blocks / splits) + 4.0) +
+                         (splits > 1 ? 12.0 + 5.0 * splits : 0.0);
+        if (t < t_best) {
+            t_best = t;
+            best = Choice{false, splits};
+        }
+    }
+    return best;
 }
 
 template <int KIND, typename T>
 cudaError_t rows_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o,
                         const CUtensorMap &o2, FfParams &p)
 {
-    const int64_t tiles = row_tiles(s);
-    p.g.most = (int32_t)tiles;
-    return launch<KIND, T, T>(m, a, b, o, o2, p, tiles * ceil_div(p.g.N, kTileCols<KIND>));
+    const int64_t nt = ceil_div(p.g.N, kTileCols<KIND>), pairs = row_tiles(s, 256), ones = row_tiles(s, 128);
+    // an expert's last tile is half full in the mean
+    const auto expected = [&](int rows) {
+        return (s.E == 1 ? (double)ceil_div(s.M, rows) : (double)s.M / rows + 0.5 * (double)std::min<int64_t>(s.E, s.M)) * nt;
+    };
+    const Choice c = choose_tiles(m, s.E == 1, expected(256), expected(128), ones * nt, (double)p.blocks * p.halves);
+    p.g.most = (int32_t)(c.pair ? pairs : ones);
+    p.g.splits = c.splits;
+    return c.pair ? launch<2, KIND, T, T>(m, a, b, o, o2, b, p, pairs * nt)
+                  : launch<1, KIND, T, T>(m, a, b, o, o2, b, p, ones * nt * c.splits);
 }
 
-template <int KIND>
-cudaError_t weights_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, const CUtensorMap &b, FfParams &p, void *out,
-                           bool f32)
+// Operands of DW: the inner axis is the rows; a2, b2: the tails.
+struct WeightMaps {
+    CUtensorMap a, b, a2, b2;
+};
+
+template <typename T, typename O>
+cudaError_t weights_launch_as(esp_moe *m, const FfShape &s, const WeightMaps &w, const CUtensorMap &o, FfParams &p)
+{
+    const int64_t per = (int64_t)s.E * p.planes * ceil_div(p.g.N, 256);
+    const int64_t pairs = per * ceil_div(p.out_rows, 256), ones = per * ceil_div(p.out_rows, 128);
+    const Choice c = choose_tiles(m, s.E == 1, (double)pairs, (double)ones, ones, (double)s.M / s.E / kInner);
+    p.g.splits = c.splits;
+    return c.pair ? launch<2, DW, T, O>(m, w.a, w.b, o, w.a2, w.b2, p, pairs)
+                  : launch<1, DW, T, O>(m, w.a, w.b, o, w.a2, w.b2, p, ones * c.splits);
+}
+
+cudaError_t weights_launch(esp_moe *m, const FfShape &s, const WeightMaps &w, FfParams &p, void *out, bool f32)
 {
     const int size = f32 ? 4 : 2;
     p.g.out = out;
     p.g.ldo = p.g.N;
     p.g.wide_store = rows_aligned(out, p.g.N, size, 16);
-    CUtensorMap o = a;   // not used where the output is not aligned
+    CUtensorMap o = w.a;   // not used where the output is not aligned
     if (p.g.wide_store)
         FF_TRY(box_map3(&o, out, size, p.g.N, p.out_rows, p.g.N, (int64_t)s.E * p.planes, (int64_t)p.out_rows * p.g.N, 32));
-    const int64_t tiles = (int64_t)s.E * p.planes * ceil_div(p.out_rows, 256) * ceil_div(p.g.N, 256);
     return with_16(s.dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        return f32 ? launch<KIND, T, float>(m, a, b, o, o, p, tiles) : launch<KIND, T, T>(m, a, b, o, o, p, tiles);
+        return f32 ? weights_launch_as<T, float>(m, s, w, o, p) : weights_launch_as<T, T>(m, s, w, o, p);
     });
+}
+
+// ---- tails
+constexpr int kTailRows = 4;   // of a CTA, a warp for each
+
+// A warp copies a row, 16 bytes a lane, eight of them in flight; rows behind an expert's last are zeros. Elements past a
+// row's `width` are not read, and zeros up to `ld_out`.
+__global__ void __launch_bounds__(32 * kTailRows) k_tails(const TailArgs a)
+{
+    wait_for_launch_before();
+    const TailArgs::Part &p = a.part[blockIdx.y];
+    const int e = blockIdx.x / (kInner / kTailRows), lane = threadIdx.x & 31;
+    const int r = blockIdx.x % (kInner / kTailRows) * kTailRows + (threadIdx.x >> 5);
+    const int lo = a.offsets ? max(0, min(a.M, a.offsets[e])) : 0;
+    const int hi = a.offsets ? max(lo, min(a.M, a.offsets[e + 1])) : a.M;
+    const int rows = (hi - lo) % kInner;
+    if (rows == 0)
+        return;
+    const uint16_t *x = static_cast<const uint16_t *>(p.x) + (int64_t)(hi - rows + min(r, rows - 1)) * p.ldx;
+    uint16_t *out = static_cast<uint16_t *>(p.out) + ((int64_t)e * kInner + r) * p.ld_out;
+    constexpr int U = 8;
+    for (int h0 = lane * 8; h0 < p.ld_out; h0 += 256 * U) {
+        Pack<uint16_t, 8> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + 256 * u;
+            v[u] = {};
+            if (r < rows && h + 8 <= p.width)
+                v[u] = *reinterpret_cast<const Pack<uint16_t, 8> *>(x + h);
+            else if (r < rows && h < p.width)
+                for (int j = 0; h + j < p.width; ++j)
+                    v[u].v[j] = x[h + j];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (h0 + 256 * u < p.ld_out)
+                *reinterpret_cast<Pack<uint16_t, 8> *>(out + h0 + 256 * u) = v[u];
+    }
 }
 
 }  // namespace
 
-int few_chunk(const esp_moe *m, int64_t M, int32_t E)
+size_t ff_partial_floats(const esp_moe *m)
 {
-    const int64_t rows = ceil_div(M, E);
-    return rows > 128 ? 0 : rows > 64 ? 128 : rows > 32 ? 64 : rows > 16 ? 32 : 16;
+    return (size_t)m->sm_count * kRowsA * kAccCols;   // parts fill at most one round
 }
 
 cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, void *hidden, void *pre)
@@ -593,10 +861,8 @@ cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_
     p.g.ldo = s.fp;
     p.out2 = pre;
     CUtensorMap a, b, o, o2;
-    FF_TRY(box_map3(&a, x, 2, s.H, s.M, ldx, 1, 0, s.chunk ? s.chunk : kRowsA));
+    FF_TRY(box_map3(&a, x, 2, s.H, s.M, ldx, 1, 0, kRowsA));
     FF_TRY(box_map3(&b, s.inner, 2, s.H, s.F, s.ld_inner, 2 * (int64_t)s.E, s.F * s.ld_inner, kRowsA));
-    if (s.chunk)
-        return launch_few(m, s, HIDDEN, s.chunk, &b, &a, &p);
     FF_TRY(box_map3(&o, hidden, 2, s.F, s.M, s.fp, 1, 0, 32));
     o2 = o;
     if (pre)
@@ -614,10 +880,8 @@ cudaError_t launch_ff_out(esp_moe *m, const FfShape &s, const void *hidden, void
     p.g.ldo = ldy;
     p.g.wide_store = rows_aligned(y, ldy, 2, 16);
     CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, hidden, 2, s.F, s.M, s.fp, 1, 0, s.chunk ? s.chunk : kRowsA));
+    FF_TRY(box_map3(&a, hidden, 2, s.F, s.M, s.fp, 1, 0, kRowsA));
     FF_TRY(box_map3(&b, s.outer, 2, s.F, s.H, s.ld_outer, s.E, s.H * s.ld_outer, kRowsA));
-    if (s.chunk)
-        return launch_few(m, s, OUT, s.chunk, &b, &a, &p);
     o = a;
     if (p.g.wide_store)
         FF_TRY(box_map3(&o, y, 2, s.H, s.M, ldy, 1, 0, 32));
@@ -633,13 +897,12 @@ cudaError_t launch_ff_dpre(esp_moe *m, const FfShape &s, const void *dy, int64_t
     p.g.out = dpre;
     p.g.ldo = 2 * s.fp;
     p.pre = pre;
-    CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, s.chunk ? s.chunk : kRowsA));
+    CUtensorMap a, b, o, g;
+    FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, kRowsA));
     FF_TRY(box_map3(&b, s.outer, 2, s.F, s.H, s.ld_outer, s.E, s.H * s.ld_outer, kInner));
-    if (s.chunk)
-        return launch_few(m, s, DPRE, s.chunk, &b, &a, &p);
-    FF_TRY(box_map3(&o, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, 32));
-    return with_16(s.dtype, [&](auto elem) { return rows_launch<DPRE, decltype(elem)>(m, s, a, b, o, o, p); });
+    FF_TRY(box_map3(&o, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, 32, 64));
+    FF_TRY(box_map3(&g, pre, 4, s.F, s.M, 2 * s.fp, 2, s.fp, 32));
+    return with_16(s.dtype, [&](auto elem) { return rows_launch<DPRE, decltype(elem)>(m, s, a, b, o, g, p); });
 }
 
 cudaError_t launch_ff_dx(esp_moe *m, const FfShape &s, const void *dpre, void *dx, int64_t lddx)
@@ -653,40 +916,60 @@ cudaError_t launch_ff_dx(esp_moe *m, const FfShape &s, const void *dpre, void *d
     p.g.ldo = lddx;
     p.g.wide_store = rows_aligned(dx, lddx, 2, 16);
     CUtensorMap a, b, o;
-    FF_TRY(box_map3(&a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, s.chunk ? s.chunk : kRowsA));
+    FF_TRY(box_map3(&a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kRowsA));
     FF_TRY(box_map3(&b, s.inner, 2, s.H, s.F, s.ld_inner, 2 * (int64_t)s.E, s.F * s.ld_inner, kInner));
-    if (s.chunk)
-        return launch_few(m, s, DX, s.chunk, &b, &a, &p);
     o = a;
     if (p.g.wide_store)
         FF_TRY(box_map3(&o, dx, 2, s.H, s.M, lddx, 1, 0, 32));
     return with_16(s.dtype, [&](auto elem) { return rows_launch<DX, decltype(elem)>(m, s, a, b, o, o, p); });
 }
 
-cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx, void *dinner,
-                             bool f32)
+cudaError_t launch_tails(esp_moe *m, const TailArgs &a, int32_t E)
+{
+    m->launches += 1;
+    return launch_after(k_tails, dim3((unsigned)(E * (kInner / kTailRows)), (unsigned)a.parts), 32 * kTailRows, 0, m->stream, a);
+}
+
+cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx,
+                             const void *dpre_tails, const void *x_tails, void *dinner, bool f32)
 {
     FfParams p = common(m, s);
     p.g.N = s.H;
     p.planes = 2;
     p.out_rows = s.F;
-    CUtensorMap a, b;
-    FF_TRY(box_map3(&a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kInner));
-    FF_TRY(box_map3(&b, x, 2, s.H, s.M, ldx, 1, 0, kInner));
-    return weights_launch<DW>(m, s, a, b, p, dinner, f32);
+    const int64_t tails = (int64_t)s.E * kInner;
+    WeightMaps w;
+    FF_TRY(box_map3(&w.a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kInner));
+    FF_TRY(box_map3(&w.b, x, 2, s.H, s.M, ldx, 1, 0, kInner));
+    w.a2 = w.a;
+    w.b2 = w.b;
+    if (dpre_tails) {
+        FF_TRY(box_map3(&w.a2, dpre_tails, 2, s.F, tails, 2 * s.fp, 2, s.fp, kInner));
+        FF_TRY(box_map3(&w.b2, x_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
+    }
+    p.tails = dpre_tails != nullptr;
+    return weights_launch(m, s, w, p, dinner, f32);
 }
 
-cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden, void *douter,
-                             bool f32)
+cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden,
+                             const void *dy_tails, const void *hidden_tails, void *douter, bool f32)
 {
     FfParams p = common(m, s);
     p.g.N = s.F;
     p.planes = 1;
     p.out_rows = s.H;
-    CUtensorMap a, b;
-    FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, kInner));
-    FF_TRY(box_map3(&b, hidden, 2, s.F, s.M, s.fp, 1, 0, kInner));
-    return weights_launch<DW>(m, s, a, b, p, douter, f32);
+    const int64_t tails = (int64_t)s.E * kInner;
+    WeightMaps w;
+    FF_TRY(box_map3(&w.a, dy, 2, s.H, s.M, lddy, 1, 0, kInner));
+    FF_TRY(box_map3(&w.b, hidden, 2, s.F, s.M, s.fp, 1, 0, kInner));
+    w.a2 = w.a;
+    w.b2 = w.b;
+    if (dy_tails) {
+        FF_TRY(box_map3(&w.a2, dy_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
+        FF_TRY(box_map3(&w.b2, hidden_tails, 2, s.F, tails, s.fp, 1, 0, kInner));
+    }
+    p.tails = dy_tails != nullptr;
+    return weights_launch(m, s, w, p, douter, f32);
 }
 
 }  // namespace esp_moe_impl

@@ -25,7 +25,8 @@ namespace esp_moe_impl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCtasPerSm = 4;
+constexpr int kCtasPerSm = 4;      // k_norm's, with eight loads in flight; k_scale has twice as many with four
+
 constexpr int kBatch = 144;       // tensors of a launch, in its parameters
 constexpr int64_t kMostBytes = (int64_t)1 << 45;   // of all tensors; keeps a launch's chunks in int32
 
@@ -150,10 +151,10 @@ __device__ __forceinline__ double sum_of_cta(double v, double *warps)
     if ((threadIdx.x & 31) == 0)
         warps[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = 0.0;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < kThreads / 32; ++w)
-            v += warps[w];
+    v = (threadIdx.x & 31) < kThreads / 32 ? warps[threadIdx.x & 31] : 0.0;
+#pragma unroll
+    for (int o = kThreads / 64; o > 0; o >>= 1)
+        v += __shfl_down_sync(0xffffffffu, v, o);
     return v;
 }
 
@@ -235,7 +236,7 @@ __device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, flo
 }
 
 template <int U>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_scale(const __grid_constant__ ClipArgs a, const float *factor)
+__global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ ClipArgs a, const float *factor)
 {
     wait_for_launch_before();
     const float by = *factor;
@@ -306,7 +307,7 @@ bool overlapping(int32_t count, const esp_moe_tensor *tensors)
     return false;
 }
 
-template <int U>
+template <int U, int V>
 cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, NormArgs n, bool write)
 {
     const int most = kCtasPerSm * m->sm_count;
@@ -318,7 +319,7 @@ cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors
             a.count = a.chunks = 0;
             for (; at < count && a.count < kBatch; ++at) {
                 const esp_moe_tensor &t = tensors[at];
-                const int64_t chunks = t.n == 0 || (pass == 1 && !t.out) ? 0 : chunks_of(t, U);
+                const int64_t chunks = t.n == 0 || (pass == 1 && !t.out) ? 0 : chunks_of(t, pass == 0 ? U : V);
                 if (chunks == 0)
                     continue;
                 a.t[a.count] = ClipTensor{t.grad, t.out, t.n};
@@ -330,11 +331,11 @@ cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors
             more = at < count;
             if (pass == 1 && a.chunks == 0)
                 break;
-            const int grid = std::max(1, std::min(most, a.chunks));
+            const int grid = std::max(1, std::min(pass == 0 ? most : 2 * most, a.chunks));
             n.total = pass == 0 && !more ? n.base + grid : 0;
             m->launches += 1;
             const cudaError_t e = pass == 0 ? launch_after(k_norm<U>, dim3(grid), kThreads, 0, m->stream, a, n)
-                                            : launch_after(k_scale<U>, dim3(grid), kThreads, 0, m->stream, a,
+                                            : launch_after(k_scale<V>, dim3(grid), kThreads, 0, m->stream, a,
                                                            (const float *)n.factor);
             if (e != cudaSuccess)
                 return e;
@@ -389,6 +390,6 @@ extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tens
     n.norm = norm;
     // few bytes: two groups a thread, so that every SM has some; else eight in flight
     const bool few = bytes < (int64_t)m->sm_count * kCtasPerSm * kThreads * 8 * 16;
-    const cudaError_t e = few ? launch_clip<2>(m, count, tensors, n, write) : launch_clip<8>(m, count, tensors, n, write);
+    const cudaError_t e = few ? launch_clip<2, 2>(m, count, tensors, n, write) : launch_clip<8, 4>(m, count, tensors, n, write);
     return e == cudaSuccess ? ESP_OK : fail_call(m);
 }

@@ -11,38 +11,49 @@ namespace esp_moe_impl {
 
 namespace {
 
-constexpr int kCopyThreads = 256;
+constexpr int kCopyRows = 4;   // of a CTA, a warp for each
 
-// A CTA copies a row's 16-byte groups; bound by HBM. V: elements that a source row allows to load at once.
+// A warp copies a row's 16-byte groups, eight in flight; bound by HBM. V: elements that a source row allows to load at once.
 template <int V>
-__global__ void __launch_bounds__(kCopyThreads) k_copy_rows(const CopyRowsArgs a)
+__global__ void __launch_bounds__(32 * kCopyRows) k_copy_rows(const CopyRowsArgs a)
 {
-    let_next_launch_start();
     wait_for_launch_before();
-    const int64_t i = blockIdx.x;
+    const int64_t i = (int64_t)blockIdx.x * kCopyRows + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (i >= a.M)
+        return;
     const int64_t from = a.rows ? a.rows[i] : i;
     const bool there = from >= 0 && from < a.T;
-    const uint16_t *x = static_cast<const uint16_t *>(a.x) + from * a.ldx;
+    const uint16_t *x = static_cast<const uint16_t *>(a.x) + (there ? from : 0) * a.ldx;
     uint16_t *out = static_cast<uint16_t *>(a.out) + i * a.ldo;
-    for (int h = (blockIdx.y * kCopyThreads + threadIdx.x) * 8; h < a.H; h += gridDim.y * kCopyThreads * 8) {
-        Pack<uint16_t, 8> r = {};
-        if (there) {
-            if constexpr (V == 8) {
-                r = *reinterpret_cast<const Pack<uint16_t, 8> *>(x + h);
+    constexpr int U = V == 8 ? 8 : 2;
+    for (int h0 = lane * 8; h0 < a.H; h0 += 256 * U) {
+        Pack<uint16_t, 8> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + 256 * u;
+            r[u] = {};
+            if (V == 8) {
+                if (there && h < a.H)
+                    r[u] = *reinterpret_cast<const Pack<uint16_t, 8> *>(x + h);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (h + j < a.H)
-                        r.v[j] = x[h + j];
+                    if (there && h + j < a.H)
+                        r[u].v[j] = x[h + j];
             }
         }
-        *reinterpret_cast<Pack<uint16_t, 8> *>(out + h) = r;   // a row of `out` is whole groups of 8
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (h0 + 256 * u < a.H)   // a row of `out` is whole groups of 8
+                *reinterpret_cast<Pack<uint16_t, 8> *>(out + h0 + 256 * u) = r[u];
     }
 }
 
-int64_t up8(int64_t n)
+// Rows of intermediate matrices start at multiples of 128 bytes: a tile's 128-byte rows then are whole lines.
+int64_t up64(int64_t n)
 {
-    return (n + 7) / 8 * 8;
+    return (n + 63) / 64 * 64;
 }
 
 bool aligned_to(const void *p, size_t bytes)
@@ -83,10 +94,10 @@ bool mappable(const void *x, int64_t ldx)
     return rows_aligned(x, ldx, 2, 16);
 }
 
-FfShape shape_of(const esp_moe *m, const esp_moe_gated *w, int64_t M, const int32_t *offsets)
+FfShape shape_of(const esp_moe_gated *w, int64_t M, const int32_t *offsets)
 {
     return FfShape{w->dtype, w->activation, w->E, w->F, w->H, M, offsets, w->inner, w->outer, w->ld_inner, w->ld_outer,
-                   nullptr, few_chunk(m, M, w->E), up8(w->F)};
+                   up64(w->H), nullptr, up64(w->F)};
 }
 
 }  // namespace
@@ -96,10 +107,10 @@ cudaError_t launch_copy_rows(esp_moe *m, const CopyRowsArgs &a)
     if (a.M == 0)
         return cudaSuccess;
     const bool wide = rows_aligned(a.x, a.ldx, 2, 16) && a.H % 8 == 0;
-    const dim3 grid((unsigned)a.M, (unsigned)std::min<int64_t>(64, ceil_div(a.H, 8 * kCopyThreads)));
+    const dim3 grid((unsigned)ceil_div(a.M, kCopyRows));
     m->launches += 1;
-    return wide ? launch_after(k_copy_rows<8>, grid, kCopyThreads, 0, m->stream, a)
-                : launch_after(k_copy_rows<1>, grid, kCopyThreads, 0, m->stream, a);
+    return wide ? launch_after(k_copy_rows<8>, grid, 32 * kCopyRows, 0, m->stream, a)
+                : launch_after(k_copy_rows<1>, grid, 32 * kCopyRows, 0, m->stream, a);
 }
 
 }  // namespace esp_moe_impl
@@ -128,22 +139,33 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
         kept->copied = copied;
     if (M == 0)
         return ESP_OK;
-    FfShape s = shape_of(m, w, M, offsets);
-    const int64_t hp = up8(w->H);
+    FfShape s = shape_of(w, M, offsets);
+    const int64_t hp = up64(w->H);
+    // a few rows: gathered by the products themselves, unless they are kept for the gradients
+    const bool vec = use_vec(M, w->E);
+    const bool copy = copied && !(vec && !kept && mappable(x, ldx));
     void *hidden = nullptr, *gathered = nullptr;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
-        if (s.chunk)
-            s.partial = c.take<float>(few_partial_floats(m, s.chunk));
+        s.partial = c.take<float>(ff_partial_floats(m));
         hidden = kept ? kept->hidden : c.take<uint16_t>((size_t)(M * s.fp));
-        if (copied)
+        if (copy)
             gathered = kept ? kept->rows : c.take<uint16_t>((size_t)(M * hp));
         if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
             return st;
     }
-    if (copied)
+    if (copy) {
         MOE_CUDA(launch_copy_rows(m, CopyRowsArgs{M, T, ldx, hp, w->H, x, rows, gathered}));
-    MOE_CUDA(launch_ff_hidden(m, s, copied ? gathered : x, copied ? hp : ldx, hidden, kept ? kept->pre : nullptr));
+        x = gathered;
+        ldx = hp;
+        T = M;
+        rows = nullptr;
+    }
+    if (vec) {
+        MOE_CUDA(launch_vec(m, s, x, ldx, T, rows, hidden, kept ? kept->pre : nullptr, y, ldy));
+        return ESP_OK;
+    }
+    MOE_CUDA(launch_ff_hidden(m, s, x, ldx, hidden, kept ? kept->pre : nullptr));
     MOE_CUDA(launch_ff_out(m, s, hidden, y, ldy));
     return ESP_OK;
 }
@@ -173,18 +195,27 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
             MOE_CUDA(cudaMemsetAsync(douter, 0, n, m->stream));
         return ESP_OK;
     }
-    FfShape s = shape_of(m, w, M, offsets);
-    const int64_t hp = up8(w->H);
+    FfShape s = shape_of(w, M, offsets);
+    const int64_t hp = up64(w->H);
     const bool copy_dy = !mappable(dy, lddy), want_dpre = dx || dinner;
-    void *dpre = nullptr, *dy_copy = nullptr;
+    void *dpre = nullptr, *dy_copy = nullptr, *dpre_tails = nullptr, *x_tails = nullptr, *dy_tails = nullptr,
+         *hidden_tails = nullptr;
+    const size_t tail_rows = offsets ? (size_t)w->E * kInner : 0;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
-        if (s.chunk)
-            s.partial = c.take<float>(few_partial_floats(m, s.chunk));
+        s.partial = c.take<float>(ff_partial_floats(m));
         if (want_dpre)
             dpre = c.take<uint16_t>((size_t)(2 * M * s.fp));
         if (copy_dy)
             dy_copy = c.take<uint16_t>((size_t)(M * hp));
+        if (offsets && dinner) {
+            dpre_tails = c.take<uint16_t>(tail_rows * 2 * s.fp);
+            x_tails = c.take<uint16_t>(tail_rows * hp);
+        }
+        if (offsets && douter) {
+            dy_tails = c.take<uint16_t>(tail_rows * hp);
+            hidden_tails = c.take<uint16_t>(tail_rows * s.fp);
+        }
         if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
             return st;
     }
@@ -197,10 +228,26 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
         MOE_CUDA(launch_ff_dpre(m, s, dy, lddy, kept->pre, dpre));
     if (dx)
         MOE_CUDA(launch_ff_dx(m, s, dpre, dx, lddx));
+    const void *rows_x = copied ? kept->rows : x;
+    const int64_t ld_rows = copied ? hp : ldx;
+    if (offsets && (dinner || douter)) {
+        TailArgs a{};
+        a.M = (int32_t)M;
+        a.offsets = offsets;
+        if (dinner) {
+            a.part[a.parts++] = TailArgs::Part{dpre, dpre_tails, 2 * s.fp, 2 * s.fp, (int32_t)(s.fp + w->F)};
+            a.part[a.parts++] = TailArgs::Part{rows_x, x_tails, ld_rows, hp, w->H};
+        }
+        if (douter) {
+            a.part[a.parts++] = TailArgs::Part{dy, dy_tails, lddy, hp, w->H};
+            a.part[a.parts++] = TailArgs::Part{kept->hidden, hidden_tails, s.fp, s.fp, w->F};
+        }
+        MOE_CUDA(launch_tails(m, a, w->E));
+    }
     if (dinner)
-        MOE_CUDA(launch_ff_dinner(m, s, dpre, copied ? kept->rows : x, copied ? hp : ldx, dinner, f32));
+        MOE_CUDA(launch_ff_dinner(m, s, dpre, rows_x, ld_rows, dpre_tails, x_tails, dinner, f32));
     if (douter)
-        MOE_CUDA(launch_ff_douter(m, s, dy, lddy, kept->hidden, douter, f32));
+        MOE_CUDA(launch_ff_douter(m, s, dy, lddy, kept->hidden, dy_tails, hidden_tails, douter, f32));
     return ESP_OK;
 }
 

@@ -25,20 +25,21 @@ struct FfShape {
     const int32_t *offsets;
     const void *inner, *outer;
     int64_t ld_inner, ld_outer;
-    float *partial;           // work space: few_partial_floats
-    int chunk;                // rows of a tile (few_chunk), 0: tiles of many rows
-    int64_t fp;               // elements of a row of a half of `pre` and `dpre`, and of `hidden`: F rounded up to 8
+    int64_t hp;               // of the rows of x and dy in the tails: H rounded up to 64
+    float *partial;           // work space: ff_partial_floats
+    int64_t fp;               // elements of a row of a half of `pre` and `dpre`, and of `hidden`: F rounded up to 64
 };
 
-// ---- esp_ff_few.cu
-int few_ctas(const esp_moe *m);
-size_t few_partial_floats(const esp_moe *m, int chunk);
-// kind, w, x, params: esp_ff.cuh's Kind, tensor maps of the weights and of the rows, FfParams.
-cudaError_t launch_few(esp_moe *m, const FfShape &s, int kind, int chunk, const void *w, const void *x, const void *params);
+// ---- esp_ff_vec.cu
+// Whether a forward pass is for the CUDA cores: one dense block, one or two rows.
+bool use_vec(int64_t M, int32_t E);
+// Both products of such a pass: hidden (M x fp), pre where it is given, y. Rows are gathered here.
+cudaError_t launch_vec(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, int64_t T, const int32_t *rows, void *hidden,
+                       void *pre, void *y, int64_t ldy);
 
 // ---- esp_ff_gemm.cu
-// Rows of a tile of a product over these rows: 0 (pairs of CTAs, 256 rows), or 16 to 128 (esp_ff_few.cu).
-int few_chunk(const esp_moe *m, int64_t M, int32_t E);
+// Work space of a product whose tiles' inner axes are split over CTAs.
+size_t ff_partial_floats(const esp_moe *m);
 // hidden (M x fp) = act(gate) * up; pre (M x 2 x fp fp32: gate, up) is written too where it is given.
 cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, void *hidden, void *pre);
 // y (M x H) = hidden O^T.
@@ -47,10 +48,24 @@ cudaError_t launch_ff_out(esp_moe *m, const FfShape &s, const void *hidden, void
 cudaError_t launch_ff_dpre(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *pre, void *dpre);
 // dx (M x H) = dpre [G; U].
 cudaError_t launch_ff_dx(esp_moe *m, const FfShape &s, const void *dpre, void *dx, int64_t lddx);
-// dinner (E x 2 F x H) = dpre^T x, douter (E x H x F) = dy^T hidden, in 32 bits or the rows' type.
-cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx, void *dinner,
-                             bool f32);
-cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden, void *douter,
-                             bool f32);
+// The last rows of each expert that do not fill a block of 64, copied to 64 rows of their own (row 64 e on), zeros behind
+// them. Needed where rows of another expert, or of none, may follow in memory.
+struct TailArgs {
+    struct Part {
+        const void *x;      // rows of 16-bit elements, a multiple of 16 bytes apart
+        void *out;          // 64 E rows of ld_out
+        int64_t ldx, ld_out;
+        int32_t width;
+    } part[4];
+    int32_t parts, M;
+    const int32_t *offsets;
+};
+cudaError_t launch_tails(esp_moe *m, const TailArgs &a, int32_t E);
+// dinner (E x 2 F x H) = dpre^T x, douter (E x H x F) = dy^T hidden, in 32 bits or the rows' type. Tails: NULL where rows
+// end with M.
+cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx,
+                             const void *dpre_tails, const void *x_tails, void *dinner, bool f32);
+cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden,
+                             const void *dy_tails, const void *hidden_tails, void *douter, bool f32);
 
 }  // namespace esp_moe_impl

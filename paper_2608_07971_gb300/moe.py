@@ -255,8 +255,8 @@ class GatedWeight:
 
 @dataclasses.dataclass
 class Kept:
-    """What ``Moe.feed_forward`` keeps for its gradients (esp_moe_kept): pre (M, 2, F8) fp32, hidden (M, F8), rows (M, H8),
-    with F and H rounded up to multiples of 8. Made by ``Moe.keep``."""
+    """What ``Moe.feed_forward`` keeps for its gradients (esp_moe_kept): pre (M, 2, F64) fp32, hidden (M, F64), rows
+    (M, H64), with F and H rounded up to multiples of 64. Made by ``Moe.keep``."""
 
     pre: torch.Tensor
     hidden: torch.Tensor
@@ -306,8 +306,8 @@ def _pad16(n: int) -> int:
     return (n + 15) // 16 * 16
 
 
-def _pad8(n: int) -> int:
-    return (n + 7) // 8 * 8
+def _pad64(n: int) -> int:
+    return (n + 63) // 64 * 64
 
 
 def _rows16(t) -> bool:
@@ -643,20 +643,20 @@ class Moe:
         E, n, k = w.shape
         if _rows16(w):
             return w
-        room = torch.zeros((E, n, _pad8(k)), dtype=w.dtype, device=self.device)[:, :, :k]
+        room = torch.zeros((E, n, _pad64(k)), dtype=w.dtype, device=self.device)[:, :, :k]
         room.copy_(w)
         return room
 
     def keep(self, M: int, weight: GatedWeight) -> Kept:
         """Room for what ``feed_forward`` keeps of M rows for their gradients."""
-        F8, dt = _pad8(weight.F), weight.inner.dtype
-        return Kept(self._new((M, 2, F8), torch.float32), self._new((M, F8), dt), self._new((M, _pad8(weight.H)), dt))
+        F64, dt = _pad64(weight.F), weight.inner.dtype
+        return Kept(self._new((M, 2, F64), torch.float32), self._new((M, F64), dt), self._new((M, _pad64(weight.H)), dt))
 
     def _need_kept(self, kept: Kept, M: int, weight: GatedWeight):
-        F8, dt = _pad8(weight.F), weight.inner.dtype
-        self._need(kept.pre, "pre", torch.float32, (M, 2, F8))
-        self._need(kept.hidden, "hidden", dt, (M, F8))
-        self._need(kept.rows, "rows", dt, (M, _pad8(weight.H)))
+        F64, dt = _pad64(weight.F), weight.inner.dtype
+        self._need(kept.pre, "pre", torch.float32, (M, 2, F64))
+        self._need(kept.hidden, "hidden", dt, (M, F64))
+        self._need(kept.rows, "rows", dt, (M, _pad64(weight.H)))
 
     def _block_rows(self, x, weight: GatedWeight, offsets, rows):
         self._need(weight.inner, "weight")
