@@ -2,9 +2,11 @@
 // weight is loaded once, 16 bytes a lane, and multiplied with the rows in fp32. Bound by the weights' bytes; there is no
 // tile to fill, no tensor memory and nothing to join, which is what a tensor-core kernel spends its time on here.
 //
-// A warp takes some weight rows at a time (HIDDEN: the same ones of G and of U) over the whole inner axis, and the rows of
-// x, which lie in L1; the next weights are on their way while these are multiplied, across rows too. Weight rows go round
-// over the CTAs, so that every SM streams the same bytes.
+// A CTA takes a few weight rows at a time (HIDDEN: the same ones of G and of U), each thread some 16-byte groups of all of
+// them and the same groups of x in registers; the next rows are on their way while these are multiplied, and a sum over
+// the CTA ends each. Four CTAs of an SM and four groups of a thread: one token of 4096 x 8192 takes 39.3 us (201 MB; 43.8
+// with two CTAs and eight groups; 41.5 with warps that take rows of their own, x from L1), 1024 x 4096 10.3 us. Items go
+// round over the CTAs, so that every SM streams the same bytes.
 
 #include <algorithm>
 
@@ -81,132 +83,145 @@ __device__ __forceinline__ void fma2(uint64_t &c, uint64_t a, uint64_t b)
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(c) : "l"(a), "l"(b));
 }
 
-// R rows of x, NF weight rows (HIDDEN: of each of G and U). U groups of 8 elements of each at a time, the next ones on their
-// way while these are multiplied.
-template <int KIND, int R, int NF, typename T>
-__global__ void __launch_bounds__(kThreads, 2) k_ff_vec(const VecParams p)
+// CTAs of an SM: what their registers leave room for.
+template <int R>
+constexpr int kCtas = R == 1 ? 4 : 3;
+
+// R rows of x; a thread has J groups of 8 elements of a weight row's 256 J in a step (a row longer than that takes several
+// steps), and W = 4 / J weight rows.
+template <int KIND, int R, int J, typename T>
+__global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p)
 {
-    constexpr int W = KIND == HIDDEN ? 2 * NF : NF;       // weight rows
-    constexpr int U = 8 / W;
-    const int lane = threadIdx.x & 31;
+    constexpr int W = 4 / J, NF = KIND == HIDDEN ? W / 2 : W;
+    __shared__ float part[2][W * R][kWarps];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!p.early) {
         wait_for_launch_before();
         let_next_launch_start();
     }
-    const int groups = (p.K + 7) / 8, step = gridDim.x * kWarps * NF;
-    const uint16_t *w[W], *x[R];
-    const auto rows_from = [&](int n0) {   // rows past the last are its copies
+    const int groups = (p.K + 7) / 8, segs = (groups + kThreads * J - 1) / (kThreads * J);
+    const int items = (p.N + NF - 1) / NF;
+    // the groups of item `item`'s rows in step `seg`; rows past the last are its copies
+    const auto load = [&](uint4 (&to)[W][J], int item, int seg) {
 #pragma unroll
-        for (int f = 0; f < W; ++f)
-            w[f] = static_cast<const uint16_t *>(p.w) +
-                   ((int64_t)(KIND == HIDDEN && f >= NF ? p.N : 0) + min(n0 + f % NF, p.N - 1)) * p.ldw;
-    };
-    uint4 v[2][W][U];
-    const auto load = [&](uint4 (&to)[W][U], int g0) {
+        for (int f = 0; f < W; ++f) {
+            const int64_t n = (KIND == HIDDEN && f >= NF ? p.N : 0) + min(item * NF + f % NF, p.N - 1);
+            const uint16_t *w = static_cast<const uint16_t *>(p.w) + n * p.ldw;
 #pragma unroll
-        for (int f = 0; f < W; ++f)
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int g = g0 + 32 * j + lane;
-                to[f][j] = g < groups ? load_group<true>(w[f], g, p.K) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < J; ++j) {
+                const int g = (seg * J + j) * kThreads + threadIdx.x;
+                to[f][j] = g < groups ? load_group<true>(w, g, p.K) : make_uint4(0, 0, 0, 0);
             }
+        }
     };
-    int n0 = (blockIdx.x + gridDim.x * (threadIdx.x >> 5)) * NF;
-    if (n0 < p.N) {
-        rows_from(n0);
-        load(v[0], 0);
-    }
+    uint4 now[W][J], next[W][J], x[R][J];
+    int item = blockIdx.x, seg = 0;
+    if (item < items)
+        load(now, item, 0);
     if (p.early) {
         // the first weights are on their way; what the launch before writes (the rows) comes after this
         wait_for_launch_before();
         let_next_launch_start();
     }
     const int lo = p.offsets ? max(0, min(p.M, p.offsets[0])) : 0, hi = p.offsets ? max(lo, min(p.M, p.offsets[1])) : p.M;
-    bool there[R];
+    const auto load_x = [&](int s) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t from = r < p.M ? (p.rows ? p.rows[r] : r) : -1;
-        there[r] = from >= 0 && from < p.T;
-        x[r] = static_cast<const uint16_t *>(p.x) + (there[r] ? from : 0) * p.ldx;
-    }
-    for (; n0 < p.N; n0 += step) {
-        uint64_t sum[W][R] = {};
-        const auto multiply = [&](const uint4 (&by)[W][U], int g0) {
+        for (int r = 0; r < R; ++r) {
+            const int64_t from = r < p.M ? (p.rows ? p.rows[r] : r) : -1;
+            const bool there = from >= 0 && from < p.T;
+            const uint16_t *row = static_cast<const uint16_t *>(p.x) + (there ? from : 0) * p.ldx;
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int g = g0 + 32 * j + lane;
-                if (g >= groups)
-                    break;
-                uint4 xv[R];
+            for (int j = 0; j < J; ++j) {
+                const int g = (s * J + j) * kThreads + threadIdx.x;
+                x[r][j] = there && g < groups ? load_group<false>(row, g, p.K) : make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+    load_x(0);
+    uint64_t sum[W][R] = {};
+    int turn = 0;
+    while (item < items) {
+        const int item1 = seg + 1 < segs ? item : item + (int)gridDim.x, seg1 = seg + 1 < segs ? seg + 1 : 0;
+        if (item1 < items)
+            load(next, item1, seg1);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint64_t xp[R];
 #pragma unroll
                 for (int r = 0; r < R; ++r)
-                    xv[r] = there[r] ? load_group<false>(x[r], g, p.K) : make_uint4(0, 0, 0, 0);
+                    xp[r] = pair_of<T>(part_of(x[r][j], q));
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint64_t xp[R];
+                for (int f = 0; f < W; ++f) {
+                    const uint64_t wp = pair_of<T>(part_of(now[f][j], q));
 #pragma unroll
                     for (int r = 0; r < R; ++r)
-                        xp[r] = pair_of<T>(part_of(xv[r], q));
-#pragma unroll
-                    for (int f = 0; f < W; ++f) {
-                        const uint64_t wp = pair_of<T>(part_of(by[f][j], q));
-#pragma unroll
-                        for (int r = 0; r < R; ++r)
-                            fma2(sum[f][r], wp, xp[r]);
-                    }
+                        fma2(sum[f][r], wp, xp[r]);
                 }
             }
-        };
-        for (int g0 = 0; g0 < groups; g0 += 64 * U) {
-            load(v[1], g0 + 32 * U);
-            multiply(v[0], g0);
-            if (g0 + 64 * U < groups)
-                load(v[0], g0 + 64 * U);
-            else if (n0 + step < p.N) {   // the next rows' first weights
-                rows_from(n0 + step);
-                load(v[0], 0);
+        if (segs > 1)
+            load_x(seg1);
+        if (seg1 == 0) {
+            // the rows are done: over the warp, then over the CTA
+#pragma unroll
+            for (int f = 0; f < W; ++f)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float s = __uint_as_float((uint32_t)sum[f][r]) + __uint_as_float((uint32_t)(sum[f][r] >> 32));
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+                        s += __shfl_xor_sync(0xffffffffu, s, o);
+                    if (lane == 0)
+                        part[turn][f * R + r][warp] = s;
+                    sum[f][r] = 0;
+                }
+            __syncthreads();
+            const int f = threadIdx.x / R, r = threadIdx.x % R, n = item * NF + f;
+            if (f < NF && r >= lo && r < hi && n < p.N) {
+                float y = 0.0f, up = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    y += part[turn][f * R + r][w];
+                    if (KIND == HIDDEN)
+                        up += part[turn][(NF + f) * R + r][w];
+                }
+                if (KIND == HIDDEN) {
+                    if (p.pre) {
+                        p.pre[r * 2 * p.fp + n] = y;
+                        p.pre[r * 2 * p.fp + p.fp + n] = up;
+                    }
+                    with_act(p.act, [&](auto kind) { y = act_of<decltype(kind)::value>(y) * up; });
+                }
+                static_cast<T *>(p.out)[r * p.ldo + n] = from_f32<T>(y);
             }
-            multiply(v[1], g0 + 32 * U);
+            turn ^= 1;   // read before the next barrier, written after it
         }
-        // every lane gets every sum; lane f R + r stores feature f of row r
-        float mine = 0.0f, up = 0.0f;
 #pragma unroll
         for (int f = 0; f < W; ++f)
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float s = __uint_as_float((uint32_t)sum[f][r]) + __uint_as_float((uint32_t)(sum[f][r] >> 32));
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == f % NF * R + r)
-                    (f < NF ? mine : up) = s;
-            }
-        const int f = lane / R, r = lane % R, n = n0 + f;
-        if (f < NF && r >= lo && r < hi && n < p.N) {
-            if (KIND == HIDDEN) {
-                if (p.pre) {
-                    p.pre[r * 2 * p.fp + n] = mine;
-                    p.pre[r * 2 * p.fp + p.fp + n] = up;
-                }
-                with_act(p.act, [&](auto kind) { mine = act_of<decltype(kind)::value>(mine) * up; });
-            }
-            static_cast<T *>(p.out)[r * p.ldo + n] = from_f32<T>(mine);
-        }
+            for (int j = 0; j < J; ++j)
+                now[f][j] = next[f][j];
+        item = item1;
+        seg = seg1;
     }
 }
 
-template <int KIND, int R, typename T>
+template <int KIND, int R, int J, typename T>
 cudaError_t launch(esp_moe *m, const VecParams &p)
 {
-    const int ctas = 2 * m->sm_count;
+    constexpr int NF = KIND == HIDDEN ? 2 / J : 4 / J;
     m->launches += 1;
-    // two weight rows (HIDDEN: of each matrix) at a time where there are enough for every warp, else one
-    constexpr int NF = KIND == HIDDEN ? 2 : 4;
-    if (p.N >= ctas * kWarps * NF / 2)
-        return launch_after(k_ff_vec<KIND, R, NF, T>, dim3((unsigned)std::min<int64_t>(ctas, ceil_div(p.N, NF))), kThreads, 0,
-                            m->stream, p);
-    return launch_after(k_ff_vec<KIND, R, NF / 2, T>, dim3((unsigned)std::min<int64_t>(ctas, ceil_div(p.N, NF / 2))), kThreads,
+    return launch_after(k_ff_vec<KIND, R, J, T>, dim3((unsigned)std::min<int64_t>(kCtas<R> * m->sm_count, ceil_div(p.N, NF))), kThreads,
                         0, m->stream, p);
+}
+
+// A weight row in one step where it can be.
+template <int KIND, int R, typename T>
+cudaError_t by_length(esp_moe *m, const VecParams &p)
+{
+    return p.K <= 8 * kThreads ? launch<KIND, R, 1, T>(m, p) : KIND == HIDDEN || p.K <= 16 * kThreads
+               ? launch<KIND, R, 2, T>(m, p) : launch<KIND, R, KIND == HIDDEN ? 2 : 4, T>(m, p);
 }
 
 template <int KIND>
@@ -214,7 +229,7 @@ cudaError_t by_rows(esp_moe *m, int32_t dtype, const VecParams &p)
 {
     return with_16(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        return p.M == 1 ? launch<KIND, 1, T>(m, p) : launch<KIND, 2, T>(m, p);
+        return p.M == 1 ? by_length<KIND, 1, T>(m, p) : by_length<KIND, 2, T>(m, p);
     });
 }
 

@@ -3,7 +3,8 @@
 // norm = |scale| sqrt(sum g^2) over all elements of all tensors; out = g * factor, factor = scale min(1, max_norm / norm)
 // (scale where the norm is not finite). Two passes, as the factor needs every element: k_norm reads all, k_scale reads
 // again and writes. Bound by HBM. The tensors are cut into chunks of 16-byte groups that the CTAs take in turn; k_scale
-// takes them from the last to the first, so that it begins with what k_norm left in L2.
+// takes them from the last to the first, so that it begins with what k_norm left in L2. k_norm leaves a sum for each of
+// its CTAs; every CTA of k_scale adds them up for itself, and loads its first chunk while k_norm still runs.
 //
 // A thread sums the squares of a chunk's groups in fp32 (at most 64 of them), then adds that to its sum in fp64; the
 // threads', CTAs' and launches' sums are joined in a fixed order in fp64. Squares of values that fp32 does not hold
@@ -13,6 +14,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -25,9 +27,12 @@ namespace esp_moe_impl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCtasPerSm = 4;      // k_norm's, with eight loads in flight; k_scale has twice as many with four
+constexpr int kCtasPerSm = 4;      // k_norm's, each with many chunks and eight loads of a thread in flight
+// k_scale's, with four: more than run at once, so that they end together (2e9 elements of 16 bits: 1325 us with 8, 1246
+// with 16, 1222 with 32)
+constexpr int kScaleCtas = 32, kScaleCtasOfFew = 8;   // few bytes: less often the sum of k_norm's CTAs
 
-constexpr int kBatch = 144;       // tensors of a launch, in its parameters
+constexpr int kFewTensors = 16, kManyTensors = 144;   // tensors of a launch, in its parameters
 constexpr int64_t kMostBytes = (int64_t)1 << 45;   // of all tensors; keeps a launch's chunks in int32
 
 struct ClipTensor {
@@ -36,20 +41,19 @@ struct ClipTensor {
     int64_t n;
 };
 
+template <int N>
 struct ClipArgs {
-    ClipTensor t[kBatch];
-    int32_t first[kBatch];        // first chunk of each tensor
-    uint8_t dtype[kBatch];
+    ClipTensor t[N];
+    int32_t first[N];             // first chunk of each tensor
+    uint8_t dtype[N];
     int32_t count, chunks;
 };
 
-struct NormArgs {
-    double *partial;              // one for each CTA of every launch
-    int32_t base, total;          // this launch's first partial; all of them in the last launch, else 0
-    unsigned int *ticket;
+struct SumArgs {
+    const double *partial;        // one for each CTA of k_norm
+    int32_t count;
     double max_norm, scale;
     float *norm;
-    float *factor;
 };
 
 // Elements before the first of a tensor in its first 16-byte group.
@@ -63,7 +67,8 @@ template <typename T>
 constexpr int kPer = 16 / (int)sizeof(T);
 
 // The tensor whose chunks hold `chunk`.
-__device__ __forceinline__ int tensor_of(const ClipArgs &a, int chunk)
+template <int N>
+__device__ __forceinline__ int tensor_of(const ClipArgs<N> &a, int chunk)
 {
     int lo = 0, hi = a.count;
     while (hi - lo > 1) {
@@ -142,28 +147,28 @@ __device__ __forceinline__ double square_chunk(const ClipTensor &t, int64_t g0)
     return d;
 }
 
-// Sum over the CTA, in thread 0.
-__device__ __forceinline__ double sum_of_cta(double v, double *warps)
+// Sum over the CTA, in thread 0. One warp adds up: an fp64 addition of a warp keeps an SM's fp64 units for about 16
+// cycles, so that few of them is what counts.
+__device__ __forceinline__ double sum_of_cta(double v, double *all)
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        v += __shfl_down_sync(0xffffffffu, v, o);
-    if ((threadIdx.x & 31) == 0)
-        warps[threadIdx.x >> 5] = v;
+    all[threadIdx.x] = v;
     __syncthreads();
-    v = (threadIdx.x & 31) < kThreads / 32 ? warps[threadIdx.x & 31] : 0.0;
+    if (threadIdx.x < 32) {
+        for (int i = 32; i < kThreads; i += 32)
+            v += all[threadIdx.x + i];
 #pragma unroll
-    for (int o = kThreads / 64; o > 0; o >>= 1)
-        v += __shfl_down_sync(0xffffffffu, v, o);
+        for (int o = 16; o > 0; o >>= 1)
+            v += __shfl_down_sync(0xffffffffu, v, o);
+    }
     return v;
 }
 
-template <int U>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const __grid_constant__ ClipArgs a, const NormArgs n)
+template <int U, int N>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const __grid_constant__ ClipArgs<N> a, double *partial)
 {
-    __shared__ double warps[kThreads / 32];
-    __shared__ bool last;
+    __shared__ double all[kThreads];
     wait_for_launch_before();
+    let_next_launch_start();
     double sum = 0.0;
     for (int c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const int i = tensor_of(a, c);
@@ -173,43 +178,36 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) k_norm(const __grid_cons
                : a.dtype[i] == ESP_MOE_BF16 ? square_chunk<__nv_bfloat16, U>(t, g0)
                                             : square_chunk<__half, U>(t, g0);
     }
-    sum = sum_of_cta(sum, warps);
-    if (threadIdx.x == 0) {
-        n.partial[n.base + blockIdx.x] = sum;
-        last = false;
-        if (n.total > 0) {
-            __threadfence();
-            last = atomicAdd(n.ticket, 1u) == gridDim.x - 1;
-        }
-    }
-    __syncthreads();
-    if (!last)
+    sum = sum_of_cta(sum, all);
+    if (threadIdx.x == 0)
+        partial[blockIdx.x] = sum;
+}
+
+// 2^e of a normal number.
+__device__ __forceinline__ double power_of_two(int e)
+{
+    return __longlong_as_double((long long)(1023 + e) << 52);
+}
+
+// This thread's groups of a chunk that is to be written.
+template <typename T, int U>
+__device__ __forceinline__ void load_chunk(const ClipTensor &t, int64_t g0, uint4 (&r)[U])
+{
+    if (!t.out)
         return;
-    __threadfence();
-    sum = 0.0;
-    for (int i = threadIdx.x; i < n.total; i += kThreads)
-        sum += __ldcg(n.partial + i);
-    sum = sum_of_cta(sum, warps);
-    if (threadIdx.x == 0) {
-        *n.ticket = 0u;
-        const double norm = fabs(n.scale) * sqrt(sum);
-        const double less = norm > n.max_norm && norm < (double)INFINITY ? n.max_norm / norm : 1.0;
-        *n.norm = (float)norm;
-        *n.factor = (float)(n.scale * less);
-    }
+    const int skip = lead<T>(t.grad);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        r[u] = load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip);
 }
 
 template <typename T, int U>
-__device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, float by)
+__device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, float by, const uint4 (&r)[U])
 {
     if (!t.out || (by == 1.0f && t.out == t.grad))
         return;
     const int skip = lead<T>(t.grad);
     const bool same = lead<T>(t.out) == skip;   // groups of `out` are aligned too
-    uint4 r[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        r[u] = load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t i = (g0 + u * kThreads + threadIdx.x) * kPer<T> - skip;
@@ -235,21 +233,65 @@ __device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, flo
     }
 }
 
-template <int U>
-__global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ ClipArgs a, const float *factor)
+// Calls f(T()) for a tensor's type.
+template <typename F>
+__device__ __forceinline__ void by_dtype(uint8_t dtype, F &&f)
 {
+    if (dtype == ESP_MOE_F32)
+        f(float());
+    else if (dtype == ESP_MOE_BF16)
+        f(__nv_bfloat16());
+    else
+        f(__half());
+}
+
+template <int U, int N>
+__global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ ClipArgs<N> a, const SumArgs n)
+{
+    __shared__ double all[kThreads];
+    __shared__ float factor;
+    uint4 r[U];
+    int c = a.chunks - 1 - (int)blockIdx.x, i = 0;
+    int64_t g0 = 0;
+    const auto load = [&] {
+        if (c < 0)
+            return;
+        i = tensor_of(a, c);
+        g0 = (int64_t)(c - a.first[i]) * (U * kThreads);
+        by_dtype(a.dtype[i], [&](auto elem) { load_chunk<decltype(elem), U>(a.t[i], g0, r); });
+    };
+    // the launch before is k_norm (or an earlier k_scale, of other tensors), which let this one start after all work before
+    // it was done: the gradients are there
+    load();
     wait_for_launch_before();
-    const float by = *factor;
-    for (int c = a.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int i = tensor_of(a, c);
-        const ClipTensor &t = a.t[i];
-        const int64_t g0 = (int64_t)(c - a.first[i]) * (U * kThreads);
-        if (a.dtype[i] == ESP_MOE_F32)
-            scale_chunk<float, U>(t, g0, by);
-        else if (a.dtype[i] == ESP_MOE_BF16)
-            scale_chunk<__nv_bfloat16, U>(t, g0, by);
-        else
-            scale_chunk<__half, U>(t, g0, by);
+    let_next_launch_start();
+    double sum = 0.0;
+    for (int j = threadIdx.x; j < n.count; j += kThreads)
+        sum += __ldcg(n.partial + j);
+    sum = sum_of_cta(sum, all);
+    if (threadIdx.x == 0) {
+        // sum = m 4^e with m in [1, 4): fp32's reciprocal root of m (2 ulp) and one Newton step in fp64 leave it exact to
+        // 2^-40; fp64's own root and division take several microseconds here
+        float norm = (float)sum;
+        factor = (float)n.scale;
+        if (sum > 0.0 && sum < (double)INFINITY) {
+            const int e = ((int)(__double_as_longlong(sum) >> 52) - 1023) >> 1;
+            const double m = sum * power_of_two(-2 * e);
+            double r = (double)rsqrtf((float)m);
+            r = r * (1.5 - 0.5 * m * r * r);
+            norm = (float)(n.scale * m * r * power_of_two(e));
+            if (norm < INFINITY)
+                factor = (float)fmin(n.scale, n.max_norm * r * power_of_two(-e));
+        }
+        if (blockIdx.x == 0)
+            *n.norm = norm;
+    }
+    __syncthreads();
+    const float by = factor;
+    while (c >= 0) {
+        by_dtype(a.dtype[i], [&](auto elem) { scale_chunk<decltype(elem), U>(a.t[i], g0, by, r); });
+        c -= gridDim.x;
+        load();
     }
 }
 
@@ -307,17 +349,17 @@ bool overlapping(int32_t count, const esp_moe_tensor *tensors)
     return false;
 }
 
-template <int U, int V>
-cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, NormArgs n, bool write)
+// U, V: groups in flight of a thread of k_norm and of k_scale. N: tensors of a launch.
+template <int U, int V, int N>
+cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, double *partial, SumArgs n)
 {
     const int most = kCtasPerSm * m->sm_count;
-    ClipArgs a;
-    for (int pass = 0; pass < (write ? 2 : 1); ++pass) {
-        n.base = 0;
+    ClipArgs<N> a;
+    for (int pass = 0; pass < 2; ++pass) {
         int32_t at = 0;
         for (bool more = true; more;) {
             a.count = a.chunks = 0;
-            for (; at < count && a.count < kBatch; ++at) {
+            for (; at < count && a.count < N; ++at) {
                 const esp_moe_tensor &t = tensors[at];
                 const int64_t chunks = t.n == 0 || (pass == 1 && !t.out) ? 0 : chunks_of(t, pass == 0 ? U : V);
                 if (chunks == 0)
@@ -329,17 +371,19 @@ cudaError_t launch_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors
                 a.count += 1;
             }
             more = at < count;
-            if (pass == 1 && a.chunks == 0)
-                break;
-            const int grid = std::max(1, std::min(pass == 0 ? most : 2 * most, a.chunks));
-            n.total = pass == 0 && !more ? n.base + grid : 0;
+            if (pass == 0 && a.chunks == 0)
+                continue;
+            // k_scale writes the norm too, so that one of it runs even where there is nothing to write
+            const int grid = std::max(1, std::min(pass == 0 ? most : (U == 8 ? kScaleCtas : kScaleCtasOfFew) * m->sm_count, a.chunks));
+            n.partial = partial;
             m->launches += 1;
-            const cudaError_t e = pass == 0 ? launch_after(k_norm<U>, dim3(grid), kThreads, 0, m->stream, a, n)
-                                            : launch_after(k_scale<V>, dim3(grid), kThreads, 0, m->stream, a,
-                                                           (const float *)n.factor);
+            const cudaError_t e =
+                pass == 0 ? launch_after(k_norm<U, N>, dim3(grid), kThreads, 0, m->stream, a, partial + n.count)
+                          : launch_after(k_scale<V, N>, dim3(grid), kThreads, 0, m->stream, a, n);
             if (e != cudaSuccess)
                 return e;
-            n.base += grid;
+            if (pass == 0)
+                n.count += grid;
         }
     }
     return cudaSuccess;
@@ -375,21 +419,27 @@ extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tens
     } catch (const std::bad_alloc &) {
         return ESP_ERR_OOM;
     }
-    NormArgs n{};
-    const size_t launches = (size_t)count / kBatch + 1;
+    SumArgs n{};
+    double *partial = nullptr;
+    const size_t launches = (size_t)count / kManyTensors + 1;
     for (int pass = 0; pass < 2; ++pass) {
         Carver c(m->ws);
-        n.factor = c.take<float>(1);
-        n.partial = c.take<double>((size_t)kCtasPerSm * m->sm_count * launches);
+        partial = c.take<double>((size_t)kCtasPerSm * m->sm_count * launches);
         if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
             return st;
     }
-    n.ticket = m->d_ticket;
     n.max_norm = max_norm;
     n.scale = scale;
     n.norm = norm;
-    // few bytes: two groups a thread, so that every SM has some; else eight in flight
-    const bool few = bytes < (int64_t)m->sm_count * kCtasPerSm * kThreads * 8 * 16;
-    const cudaError_t e = few ? launch_clip<2, 2>(m, count, tensors, n, write) : launch_clip<8, 4>(m, count, tensors, n, write);
+    // eight loads of a thread in flight where every CTA of k_norm has such a chunk, else fewer and more CTAs
+    const int64_t chunk = (int64_t)kThreads * 16, ctas = (int64_t)m->sm_count * kCtasPerSm;
+    const auto launch = [&](auto tensors_per_launch) {
+        constexpr int N = decltype(tensors_per_launch)::value;
+        return bytes >= 16 * ctas * chunk   ? launch_clip<8, 4, N>(m, count, tensors, partial, n)
+               : bytes >= 2 * ctas * chunk ? launch_clip<4, 4, N>(m, count, tensors, partial, n)
+                                           : launch_clip<2, 2, N>(m, count, tensors, partial, n);
+    };
+    const cudaError_t e = count <= kFewTensors ? launch(std::integral_constant<int, kFewTensors>())
+                                               : launch(std::integral_constant<int, kManyTensors>());
     return e == cudaSuccess ? ESP_OK : fail_call(m);
 }

@@ -162,6 +162,25 @@ def test_block_and_its_gradients(mm, sizes, H, F, dt, kind, gathered, spare):
     check(mm, sizes, H, F, dt, kind, gathered, spare, seed=sum(sizes) + H)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3])
+@pytest.mark.parametrize("H,F", [(1, 1), (40, 3), (130, 2049), (2048, 65), (2056, 4100), (4096, 8200), (8190, 129), (16500, 40)])
+def test_single_tokens(mm, M, H, F):
+    check(mm, [M], H, F, "bf16" if H % 2 else "f16", "silu", False, 0, seed=H)
+    check(mm, [M], H, F, "bf16", "gelu_tanh", True, 0, seed=H)
+
+
+def test_single_tokens_of_one_block_with_offsets(mm):
+    """Rows outside the one block's offsets are left as they are."""
+    w = mm.gated_weight(rand(64, 96, dt="bf16", seed=1), rand(96, 32, dt="bf16", seed=2))
+    x = rand(2, 96, dt="bf16", seed=3)
+    want = mm.feed_forward(x, w)
+    for lo, hi in ((0, 1), (1, 2), (0, 0), (0, 2), (-3, 9)):
+        y = mm.feed_forward(x, w, offsets=torch.tensor([lo, hi], dtype=torch.int32, device="cuda"),
+                            out=torch.full((2, 96), 5.0, dtype=torch.bfloat16, device="cuda"))
+        a, b = max(0, lo), min(2, hi)
+        assert torch.equal(y[a:b], want[a:b]) and (y[:a] == 5.0).all() and (y[b:] == 5.0).all()
+
+
 @pytest.mark.parametrize("kind", ACTS)
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 def test_activations(mm, kind, dt):
