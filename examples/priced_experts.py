@@ -7,6 +7,11 @@ the prices stepped by excess demand (Eq. price_update in capacity fractions). Th
 
 with 8-bit products; gradients come from the library's calls, the elementwise parts from torch. Run it with
 ``python examples/priced_experts.py`` on a GB300 (random data: it learns to reproduce a fixed random map).
+``--gated`` trains the same router over gated blocks in 16 bits instead (``GatedExperts``),
+
+    out = x + combine(O (silu(G x_rows) * (U x_rows)))
+
+with all gradients clipped together.
 """
 
 from __future__ import annotations
@@ -80,6 +85,56 @@ class PricedExperts:
         return loss, b.loss[0], heavy
 
 
+class GatedExperts:
+    """Router, prices and a gated feed-forward block per expert; fp32 master weights, bf16 rows and blocks."""
+
+    def __init__(self, m: Moe, hidden: int, inner: int, experts: int, k: int, seed: int = 0):
+        g = torch.Generator(device=m.device).manual_seed(seed)
+        rand = lambda *s: torch.randn(*s, generator=g, device=m.device)  # noqa: E731
+        self.m, self.k, self.gate = m, k, Gate("softmax", renorm=True)
+        self.wr = rand(experts, hidden) * hidden ** -0.5
+        self.inner, self.outer = rand(experts, 2 * inner, hidden) * hidden ** -0.5, rand(experts, hidden, inner) * inner ** -0.5
+        self.prices = torch.zeros(experts, device=m.device)
+        self.blocks = m.gated_weight(self.inner.bfloat16(), self.outer.bfloat16(), "silu")
+
+    def forward(self, x, keep: bool = False):
+        m = self.m
+        logits = x.float() @ self.wr.t()
+        r = m.route(logits, self.k, gate=self.gate, prices=self.prices)
+        kept = m.keep(r.rows.shape[0], self.blocks) if keep else None
+        y = m.feed_forward(x, self.blocks, offsets=r.offsets, rows=r.rows, keep=kept)
+        return x + m.combine(y, r.pos, r.weight), (logits, r, kept, y)
+
+    def gradients(self, x, dout, logits, r, kept, y, balance: float = 0.0):
+        """Gradients of the router and of the blocks at dout, all in fp32."""
+        m = self.m
+        b = m.balance(logits, r.idx, gate=self.gate)
+        dy, dweight = m.combine_backward(dout, y, r.pos, r.weight)
+        _, dinner, douter = m.feed_forward_backward(dy, x, self.blocks, kept, offsets=r.offsets, rows=r.rows,
+                                                    need=(False, True, True), dtype=torch.float32)
+        dl = torch.tensor([balance, 0.0], device=m.device)
+        dlogits = m.route_backward(logits, r.idx, gate=self.gate, dweight=dweight, balance=b, dloss=dl)
+        return dlogits.t() @ x.float(), dinner, douter
+
+    def train_step(self, x, target, lr: float = 0.05, balance: float = 0.01, eta: float = 0.1, max_norm: float = 0.02):
+        """One step on mean (out - target)^2 plus the balance loss; returns (loss, the gradients' norm, heaviest load /
+        mean load)."""
+        m = self.m
+        out, (logits, r, kept, y) = self.forward(x, keep=True)
+        diff = (out - target).float()
+        loss = (diff * diff).mean()
+        grads = self.gradients(x, (2.0 / diff.numel() * diff).to(x.dtype), logits, r, kept, y, balance)
+        norm = m.clip(grads, max_norm)
+        step = lr * x.numel() ** 0.5
+        for w, d in zip((self.wr, self.inner, self.outer), grads):
+            w.sub_(step * d)
+        self.blocks.inner.copy_(self.inner)
+        self.blocks.outer.copy_(self.outer)
+        m.step_prices(self.prices, r.counts, eta)
+        heavy = r.counts.max().float() * r.counts.numel() / (x.shape[0] * self.k)
+        return loss, norm, heavy
+
+
 class Server:
     """The trained layer for a fixed number of tokens in flight, captured in a CUDA graph."""
 
@@ -121,7 +176,24 @@ def tokens(n: int, hidden: int, device):
     return x.bfloat16()
 
 
+def train_gated():
+    m = Moe()
+    torch.manual_seed(0)
+    hidden = 256
+    layer = GatedExperts(m, hidden, 512, 16, k=2)
+    mix = torch.randn(hidden, hidden, device=m.device) * hidden ** -0.5
+    for i in range(60):
+        x = tokens(2048, hidden, m.device)
+        loss, norm, heavy = layer.train_step(x, x + torch.tanh(x.float() @ mix).bfloat16())
+        if i % 10 == 0 or i == 59:
+            print(f"step {i:3d}  loss {loss.item():.4f}  norm {norm.item():.4f}  heaviest expert {heavy.item():.2f} x mean")
+    m.synchronize()
+    m.close()
+
+
 def main():
+    if "--gated" in sys.argv[1:]:
+        return train_gated()
     m = Moe()
     torch.manual_seed(0)
     hidden, experts = 256, 16

@@ -1,5 +1,5 @@
-// What the products of the gated feed-forward blocks share (esp_ff_gemm.cu; esp_ff_vec.cu for single rows): parameters,
-// bounded waits, operand descriptors, activations, tensor maps.
+// What the products of the gated feed-forward blocks share (esp_ff_gemm.cu; esp_ff_vec.cu for single rows): bounded waits,
+// operand descriptors, activations, tensor maps.
 #pragma once
 
 #include <type_traits>
@@ -7,30 +7,12 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "esp_fp8_tiles.cuh"
-#include "esp_moe_ff_impl.h"
+#include "esp_ff_tiles.cuh"
 #include "esp_tcgen.cuh"
 
 namespace esp_moe_impl {
 
 namespace {
-
-enum Kind { HIDDEN, OUT, DPRE, DX, DW };
-
-constexpr int kHalfTile = 64 * 128;   // MN-major: 64 inner indices of 64 outer elements
-
-struct FfParams {
-    GemmParams g;             // rows, experts, N (columns of the output), waits
-    int32_t blocks, halves;   // blocks of the inner axis in a half, halves (DX: G and U)
-    int32_t planes;           // DW: outputs of an expert (G and U, or O), each of out_rows x N
-    int32_t out_rows;
-    bool tails;               // DW: a block that an expert's rows do not fill is read from the tails
-    int32_t act;
-    int32_t half_f16;         // operands are fp16 (else bf16)
-    const void *pre;          // DPRE
-    int64_t fp;
-    void *out2;               // HIDDEN: pre (or null)
-};
 
 // ---- waits, by the barrier's scope: one at which this CTA's copies, MMAs and threads arrive, or at which another CTA's
 // warps hand tensor memory back (both sides relaxed at cluster scope: the tcgen05 fences around them order it).

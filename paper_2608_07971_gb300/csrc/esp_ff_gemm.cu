@@ -45,7 +45,6 @@ constexpr int kOrdered = 512;                        // experts that DW can put 
 // the next g and u, at the cost of a stage of the operands: 16384 x 2048 x 4096 234 us, 210 with two).
 template <int CG, int KIND>
 struct Shape {
-    static constexpr int kRows = 128 * CG;                        // of a tile
     static constexpr int kStageB = CG == 2 ? kTileBytes : 2 * kTileBytes;
     static constexpr int kStage = kTileBytes + kStageB;
     static constexpr int kStages = (CG == 2 ? 5 : 4) - (KIND == DPRE && CG == 1 ? 1 : 0);
@@ -53,88 +52,6 @@ struct Shape {
     static constexpr int kSmem = kStages * kStage + kEpilogueWarps * kBoxes * kBox + kBars + 2 * kOrdered + 1024;
     static_assert((2 * kStages + 2 * 2 + 1 + kEpilogueWarps) * 8 + 16 <= kBars, "barriers");
     static_assert(kSmem <= 232448, "shared memory");
-};
-
-// One item of the list: blocks k0 .. k1 - 1 of the inner axis of a tile. Row kinds: rows m0 .. m0 + rows - 1 of expert e,
-// columns n0 ..; DW: output rows m0 .. of plane z, over the rows lo .. hi - 1, the last block from the tails where `cut` is set.
-struct FfTile {
-    int item, e, m0, rows, n0, k0, k1, z, lo, hi;
-    bool cut;
-};
-
-template <int KIND>
-constexpr int kTileCols = KIND == HIDDEN ? 128 : 256;
-
-// A role's way through the list, in rounds of an item for every CTA (pair), every second round backwards, so that nobody
-// gets the longer item of every round (experts' rows differ). Tiles run over an expert's rows first, so that the tiles in
-// flight share columns of B. Items ascend: the row kinds' expert is kept from one to the next.
-template <int CG, int KIND>
-class Walk {
-public:
-    const uint16_t *order = nullptr;   // DW: the experts in the order of the list
-
-    __device__ __forceinline__ bool next(const FfParams &p, FfTile &t)
-    {
-        const int n = gridDim.x / CG, me = blockIdx.x / CG, item = round_ * n + (round_ & 1 ? n - 1 - me : me);
-        ++round_;
-        t.item = item;
-        if (CG == 2 || p.g.splits == 1)
-            return tile(p, item, t);
-        const int part = item % p.g.splits;
-        if (!tile(p, item / p.g.splits, t))
-            return false;
-        const int blocks = t.k1;
-        t.k0 = (int)((int64_t)blocks * part / p.g.splits);
-        t.k1 = (int)((int64_t)blocks * (part + 1) / p.g.splits);
-        t.cut = t.cut && t.k0 < t.k1 && t.k1 == blocks;
-        return true;
-    }
-
-private:
-    __device__ __forceinline__ bool tile(const FfParams &p, int item, FfTile &t)
-    {
-        constexpr int kRows = Shape<CG, KIND>::kRows;
-        t.k0 = 0;
-        t.cut = false;
-        if (KIND != DW) {
-            const int nt = (p.g.N + kTileCols<KIND> - 1) / kTileCols<KIND>;
-            while (item >= (before_ + tiles_) * nt) {
-                before_ += tiles_;
-                if (++e_ >= p.g.E)
-                    return false;
-                expert_rows(p.g, e_, lo_, hi_);
-                // offsets that do not ascend have more tiles than the list
-                tiles_ = min((hi_ - lo_) / kRows + ((hi_ - lo_) % kRows != 0), p.g.most - before_);
-            }
-            const int i = item - before_ * nt;
-            t.e = e_;
-            t.m0 = lo_ + (i % tiles_) * kRows;
-            t.rows = min(kRows, hi_ - t.m0);
-            t.n0 = (i / tiles_) * kTileCols<KIND>;
-            t.k1 = p.blocks * p.halves;
-            return true;
-        }
-        const int mt = (p.out_rows + kRows - 1) / kRows, nt = (p.g.N + 255) / 256, per = mt * nt * p.planes;
-        if (item >= per * p.g.E)
-            return false;
-        t.e = item / per;
-        int i = item - t.e * per;
-        if (order)
-            t.e = order[t.e];
-        t.z = i / (mt * nt);
-        i -= t.z * (mt * nt);
-        t.m0 = (i % mt) * kRows;
-        t.n0 = (i / mt) * 256;
-        t.rows = min(kRows, p.out_rows - t.m0);
-        expert_rows(p.g, t.e, t.lo, t.hi);
-        const bool part = (t.hi - t.lo) % kInner != 0;   // without tails, what follows the last row is outside: zeros
-        t.cut = part && p.tails;
-        t.k1 = (t.hi - t.lo) / kInner + part;
-        return true;
-    }
-
-    int round_ = 0;
-    int e_ = -1, before_ = 0, tiles_ = 0, lo_ = 0, hi_ = 0;   // expert, row tiles of those before it, its own, its rows
 };
 
 // A box into this CTA's shared memory; its bytes arrive at a barrier of this CTA or of the other one of a pair.
@@ -350,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     wait_for_launch_before();
     const uint32_t tmem = *slot;
     uint32_t issued = 0;   // loads of this CTA's loading warp
+    const int me = blockIdx.x / CG, n = gridDim.x / CG;
     FfTile t;
     Walk<CG, KIND> walk;
     if (KIND == DW && p.g.E > 1 && p.g.E <= kOrdered) {
@@ -381,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int s = 0;
         uint32_t ph = 1;
         bool ok = true;
-        while (ok && walk.next(p, t)) {
+        while (ok && walk.next(p, me, n, t)) {
             const int outer_a = t.m0 + (int)rank * kRowsA;
             const int outer_b = t.n0 + (KIND == HIDDEN ? 0 : (int)rank * 128);
             for (int kb = t.k0; kb < t.k1; ++kb) {
@@ -438,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             int s = 0, acc = 0;
             uint32_t ph = 0, aph = 1;
             bool ok = true;
-            while (ok && walk.next(p, t)) {
+            while (ok && walk.next(p, me, n, t)) {
                 if (t.k0 == t.k1)
                     continue;
                 if (!(ok = wait_phase<CG == 2 ? HANDBACK : OWN>(tempty + 8 * acc, aph, p.g, dead)))
@@ -476,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int acc = 0;
         uint32_t aph = 0, lph = 0;
         bool loading = false;   // DPRE: g and u are on their way to the staging boxes
-        while (walk.next(p, t)) {
+        while (walk.next(p, me, n, t)) {
             const int rows = t.rows - (int)rank * kRowsA - 32 * quarter;   // of this warp's 32 that exist, from the first
             const int y = t.m0 + (int)rank * kRowsA + 32 * quarter;        // the first
             const bool split = CG == 1 && p.g.splits > 1, some = t.k0 < t.k1;

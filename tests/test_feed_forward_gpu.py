@@ -197,6 +197,77 @@ def test_long_inner_axes(mm):
     check(mm, [260], 72, 4100, "bf16", "silu", False, 0)
 
 
+TILES = [  # rows of each expert, H, F, type: the choice of tiles in csrc/esp_ff_gemm.cu, on both sides of its rules
+    ([100], 64, 25600, "bf16"),          # single CTAs: HIDDEN, DPRE
+    ([100], 25600, 64, "f16"),           # single CTAs: OUT, DX
+    ([20], 4160, 100, "bf16"),           # split inner axes: HIDDEN, DPRE; a tile of few rows
+    ([140], 100, 4160, "f16"),           # split inner axes: OUT, DX
+    ([5000], 64, 72, "bf16"),            # split inner axes: both weights' gradients
+    ([4000, 9, 2300], 40, 200, "bf16"),  # the same, of experts of which one has fewer blocks than parts
+    ([1500] * 6, 520, 264, "bf16"),      # pairs
+]
+
+
+@pytest.mark.parametrize("sizes,H,F,dt", TILES)
+def test_tiles(mm, sizes, H, F, dt):
+    check(mm, sizes, H, F, dt, "silu", False, 0, seed=H)
+    if len(sizes) > 1:
+        check(mm, sizes, H, F, dt, "gelu", True, 70, dw_dtype=torch.float32, seed=F)
+
+
+def test_many_experts(mm):
+    """As many experts as there can be, most of them with few rows or none."""
+    rng = np.random.default_rng(3)
+    check(mm, list(rng.integers(0, 5, 700)), 40, 24, "bf16", "silu", True, 10)
+    check(mm, [0] * 1000 + [3] + [0] * 22 + [80], 32, 16, "f16", "relu", False, 0)
+
+
+def test_a_stream_of_its_own(mm):
+    from paper_2608_07971_gb300 import moe
+    s = torch.cuda.Stream()
+    m = moe.Moe(stream=s.cuda_stream)
+    x, dy = rand(300, 96, dt="bf16", seed=1), rand(300, 96, dt="bf16", seed=2)
+    inner, outer = rand(2, 128, 96, dt="bf16", seed=3, size=0.1), rand(2, 96, 64, dt="bf16", seed=4, size=0.1)
+    off = torch.tensor([0, 130, 300], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+
+    def step(m):
+        w = m.gated_weight(inner, outer)
+        kept = m.keep(300, w)
+        y = m.feed_forward(x, w, offsets=off, keep=kept)
+        grads = m.feed_forward_backward(dy, x, w, kept, offsets=off)
+        m.synchronize()
+        norm = m.clip(list(grads), 1.0)
+        m.synchronize()
+        return (y, norm, *grads)
+
+    assert all(torch.equal(a, b) for a, b in zip(step(m), step(mm)))
+    m.close()
+
+
+def test_growing_work_space_under_a_graph(mm):
+    """A captured step is replayed after the same handle's work space has grown."""
+    from paper_2608_07971_gb300 import moe
+    m = moe.Moe()
+    w = m.gated_weight(rand(2, 128, 96, dt="bf16", seed=3, size=0.1), rand(2, 96, 64, dt="bf16", seed=4, size=0.1))
+    x = rand(300, 96, dt="bf16", seed=1)
+    off = torch.tensor([0, 130, 300], dtype=torch.int32, device="cuda")
+    rows = torch.arange(299, -1, -1, dtype=torch.int32, device="cuda")
+    want = m.feed_forward(x, w, offsets=off, rows=rows)
+    out = torch.empty_like(want)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.feed_forward(x, w, offsets=off, rows=rows, out=out)
+    big = rand(200_000, 96, dt="bf16", seed=2)
+    m.feed_forward(big, w, offsets=torch.tensor([0, 9, 200_000], dtype=torch.int32, device="cuda"))
+    out.zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    m.close()
+
+
 def test_activations_far_out(mm):
     """Gate values of hundreds: the activations' tails and their slopes stay finite."""
     for kind in ACTS:

@@ -1,0 +1,96 @@
+"""Host-side checks of the gated feed-forward blocks and of clipping that need no GPU: null handles, weights and lists of
+gradients that are refused, the products' work items (tests/ff_tiles_driver.cpp)."""
+
+import copy
+import ctypes
+import os
+import pickle
+import subprocess
+
+import pytest
+import torch
+
+from paper_2608_07971_gb300 import build, esp, moe
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return moe.load_library()
+
+
+def test_null_handle_rejected(lib):
+    bad, N = esp.ESP_ERR_INVALID_ARG, None
+    w, k, t = moe._CGated(), moe._CKept(), (moe._CTensor * 1)()
+    assert lib.esp_moe_feed_forward(N, w, 0, 1, N, 0, N, N, 1, N, k) == bad
+    assert lib.esp_moe_feed_forward_backward(N, w, 0, 1, N, 0, N, N, k, 1, N, 1, N, 0, N, N) == bad
+    assert lib.esp_moe_clip(N, 1, t, 1.0, 1.0, N) == bad
+
+
+def test_work_items_stay_in_range(tmp_path):
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(build.nvcc()))), "include")
+    out = str(tmp_path / "driver")
+    subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-I", build.INCLUDE, "-I", build.CSRC, "-I", cuda, os.path.join(HERE, "ff_tiles_driver.cpp"), "-o", out],
+                   check=True, capture_output=True, text=True)
+    res = subprocess.run([out], capture_output=True, text=True, timeout=120)
+    assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
+
+
+def weights(E=2, F=16, H=24, dtype=torch.bfloat16):
+    return torch.zeros(E, 2 * F, H, dtype=dtype), torch.zeros(E, H, F, dtype=dtype)
+
+
+def test_weights_are_checked():
+    inner, outer = weights()
+    w = moe.GatedWeight(inner, outer, "gelu")
+    assert (w.E, w.F, w.H) == (2, 16, 24)
+    odd = torch.zeros(2, 32, 23, dtype=torch.bfloat16)
+    for a, b, act in ((inner, outer, "tanh"), (inner, outer[:1], "silu"), (inner[:, :31], outer, "silu"), (inner, outer.half(), "silu"),
+                      (inner.float(), outer.float(), "silu"), (inner[0], outer[0], "silu"), (inner[:, :, ::2], outer[:, ::2], "silu"),
+                      (odd, torch.zeros(2, 23, 16, dtype=torch.bfloat16), "silu"), (inner[:0], outer[:0], "silu"),
+                      (inner.transpose(1, 2), outer, "silu")):
+        with pytest.raises(ValueError):
+            moe.GatedWeight(a, b, act)
+
+
+def test_assigned_weights_are_checked_anew():
+    inner, outer = weights()
+    w = moe.GatedWeight(inner, outer)
+    w._arg()
+    w.outer = outer[:, :8]
+    with pytest.raises(ValueError):
+        w._arg()
+    w.outer = outer
+    w.activation = "relu"
+    assert w._arg() is not None and w._c.activation == 3
+    w.inner.data = torch.ones_like(inner)   # moved
+    w._arg()
+    assert w._c.inner == w.inner.data_ptr()
+
+
+def test_weights_can_be_copied():
+    w = moe.GatedWeight(*weights(), "gelu_tanh")
+    for v in (copy.copy(w), copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
+        assert v.activation == "gelu_tanh" and torch.equal(v.inner, w.inner) and v._c.inner == v.inner.data_ptr()
+
+
+def test_weights_of_padded_rows():
+    room = torch.zeros(2, 32, 64, dtype=torch.float16)[:, :, :23]
+    w = moe.GatedWeight(room, torch.zeros(2, 23, 16, dtype=torch.float16))
+    assert w.H == 23 and w._c.ld_inner == 64 and w._c.ld_outer == 16
+
+
+def test_lists_of_gradients_are_checked():
+    g = [torch.zeros(4), torch.zeros(3, dtype=torch.bfloat16)]
+    li = moe.Gradients(g, None, -1)   # -1: tensors on the CPU
+    assert len(li._arg()) == 2 and li._arg()[1].dtype == 1 and li._arg()[1].out == g[1].data_ptr()
+    for tensors, out in (([torch.zeros(4).double()], None), ([torch.zeros(4, 4).t()], None), (g, g[:1]), (g, [g[0], g[1].float()]),
+                         ([torch.zeros(4)], [torch.zeros(5)])):
+        with pytest.raises(ValueError):
+            moe.Gradients(tensors, out, -1)
+    with pytest.raises(ValueError):
+        moe.Gradients(g, None, 0)
+    assert ctypes.sizeof(moe._CTensor) == 32
