@@ -18,6 +18,19 @@
 // Two accumulators of 256 columns: warps 0-7 empty one while the tensor core fills the other. Warp 8 loads by TMA,
 // warp 9 issues the MMAs. CTAs are persistent.
 //
+// Bound by the tensor pipe where it can be kept fed, and under a long load by the card's power: 8192 rows x 4096 x 8192
+// (HIDDEN and OUT) takes 861 us in a burst (1.92 PFLOP/s, the library's bf16 product 1.88) and 990 to 1020 after a second
+// of load. What else the kernels move is nearly on top of that, as the operands already take 64 bytes of L2 a clock and
+// SM: with half of the operands' loads left out, the same takes 790 us; with g and u kept in 32 bits, HIDDEN of 9728 rows x
+// 2048 x 2048 takes 22 us more, their bytes at HBM's rate. Experts' rows are the other loss: tiles of 256 rows are half
+// empty at each expert's end (16384 rows over 16 experts of uneven load as if they were 18400).
+//   single CTAs: 128 rows x 256 columns, 48 instead of 32 KB for the same MMAs (8192 x 2048 x 2048: 137 us, pairs 119); for
+//     few tiles, or many experts of few rows (8 x 256 rows, 2048 x 1024: 37 us, pairs 46)
+//   split inner axes: a tile's parts meet in memory (one of 16 rows, 4096 x 8192: 58 us, whole 82, pairs 71)
+// What did not help: gathering rows of A by the kernel itself with 16-byte asynchronous copies (64 experts of 1024 rows,
+// 2048 x 1024: 1490 us, with a copy of the rows before 530 + 55), a third box for DPRE's g and u at the cost of a stage (234 us,
+// 210 with two), g and u in 16 bits with block scales (15 us less in HIDDEN of a training step, 25 more in ragged small ones).
+//
 // Every wait is bounded, as in esp_fp8_gemm.cu.
 
 #include <algorithm>
@@ -688,7 +701,8 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const
 }
 
 // Which tiles a product takes: pairs of CTAs with 256 x 256, or single ones with 128 x 256 whose inner axis may be split
-// into parts. Times in blocks of the inner axis (0.27 us of a pair's MMAs).
+// into parts. Times in blocks of the inner axis (0.27 us of a pair's MMAs): a tile's start and end take about four, a single
+// CTA's block 1.17, joining parts 12 and 5 for each (5000 x 64 x 72: both weights' gradients 25 us in parts, 34 whole).
 struct Choice {
     bool pair;
     int splits;
