@@ -24,6 +24,7 @@ struct FfParams {
     int32_t out_rows;
     bool tails;               // DW: a block that an expert's rows do not fill is read from the tails
     int32_t act;
+    bool few_ctas;            // most SMs are free
     int32_t half_f16;         // operands are fp16 (else bf16)
     const void *pre;          // DPRE
     int64_t fp;

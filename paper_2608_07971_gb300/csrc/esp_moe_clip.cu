@@ -29,8 +29,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCtasPerSm = 4;      // k_norm's, each with many chunks and eight loads of a thread in flight
-// k_scale's, with four: more than run at once, so that they end together (2e9 elements of 16 bits: 1325 us with 8, 1246
-// with 16, 1222 with 32)
+// k_scale's, with four: more than run at once, so that they end together (1.4e9 elements, 2.8 GB: 1325 us with 8,
+// 1246 with 16, 1222 with 32)
 constexpr int kScaleCtas = 32, kScaleCtasOfFew = 8;   // few bytes: less often the sum of k_norm's CTAs
 
 constexpr int kFewTensors = 16, kManyTensors = 144;   // tensors of a launch, in its parameters

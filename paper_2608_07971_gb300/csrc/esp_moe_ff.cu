@@ -19,6 +19,7 @@ template <int V>
 __global__ void __launch_bounds__(32 * kCopyRows) k_copy_rows(const CopyRowsArgs a)
 {
     wait_for_launch_before();
+    let_next_launch_start();
     const int64_t i = (int64_t)blockIdx.x * kCopyRows + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (i >= a.M)

@@ -170,6 +170,31 @@ def test_repeatable_and_in_graphs(mm):
     m.close()
 
 
+def test_gradients_written_right_before(mm):
+    """The scaling loads its first gradients ahead of the norm's end: never ones that earlier work still writes."""
+    sizes = [300_000, 17, 40_000]
+    sets = [make(sizes, TYPES, s, 0.5) for s in range(3)]
+    grads, outs = make(sizes, TYPES, 9), [[torch.empty_like(t) for t in sets[0]] for _ in range(30)]
+    lists = [mm.gradients(grads, out=o) for o in outs]
+    norms = [torch.zeros((), device="cuda") for _ in outs]
+    torch.cuda.synchronize()
+    for i, li in enumerate(lists):
+        for g, s in zip(grads, sets[i % 3]):
+            g.copy_(s)
+        mm.clip(li, 1.0, norm=norms[i])
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        check(sets[i % 3], o, norms[i], 1.0, 1.0)
+    # in place, one after another: each call begins with what the one before left
+    a, b = [t.clone() for t in sets[0]], [t.clone() for t in sets[0]]
+    for k in range(20):
+        before = [t.clone() for t in a]
+        check(before, a, mm.clip(a, 2.0 ** -k), 2.0 ** -k, 1.0)
+    for k in range(20):   # nothing waits between
+        mm.clip(b, 2.0 ** -k)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
 def test_moved_memory_is_used(mm):
     p = [torch.ones(10, device="cuda"), torch.ones(6, device="cuda")]
     li = mm.gradients(p)

@@ -465,6 +465,41 @@ def test_repeatable_on_streams_and_in_graphs(mm):
     m.close()
 
 
+def test_weights_written_right_before(mm):
+    """Single tokens load their first weights ahead of the launch before: never ones that earlier work still writes."""
+    from paper_2608_07971_gb300 import moe
+    H, F = 1024, 2048
+    w = mm.gated_weight(rand(2 * F, H, dt="bf16", seed=0), rand(H, F, dt="bf16", seed=0))
+    x = rand(1, H, dt="bf16", seed=1)
+    sets = [(rand(1, 2 * F, H, dt="bf16", seed=s, size=H ** -0.5), rand(1, H, F, dt="bf16", seed=s + 9, size=F ** -0.5))
+            for s in range(2, 6)]
+    want = []
+    for a, b in sets:
+        torch.cuda.synchronize()
+        want.append(mm.feed_forward(x, moe.GatedWeight(a, b)))
+    torch.cuda.synchronize()
+    out = [torch.empty_like(x) for _ in range(40)]
+
+    def run():
+        for i, y in enumerate(out):
+            w.inner.copy_(sets[i % 4][0])
+            w.outer.copy_(sets[i % 4][1])
+            mm.feed_forward(x, w, out=y)
+
+    run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 4]) for i, y in enumerate(out))
+    for y in out:
+        y.zero_()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        run()
+    g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i % 4]) for i, y in enumerate(out))
+
+
 def test_copies_of_weights_and_kept(mm):
     import copy
     import pickle
