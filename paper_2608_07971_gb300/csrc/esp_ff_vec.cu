@@ -1,4 +1,4 @@
-// The forward products of one dense gated feed-forward block for one or two rows (single tokens), on the CUDA cores: every
+// The forward products of one dense gated feed-forward block for up to eight rows (single tokens), on the CUDA cores: every
 // weight is loaded once, 16 bytes a lane, and multiplied with the rows in fp32. Bound by the weights' bytes; there is no
 // tile to fill, no tensor memory and nothing to join, which is what a tensor-core kernel spends its time on here.
 //
@@ -21,7 +21,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 struct VecParams {
-    int32_t M, T, N, K;          // M: at most 2; N: weight rows (HIDDEN: of G), K: inner axis
+    int32_t M, T, N, K;          // M: at most 8; N: weight rows (HIDDEN: of G), K: inner axis
     const int32_t *offsets, *rows;
     const void *w, *x;
     int64_t ldw, ldx;
@@ -85,14 +85,16 @@ __device__ __forceinline__ void fma2(uint64_t &c, uint64_t a, uint64_t b)
 
 // CTAs of an SM: what their registers leave room for.
 template <int R>
-constexpr int kCtas = R == 1 ? 4 : 3;
+constexpr int kCtas = R == 1 ? 4 : R == 2 ? 3 : 2;
+template <int R>
+constexpr int kLoads = R == 8 ? 2 : 4;
 
 // R rows of x; a thread has J groups of 8 elements of a weight row's 256 J in a step (a row longer than that takes several
-// steps), and W = 4 / J weight rows.
+// steps), and W weight rows: four loads in flight, with eight rows two.
 template <int KIND, int R, int J, typename T>
 __global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p)
 {
-    constexpr int W = 4 / J, NF = KIND == HIDDEN ? W / 2 : W;
+    constexpr int W = kLoads<R> / J, NF = KIND == HIDDEN ? W / 2 : W;
     __shared__ float part[2][W * R][kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!p.early) {
@@ -210,18 +212,22 @@ __global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p
 template <int KIND, int R, int J, typename T>
 cudaError_t launch(esp_moe *m, const VecParams &p)
 {
-    constexpr int NF = KIND == HIDDEN ? 2 / J : 4 / J;
+    constexpr int W = kLoads<R> / J, NF = KIND == HIDDEN ? W / 2 : W;
     m->launches += 1;
     return launch_after(k_ff_vec<KIND, R, J, T>, dim3((unsigned)std::min<int64_t>(kCtas<R> * m->sm_count, ceil_div(p.N, NF))), kThreads,
                         0, m->stream, p);
 }
 
-// A weight row in one step where it can be.
+// A weight row in one step where it can be; HIDDEN has rows of both matrices.
 template <int KIND, int R, typename T>
 cudaError_t by_length(esp_moe *m, const VecParams &p)
 {
-    return p.K <= 8 * kThreads ? launch<KIND, R, 1, T>(m, p) : KIND == HIDDEN || p.K <= 16 * kThreads
-               ? launch<KIND, R, 2, T>(m, p) : launch<KIND, R, KIND == HIDDEN ? 2 : 4, T>(m, p);
+    constexpr int kMost = KIND == HIDDEN ? kLoads<R> / 2 : kLoads<R>;   // J
+    if (kMost == 1 || p.K <= 8 * kThreads)
+        return launch<KIND, R, 1, T>(m, p);
+    if (kMost == 2 || p.K <= 16 * kThreads)
+        return launch<KIND, R, std::min(2, kMost), T>(m, p);
+    return launch<KIND, R, kMost, T>(m, p);
 }
 
 template <int KIND>
@@ -229,15 +235,24 @@ cudaError_t by_rows(esp_moe *m, int32_t dtype, const VecParams &p)
 {
     return with_16(dtype, [&](auto elem) -> cudaError_t {
         using T = decltype(elem);
-        return p.M == 1 ? by_length<KIND, 1, T>(m, p) : by_length<KIND, 2, T>(m, p);
+        return p.M == 1   ? by_length<KIND, 1, T>(m, p)
+               : p.M == 2 ? by_length<KIND, 2, T>(m, p)
+               : p.M <= 4 ? by_length<KIND, 4, T>(m, p)
+                          : by_length<KIND, 8, T>(m, p);
     });
 }
 
 }  // namespace
 
-bool use_vec(int64_t M, int32_t E)
+bool use_vec(int64_t M, int32_t E, int32_t F, int32_t H)
 {
-    return E == 1 && M <= 2;
+    // Times of both products (us), here and on the tensor cores, whose kernels take 20 before the weights' bytes count:
+    //   rows  512 x 512  1024 x 2048  2048 x 4096  4096 x 8192 (201 MB)
+    //   1, 2  7.8  13.6    8.0  23.6   13 to 16  33   40 to 48  58
+    //   4     7.2  13.5   11.0  23.5       22  33       69  62
+    //   8     7.5  13.6   17.4  23.5       38  33      185  58
+    const int64_t bytes = 6 * (int64_t)F * H;
+    return E == 1 && (M <= 2 || (M <= 4 && bytes <= 96 << 20) || (M <= 8 && bytes <= 20 << 20));
 }
 
 cudaError_t launch_vec(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, int64_t T, const int32_t *rows, void *hidden,

@@ -144,7 +144,7 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
     FfShape s = shape_of(w, M, offsets);
     const int64_t hp = up64(w->H);
     // a few rows: gathered by the products themselves, unless they are kept for the gradients
-    const bool vec = use_vec(M, w->E);
+    const bool vec = use_vec(M, w->E, w->F, w->H);
     const bool copy = copied && !(vec && !kept && mappable(x, ldx));
     void *hidden = nullptr, *gathered = nullptr;
     for (int pass = 0; pass < 2; ++pass) {

@@ -31,8 +31,8 @@ struct FfShape {
 };
 
 // ---- esp_ff_vec.cu
-// Whether a forward pass is for the CUDA cores: one dense block, one or two rows.
-bool use_vec(int64_t M, int32_t E);
+// Whether a forward pass is for the CUDA cores: one dense block, a few rows.
+bool use_vec(int64_t M, int32_t E, int32_t F, int32_t H);
 // Both products of such a pass: hidden (M x fp), pre where it is given, y. Rows are gathered here.
 cudaError_t launch_vec(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, int64_t T, const int32_t *rows, void *hidden,
                        void *pre, void *y, int64_t ldy);

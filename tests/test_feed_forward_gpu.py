@@ -162,7 +162,7 @@ def test_block_and_its_gradients(mm, sizes, H, F, dt, kind, gathered, spare):
     check(mm, sizes, H, F, dt, kind, gathered, spare, seed=sum(sizes) + H)
 
 
-@pytest.mark.parametrize("M", [1, 2, 3])
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 8, 9])
 @pytest.mark.parametrize("H,F", [(1, 1), (40, 3), (130, 2049), (2048, 65), (2056, 4100), (4096, 8200), (8190, 129), (16500, 40)])
 def test_single_tokens(mm, M, H, F):
     check(mm, [M], H, F, "bf16" if H % 2 else "f16", "silu", False, 0, seed=H)
