@@ -216,12 +216,20 @@ __device__ __forceinline__ bool all_of_epilogue(bool v)
     return r != 0;
 }
 
-// T: operands; O: output. map_a2, map_b2: DW's tails; map_a2: HIDDEN's and DPRE's pre.
+// Tensor maps of a product. a2, b2: DW's tails; a2: HIDDEN's and DPRE's pre.
+struct OneMaps {
+    CUtensorMap a, b, out, a2, b2;
+};
+
+template <int KIND>
+struct FfMaps {
+    OneMaps of[KIND == DW ? 2 : 1];   // DW: of each gradient
+};
+
+// T: operands; O: output.
 template <int CG, int KIND, typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_ff(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-         const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_a2,
-         const __grid_constant__ CUtensorMap map_b2, const FfParams p)
+    k_ff(const __grid_constant__ FfMaps<KIND> maps, const FfParams p)
 {
     using S = Shape<CG, KIND>;
     constexpr int kStages = S::kStages, kStage = S::kStage;
@@ -255,9 +263,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8 && lane == 0) {
-        prefetch_map(&map_a);
-        prefetch_map(&map_b);
-        prefetch_map(&map_out);
+        prefetch_map(&maps.of[0].a);
+        prefetch_map(&maps.of[0].b);
+        prefetch_map(&maps.of[0].out);
     }
     if (warp == 9) {
         if (CG == 2) {
@@ -317,6 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t ph = 1;
         bool ok = true;
         while (ok && walk.next(p, me, n, t)) {
+            const OneMaps &map = maps.of[KIND == DW ? t.q : 0];
             const int outer_a = t.m0 + (int)rank * kRowsA;
             const int outer_b = t.n0 + (KIND == HIDDEN ? 0 : (int)rank * 128);
             for (int kb = t.k0; kb < t.k1; ++kb) {
@@ -333,13 +342,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         constexpr int kHalves = S::kStageB / kHalfTile;   // MN-major halves of B
                         // DW: the inner axis' first row, and the tensors that hold it
                         const int y = KIND == DW ? (cut ? t.e * kInner : t.lo + k) : k;
-                        const CUtensorMap *const a_map = KIND == DW && cut ? &map_a2 : &map_a;
-                        const CUtensorMap *const b_map = KIND == DW && cut ? &map_b2 : &map_b;
+                        const CUtensorMap *const a_map = KIND == DW && cut ? &map.a2 : &map.a;
+                        const CUtensorMap *const b_map = KIND == DW && cut ? &map.b2 : &map.b;
                         if (A_MN) {
                             load_box<CG>(a, a_map, outer_a, y, t.z, bar);
                             load_box<CG>(a + kHalfTile, a_map, outer_a + 64, y, t.z, bar);
                         } else {
-                            load_box<CG>(a, &map_a, k, outer_a, half, bar);
+                            load_box<CG>(a, &map.a, k, outer_a, half, bar);
                         }
                         if (B_MN) {
                             const int z = KIND == DW ? 0 : KIND == DX ? 2 * t.e + half : t.e;
@@ -347,13 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             for (int i = 0; i < kHalves; ++i)
                                 load_box<CG>(b + i * kHalfTile, b_map, outer_b + 64 * i, y, z, bar);
                         } else if (KIND == HIDDEN) {
-                            load_box<CG>(b, &map_b, k, outer_b, 2 * t.e + (int)rank, bar);
+                            load_box<CG>(b, &map.b, k, outer_b, 2 * t.e + (int)rank, bar);
                             if (CG == 1)
-                                load_box<CG>(b + kTileBytes, &map_b, k, outer_b, 2 * t.e + 1, bar);
+                                load_box<CG>(b + kTileBytes, &map.b, k, outer_b, 2 * t.e + 1, bar);
                         } else {
-                            load_box<CG>(b, &map_b, k, outer_b, t.e, bar);
+                            load_box<CG>(b, &map.b, k, outer_b, t.e, bar);
                             if (CG == 1)
-                                load_box<CG>(b + kTileBytes, &map_b, k, outer_b + 128, t.e, bar);
+                                load_box<CG>(b + kTileBytes, &map.b, k, outer_b + 128, t.e, bar);
                         }
                     }
                 }
@@ -412,6 +421,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         uint32_t aph = 0, lph = 0;
         bool loading = false;   // DPRE: g and u are on their way to the staging boxes
         while (walk.next(p, me, n, t)) {
+            const OneMaps &map = maps.of[KIND == DW ? t.q : 0];
+            const int N = KIND == DW ? p.dw[t.q].N : p.g.N;   // columns of the output
             const int rows = t.rows - (int)rank * kRowsA - 32 * quarter;   // of this warp's 32 that exist, from the first
             const int y = t.m0 + (int)rank * kRowsA + 32 * quarter;        // the first
             const bool split = CG == 1 && p.g.splits > 1, some = t.k0 < t.k1;
@@ -420,12 +431,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             const auto load_pre = [&](int c) {
                 if (lane == 0) {
                     mbar_expect(landed + 8 * warp, 2 * kBox);
-                    load_box<CG>(smem_u32(gbox), &map_a2, t.n0 + c, y, 0, landed + 8 * warp);
-                    load_box<CG>(smem_u32(ubox), &map_a2, t.n0 + c, y, 1, landed + 8 * warp);
+                    load_box<CG>(smem_u32(gbox), &map.a2, t.n0 + c, y, 0, landed + 8 * warp);
+                    load_box<CG>(smem_u32(ubox), &map.a2, t.n0 + c, y, 1, landed + 8 * warp);
                 }
                 loading = true;
             };
-            const int first = 128 * wg, columns = min(128, p.g.N - t.n0 - first);   // of this warp (not HIDDEN)
+            const int first = 128 * wg, columns = min(128, N - t.n0 - first);   // of this warp (not HIDDEN)
             if (KIND == DPRE && !split && rows > 0 && columns > 0) {
                 boxes.drain();
                 load_pre(first);
@@ -514,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (!skip) {
                 if (KIND == HIDDEN) {
-                    const int c = 64 * wg, n = t.n0 + c, cols = p.g.N - n;
+                    const int c = 64 * wg, n = t.n0 + c, cols = N - n;
                     if (cols > 0) {
                         if (p.out2) {
                             for (int half = 0; half < 2; ++half) {   // g, u
@@ -530,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                         box_put<float, 128>(box, lane, j,
                                                             reinterpret_cast<const float *>(&v[2 * b + j / 4][4 * (j & 3)]));
                                     box_store<float, 128>(
-                                        &map_a2, n + 32 * b, y, half,
+                                        &map.a2, n + 32 * b, y, half,
                                         static_cast<float *>(p.out2) + y * 2 * p.fp + half * p.fp + n + 32 * b, 2 * p.fp, rows,
                                         cols - 32 * b, true, box, lane);
                                 }
@@ -552,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 }
                             }
                         });
-                        box_store<T, 128>(&map_out, n, y, 0, static_cast<T *>(p.g.out) + y * p.g.ldo + n, p.g.ldo, rows, cols,
+                        box_store<T, 128>(&map.out, n, y, 0, static_cast<T *>(p.g.out) + y * p.g.ldo + n, p.g.ldo, rows, cols,
                                           true, box, lane);
                     }
                 } else if (KIND == DPRE) {
@@ -590,8 +601,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                             box_put<T, 64>(ubox + kBox / 2, lane, j, u + 8 * j);
                         }
                         T *out = static_cast<T *>(p.g.out) + y * 2 * p.fp + n;
-                        box_store<T, 64>(&map_out, n, y, 0, out, 2 * p.fp, rows, p.g.N - n, true, ubox, lane);
-                        box_store<T, 64>(&map_out, n, y, 1, out + p.fp, 2 * p.fp, rows, p.g.N - n, true, ubox + kBox / 2, lane);
+                        box_store<T, 64>(&map.out, n, y, 0, out, 2 * p.fp, rows, N - n, true, ubox, lane);
+                        box_store<T, 64>(&map.out, n, y, 1, out + p.fp, 2 * p.fp, rows, N - n, true, ubox + kBox / 2, lane);
                         if (c + 32 < first + columns) {
                             boxes.drain();
                             load_pre(c + 32);
@@ -601,13 +612,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                         break;
                 } else {
                     constexpr int C = kBoxBytes / (int)sizeof(O), V = 16 / (int)sizeof(O);
-                    const int z = KIND == DW ? t.e * p.planes + t.z : 0;
-                    O *out = static_cast<O *>(p.g.out) + ((int64_t)z * p.out_rows + y) * p.g.ldo + t.n0;
+                    const int z = KIND == DW ? t.e * p.dw[t.q].planes + t.z : 0;
+                    const int64_t ldo = KIND == DW ? N : p.g.ldo;
+                    const bool wide = KIND == DW ? p.dw[t.q].wide : p.g.wide_store;
+                    O *out = KIND == DW ? static_cast<O *>(p.dw[t.q].out) + ((int64_t)z * p.dw[t.q].out_rows + y) * ldo + t.n0
+                                        : static_cast<O *>(p.g.out) + y * ldo + t.n0;
                     for (int c = first; c < first + columns; c += 64) {
                         fetch(c, c + 16, c + 32, c + 48);
 #pragma unroll
                         for (int b = 0; b < 64 / C; ++b) {
-                            const int n = c + b * C, cols = p.g.N - t.n0 - n;
+                            const int n = c + b * C, cols = N - t.n0 - n;
                             if (cols <= 0)
                                 break;
                             unsigned char *box = boxes.next();
@@ -617,8 +631,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 box_put<O, 128>(box, lane, j, reinterpret_cast<const float *>(&v[i / 16][i % 16]));
                             }
                             // rows past the plane's last are dropped by a TMA store
-                            box_store<O, 128>(&map_out, t.n0 + n, y, z, out + n, p.g.ldo,
-                                              KIND == DW && p.g.wide_store ? 32 : rows, cols, p.g.wide_store, box, lane);
+                            box_store<O, 128>(&map.out, t.n0 + n, y, z, out + n, ldo, KIND == DW && wide ? 32 : rows, cols,
+                                              wide, box, lane);
                         }
                     }
                 }
@@ -669,8 +683,7 @@ int64_t row_tiles(const FfShape &s, int rows)
 }
 
 template <int CG, int KIND, typename T, typename O>
-cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o, const CUtensorMap &a2,
-                   const CUtensorMap &b2, FfParams p, int64_t tiles)
+cudaError_t launch(esp_moe *m, const FfMaps<KIND> &maps, FfParams p, int64_t tiles)
 {
     constexpr int kSmem = Shape<CG, KIND>::kSmem;
     auto kernel = k_ff<CG, KIND, T, O>;
@@ -702,7 +715,7 @@ cudaError_t launch(esp_moe *m, const CUtensorMap &a, const CUtensorMap &b, const
     cfg.gridDim = dim3((unsigned)(CG * std::max<int64_t>(1, std::min<int64_t>(groups, tiles))));
     p.few_ctas = 2 * (int64_t)cfg.gridDim.x <= m->sm_count;
     m->launches += 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, b, o, a2, b2, p);
+    return cudaLaunchKernelEx(&cfg, kernel, maps, p);
 }
 
 // Which tiles a product takes: pairs of CTAs with 256 x 256, or single ones with 128 x 256 whose inner axis may be split
@@ -739,6 +752,7 @@ template <int KIND, typename T>
 cudaError_t rows_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &o,
                         const CUtensorMap &o2, FfParams &p)
 {
+    const FfMaps<KIND> maps = {{{a, b, o, o2, b}}};
     const int64_t nt = ceil_div(p.g.N, kTileCols<KIND>), pairs = row_tiles(s, 256), ones = row_tiles(s, 128);
     // an expert's last tile is half full in the mean
     const auto expected = [&](int rows) {
@@ -747,39 +761,30 @@ cudaError_t rows_launch(esp_moe *m, const FfShape &s, const CUtensorMap &a, cons
     const Choice c = choose_tiles(m, s.E == 1, expected(256), expected(128), ones * nt, (double)p.blocks * p.halves);
     p.g.most = (int32_t)(c.pair ? pairs : ones);
     p.g.splits = c.splits;
-    return c.pair ? launch<2, KIND, T, T>(m, a, b, o, o2, b, p, pairs * nt)
-                  : launch<1, KIND, T, T>(m, a, b, o, o2, b, p, ones * nt * c.splits);
+    return c.pair ? launch<2, KIND, T, T>(m, maps, p, pairs * nt)
+                  : launch<1, KIND, T, T>(m, maps, p, ones * nt * c.splits);
 }
-
-// Operands of DW: the inner axis is the rows; a2, b2: the tails.
-struct WeightMaps {
-    CUtensorMap a, b, a2, b2;
-};
 
 template <typename T, typename O>
-cudaError_t weights_launch_as(esp_moe *m, const FfShape &s, const WeightMaps &w, const CUtensorMap &o, FfParams &p)
+cudaError_t weights_launch(esp_moe *m, const FfShape &s, FfMaps<DW> &maps, FfParams &p)
 {
-    const int64_t per = (int64_t)s.E * p.planes * ceil_div(p.g.N, 256);
-    const int64_t pairs = per * ceil_div(p.out_rows, 256), ones = per * ceil_div(p.out_rows, 128);
+    int64_t pairs = 0, ones = 0;
+    for (int q = 0; q < p.dws; ++q) {
+        DwOut &d = p.dw[q];
+        d.wide = rows_aligned(d.out, d.N, sizeof(O), 16);
+        maps.of[q].out = maps.of[q].a;   // not used where the output is not aligned
+        if (d.wide)
+            FF_TRY(box_map3(&maps.of[q].out, d.out, sizeof(O), d.N, d.out_rows, d.N, (int64_t)s.E * d.planes,
+                            (int64_t)d.out_rows * d.N, 32));
+        const int64_t per = (int64_t)s.E * d.planes * ceil_div(d.N, 256);
+        pairs += per * ceil_div(d.out_rows, 256);
+        ones += per * ceil_div(d.out_rows, 128);
+    }
+    if (p.dws == 1)
+        maps.of[1] = maps.of[0];
     const Choice c = choose_tiles(m, s.E == 1, (double)pairs, (double)ones, ones, (double)s.M / s.E / kInner);
     p.g.splits = c.splits;
-    return c.pair ? launch<2, DW, T, O>(m, w.a, w.b, o, w.a2, w.b2, p, pairs)
-                  : launch<1, DW, T, O>(m, w.a, w.b, o, w.a2, w.b2, p, ones * c.splits);
-}
-
-cudaError_t weights_launch(esp_moe *m, const FfShape &s, const WeightMaps &w, FfParams &p, void *out, bool f32)
-{
-    const int size = f32 ? 4 : 2;
-    p.g.out = out;
-    p.g.ldo = p.g.N;
-    p.g.wide_store = rows_aligned(out, p.g.N, size, 16);
-    CUtensorMap o = w.a;   // not used where the output is not aligned
-    if (p.g.wide_store)
-        FF_TRY(box_map3(&o, out, size, p.g.N, p.out_rows, p.g.N, (int64_t)s.E * p.planes, (int64_t)p.out_rows * p.g.N, 32));
-    return with_16(s.dtype, [&](auto elem) -> cudaError_t {
-        using T = decltype(elem);
-        return f32 ? weights_launch_as<T, float>(m, s, w, o, p) : weights_launch_as<T, T>(m, s, w, o, p);
-    });
+    return c.pair ? launch<2, DW, T, O>(m, maps, p, pairs) : launch<1, DW, T, O>(m, maps, p, ones * c.splits);
 }
 
 // ---- tails
@@ -907,46 +912,40 @@ cudaError_t launch_tails(esp_moe *m, const TailArgs &a, int32_t E)
     return launch_after(k_tails, dim3((unsigned)(E * (kInner / kTailRows)), (unsigned)a.parts), 32 * kTailRows, 0, m->stream, a);
 }
 
-cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx,
-                             const void *dpre_tails, const void *x_tails, void *dinner, bool f32)
+cudaError_t launch_ff_weights(esp_moe *m, const FfShape &s, const FfWeightArgs &a)
 {
     FfParams p = common(m, s);
-    p.g.N = s.H;
-    p.planes = 2;
-    p.out_rows = s.F;
+    FfMaps<DW> maps;
     const int64_t tails = (int64_t)s.E * kInner;
-    WeightMaps w;
-    FF_TRY(box_map3(&w.a, dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kInner));
-    FF_TRY(box_map3(&w.b, x, 2, s.H, s.M, ldx, 1, 0, kInner));
-    w.a2 = w.a;
-    w.b2 = w.b;
-    if (dpre_tails) {
-        FF_TRY(box_map3(&w.a2, dpre_tails, 2, s.F, tails, 2 * s.fp, 2, s.fp, kInner));
-        FF_TRY(box_map3(&w.b2, x_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
+    p.tails = a.tails;
+    if (a.dinner) {   // dpre^T x
+        OneMaps &w = maps.of[p.dws];
+        p.dw[p.dws++] = DwOut{2, s.F, s.H, false, a.dinner};
+        FF_TRY(box_map3(&w.a, a.dpre, 2, s.F, s.M, 2 * s.fp, 2, s.fp, kInner));
+        FF_TRY(box_map3(&w.b, a.x, 2, s.H, s.M, a.ldx, 1, 0, kInner));
+        w.a2 = w.a;
+        w.b2 = w.b;
+        if (a.tails) {
+            FF_TRY(box_map3(&w.a2, a.dpre_tails, 2, s.F, tails, 2 * s.fp, 2, s.fp, kInner));
+            FF_TRY(box_map3(&w.b2, a.x_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
+        }
     }
-    p.tails = dpre_tails != nullptr;
-    return weights_launch(m, s, w, p, dinner, f32);
-}
-
-cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden,
-                             const void *dy_tails, const void *hidden_tails, void *douter, bool f32)
-{
-    FfParams p = common(m, s);
-    p.g.N = s.F;
-    p.planes = 1;
-    p.out_rows = s.H;
-    const int64_t tails = (int64_t)s.E * kInner;
-    WeightMaps w;
-    FF_TRY(box_map3(&w.a, dy, 2, s.H, s.M, lddy, 1, 0, kInner));
-    FF_TRY(box_map3(&w.b, hidden, 2, s.F, s.M, s.fp, 1, 0, kInner));
-    w.a2 = w.a;
-    w.b2 = w.b;
-    if (dy_tails) {
-        FF_TRY(box_map3(&w.a2, dy_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
-        FF_TRY(box_map3(&w.b2, hidden_tails, 2, s.F, tails, s.fp, 1, 0, kInner));
+    if (a.douter) {   // dy^T hidden
+        OneMaps &w = maps.of[p.dws];
+        p.dw[p.dws++] = DwOut{1, s.H, s.F, false, a.douter};
+        FF_TRY(box_map3(&w.a, a.dy, 2, s.H, s.M, a.lddy, 1, 0, kInner));
+        FF_TRY(box_map3(&w.b, a.hidden, 2, s.F, s.M, s.fp, 1, 0, kInner));
+        w.a2 = w.a;
+        w.b2 = w.b;
+        if (a.tails) {
+            FF_TRY(box_map3(&w.a2, a.dy_tails, 2, s.H, tails, s.hp, 1, 0, kInner));
+            FF_TRY(box_map3(&w.b2, a.hidden_tails, 2, s.F, tails, s.fp, 1, 0, kInner));
+        }
     }
-    p.tails = dy_tails != nullptr;
-    return weights_launch(m, s, w, p, douter, f32);
+    return with_16(s.dtype, [&](auto elem) -> cudaError_t {
+        using T = decltype(elem);
+        return a.f32 ? weights_launch<T, float>(m, s, maps, p) : weights_launch<T, T>(m, s, maps, p);
+    });
 }
 
 }  // namespace esp_moe_impl

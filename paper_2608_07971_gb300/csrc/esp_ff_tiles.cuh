@@ -17,11 +17,18 @@ enum Kind { HIDDEN, OUT, DPRE, DX, DW };
 
 constexpr int kHalfTile = 64 * 128;   // MN-major: 64 inner indices of 64 outer elements
 
+// DW: one of a launch's weight gradients, E x planes matrices of out_rows x N.
+struct DwOut {
+    int32_t planes, out_rows, N;
+    bool wide;                // rows on 16 bytes
+    void *out;
+};
+
 struct FfParams {
     GemmParams g;             // rows, experts, N (columns of the output), waits
     int32_t blocks, halves;   // blocks of the inner axis in a half, halves (DX: G and U)
-    int32_t planes;           // DW: outputs of an expert (G and U, or O), each of out_rows x N
-    int32_t out_rows;
+    DwOut dw[2];              // DW (the second one of a launch with one: zeros)
+    int32_t dws;              // how many
     bool tails;               // DW: a block that an expert's rows do not fill is read from the tails
     int32_t act;
     bool few_ctas;            // most SMs are free
@@ -32,9 +39,9 @@ struct FfParams {
 };
 
 // One item of the list: blocks k0 .. k1 - 1 of the inner axis of a tile. Row kinds: rows m0 .. m0 + rows - 1 of expert e,
-// columns n0 ..; DW: output rows m0 .. of plane z, over the rows lo .. hi - 1, the last block from the tails where `cut` is set.
+// columns n0 ..; DW: output rows m0 .. of plane z of gradient q, over the rows lo .. hi - 1, the last block from the tails where `cut` is set.
 struct FfTile {
-    int item, e, m0, rows, n0, k0, k1, z, lo, hi;
+    int item, e, m0, rows, n0, k0, k1, q, z, lo, hi;
     bool cut;
 };
 
@@ -91,18 +98,23 @@ private:
             t.k1 = p.blocks * p.halves;
             return true;
         }
-        const int mt = (p.out_rows + kRows - 1) / kRows, nt = (p.g.N + 255) / 256, per = mt * nt * p.planes;
-        if (item >= per * p.g.E)
+        // an expert's tiles of both gradients together
+        const int mt0 = (p.dw[0].out_rows + kRows - 1) / kRows, per0 = mt0 * ((p.dw[0].N + 255) / 256) * p.dw[0].planes;
+        const int mt1 = (p.dw[1].out_rows + kRows - 1) / kRows, per1 = mt1 * ((p.dw[1].N + 255) / 256) * p.dw[1].planes;
+        if (item >= (per0 + per1) * p.g.E)
             return false;
-        t.e = item / per;
-        int i = item - t.e * per;
+        t.e = item / (per0 + per1);
+        int i = item - t.e * (per0 + per1);
         if (order)
             t.e = order[t.e];
-        t.z = i / (mt * nt);
-        i -= t.z * (mt * nt);
-        t.m0 = (i % mt) * kRows;
-        t.n0 = (i / mt) * 256;
-        t.rows = std::min(kRows, p.out_rows - t.m0);
+        t.q = i >= per0;
+        i -= t.q ? per0 : 0;
+        const int m = t.q ? mt1 : mt0, plane = t.q ? per1 / p.dw[1].planes : per0 / p.dw[0].planes;
+        t.z = i / plane;
+        i -= t.z * plane;
+        t.m0 = (i % m) * kRows;
+        t.n0 = (i / m) * 256;
+        t.rows = std::min(kRows, (t.q ? p.dw[1].out_rows : p.dw[0].out_rows) - t.m0);
         expert_rows(p.g, t.e, t.lo, t.hi);
         const bool part = (t.hi - t.lo) % kInner != 0;   // without tails, what follows the last row is outside: zeros
         t.cut = part && p.tails;

@@ -246,10 +246,9 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
         }
         MOE_CUDA(launch_tails(m, a, w->E));
     }
-    if (dinner)
-        MOE_CUDA(launch_ff_dinner(m, s, dpre, rows_x, ld_rows, dpre_tails, x_tails, dinner, f32));
-    if (douter)
-        MOE_CUDA(launch_ff_douter(m, s, dy, lddy, kept->hidden, dy_tails, hidden_tails, douter, f32));
+    if (dinner || douter)
+        MOE_CUDA(launch_ff_weights(m, s, FfWeightArgs{dpre, rows_x, dy, kept->hidden, ld_rows, lddy, dpre_tails, x_tails, dy_tails,
+                                                      hidden_tails, offsets != nullptr, f32, dinner, douter}));
     return ESP_OK;
 }
 

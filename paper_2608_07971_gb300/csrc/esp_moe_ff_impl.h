@@ -61,11 +61,15 @@ struct TailArgs {
     const int32_t *offsets;
 };
 cudaError_t launch_tails(esp_moe *m, const TailArgs &a, int32_t E);
-// dinner (E x 2 F x H) = dpre^T x, douter (E x H x F) = dy^T hidden, in 32 bits or the rows' type. Tails: NULL where rows
-// end with M.
-cudaError_t launch_ff_dinner(esp_moe *m, const FfShape &s, const void *dpre, const void *x, int64_t ldx,
-                             const void *dpre_tails, const void *x_tails, void *dinner, bool f32);
-cudaError_t launch_ff_douter(esp_moe *m, const FfShape &s, const void *dy, int64_t lddy, const void *hidden,
-                             const void *dy_tails, const void *hidden_tails, void *douter, bool f32);
+// dinner (E x 2 F x H) = dpre^T x and douter (E x H x F) = dy^T hidden, either NULL, in one launch; in 32 bits or the rows'
+// type. Without tails rows end with M.
+struct FfWeightArgs {
+    const void *dpre, *x, *dy, *hidden;
+    int64_t ldx, lddy;
+    const void *dpre_tails, *x_tails, *dy_tails, *hidden_tails;
+    bool tails, f32;
+    void *dinner, *douter;
+};
+cudaError_t launch_ff_weights(esp_moe *m, const FfShape &s, const FfWeightArgs &a);
 
 }  // namespace esp_moe_impl

@@ -20,7 +20,7 @@ int pick(int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng
 
 [[noreturn]] void fault(const char *what, const FfParams &p)
 {
-    printf("%s: M %d E %d N %d out_rows %d splits %d\n", what, p.g.M, p.g.E, p.g.N, p.out_rows, p.g.splits);
+    printf("%s: M %d E %d N %d gradients %d splits %d\n", what, p.g.M, p.g.E, p.g.N, p.dws, p.g.splits);
     std::exit(1);
 }
 
@@ -74,30 +74,39 @@ void weights(bool ascending)
 {
     std::vector<int32_t> off;
     FfParams p = some(off, ascending, CG == 1 ? pick(1, 4) : 1);
-    p.planes = pick(1, 2);
-    p.out_rows = pick(1, 700);
+    p.dws = pick(1, 2);
+    for (int q = 0; q < p.dws; ++q)
+        p.dw[q] = DwOut{pick(1, 2), pick(1, 700), pick(1, 900), false, nullptr};
     p.tails = pick(0, 1);
     std::vector<uint16_t> order(p.g.E);
     for (int e = 0; e < p.g.E; ++e)
         order[e] = (uint16_t)e;
     std::shuffle(order.begin(), order.end(), rng);
     const bool ordered = pick(0, 1);
-    const int ctas = pick(1, 160), nt = (p.g.N + 255) / 256;
-    std::vector<int> seen((size_t)p.g.E * p.planes * p.out_rows * nt, 0);
+    const int ctas = pick(1, 160);
+    int nt[2] = {};
+    std::vector<int> seen[2];
+    for (int q = 0; q < p.dws; ++q) {
+        nt[q] = (p.dw[q].N + 255) / 256;
+        seen[q].assign((size_t)p.g.E * p.dw[q].planes * p.dw[q].out_rows * nt[q], 0);
+    }
     for (int me = 0; me < ctas; ++me) {
         Walk<CG, DW> walk;
         if (ordered)
             walk.order = order.data();
         for (FfTile t; walk.next(p, me, ctas, t);) {
-            if (t.e < 0 || t.e >= p.g.E || t.z < 0 || t.z >= p.planes || t.m0 < 0 || t.rows < 1 || t.rows > 128 * CG ||
-                t.m0 + t.rows > p.out_rows || t.n0 < 0 || t.n0 >= p.g.N || t.n0 % 256 || t.k0 < 0 || t.k1 < t.k0 ||
+            if (t.q < 0 || t.q >= p.dws)
+                fault("item of no gradient", p);
+            const DwOut &d = p.dw[t.q];
+            if (t.e < 0 || t.e >= p.g.E || t.z < 0 || t.z >= d.planes || t.m0 < 0 || t.rows < 1 || t.rows > 128 * CG ||
+                t.m0 + t.rows > d.out_rows || t.n0 < 0 || t.n0 >= d.N || t.n0 % 256 || t.k0 < 0 || t.k1 < t.k0 ||
                 t.lo < 0 || t.hi < t.lo || t.hi > p.g.M || t.k1 > (t.hi - t.lo + kInner - 1) / kInner)
                 fault("item out of range", p);
             const int last = (t.hi - t.lo + kInner - 1) / kInner;
             if (t.cut != (p.tails && (t.hi - t.lo) % kInner != 0 && t.k1 == last && t.k0 < t.k1))
                 fault("the block that is not full", p);
             for (int i = 0; i < t.rows; ++i)   // an expert without rows has its output all the same
-                seen[(((size_t)t.e * p.planes + t.z) * p.out_rows + t.m0 + i) * nt + t.n0 / 256] +=
+                seen[t.q][(((size_t)t.e * d.planes + t.z) * d.out_rows + t.m0 + i) * nt[t.q] + t.n0 / 256] +=
                     last ? t.k1 - t.k0 : (t.item % p.g.splits == 0);
         }
     }
@@ -105,9 +114,12 @@ void weights(bool ascending)
         int lo, hi;
         expert_rows(p.g, e, lo, hi);
         const int want = std::max(1, (hi - lo + kInner - 1) / kInner);
-        for (int i = 0; i < p.planes * p.out_rows * nt; ++i)
-            if (seen[(size_t)e * p.planes * p.out_rows * nt + i] != want)
-                fault("an output not covered once", p);
+        for (int q = 0; q < p.dws; ++q) {
+            const int n = p.dw[q].planes * p.dw[q].out_rows * nt[q];
+            for (int i = 0; i < n; ++i)
+                if (seen[q][(size_t)e * n + i] != want)
+                    fault("an output not covered once", p);
+        }
     }
 }
 
