@@ -135,7 +135,7 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
         return st;
     const bool copied = rows || !mappable(x, ldx);
     if (!good_rows(w, T, ldx, x, M, rows, offsets) || ldy < w->H || ldy >= (int64_t)1 << 39 || (M > 0 && !y) ||
-        !aligned_to(y, 2) || (kept && M > 0 && !good_kept(kept, copied)))
+        !aligned_to(y, 2) || (kept && M > 0 && (!good_kept(kept, copied) || (!copied && y == x))))
         return ESP_ERR_INVALID_ARG;
     if (kept)
         kept->copied = copied;
@@ -187,6 +187,8 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
         (dw_dtype != w->dtype && dw_dtype != ESP_MOE_F32))
         return ESP_ERR_INVALID_ARG;
     const bool f32 = dw_dtype == ESP_MOE_F32;
+    if (M > 0 && dx && (dx == dy || (!copied && dx == x)))   // read after dx is written
+        return ESP_ERR_INVALID_ARG;
     if (!aligned_to(dinner, f32 ? 4 : 2) || !aligned_to(douter, f32 ? 4 : 2))
         return ESP_ERR_INVALID_ARG;
     if (M == 0) {

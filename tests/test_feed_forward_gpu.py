@@ -574,9 +574,12 @@ def test_refusals(mm):
     for f in bad:
         with pytest.raises(ValueError):
             f()
-    # gathered rows, but kept from a pass over rows in place; rows that overlap one another
+    # gathered rows, but kept from a pass over rows in place; rows that overlap one another; results in place of what is read
     for f in (lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, rows=torch.zeros(4, dtype=torch.int32, device="cuda")),
-              lambda: mm.feed_forward(x[:1].expand(4, 32), w, offsets=off)):
+              lambda: mm.feed_forward(x[:1].expand(4, 32), w, offsets=off),
+              lambda: mm.feed_forward(x, w, offsets=off, keep=kept, out=x),
+              lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, out=(y, None, None)),
+              lambda: mm.feed_forward_backward(y, x, w, kept, offsets=off, out=(x, None, None))):
         with pytest.raises(esp.EspError) as err:
             f()
         assert err.value.status == esp.ESP_ERR_INVALID_ARG
