@@ -36,6 +36,11 @@ struct FfParams {
     const void *pre;          // DPRE
     int64_t fp;
     void *out2;               // HIDDEN: pre (or null)
+    // HIDDEN with pre and a kinked activation: the operands, and below which part of the larger values around it a g is
+    // summed again (0: none is)
+    const void *x, *inner;
+    int64_t ldx, ld_inner;
+    float near_zero;
 };
 
 // One item of the list: blocks k0 .. k1 - 1 of the inner axis of a tile. Row kinds: rows m0 .. m0 + rows - 1 of expert e,

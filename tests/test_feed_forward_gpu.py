@@ -187,6 +187,30 @@ def test_activations(mm, kind, dt):
     check(mm, [90, 40], 200, 144, dt, kind, True, 3, seed=5)
 
 
+@pytest.mark.parametrize("sizes,H,F,dt,gathered", [
+    ([2500], 8192, 1000, "bf16", False), ([300], 1071, 454, "f16", True), ([40], 8200, 130, "bf16", False),
+    ([3, 0, 70, 1, 200], 2100, 200, "bf16", True), ([20, 30], 1071, 5, "f16", False)])
+def test_signs_of_gates_near_zero(mm, sizes, H, F, dt, gathered):
+    # relu's slope is 0 or 1: what is kept for it near 0 has to be right relative to itself. The terms a b are exact in 32
+    # bits, the sum of n of them is off by at most u of itself and n 2 u^2 sum |a b|, and is rounded once.
+    E, M = len(sizes), sum(sizes)
+    x, inner = rand(M, H, dt=dt, seed=31), rand(E, 2 * F, H, dt=dt, seed=32, size=H ** -0.5)
+    w = mm.gated_weight(inner, rand(E, H, F, dt=dt, seed=33, size=F ** -0.5), "relu")
+    offsets = torch.tensor([0, *np.cumsum(sizes)], dtype=torch.int32, device="cuda")
+    rows = torch.arange(M - 1, -1, -1, dtype=torch.int32, device="cuda") if gathered else None
+    kept = mm.keep(M, w)
+    mm.feed_forward(x, w, offsets=offsets, rows=rows, keep=kept)
+    a = 0
+    for e, n in enumerate(sizes):
+        xe = (x.flip(0) if gathered else x)[a:a + n].double()
+        g = xe @ inner[e, :F].double().t()
+        got = kept.pre[a:a + n, 0, :F].double()
+        lim = 2 * U * g.abs() + 2 * H * U * U * (xe.abs() @ inner[e, :F].double().abs().t())
+        near = g.abs() < H * 2.0 ** -27   # of values around 1
+        assert ((got - g).abs() <= lim)[near].all()
+        a += n
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 def test_weight_gradients_in_32_bits(mm, dt):
     check(mm, [70, 0, 333], 136, 100, dt, "silu", True, 0, dw_dtype=torch.float32)
