@@ -928,11 +928,11 @@ cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_
     p.g.ldo = s.fp;
     p.out2 = pre;
     if (pre && s.act == ESP_MOE_RELU) {
-        // The tensor core cuts off what it adds below its accumulator's last bit: of 8192 products of unit sum a g is off by
-        // 9e-6 (rms; up to 6e-5), ten times an ordinary 32-bit sum, and the sign of one in half a million is wrong, which takes
-        // a whole gradient away or adds one. The error grows with the steps of 16: the largest g of a wrong sign was 0.7 to 1.3
-        // of H 2^-30 (H 1071 to 8192), the bound is about ten times that.
-        // 8192 rows x 2048 x 2048 with g and u kept: 140 us (silu 136); 4416 x 8192 x 1024: 155 (138).
+        // The tensor core cuts off what it adds below its accumulator's last bit: of 8192 products whose sum is around 1 a g is
+        // off by 9e-6 (rms; up to 6e-5), ten times an ordinary 32-bit sum, and the sign of one in half a million is wrong,
+        // which takes a whole gradient away or adds one. The error grows with the steps of 16: the largest g of a wrong sign
+        // was 0.7 to 1.2 of H 2^-30 (H 1071 to 8192), the bound is about ten times that. 8192 rows x 2048 x 2048 with g and u
+        // kept: 140 us (silu 136); 4416 x 8192 x 1024: 155 (138).
         p.x = x;
         p.ldx = ldx;
         p.inner = s.inner;
