@@ -4,9 +4,11 @@
 //
 // A CTA takes a few weight rows at a time (HIDDEN: the same ones of G and of U), each thread some 16-byte groups of all of
 // them and the same groups of x in registers; the next rows are on their way while these are multiplied, and a sum over
-// the CTA ends each. Four CTAs of an SM and four groups of a thread: one token of 4096 x 8192 takes 39.3 us (201 MB; 43.8
-// with two CTAs and eight groups; 41.5 with warps that take rows of their own, x from L1), 1024 x 4096 10.3 us. Items go
-// round over the CTAs, so that every SM streams the same bytes.
+// the CTA ends each. Items go round over the CTAs, so that every SM streams the same bytes. Four CTAs of an SM and four
+// groups of a thread: two CTAs and eight groups took 11% longer, warps that take rows of their own, x from L1, 6%.
+// Registers hold the loads of one item ahead; the rows of the item after that are on their way to L2. One token of 4096 x
+// 8192 (201 MB) takes 34.9 us in a graph, 41.0 without this; 2, 4 and 8 rows of 2048 x 4096 14.7, 20.5 and 32 (15.9, 21.8 and
+// 32). One item further ahead: 34.9, 15.4, 20.9.
 
 #include <algorithm>
 
@@ -40,6 +42,13 @@ __device__ __forceinline__ uint4 load_stream(const void *p)
                  : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
                  : "l"(p));
     return r;
+}
+
+// Asks L2 for a row of K elements (what does not fill its last 16 bytes comes with the load).
+__device__ __forceinline__ void prefetch_row(const uint16_t *row, int K)
+{
+    if (K >= 8)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"((uint32_t)(K & ~7) * 2) : "memory");
 }
 
 // Elements 8 g .. 8 g + 7 of a row of K; those past its end are 0 and not read.
@@ -103,12 +112,16 @@ __global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p
     }
     const int groups = (p.K + 7) / 8, segs = (groups + kThreads * J - 1) / (kThreads * J);
     const int items = (p.N + NF - 1) / NF;
-    // the groups of item `item`'s rows in step `seg`; rows past the last are its copies
+    // weight row f of an item; rows past the last are its copies
+    const auto weight_row = [&](int item, int f) {
+        const int64_t n = (KIND == HIDDEN && f >= NF ? p.N : 0) + min(item * NF + f % NF, p.N - 1);
+        return static_cast<const uint16_t *>(p.w) + n * p.ldw;
+    };
+    // the groups of an item's rows in step `seg`
     const auto load = [&](uint4 (&to)[W][J], int item, int seg) {
 #pragma unroll
         for (int f = 0; f < W; ++f) {
-            const int64_t n = (KIND == HIDDEN && f >= NF ? p.N : 0) + min(item * NF + f % NF, p.N - 1);
-            const uint16_t *w = static_cast<const uint16_t *>(p.w) + n * p.ldw;
+            const uint16_t *w = weight_row(item, f);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int g = (seg * J + j) * kThreads + threadIdx.x;
@@ -116,10 +129,16 @@ __global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p
             }
         }
     };
+    // registers hold the loads of one item ahead; the item after it is on its way to L2
+    const auto prefetch = [&](int64_t item) {
+        if (threadIdx.x < W && item < items)
+            prefetch_row(weight_row((int)item, threadIdx.x), p.K);
+    };
     uint4 now[W][J], next[W][J], x[R][J];
     int item = blockIdx.x, seg = 0;
     if (item < items)
         load(now, item, 0);
+    prefetch((int64_t)item + gridDim.x);
     if (p.early) {
         // the first weights are on their way; what the launch before writes (the rows) comes after this
         wait_for_launch_before();
@@ -146,6 +165,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<R>) k_ff_vec(const VecParams p
         const int item1 = seg + 1 < segs ? item : item + (int)gridDim.x, seg1 = seg + 1 < segs ? seg + 1 : 0;
         if (item1 < items)
             load(next, item1, seg1);
+        if (seg == 0)
+            prefetch((int64_t)item + 2 * gridDim.x);
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -246,13 +267,15 @@ cudaError_t by_rows(esp_moe *m, int32_t dtype, const VecParams &p)
 
 bool use_vec(int64_t M, int32_t E, int32_t F, int32_t H)
 {
-    // Times of both products (us), here and on the tensor cores, whose kernels take 20 before the weights' bytes count:
-    //   rows  512 x 512  1024 x 2048  2048 x 4096  4096 x 8192 (201 MB)
-    //   1, 2  7.8  13.6    8.0  23.6   13 to 16  33   40 to 48  58
-    //   4     7.2  13.5   11.0  23.5       22  33       69  62
-    //   8     7.5  13.6   17.4  23.5       38  33      185  58
+    // Times of both products in a graph, weights not in L2 (us), here and on the tensor cores, whose kernels take 12 before the
+    // weights' bytes count:
+    //   rows  512 x 512  1024 x 2048  2048 x 2048  2048 x 4096  4096 x 4096  4096 x 8192  8192 x 8192  6144 x 16384 (604 MB)
+    //   1     3.3  13.4    6.1  22.4    7.6  27.3   12.2  32.0   19.1  48     34.9  67      72  95      121  127
+    //   2     3.4  13.4    7.3  22.4    8.9  27.3   14.7  32.0   23.1  48     45.2  67      94  95      170  127
+    //   4     5.1  13.4   10.0  22.4   12.5  27.3   20.5  32.0   34.3  48     65.7  67     152  95      295  127
+    //   8     6.9  13.4   16.0  22.4   20.2  27.3   34.7  32.0   76.8  48      179  67     335  95      498  127
     const int64_t bytes = 6 * (int64_t)F * H;
-    return E == 1 && (M <= 2 || (M <= 4 && bytes <= 96 << 20) || (M <= 8 && bytes <= 20 << 20));
+    return E == 1 && (M == 1 || (M == 2 && bytes <= 384 << 20) || (M <= 4 && bytes <= 160 << 20) || (M <= 8 && bytes <= 32 << 20));
 }
 
 cudaError_t launch_vec(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, int64_t T, const int32_t *rows, void *hidden,
