@@ -91,13 +91,35 @@ __device__ __forceinline__ float logistic(float g)
     return __fdividef(1.0f, 1.0f + __expf(-g));
 }
 
+// The normal distribution's c = (1 + erf(g / sqrt 2)) / 2, and e = exp(-g^2 / 2), which its slope needs too. With x = |g| / sqrt 2
+// and t = 1 / (1 + 0.42 x): erfc(x) = t Q(t) exp(-x^2), Q of degree 7 fitted to the least relative error over x < 6.5 (4e-8; with
+// the arithmetic 1.2e-6 down to g = -6 and 2e-7 absolute). As fast as
+// the library's erff next to __expf (hidden rows), whose code is longer.
+__device__ __forceinline__ float normal(float g, float &e)
+{
+    const float t = __fdividef(1.0f, 1.0f + 0.29698485f * fabsf(g));
+    e = __expf(-0.5f * g * g);
+    float q = 0.0380021187f;
+    q = fmaf(q, t, -0.172525816f);
+    q = fmaf(q, t, 0.242480139f);
+    q = fmaf(q, t, -0.0865336997f);
+    q = fmaf(q, t, 0.146210648f);
+    q = fmaf(q, t, 0.093552403f);
+    q = fmaf(q, t, 0.120448583f);
+    q = fmaf(q, t, 0.118365633f);
+    q *= t * e;
+    return g > 0.0f ? 1.0f - q : q;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_of(float g)
 {
     if (ACT == ESP_MOE_SILU)
         return g * logistic(g);
-    if (ACT == ESP_MOE_GELU)
-        return 0.5f * g * (1.0f + erff(g * 0.70710678f));
+    if (ACT == ESP_MOE_GELU) {
+        float e;
+        return g * normal(g, e);
+    }
     if (ACT == ESP_MOE_GELU_TANH)   // (1 + tanh t) / 2 = logistic(2 t)
         return g * logistic(1.59576912f * (g + 0.044715f * g * g * g));
     return fmaxf(g, 0.0f);
@@ -111,9 +133,10 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &d)
         a = g * s;
         d = s * (1.0f + g * (1.0f - s));
     } else if (ACT == ESP_MOE_GELU) {
-        const float c = 0.5f * (1.0f + erff(g * 0.70710678f));
+        float e;
+        const float c = normal(g, e);
         a = g * c;
-        d = c + g * 0.39894228f * __expf(-0.5f * g * g);
+        d = c + g * 0.39894228f * e;
     } else if (ACT == ESP_MOE_GELU_TANH) {
         const float s = logistic(1.59576912f * (g + 0.044715f * g * g * g));
         a = g * s;
