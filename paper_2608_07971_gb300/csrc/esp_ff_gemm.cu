@@ -634,6 +634,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                         }
                         unsigned char *box = boxes.next();
+                        // A loop, as is the one above: where there is one round of tiles this runs once, from a cold
+                        // instruction cache (1801 rows of 5 experts, 2050 x 999, gelu: both products 50 us, unrolled 56).
                         with_act(p.act, [&](auto kind) {
 #pragma unroll 1
                             for (int h = 0; h < 2; ++h) {

@@ -187,6 +187,29 @@ def test_activations(mm, kind, dt):
     check(mm, [90, 40], 200, 144, dt, kind, True, 3, seed=5)
 
 
+@pytest.mark.parametrize("M", [1, 64])
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_gelu_of_exact_gates(mm, M, dt):
+    # x = (1, 0, ...), u = 1: hidden is gelu(g), g exact. c = (1 + erf) / 2 is q or 1 - q, q a fit to 4e-8 = 0.7 u times an
+    # exponential (2 ulp = 4 u and |argument| u twice, argument g^2 / 2), a quotient (4 u), eight steps of Horner's rule whose terms
+    # are below three times the sum (24 u) and two products (2 u): q (36 + g^2) u, and u for 1 - q and for g c.
+    r, tiny = UNIT[dt]
+    F, H = 4096, 64
+    g = torch.linspace(-9, 9, F, device="cuda").to(DT[dt])
+    x, inner = torch.zeros(M, H, device="cuda", dtype=DT[dt]), torch.zeros(1, 2 * F, H, device="cuda", dtype=DT[dt])
+    x[:, 0], inner[0, :F, 0], inner[0, F:, 0] = 1, g, 1
+    w = mm.gated_weight(inner, torch.zeros(1, H, F, device="cuda", dtype=DT[dt]), "gelu")
+    kept = mm.keep(M, w)
+    mm.feed_forward(x, w, keep=kept)
+    g = g.double()
+    q = 0.5 * torch.erfc(g.abs() / math.sqrt(2))
+    want = g * torch.where(g > 0, 1 - q, q)
+    lim = g.abs() * q * (36 + g * g) * U + 2 * U * want.abs()
+    lim = lim + r * (want.abs() + lim) + tiny
+    assert torch.equal(kept.pre[:, 0, :F].double(), g.expand(M, F))
+    assert ((kept.hidden[:, :F].double() - want).abs() <= lim).all()
+
+
 @pytest.mark.parametrize("sizes,H,F,dt,gathered", [
     ([2500], 8192, 1000, "bf16", False), ([300], 1071, 454, "f16", True), ([40], 8200, 130, "bf16", False),
     ([3, 0, 70, 1, 200], 2100, 200, "bf16", True), ([20, 30], 1071, 5, "f16", False)])
