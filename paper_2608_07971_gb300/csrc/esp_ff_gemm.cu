@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     Walk<CG, KIND> walk;
     if (KIND == DW && p.g.E > 1 && p.g.E <= kOrdered) {
         // longest inner axes first, so that the list ends with short items (dinner and douter of 16384 rows over 16 uneven experts,
-        // 4096 x 2048: 328 and 170 us; in the experts' own order 345 and 178)
+        // 4096 x 2048: a launch each 328 and 170 us; in the experts' own order 345 and 178)
         int *blocks = reinterpret_cast<int *>(sm);   // nothing is loaded yet
         for (int e = threadIdx.x; e < p.g.E; e += kThreads) {
             int lo, hi;
