@@ -122,7 +122,7 @@ __device__ __forceinline__ float act_of(float g)
     }
     if (ACT == ESP_MOE_GELU_TANH)   // (1 + tanh t) / 2 = logistic(2 t)
         return g * logistic(1.59576912f * (g + 0.044715f * g * g * g));
-    return fmaxf(g, 0.0f);
+    return g < 0.0f ? 0.0f : g;   // a maximum with 0 would drop NaN
 }
 
 template <int ACT>
@@ -142,8 +142,8 @@ __device__ __forceinline__ void act_and_slope(float g, float &a, float &d)
         a = g * s;
         d = s + a * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * g * g);
     } else {
-        a = fmaxf(g, 0.0f);
-        d = g > 0.0f ? 1.0f : 0.0f;
+        a = g < 0.0f ? 0.0f : g;
+        d = g > 0.0f ? 1.0f : g <= 0.0f ? 0.0f : g;
     }
 }
 

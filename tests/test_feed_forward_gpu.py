@@ -678,3 +678,35 @@ def test_a_layer_as_it_is_used(mm):
         want = b.double() * (0.5 / n)
         unit = 2.0 ** -8 if g.dtype is torch.bfloat16 else U
         assert ((g.double() - want).abs() <= (unit + 1e-6) * want.abs() + 2.0 ** -134).all()
+
+
+@pytest.mark.parametrize("sizes", [[1], [8], [9], [40, 70, 3]])   # on the CUDA cores, on the tensor cores
+@pytest.mark.parametrize("kind", ACTS)
+def test_nan_of_a_gate_reaches_the_results(mm, sizes, kind):
+    """NaN in one weight of G alone, as of a step that went wrong: every sum that takes its g in is NaN, and the norm of the
+    gradients; the others are what they are without it."""
+    E, M, H, F, e, f = len(sizes), sum(sizes), 72, 40, len(sizes) // 2, 7
+    x, dy = rand(M, H, dt="bf16", seed=51), rand(M, H, dt="bf16", seed=52)
+    inner, outer = rand(E, 2 * F, H, dt="bf16", seed=53, size=H ** -0.5), rand(E, H, F, dt="bf16", seed=54, size=F ** -0.5)
+    offsets = torch.tensor([0, *np.cumsum(sizes)], dtype=torch.int32, device="cuda")
+    own = torch.zeros(M, dtype=torch.bool, device="cuda")
+    own[int(offsets[e]):int(offsets[e + 1])] = True
+    got = []
+    for v in (0.5, math.nan):
+        inner[e, f, 3] = v
+        w, kept = mm.gated_weight(inner, outer, kind), mm.keep(M, mm.gated_weight(inner, outer, kind))
+        y = mm.feed_forward(x, w, offsets=offsets, keep=kept)
+        bare = mm.feed_forward(x, w, offsets=offsets)
+        assert torch.equal(bare.nan_to_num(nan=7.0), y.nan_to_num(nan=7.0))
+        got.append((y, *mm.feed_forward_backward(dy, x, w, kept, offsets=offsets)))
+    plain, bad = got
+    for a, b in zip(plain[:2], bad[:2]):   # y, dx: the rows of this expert
+        assert a.isfinite().all() and b[own].isnan().all() and torch.equal(a[~own], b[~own])
+    here = torch.zeros(E, 2 * F, dtype=torch.bool, device="cuda")
+    here[e, [f, F + f]] = True   # the gradients of G x and of U x
+    assert plain[2].isfinite().all() and bad[2][here].isnan().all() and torch.equal(plain[2][~here], bad[2][~here])
+    a, b = (v[3].transpose(1, 2) for v in (plain, bad))
+    here[e, F + f] = False
+    assert a.isfinite().all() and b[here[:, :F]].isnan().all() and torch.equal(a[~here[:, :F]], b[~here[:, :F]])
+    for i in (2, 3):
+        assert math.isnan(float(mm.clip([bad[i].clone()], 1.0))) and math.isfinite(float(mm.clip([plain[i].clone()], 1.0)))
