@@ -189,7 +189,7 @@ class Weight:
         if not codes(q, N, K) or (qt is not None and not codes(qt, K, N)) or scale.dtype is not torch.float32 or \
                 scale.shape != (E, -(-N // BLOCK), -(-K // BLOCK)) or not scale.is_contiguous():
             raise ValueError("8-bit weights: contiguous uint8 codes (E, N, >= K), fp32 scales (E, N / 128, K / 128)")
-        self._c = _CWeight(E, N, K, q.shape[2], qt.shape[2] if qt is not None else 0, *self._places())
+        self._c = _CWeight(E, N, K, q.shape[2], qt.shape[2] if qt is not None else 0, q.data_ptr(), _ptr(qt), scale.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._made_at = self._places()
 
@@ -201,10 +201,11 @@ class Weight:
             self._ref = None   # checked and made anew by the next call
 
     def _places(self):
-        return self.q.data_ptr(), _ptr(self.qt), self.scale.data_ptr()
+        return _place(self.q), None if self.qt is None else _place(self.qt), _place(self.scale)
 
     def _arg(self):
-        """The C argument for the fields as they are, whether assigned since or their memory moved (``.data``)."""
+        """The C argument for the fields as they are, whether assigned since or given other memory, another shape or type
+        in place (``.data``)."""
         if self._ref is None or self._places() != self._made_at:
             self.__post_init__()
         return self._ref
@@ -233,7 +234,7 @@ class GatedWeight:
             raise ValueError("gated weights: bf16 or fp16, inner (E, 2 F, H) and outer (E, H, F), rows on multiples of 16 bytes")
         self.E, self.F, self.H = a.shape[0], b.shape[2], a.shape[2]
         self._c = _CGated(_DTYPES[a.dtype], _ACTIVATIONS[self.activation], self.E, self.F, self.H, a.stride(1), b.stride(1),
-                          *self._places())
+                          a.data_ptr(), b.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._made_at = self._places()
 
@@ -245,9 +246,10 @@ class GatedWeight:
             self._ref = None   # checked and made anew by the next call
 
     def _places(self):
-        return self.inner.data_ptr(), self.outer.data_ptr()
+        return _place(self.inner), _place(self.outer)
 
     def _arg(self):
+        """As ``Weight._arg``; E, F and H follow the fields, so that it comes before what is checked against them."""
         if self._ref is None or self._places() != self._made_at:
             self.__post_init__()
         return self._ref
@@ -285,18 +287,26 @@ class Gradients:
                 if v.shape != t.shape or not v.is_contiguous():
                     raise ValueError("gradients: contiguous tensors expected, out of the same shapes")
         self.index = index
-        self._made_at = self._places()
         self._c = (_CTensor * len(self.tensors))(*(
             (t.data_ptr(), o.data_ptr(), t.numel(), _DTYPES[t.dtype]) for t, o in zip(self.tensors, outs)))
+        all_of = self._all()
+        self._made_at = list(map(_data_ptr, all_of))
+        self._made_of = _TensorGuards(*all_of, dynamic_dims_sizes=None, dynamic_dims_strides=None)
 
-    def _places(self):
-        return [t.data_ptr() for t in self.tensors] + [t.data_ptr() for t in self.out or ()]
+    def _all(self):
+        return self.tensors if self.out is None else self.tensors + self.out
 
     def _arg(self):
-        if self._places() != self._made_at:   # memory moved (``.data``)
+        all_of = self._all()
+        # other memory, sizes, strides or types (``.data``)
+        if list(map(_data_ptr, all_of)) != self._made_at or not self._made_of.check(*all_of):
             self.__init__(self.tensors, self.out, self.index)
         return self._c
 
+
+_data_ptr = torch.Tensor.data_ptr
+# whether each of many tensors has the sizes, strides and type that it had: 0.05 us a tensor, its attributes one by one 0.2
+_TensorGuards = torch._C._dynamo.guards.TensorGuards
 
 # the current stream's handle without a Stream object around it (0.1 instead of 2 us per call)
 _raw_stream = torch._C._cuda_getCurrentRawStream
@@ -314,6 +324,11 @@ def _rows16(t) -> bool:
     """Whether the rows of a 3-D 16-bit tensor start at multiples of 16 bytes, planes following one another."""
     return t.stride(2) == 1 and t.stride(1) % 8 == 0 and t.stride(1) >= t.shape[2] and t.data_ptr() % 16 == 0 and \
         (t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1))
+
+
+def _place(t):
+    """What a C argument made from a tensor depends on."""
+    return t.data_ptr(), t.shape, t.stride(), t.dtype
 
 
 def _ptr(t):
@@ -649,6 +664,7 @@ class Moe:
 
     def keep(self, M: int, weight: GatedWeight) -> Kept:
         """Room for what ``feed_forward`` keeps of M rows for their gradients."""
+        weight._arg()
         F64, dt = _pad64(weight.F), weight.inner.dtype
         return Kept(self._new((M, 2, F64), torch.float32), self._new((M, F64), dt), self._new((M, _pad64(weight.H)), dt))
 
@@ -659,6 +675,7 @@ class Moe:
         self._need(kept.rows, "rows", dt, (M, _pad64(weight.H)))
 
     def _block_rows(self, x, weight: GatedWeight, offsets, rows):
+        weight._arg()
         self._need(weight.inner, "weight")
         code, ldx = self._matrix(x, "x", cols=weight.H, dtype=weight.inner.dtype)
         if offsets is not None:
@@ -684,7 +701,7 @@ class Moe:
             kept = keep._arg()
         self._on_stream()
         esp._check(self._lib.esp_moe_feed_forward(
-            self.h, weight._arg(), x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ldy, out.data_ptr(),
+            self.h, weight._ref, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ldy, out.data_ptr(),
             None if kept is None else ctypes.byref(kept)), "esp_moe_feed_forward")
         if keep is not None:
             keep.copied = bool(kept.copied)
@@ -715,7 +732,7 @@ class Moe:
             self._need(douter, "douter", dt, (E, H, F))
         self._on_stream()
         esp._check(self._lib.esp_moe_feed_forward_backward(
-            self.h, weight._arg(), x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ctypes.byref(kept._arg()),
+            self.h, weight._ref, x.shape[0], ldx, x.data_ptr(), M, _ptr(rows), _ptr(offsets), ctypes.byref(kept._arg()),
             lddy, dy.data_ptr(), lddx, _ptr(dx), _DTYPES[dt], _ptr(dinner), _ptr(douter)),
             "esp_moe_feed_forward_backward")
         return dx, dinner, douter

@@ -94,3 +94,78 @@ def test_lists_of_gradients_are_checked():
     with pytest.raises(ValueError):
         moe.Gradients(g, None, 0)
     assert ctypes.sizeof(moe._CTensor) == 32
+
+
+def test_weights_of_another_shape_in_place():
+    """``.data`` at the same address: what is told to the library is what the tensors are now, or the call is refused."""
+    inner, outer = weights()
+    w = moe.GatedWeight(inner, outer)
+    at = inner.data_ptr(), outer.data_ptr()
+    inner.data, outer.data = inner.data[:1], outer.data[:1]
+    w._arg()
+    assert (w._c.inner, w._c.outer) == at and (w._c.E, w.E) == (1, 1)
+    inner.data, outer.data = (t.data.view(torch.float16) for t in (inner, outer))
+    w._arg()
+    assert w._c.dtype == moe._DTYPES[torch.float16]
+    room = torch.zeros(1, 32, 32, dtype=torch.float16)
+    inner.data = room[:, :, :24]
+    w._arg()
+    assert w._c.ld_inner == 32
+    inner.data = room.flatten()[:32 * 24].view(1, 32, 24)
+    w._arg()
+    assert w._c.ld_inner == 24 and w._c.inner == room.data_ptr()
+    outer.data = outer.data[:, :8]
+    with pytest.raises(ValueError):
+        w._arg()
+
+
+def test_weights_assigned_with_other_sizes():
+    """E, F and H follow the tensors before rows and offsets are checked against them."""
+    w = moe.GatedWeight(*weights())
+    w.inner, w.outer = weights(E=3, F=8, H=40)
+    m = object.__new__(moe.Moe)   # no handle: the checks alone
+    m.h, m._index, m.device, m._side = None, -1, torch.device("cpu"), None
+    x, offsets = torch.zeros(5, 40, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    assert m._block_rows(x, w, offsets, None) == (5, 40) and (w.E, w.F, w.H) == (3, 8, 40)
+    w.inner, w.outer = weights()
+    for x1, offsets1 in ((x, offsets), (x, offsets[:3]), (x[:, :24], offsets)):
+        with pytest.raises(ValueError):
+            m._block_rows(x1, w, offsets1, None)
+    w.inner, w.outer = weights(F=80)
+    assert m.keep(2, w).pre.shape == (2, 2, 128)
+
+
+def test_codes_of_another_shape_in_place():
+    q, s = torch.zeros(2, 10, 32, dtype=torch.uint8), torch.zeros(2, 1, 1)
+    w = moe.Weight(2, 10, 20, q, s)
+    w._arg()
+    q.data = q.data[:1]
+    with pytest.raises(ValueError):
+        w._arg()
+    q.data = torch.zeros(2, 10, 64, dtype=torch.uint8)
+    w._arg()
+    assert w._c.ld == 64
+    s.data = s.data.view(torch.int32)
+    with pytest.raises(ValueError):
+        w._arg()
+
+
+def test_gradients_of_another_length_in_place():
+    a, b, o = torch.zeros(100), torch.zeros(6, 4), torch.zeros(6, 4)
+    li, to = moe.Gradients([a, b], None, -1), moe.Gradients([b], [o], -1)
+    a.data = a.data[:10]
+    assert (li._arg()[0].n, li._arg()[0].grad) == (10, a.data_ptr())
+    a.data = a.data.view(torch.bfloat16)
+    assert (li._arg()[0].n, li._arg()[0].dtype) == (20, moe._DTYPES[torch.bfloat16])
+    o.data = o.data[:3]
+    with pytest.raises(ValueError):
+        to._arg()
+    o.data = torch.zeros(6, 4)
+    assert to._arg()[0].out == o.data_ptr()
+    room = torch.zeros(6, 8)
+    b.data = room.flatten()[:24].view(6, 4)
+    assert to._arg()[0].grad == room.data_ptr()
+    b.data = room[:, :4]   # the same address, not contiguous
+    for v in (li, to):
+        with pytest.raises(ValueError):
+            v._arg()
