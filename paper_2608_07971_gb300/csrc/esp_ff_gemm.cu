@@ -471,8 +471,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int y = t.m0 + (int)rank * kRowsA + 32 * quarter;        // the first
             const bool split = CG == 1 && p.g.splits > 1, some = t.k0 < t.k1;
             const uint32_t src = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(acc * kAccCols);
-            // DPRE: 32 columns of g and u at a time, from column c of the tile on, into two boxes; they arrive together
+            // DPRE: 32 columns of g and u at a time, from column c of the tile on, into two boxes; they arrive together. The
+            // fence: the lanes' own reads and writes of the boxes come before the copies, which write through the other proxy
             const auto load_pre = [&](int c) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
                 if (lane == 0) {
                     mbar_expect(landed + 8 * warp, 2 * kBox);
                     load_box<CG>(smem_u32(gbox), &map.a2, t.n0 + c, y, 0, landed + 8 * warp);
