@@ -12,6 +12,7 @@
 // (above 2^60, or all below 2^-50) are summed again in fp64.
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -202,10 +203,17 @@ __device__ __forceinline__ void load_chunk(const ClipTensor &t, int64_t g0, uint
         r[u] = load_group<T>(t, g0 + u * kThreads + threadIdx.x, skip);
 }
 
+// What the gradients are multiplied by. Where fp32 would hold it in fewer bits (a small limit of large gradients), `wide`
+// is not 0 and is it.
+struct Factor {
+    float by;
+    double wide;
+};
+
 template <typename T, int U>
-__device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, float by, const uint4 (&r)[U])
+__device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, const Factor &k, const uint4 (&r)[U])
 {
-    if (!t.out || (by == 1.0f && t.out == t.grad))
+    if (!t.out || (k.by == 1.0f && t.out == t.grad))
         return;
     const int skip = lead<T>(t.grad);
     const bool same = lead<T>(t.out) == skip;   // groups of `out` are aligned too
@@ -217,10 +225,19 @@ __device__ __forceinline__ void scale_chunk(const ClipTensor &t, int64_t g0, flo
         T *out = static_cast<T *>(t.out) + i;
         float f[kPer<T>];
         unpack<T>(r[u], f);
+        if (k.wide == 0.0) {
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j)
+                f[j] *= k.by;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer<T>; ++j)
+                f[j] = (float)((double)f[j] * k.wide);
+        }
         T v[kPer<T>];
 #pragma unroll
         for (int j = 0; j < kPer<T>; ++j)
-            v[j] = from_f32<T>(f[j] * by);
+            v[j] = from_f32<T>(f[j]);
         if (same && i >= 0 && i + kPer<T> <= t.n) {
             uint4 w;
             memcpy(&w, v, 16);
@@ -250,7 +267,7 @@ template <int U, int N>
 __global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ ClipArgs<N> a, const SumArgs n)
 {
     __shared__ double all[kThreads];
-    __shared__ float factor;
+    __shared__ Factor factor;
     uint4 r[U];
     int c = a.chunks - 1 - (int)blockIdx.x, i = 0;
     int64_t g0 = 0;
@@ -274,7 +291,7 @@ __global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ Clip
         // sum = m 4^e with m in [1, 4): fp32's reciprocal root of m (2 ulp) and one Newton step in fp64 leave it exact to
         // 2^-40; fp64's own root and division take several microseconds here
         float norm = (float)sum;
-        factor = (float)n.scale;
+        double by = n.scale;
         if (sum > 0.0 && sum < (double)INFINITY) {
             const int e = ((int)(__double_as_longlong(sum) >> 52) - 1023) >> 1;
             const double m = sum * power_of_two(-2 * e);
@@ -282,13 +299,14 @@ __global__ void __launch_bounds__(kThreads) k_scale(const __grid_constant__ Clip
             r = r * (1.5 - 0.5 * m * r * r);
             norm = (float)(n.scale * m * r * power_of_two(e));
             if (norm < INFINITY)
-                factor = (float)fmin(n.scale, n.max_norm * r * power_of_two(-e));
+                by = fmin(n.scale, n.max_norm * r * power_of_two(-e));
         }
+        factor = Factor{(float)by, by < (double)FLT_MIN ? by : 0.0};
         if (blockIdx.x == 0)
             *n.norm = norm;
     }
     __syncthreads();
-    const float by = factor;
+    const Factor by = factor;
     while (c >= 0) {
         by_dtype(a.dtype[i], [&](auto elem) { scale_chunk<decltype(elem), U>(a.t[i], g0, by, r); });
         c -= gridDim.x;
@@ -402,7 +420,7 @@ extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tens
     esp_status st = begin_call(m);
     if (st != ESP_OK)
         return st;
-    if (count < 0 || (count > 0 && !tensors) || !norm || !(max_norm > 0.0) || !(scale > 0.0) || !std::isfinite(scale))
+    if (count < 0 || (count > 0 && !tensors) || !norm || !(max_norm > 0.0) || !(scale > 0.0) || !std::isnormal((float)scale))
         return ESP_ERR_INVALID_ARG;
     bool write = false;
     int64_t bytes = 0;

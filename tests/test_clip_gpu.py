@@ -224,3 +224,29 @@ def test_refusals(mm):
         assert err.value.status == esp.ESP_ERR_INVALID_ARG
     assert float(mm.clip([g], 1e9)) == 10.0 and (g == 1.0).all()
     mm.synchronize()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_factors_below_32_bits(mm, dt):
+    """max_norm / norm, or scale times it, is subnormal in fp32, or 0: the results are not."""
+    for size, max_norm, scale in ((2.0 ** 115, 2.0 ** -8, 1.0), (2.0 ** 100, 2.0 ** -60, 1.0), (2.0 ** 110, 1.0, 2.0 ** -126),
+                                  (2.0 ** 100, 2.0 ** -125, 2.0 ** -40), (2.0 ** 120, math.inf, 2.0 ** -126)):
+        grads = make([3000, 77, 50000], [dt], 6, size)
+        before = [g.clone() for g in grads]
+        check(before, grads, mm.clip(grads, max_norm, scale=scale), max_norm, scale)
+        out = [torch.empty_like(g) for g in grads]
+        check(before, out, mm.clip(mm.gradients(before, out=out), max_norm, scale=scale), max_norm, scale)
+
+
+def test_scales_at_the_ends_of_32_bits(mm):
+    from paper_2608_07971_gb300 import esp
+    most = float(torch.finfo(torch.float32).max)
+    for scale in (2.0 ** 128, 1e300, 2.0 ** -127, 1e-300):   # fp32 has them as infinity, 0 or with fewer bits
+        z = torch.zeros(100, device="cuda")
+        with pytest.raises(esp.EspError) as err:
+            mm.clip([z], scale=scale)
+        assert err.value.status == esp.ESP_ERR_INVALID_ARG
+    for scale, size in ((most, 2.0 ** -90), (2.0 ** -126, 2.0 ** 20)):
+        for grads in ([torch.zeros(100, device="cuda")], make([1000, 3], [torch.float32], 7, size)):
+            before = [g.clone() for g in grads]
+            check(before, grads, mm.clip(grads, scale=scale), math.inf, scale)
