@@ -225,7 +225,7 @@ typedef struct {
  * min(1, max_norm / norm), rounded once. scale is the inverse of a loss scale, 1 without. Where the norm is not finite,
  * out = grad * scale, and the program skips its step by the norm. The sum is in fp64 (fp32 within a thread's 64
  * elements); max_norm infinity: no clipping. `tensors` (on the host) is read during the call.
- * Errors: ESP_ERR_INVALID_ARG (max_norm > 0, scale > 0 and a normal number of fp32, 0 <= n <= 2^40, 2^45 bytes in all; memory
+ * Errors: ESP_ERR_INVALID_ARG (max_norm > 0, scale > 0 and a normal number of fp32, 0 <= n <= 2^40, 2^44 bytes in all; memory
  * that is written for one tensor and read or written for another). */
 esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, double max_norm, double scale,
                         float *norm);

@@ -35,7 +35,10 @@ constexpr int kCtasPerSm = 4;      // k_norm's, each with many chunks and eight 
 constexpr int kScaleCtas = 32, kScaleCtasOfFew = 8;   // few bytes: less often the sum of k_norm's CTAs
 
 constexpr int kFewTensors = 16, kManyTensors = 144;   // tensors of a launch, in its parameters
-constexpr int64_t kMostBytes = (int64_t)1 << 45;   // of all tensors; keeps a launch's chunks in int32
+constexpr int64_t kMostBytes = (int64_t)1 << 44;   // of all tensors; keeps a launch's chunks in int32
+constexpr int kGroupsOfMany = 4;                   // the least that a thread has in a chunk where there are many bytes
+// besides, a chunk of each tensor is not full, and the last step of a CTA goes past the end
+static_assert(kMostBytes / (16 * kThreads * kGroupsOfMany) + 2 * kManyTensors + kScaleCtas * 1024 < ((int64_t)1 << 31), "int32");
 
 struct ClipTensor {
     const void *grad;
@@ -454,7 +457,7 @@ extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tens
     const int64_t chunk = (int64_t)kThreads * 16, ctas = (int64_t)m->sm_count * kCtasPerSm;
     const auto launch = [&](auto tensors_per_launch) {
         constexpr int N = decltype(tensors_per_launch)::value;
-        return bytes >= 16 * ctas * chunk   ? launch_clip<8, 4, N>(m, count, tensors, partial, n)
+        return bytes >= 16 * ctas * chunk   ? launch_clip<8, kGroupsOfMany, N>(m, count, tensors, partial, n)
                : bytes >= 2 * ctas * chunk ? launch_clip<4, 4, N>(m, count, tensors, partial, n)
                                            : launch_clip<2, 2, N>(m, count, tensors, partial, n);
     };

@@ -5,6 +5,7 @@ import copy
 import ctypes
 import os
 import pickle
+import re
 import subprocess
 
 import pytest
@@ -169,3 +170,16 @@ def test_gradients_of_another_length_in_place():
     for v in (li, to):
         with pytest.raises(ValueError):
             v._arg()
+
+
+def test_clip_counts_its_chunks_in_32_bits():
+    """By the source: the limit that the header states is the one that is checked, and a launch's chunks at it, with the
+    steps past the last one, stay within int32."""
+    src = open(os.path.join(build.CSRC, "esp_moe_clip.cu")).read()
+    bits = int(re.search(r"kMostBytes = \(int64_t\)1 << (\d+);", src).group(1))
+    assert f"2^{bits} bytes in all" in open(os.path.join(build.INCLUDE, "esp_moe.h")).read()
+    number = {n: int(v) for n, v in re.findall(r"\b(k\w+) = (\d+)\b(?! <<)", src)}
+    least = re.search(r"launch_clip<8, (\w+), N>", src).group(1)   # groups of a thread in k_scale's chunk
+    chunk = 16 * number["kThreads"] * (int(least) if least.isdigit() else number[least])
+    ctas = 1024 * number["kScaleCtas"]   # a step, on more SMs than any GPU has
+    assert (1 << bits) // chunk + 2 * number["kManyTensors"] + ctas < 1 << 31
