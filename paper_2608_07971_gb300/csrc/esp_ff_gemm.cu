@@ -578,33 +578,40 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                             for (int half = 0; half < 2; ++half) {   // g, u
                                 const int at = 128 * half + c;
-                                fetch(at, at + 16, at + 32, at + 48);
-                                if (half == 0 && p.near_zero > 0.0f) {
-                                    // the g whose sign the tensor core's sum leaves open: those far below the largest of
-                                    // their row and of their column (of 64 columns and 32 rows here; of either where a row or
-                                    // a column has too few to tell)
-                                    const bool few = rows < 8 || cols < 8;
-                                    float most = 0.0f, least = INFINITY;   // least: of those that are not 0
+                                const bool again = half == 0 && p.lengths;
+                                float mine = 0.0f, length[2] = {0.0f, 0.0f};   // of this lane's row and columns; 0: not there
+                                if (again) {
+                                    const float *const of = p.lengths + p.g.M + (int64_t)t.e * N + n;
+                                    mine = lane < rows ? p.near_zero * __ldcg(p.lengths + y + lane) : 0.0f;
 #pragma unroll
-                                    for (int i = 0; i < 64; ++i) {
-                                        const float g = fabsf(__uint_as_float(v[i / 16][i % 16]));
-                                        most = fmaxf(most, g);
-                                        least = g > 0.0f ? fminf(least, g) : least;
-                                    }
+                                    for (int i = 0; i < 2; ++i)
+                                        length[i] = 32 * i + lane < cols ? __ldcg(of + 32 * i + lane) : 0.0f;
+                                }
+                                fetch(at, at + 16, at + 32, at + 48);
+                                if (again) {
+                                    // the g whose sign the tensor core's sum leaves open
+                                    const float most = __uint_as_float(
+                                        __reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(length[0], length[1]))));
+                                    float least = INFINITY;
+#pragma unroll
+                                    for (int i = 0; i < 64; ++i)
+                                        if (i < cols)
+                                            least = fminf(least, fabsf(__uint_as_float(v[i / 16][i % 16])));
                                     uint64_t open = 0;
-                                    if (__any_sync(0xffffffffu, few || least < p.near_zero * most)) {
+                                    if (__any_sync(0xffffffffu, least < mine * most)) {
+                                        uint64_t zeros = 0;
 #pragma unroll
                                         for (int i = 0; i < 64; ++i) {
                                             const float g = fabsf(__uint_as_float(v[i / 16][i % 16]));
-                                            const float column = __uint_as_float(
-                                                __reduce_max_sync(0xffffffffu, lane < rows ? __float_as_uint(g) : 0u));
-                                            if (i < cols && g > 0.0f &&
-                                                g < p.near_zero * (few ? fmaxf(most, column) : fminf(most, column)))
+                                            if (g < mine * __shfl_sync(0xffffffffu, length[i / 32], i % 32)) {
                                                 open |= 1ull << i;
+                                                zeros |= (uint64_t)(g == 0.0f) << i;
+                                            }
                                         }
+                                        // many of exactly 0 are of operands that have no common elements, not of what is cut off
+                                        if (__reduce_add_sync(0xffffffffu, (unsigned)__popcll(zeros)) > 64)
+                                            open &= ~zeros;
                                     }
-                                    if (lane >= rows)
-                                        open = 0;
                                     for (unsigned left; (left = __ballot_sync(0xffffffffu, open != 0)) != 0;) {
                                         const int r = __ffs(left) - 1, at0 = __shfl_sync(0xffffffffu, __ffsll(open) - 1, r);
                                         const float g = exact_dot(
@@ -929,6 +936,70 @@ __global__ void __launch_bounds__(32 * kTailRows) k_tails(const TailArgs a)
     }
 }
 
+// ---- lengths of rows
+constexpr int kLengthRows = 8;   // of a CTA, a warp for each
+
+struct LengthArgs {
+    int64_t M;
+    int32_t E, F, H;
+    int64_t ldx, ld_inner;
+    const void *x, *inner;       // rows on 16 bytes
+    float *out;                  // M + E F
+};
+
+// Lengths of the rows of x, and of G's of each expert; 0 for a row with NaN. Bound by the rows' bytes. Squares that leave
+// fp32's range are summed again of scaled elements.
+template <typename T>
+__global__ void __launch_bounds__(32 * kLengthRows) k_lengths(const LengthArgs a)
+{
+    wait_for_launch_before();
+    let_next_launch_start();
+    const int64_t i = (int64_t)blockIdx.x * kLengthRows + (threadIdx.x >> 5), j = i - a.M;
+    const int lane = threadIdx.x & 31;
+    if (j >= (int64_t)a.E * a.F)
+        return;
+    // U's rows lie behind G's
+    const T *row = j < 0 ? static_cast<const T *>(a.x) + i * a.ldx
+                         : static_cast<const T *>(a.inner) + (j + j / a.F * a.F) * a.ld_inner;
+    const auto squares = [&](float scale) {
+        constexpr int U = 4;
+        float s = 0.0f;
+        for (int h0 = 8 * lane; h0 < a.H; h0 += 256 * U) {
+            Pack<T, 8> r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + 256 * u;
+                r[u] = {};
+                if (h + 8 <= a.H)
+                    r[u] = *reinterpret_cast<const Pack<T, 8> *>(row + h);
+                else
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (h + k < a.H)
+                            r[u].v[k] = row[h + k];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float f = to_f32(r[u].v[k]) * scale;
+                    s = fmaf(f, f, s);
+                }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1)
+            s += __shfl_xor_sync(0xffffffffu, s, d);
+        return s;
+    };
+    float s = squares(1.0f), back = 1.0f;
+    if (!(s > 0x1p-90f && s < 0x1p120f)) {
+        back = s > 1.0f ? 0x1p80f : 0x1p-80f;
+        s = squares(1.0f / back);
+    }
+    if (lane == 0)
+        a.out[i] = s >= 0.0f ? sqrtf(s) * back : 0.0f;
+}
+
 }  // namespace
 
 size_t ff_partial_floats(const esp_moe *m)
@@ -945,17 +1016,26 @@ cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_
     p.g.out = hidden;
     p.g.ldo = s.fp;
     p.out2 = pre;
-    if (pre && s.act == ESP_MOE_RELU) {
-        // The tensor core cuts off what it adds below its accumulator's last bit: of 8192 products whose sum is around 1 a g is
-        // off by 9e-6 (rms; up to 6e-5), ten times an ordinary 32-bit sum, and the sign of one in half a million is wrong,
-        // which takes a whole gradient away or adds one. The error grows with the steps of 16: the largest g of a wrong sign
-        // was 0.7 to 1.2 of H 2^-30 (H 1071 to 8192), the bound is about ten times that. 8192 rows x 2048 x 2048 with g and u
-        // kept: 140 us (silu 136); 4416 x 8192 x 1024: 155 (138).
+    if (s.lengths) {
+        // The tensor core cuts off what it adds below its accumulator's last bit, at every step of 16: of 8192 products a g is off
+        // by ten times an ordinary 32-bit sum (9e-6 rms of products whose sum is around 1), and the sign of one in half a million
+        // is wrong, which takes a whole gradient away or adds one. The error goes with the sums on the way, not with g: of
+        // terms in no order those are around S = |x||w| / sqrt H (lengths of the two rows), whatever g itself is. Measured: an
+        // error of 0.08 to 0.16 H/16 2^-23 S (rms), of a rounding's size in g below that; the bound is 2 (H/16 + 4) 2^-23 S.
+        // Sums on the way that are far above S (terms that are sorted by sign) are not covered. 8192 rows x 2048 x 2048 with g and u
+        // kept: 148 us (silu 135); 4416 x 8192 x 1024: 179 (140); 11 and 18 of it are k_lengths.
         p.x = x;
         p.ldx = ldx;
         p.inner = s.inner;
         p.ld_inner = s.ld_inner;
-        p.near_zero = (float)(s.H / 16 + 4) * 1.1920929e-7f;   // 2^-23
+        p.near_zero = (float)(2.0 * (s.H / 16 + 4) * 0x1p-23 / std::sqrt((double)s.H));
+        p.lengths = s.lengths;
+        const LengthArgs l{s.M, s.E, s.F, s.H, ldx, s.ld_inner, x, s.inner, s.lengths};
+        FF_TRY(with_16(s.dtype, [&](auto elem) {
+            m->launches += 1;
+            return launch_after(k_lengths<decltype(elem)>, dim3((unsigned)ceil_div(s.M + (int64_t)s.E * s.F, kLengthRows)),
+                                32 * kLengthRows, 0, m->stream, l);
+        }));
     }
     CUtensorMap a, b, o, o2;
     FF_TRY(box_map3(&a, x, 2, s.H, s.M, ldx, 1, 0, kRowsA));

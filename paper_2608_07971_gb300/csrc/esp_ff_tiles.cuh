@@ -36,10 +36,11 @@ struct FfParams {
     const void *pre;          // DPRE
     int64_t fp;
     void *out2;               // HIDDEN: pre (or null)
-    // HIDDEN with pre and a kinked activation: the operands, and below which part of the larger values around it a g is
-    // summed again (0: none is)
+    // HIDDEN with pre and a kinked activation: the operands, their rows' lengths (null: no g is summed again), and below which
+    // part of the product of two of them a g is
     const void *x, *inner;
     int64_t ldx, ld_inner;
+    const float *lengths;     // M rows of x, E x F rows of G
     float near_zero;
 };
 

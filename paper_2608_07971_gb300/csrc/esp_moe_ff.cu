@@ -99,7 +99,7 @@ bool mappable(const void *x, int64_t ldx)
 FfShape shape_of(const esp_moe_gated *w, int64_t M, const int32_t *offsets)
 {
     return FfShape{w->dtype, w->activation, w->E, w->F, w->H, M, offsets, w->inner, w->outer, w->ld_inner, w->ld_outer,
-                   up64(w->H), nullptr, up64(w->F)};
+                   up64(w->H), nullptr, up64(w->F), nullptr};
 }
 
 }  // namespace
@@ -153,6 +153,8 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
         hidden = kept ? kept->hidden : c.take<uint16_t>((size_t)(M * s.fp));
         if (copy)
             gathered = kept ? kept->rows : c.take<uint16_t>((size_t)(M * hp));
+        if (kept && !vec && w->activation == ESP_MOE_RELU)
+            s.lengths = c.take<float>((size_t)(M + (int64_t)w->E * w->F));
         if (pass == 0 && (st = reserve_space(m, c.used())) != ESP_OK)
             return st;
     }

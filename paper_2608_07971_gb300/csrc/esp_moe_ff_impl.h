@@ -28,6 +28,7 @@ struct FfShape {
     int64_t hp;               // of the rows of x and dy in the tails: H rounded up to 64
     float *partial;           // work space: ff_partial_floats
     int64_t fp;               // elements of a row of a half of `pre` and `dpre`, and of `hidden`: F rounded up to 64
+    float *lengths;           // work space of hidden rows that are kept for relu's slope: M + E F
 };
 
 // ---- esp_ff_vec.cu
@@ -40,7 +41,7 @@ cudaError_t launch_vec(esp_moe *m, const FfShape &s, const void *x, int64_t ldx,
 // ---- esp_ff_gemm.cu
 // Work space of a product whose tiles' inner axes are split over CTAs.
 size_t ff_partial_floats(const esp_moe *m);
-// hidden (M x fp) = act(gate) * up; pre (M x 2 x fp fp32: gate, up) is written too where it is given.
+// hidden (M x fp) = act(gate) * up; pre (M x 2 x fp fp32: gate, up) is written too where it is given (relu: two launches).
 cudaError_t launch_ff_hidden(esp_moe *m, const FfShape &s, const void *x, int64_t ldx, void *hidden, void *pre);
 // y (M x H) = hidden O^T.
 cudaError_t launch_ff_out(esp_moe *m, const FfShape &s, const void *hidden, void *y, int64_t ldy);

@@ -710,3 +710,86 @@ def test_nan_of_a_gate_reaches_the_results(mm, sizes, kind):
     assert a.isfinite().all() and b[here[:, :F]].isnan().all() and torch.equal(a[~here[:, :F]], b[~here[:, :F]])
     for i in (2, 3):
         assert math.isnan(float(mm.clip([bad[i].clone()], 1.0))) and math.isfinite(float(mm.clip([plain[i].clone()], 1.0)))
+
+
+def cancelling(M, F, H, dt, seed):
+    """Rows far from 0 and weights whose rows nearly sum to 0: g is far below the sums on the way to it."""
+    G = torch.randn(F, H, generator=torch.Generator(device="cuda").manual_seed(seed + 1), device="cuda") * H ** -0.5
+    return (rand(M, H, dt=dt, seed=seed).float() + 64).to(DT[dt]), (G - G.mean(1, keepdim=True)).to(DT[dt])
+
+
+@pytest.mark.parametrize("sizes,H,F,dt,gathered", [
+    ([2000], 2048, 1024, "bf16", False), ([2000], 8192, 512, "f16", False), ([300, 0, 90], 2050, 300, "bf16", True),
+    ([40], 4100, 130, "f16", False)])   # the last one: split inner axes
+def test_signs_of_gates_that_cancel(mm, sizes, H, F, dt, gathered):
+    # As test_signs_of_gates_near_zero. S = |x||w| / sqrt H (lengths) is what the sums on the way to g are around; what an
+    # adder of 24 bits that cuts off loses in H / 16 steps is below H / 16 2^-23 S = 2 H U S / 16, a g below that is summed again.
+    E, M = len(sizes), sum(sizes)
+    x, G = cancelling(M, E * F, H, dt, 61)
+    inner = torch.cat([G.view(E, F, H), rand(E, F, H, dt=dt, seed=63, size=H ** -0.5)], 1)
+    w = mm.gated_weight(inner, rand(E, H, F, dt=dt, seed=64, size=F ** -0.5), "relu")
+    offsets = torch.tensor([0, *np.cumsum(sizes)], dtype=torch.int32, device="cuda")
+    rows = torch.arange(M - 1, -1, -1, dtype=torch.int32, device="cuda") if gathered else None
+    kept = mm.keep(M, w)
+    mm.feed_forward(x, w, offsets=offsets, rows=rows, keep=kept)
+    a = 0
+    for e, n in enumerate(sizes):
+        xe, Ge = (x.flip(0) if gathered else x)[a:a + n].double(), inner[e, :F].double()
+        g, got = xe @ Ge.t(), kept.pre[a:a + n, 0, :F].double()
+        lim = 2 * U * g.abs() + 2 * H * U * U * (xe.abs() @ Ge.abs().t())
+        S = xe.norm(dim=1)[:, None] * Ge.norm(dim=1) / math.sqrt(H)
+        assert ((got - g).abs() <= lim)[g.abs() < 2 * H * U * S / 16].all()
+        assert ((got > 0) == (g > 0))[g.abs() > lim].all()
+        a += n
+
+
+@pytest.mark.parametrize("M", [1, 2, 4, 8])
+@pytest.mark.parametrize("H,F,dt", [(1024, 2048, "bf16"), (4096, 500, "f16"), (7001, 300, "bf16")])
+def test_signs_of_gates_of_few_rows(mm, M, H, F, dt):
+    # One block, few rows: sums in 32 bits, each thread over 8 in 2048 elements in two chains of 4, those and the threads' joined in
+    # 1 + 5 + 8 steps; at each step U of the sum on the way, itself below sum |a b|.
+    n = 4 * -(-H // 2048) + 14
+    plain = rand(M, H, dt=dt, seed=71), rand(F, H, dt=dt, seed=72, size=H ** -0.5)
+    for x, G in (plain, cancelling(M, F, H, dt, 73)):
+        inner = torch.cat([G, rand(F, H, dt=dt, seed=75, size=H ** -0.5)])
+        w = mm.gated_weight(inner, rand(H, F, dt=dt, seed=76, size=F ** -0.5), "relu")
+        kept = mm.keep(M, w)
+        mm.feed_forward(x, w, keep=kept)
+        g, got = x.double() @ G.double().t(), kept.pre[:, 0, :F].double()
+        lim = n * (1 + n * U) * U * (x.double().abs() @ G.double().abs().t())
+        assert ((got - g).abs() <= lim).all()
+        assert ((got > 0) == (g > 0))[g.abs() > lim].all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 80, 2.0 ** -60])
+def test_signs_of_gates_of_large_and_small_rows(mm, size):
+    # the lengths' squares are beyond 32 bits; one row is 0, one is not a number, one infinite: the others' g are summed again
+    M, H, F = 64, 2048, 96
+    x, inner = rand(M, H, dt="bf16", seed=81) * size, rand(2 * F, H, dt="bf16", seed=82, size=H ** -0.5)
+    x[3], x[5, 9], x[7, 9], inner[4], inner[6, 1] = 0, math.nan, math.inf, 0, math.nan
+    w = mm.gated_weight(inner, rand(H, F, dt="bf16", seed=83), "relu")
+    kept = mm.keep(M, w)
+    mm.feed_forward(x, w, keep=kept)
+    g, got = x.double() @ inner[:F].double().t(), kept.pre[:, 0, :F].double()
+    ok = g.isfinite()
+    assert int(ok.sum()) == (M - 2) * (F - 1) and (got.isfinite() == ok).all()
+    lim = 2 * U * g.abs() + 2 * H * U * U * (x.double().abs() @ inner[:F].double().abs().t())
+    assert ((got - g).abs() <= lim)[ok & (g.abs() < H * 2.0 ** -27 * size)].all()
+    assert (got[3] == 0).logical_or(~ok[3]).all() and (got[:, 4] == 0).logical_or(~ok[:, 4]).all()
+
+
+def test_a_gate_whose_sum_is_cut_off_to_zero(mm):
+    # 1 + 2^-30 - 1, a step of 16 apart: the sum on the way holds 24 bits
+    M, H, F = 64, 64, 64
+    x, inner = rand(M, H, dt="bf16", seed=91), rand(2 * F, H, dt="bf16", seed=92, size=H ** -0.5)
+    x[9], inner[5] = 0, 0
+    for k, v in ((0, 1.0), (17, 2.0 ** -30), (40, -1.0)):
+        x[9, k], inner[5, k] = v, 1.0
+    w = mm.gated_weight(inner, rand(H, F, dt="bf16", seed=93), "relu")
+    kept = mm.keep(M, w)
+    mm.feed_forward(x, w, keep=kept)
+    assert float(kept.pre[9, 0, 5]) == 2.0 ** -30
+    # rows without common elements: many sums of exactly 0 stay what they are
+    x[:, ::2], inner[:F, 1::2] = 0, 0
+    mm.feed_forward(x, w, keep=kept)
+    assert not kept.pre[:, 0, :F].any()
