@@ -195,16 +195,18 @@ typedef struct {
 /* y[i] = O_e (act(G_e x[rows[i]]) * (U_e x[rows[i]])) for the rows i of expert e; x, M, rows, offsets and what is left as
  * it was as in esp_moe_linear. Both inner products and the hidden row are summed and computed in fp32; the hidden row is
  * rounded to 16 bits once, as the outer product's operand. kept NULL: nothing is kept. y must not overlap the weights,
- * what is kept, or x where its rows are needed for the gradients (refused where they begin at the same place).
- * Errors: ESP_ERR_INVALID_ARG (F, H <= 2^22; E x F <= 2^30; fp32 rows, as the tensor cores would round them). */
+ * what is kept, or x where its rows are needed for the gradients (without kept, y may be x).
+ * Errors: ESP_ERR_INVALID_ARG (F, H <= 2^22; E x F <= 2^30; fp32 rows, as the tensor cores would round them; memory that is
+ * written and still read: columns of one matrix side by side are not, rows of different steps that lie between one another
+ * may be taken for it). */
 esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x, int64_t M,
                                 const int32_t *rows, const int32_t *offsets, int64_t ldy, void *y, esp_moe_kept *kept);
 
 /* Gradients of esp_moe_feed_forward at dy (M x H), with the same x, rows, offsets and weights and what that call kept:
  * dx (M x H, or NULL), one row for each of y's (rows of no expert are not written), dinner (E x 2 F x H, contiguous, or
  * NULL) and douter (E x H x F, contiguous, or NULL), these two in dw_dtype: the rows' type, or ESP_MOE_F32. An expert
- * without rows has dinner and douter 0. No result may overlap what the call reads (refused where dx begins where dy or x
- * does). The gradients of G x and U x are rounded to 16 bits once, as operands
+ * without rows has dinner and douter 0. No result may overlap another or what the call reads (refused, as above; x is
+ * not read where its rows are kept). The gradients of G x and U x are rounded to 16 bits once, as operands
  * (G x and U x are kept in 32: from 16-bit ones dx and dinner were 1.77 times as far from 64 bits as results rounded once are,
  * and are 1.41 times as far). */
 esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int64_t T, int64_t ldx, const void *x,

@@ -6,6 +6,7 @@
 #include "esp_moe_ff_impl.h"
 #include "esp_moe_launch.cuh"
 #include "esp_moe_load.cuh"
+#include "esp_moe_spans.h"
 
 namespace esp_moe_impl {
 
@@ -96,6 +97,47 @@ bool mappable(const void *x, int64_t ldx)
     return rows_aligned(x, ldx, 2, 16);
 }
 
+// Rows of 16-bit elements, and the weights.
+Span rows16(const void *p, int64_t rows, int64_t ld, int64_t width)
+{
+    return Span{p, rows, 2 * ld, 2 * width};
+}
+
+Span inner_of(const esp_moe_gated *w)
+{
+    return rows16(w->inner, 2 * (int64_t)w->E * w->F, w->ld_inner, w->H);
+}
+
+Span outer_of(const esp_moe_gated *w)
+{
+    return rows16(w->outer, (int64_t)w->E * w->H, w->ld_outer, w->F);
+}
+
+Span pre_of(const esp_moe_gated *w, const esp_moe_kept *k, int64_t M)
+{
+    return rows16(k->pre, M, 4 * up64(w->F), 4 * up64(w->F));
+}
+
+Span hidden_of(const esp_moe_gated *w, const esp_moe_kept *k, int64_t M)
+{
+    return rows16(k->hidden, M, up64(w->F), up64(w->F));
+}
+
+Span rows_of(const esp_moe_gated *w, const esp_moe_kept *k, int64_t M, bool copied)
+{
+    return rows16(copied ? k->rows : nullptr, M, up64(w->H), up64(w->H));
+}
+
+// Whether the forward pass would write over what it, or its gradients, still read.
+bool forward_meets(const esp_moe_gated *w, const Span &x, const Span &y, const esp_moe_kept *k, int64_t M, bool copied)
+{
+    const Span inner = inner_of(w), outer = outer_of(w);
+    if (!k)
+        return written_over({y}, {inner, outer});   // x has been read before y is written
+    const Span pre = pre_of(w, k, M), hidden = hidden_of(w, k, M), rows = rows_of(w, k, M, copied);
+    return written_over({y, pre, hidden, rows}, {inner, outer}) || written_over({pre, hidden, rows}, {x}) || (!copied && meet(y, x));
+}
+
 FfShape shape_of(const esp_moe_gated *w, int64_t M, const int32_t *offsets)
 {
     return FfShape{w->dtype, w->activation, w->E, w->F, w->H, M, offsets, w->inner, w->outer, w->ld_inner, w->ld_outer,
@@ -135,7 +177,8 @@ esp_status esp_moe_feed_forward(esp_moe *m, const esp_moe_gated *w, int64_t T, i
         return st;
     const bool copied = rows || !mappable(x, ldx);
     if (!good_rows(w, T, ldx, x, M, rows, offsets) || ldy < w->H || ldy >= (int64_t)1 << 39 || (M > 0 && !y) ||
-        !aligned_to(y, 2) || (kept && M > 0 && (!good_kept(kept, copied) || (!copied && y == x))))
+        !aligned_to(y, 2) || (kept && M > 0 && !good_kept(kept, copied)) ||
+        (M > 0 && forward_meets(w, rows16(x, T, ldx, w->H), rows16(y, M, ldy, w->H), kept, M, copied)))
         return ESP_ERR_INVALID_ARG;
     if (kept)
         kept->copied = copied;
@@ -189,12 +232,15 @@ esp_status esp_moe_feed_forward_backward(esp_moe *m, const esp_moe_gated *w, int
         (dw_dtype != w->dtype && dw_dtype != ESP_MOE_F32))
         return ESP_ERR_INVALID_ARG;
     const bool f32 = dw_dtype == ESP_MOE_F32;
-    if (M > 0 && dx && (dx == dy || (!copied && dx == x)))   // read after dx is written
-        return ESP_ERR_INVALID_ARG;
     if (!aligned_to(dinner, f32 ? 4 : 2) || !aligned_to(douter, f32 ? 4 : 2))
         return ESP_ERR_INVALID_ARG;
+    const size_t n = (size_t)w->E * w->F * w->H * (f32 ? 4 : 2);   // bytes of douter
+    const auto all_of = [](const void *p, size_t bytes) { return Span{p, 1, (int64_t)bytes, (int64_t)bytes}; };
+    if (written_over({rows16(dx, M, lddx, w->H), all_of(dinner, 2 * n), all_of(douter, n)},
+                     {rows16(dy, M, lddy, w->H), copied ? rows_of(w, kept, M, true) : rows16(x, T, ldx, w->H), pre_of(w, kept, M),
+                      hidden_of(w, kept, M), inner_of(w), outer_of(w)}))
+        return ESP_ERR_INVALID_ARG;
     if (M == 0) {
-        const size_t n = (size_t)w->E * w->F * w->H * (f32 ? 4 : 2);
         if (dinner)
             MOE_CUDA(cudaMemsetAsync(dinner, 0, 2 * n, m->stream));
         if (douter)

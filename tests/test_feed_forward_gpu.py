@@ -793,3 +793,45 @@ def test_a_gate_whose_sum_is_cut_off_to_zero(mm):
     x[:, ::2], inner[:F, 1::2] = 0, 0
     mm.feed_forward(x, w, keep=kept)
     assert not kept.pre[:, 0, :F].any()
+
+
+def test_results_over_what_is_read(mm):
+    """Refused wherever they overlap, not where they begin alone; columns of one matrix side by side are taken."""
+    from paper_2608_07971_gb300 import esp
+    M, H, F = 40, 64, 64
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    inner, outer = rand(1, 2 * F, H, dt="bf16", seed=2), rand(1, H, F, dt="bf16", seed=3)
+    w = mm.gated_weight(inner, outer)
+    room = torch.zeros(2 * M, 3 * H, **bf)
+    x, dy, dx = (room[:M, i * H:(i + 1) * H] for i in range(3))
+    x.copy_(rand(M, H, dt="bf16", seed=1))
+    dy.copy_(rand(M, H, dt="bf16", seed=4))
+    kept = mm.keep(M, w)
+    y = mm.feed_forward(x, w, keep=kept, out=room[M:, :H])            # below x, beside dy
+    want = mm.feed_forward_backward(dy.clone(), x.clone(), w, kept)
+    got = mm.feed_forward_backward(dy, x, w, kept, out=(dx, None, None))
+    assert torch.equal(y, mm.feed_forward(x.clone(), w)) and all(torch.equal(a, b) for a, b in zip(got, want))
+    flat = torch.zeros(3 * H * F, **bf)
+    apart = flat[:2 * H * F].view(1, 2 * F, H), flat[2 * H * F:].view(1, H, F)
+    assert all(torch.equal(a, b) for a, b in zip(mm.feed_forward_backward(dy, x, w, kept, out=(None, *apart))[1:], want[1:]))
+    some = dy.clone()
+    assert torch.equal(mm.feed_forward(some, w, out=some), mm.feed_forward(dy, w))   # nothing is kept: in place
+    before = room.clone(), kept.pre.clone(), kept.hidden.clone(), inner.clone(), outer.clone()
+    both = flat[:2 * H * F].view(1, 2 * F, H), flat[H * F:2 * H * F].view(1, H, F)
+    backward = lambda **a: mm.feed_forward_backward(dy, x, w, kept, **a)   # noqa: E731
+    for f in (lambda: mm.feed_forward(x, w, keep=kept, out=room[:M, 8:H + 8]), lambda: mm.feed_forward(x, w, keep=kept, out=room[M - 1:2 * M - 1, :H]),
+              lambda: mm.feed_forward(x, w, keep=kept, out=kept.hidden),
+              lambda: mm.feed_forward(x, w, out=inner.view(-1)[:M * H].view(M, H)), lambda: mm.feed_forward(x, w, out=outer.view(-1)[-M * H:].view(M, H)),
+              lambda: backward(out=(room[:M, H + 8:2 * H + 8], None, None)), lambda: backward(out=(room[M - 1:2 * M - 1, :H], None, None)),
+              lambda: backward(out=(kept.hidden, None, None)), lambda: backward(out=(None, inner, None)),
+              lambda: backward(out=(None, None, outer)), lambda: backward(out=(None, *both))):
+        with pytest.raises((esp.EspError, ValueError)) as err:
+            f()
+        assert err.type is ValueError or err.value.status == esp.ESP_ERR_INVALID_ARG
+    assert all(torch.equal(a, b) for a, b in zip(before, (room, kept.pre, kept.hidden, inner, outer)))
+    rows = torch.arange(M, dtype=torch.int32, device="cuda")           # copied: x is not read again
+    mm.feed_forward(x, w, rows=rows, keep=kept, out=y)
+    assert torch.equal(mm.feed_forward_backward(dy, x, w, kept, rows=rows, out=(x, None, None))[0], want[0])
+    with pytest.raises(esp.EspError):
+        mm.feed_forward_backward(dy, x, w, kept, rows=rows, out=(kept.rows, None, None))
+    mm.synchronize()

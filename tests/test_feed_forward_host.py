@@ -40,6 +40,14 @@ def test_work_items_stay_in_range(tmp_path):
     assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
 
 
+def test_matrices_that_meet(tmp_path):
+    out = str(tmp_path / "driver")
+    subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-I", build.CSRC, os.path.join(HERE, "spans_driver.cpp"), "-o", out], check=True, capture_output=True, text=True)
+    res = subprocess.run([out], capture_output=True, text=True, timeout=120)
+    assert (res.returncode, res.stdout) == (0, "ok\n"), res.stdout + res.stderr
+
+
 def weights(E=2, F=16, H=24, dtype=torch.bfloat16):
     return torch.zeros(E, 2 * F, H, dtype=dtype), torch.zeros(E, H, F, dtype=dtype)
 
