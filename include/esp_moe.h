@@ -228,7 +228,7 @@ typedef struct {
  * out = grad * scale, and the program skips its step by the norm. The sum is in fp64 (fp32 within a thread's 64
  * elements); max_norm infinity: no clipping. `tensors` (on the host) is read during the call.
  * Errors: ESP_ERR_INVALID_ARG (max_norm > 0, scale > 0 and a normal number of fp32, 0 <= n <= 2^40, 2^44 bytes in all; memory
- * that is written for one tensor and read or written for another). */
+ * that is written for one tensor or the norm and read or written for another). */
 esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tensor *tensors, double max_norm, double scale,
                         float *norm);
 

@@ -339,15 +339,17 @@ bool good_tensor(const esp_moe_tensor &t)
            reinterpret_cast<uintptr_t>(t.grad) % size == 0 && reinterpret_cast<uintptr_t>(t.out) % size == 0;
 }
 
-// Whether some memory is written for one tensor and read or written for another.
-bool overlapping(int32_t count, const esp_moe_tensor *tensors)
+// Whether some memory is written for one tensor, or for the norm, and read or written for another.
+bool overlapping(int32_t count, const esp_moe_tensor *tensors, const float *norm)
 {
     struct Range {
         uintptr_t lo, hi;
         bool written;
     };
     std::vector<Range> all;
-    all.reserve(2 * (size_t)count);
+    all.reserve(2 * (size_t)count + 1);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+    all.push_back(Range{at, at + sizeof(float), true});
     for (int32_t i = 0; i < count; ++i) {
         const esp_moe_tensor &t = tensors[i];
         if (t.n == 0)
@@ -423,20 +425,19 @@ extern "C" esp_status esp_moe_clip(esp_moe *m, int32_t count, const esp_moe_tens
     esp_status st = begin_call(m);
     if (st != ESP_OK)
         return st;
-    if (count < 0 || (count > 0 && !tensors) || !norm || !(max_norm > 0.0) || !(scale > 0.0) || !std::isnormal((float)scale))
+    if (count < 0 || (count > 0 && !tensors) || !norm || reinterpret_cast<uintptr_t>(norm) % sizeof(float) != 0 ||
+        !(max_norm > 0.0) || !(scale > 0.0) || !std::isnormal((float)scale))
         return ESP_ERR_INVALID_ARG;
-    bool write = false;
     int64_t bytes = 0;
     for (int32_t i = 0; i < count; ++i) {
         if (!good_tensor(tensors[i]))
             return ESP_ERR_INVALID_ARG;
-        write = write || (tensors[i].out && tensors[i].n > 0);
         bytes += tensors[i].n * size_of(tensors[i].dtype);
         if (bytes > kMostBytes)
             return ESP_ERR_INVALID_ARG;
     }
     try {
-        if (write && overlapping(count, tensors))
+        if (overlapping(count, tensors, norm))
             return ESP_ERR_INVALID_ARG;
     } catch (const std::bad_alloc &) {
         return ESP_ERR_OOM;

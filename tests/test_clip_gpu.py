@@ -250,3 +250,21 @@ def test_scales_at_the_ends_of_32_bits(mm):
         for grads in ([torch.zeros(100, device="cuda")], make([1000, 3], [torch.float32], 7, size)):
             before = [g.clone() for g in grads]
             check(before, grads, mm.clip(grads, scale=scale), math.inf, scale)
+
+
+def test_norm_within_a_gradient(mm):
+    """Refused: it would be written while the gradients are still read. Right beside them it is taken."""
+    from paper_2608_07971_gb300 import esp, moe
+    room = torch.ones(101, device="cuda")
+    for at in (0, 57, 99):
+        with pytest.raises(esp.EspError) as err:
+            mm.clip([room[:100]], 1.0, norm=room[at])
+        assert err.value.status == esp.ESP_ERR_INVALID_ARG
+    with pytest.raises(esp.EspError):
+        mm.clip(mm.gradients([torch.ones(7, device="cuda")], out=[room[:7]]), 1.0, norm=room[6])
+    counted = (moe._CTensor * 1)((room.data_ptr(), None, 100, 0))   # not written, but not the call's to write either
+    for norm in (room.data_ptr() + 40, room.data_ptr() + 402):       # the second one not on 4 bytes
+        mm._on_stream()
+        assert moe.load_library().esp_moe_clip(mm.h, 1, counted, 1.0, 1.0, norm) == esp.ESP_ERR_INVALID_ARG
+    assert (room == 1.0).all()
+    assert float(mm.clip([room[:100]], 1e9, norm=room[100])) == 10.0 and (room[:100] == 1.0).all()
