@@ -92,9 +92,9 @@ __device__ __forceinline__ float logistic(float g)
 }
 
 // The normal distribution's c = (1 + erf(g / sqrt 2)) / 2, and e = exp(-g^2 / 2), which its slope needs too. With x = |g| / sqrt 2
-// and t = 1 / (1 + 0.42 x): erfc(x) = t Q(t) exp(-x^2), Q of degree 7 fitted to the least relative error over x < 6.5 (4e-8; with
-// the arithmetic 1.2e-6 down to g = -6 and 2e-7 absolute). 1801 rows
-// of 5 experts, 2056 x 1000: hidden rows, and the gradients of g and u, take 3 us less each than with erff.
+// and t = 1 / (1 + 0.42 x): erfc(x) = t Q(t) exp(-x^2), Q of degree 7 fitted by least squares whose weights are raised where
+// the relative error over x < 6.5 is greatest, until it is even (4e-8; with the arithmetic 1.2e-6 down to g = -6 and 2e-7
+// absolute). 1801 rows of 5 experts, 2056 x 1000: hidden rows, and the gradients of g and u, take 3 us less each than with erff.
 __device__ __forceinline__ float normal(float g, float &e)
 {
     const float t = __fdividef(1.0f, 1.0f + 0.29698485f * fabsf(g));

@@ -1073,7 +1073,6 @@ cudaError_t launch_ff_dpre(esp_moe *m, const FfShape &s, const void *dy, int64_t
     p.blocks = (int32_t)ceil_div(s.H, kInner);
     p.g.out = dpre;
     p.g.ldo = 2 * s.fp;
-    p.pre = pre;
     CUtensorMap a, b, o, g;
     FF_TRY(box_map3(&a, dy, 2, s.H, s.M, lddy, 1, 0, kRowsA));
     FF_TRY(box_map3(&b, s.outer, 2, s.F, s.H, s.ld_outer, s.E, s.H * s.ld_outer, kInner));

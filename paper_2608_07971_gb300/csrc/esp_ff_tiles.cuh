@@ -33,7 +33,6 @@ struct FfParams {
     int32_t act;
     bool few_ctas;            // most SMs are free
     int32_t half_f16;         // operands are fp16 (else bf16)
-    const void *pre;          // DPRE
     int64_t fp;
     void *out2;               // HIDDEN: pre (or null)
     // HIDDEN with pre and a kinked activation: the operands, their rows' lengths (null: no g is summed again), and below which

@@ -273,7 +273,7 @@ bool use_vec(int64_t M, int32_t E, int32_t F, int32_t H)
     //   1     3.3  13.4    6.1  22.4    7.6  27.3   12.2  32.0   19.1  48     34.9  67      72  95      121  127
     //   2     3.4  13.4    7.3  22.4    8.9  27.3   14.7  32.0   23.1  48     45.2  67      94  95      170  127
     //   4     5.1  13.4   10.0  22.4   12.5  27.3   20.5  32.0   34.3  48     65.7  67     152  95      295  127
-    //   8     6.9  13.4   16.0  22.4   20.2  27.3   34.7  32.0   76.8  48      179  67     335  95      498  127
+    //   8     6.9  13.4   16.0  22.4   20.2  27.3   32.0  32.0   76.8  48      179  67     335  95      498  127
     const int64_t bytes = 6 * (int64_t)F * H;
     return E == 1 && (M == 1 || (M == 2 && bytes <= 384 << 20) || (M <= 4 && bytes <= 160 << 20) || (M <= 8 && bytes <= 32 << 20));
 }
