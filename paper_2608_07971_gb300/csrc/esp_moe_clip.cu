@@ -5,7 +5,7 @@
 // again and writes. Bound by HBM. The tensors are cut into chunks of 16-byte groups that the CTAs take in turn; k_scale
 // takes them from the last to the first, so that it begins with what k_norm left in L2. k_norm leaves a sum for each of
 // its CTAs; every CTA of k_scale adds them up for itself, and loads its first chunk while k_norm still runs. 1.4e9 elements
-// (2.8 GB) take 1222 us, three times their bytes at the copy rate 1229; 300,000 elements of 7 tensors 12 us.
+// (2.8 GB) take 1222 us, three times their bytes at the copy rate 1229; 300,000 elements of 7 tensors 13 to 17 us.
 //
 // A thread sums the squares of a chunk's groups in fp32 (at most 64 of them), then adds that to its sum in fp64; the
 // threads', CTAs' and launches' sums are joined in a fixed order in fp64. Squares of values that fp32 does not hold
